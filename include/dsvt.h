@@ -326,6 +326,75 @@ int dsvt_vfe(const dsvt_vfe_cfg* cfg, const float* points, const int32_t* point_
              int32_t* status, void* stream);
 
 /* ---------------------------------------------------------------------------------------
+ * Training a layer: the parts of a DSVT layer that are no matrix product (Eq. 5), each as a call of
+ * its own with its gradients.  The caller's matrix products (projections, MLP) go in between.  Rows
+ * have strides in elements (ld >= row length), so that slices of wider arrays can be passed; n may be 0.
+ * ------------------------------------------------------------------------------------ */
+
+/* Multi-head attention inside every set on projected rows, with a learned relative position bias.
+ * Head h of d = C / heads channels, for every pair of voxels of one set, i as query and j as key:
+ *   s_ij = q_i.k_j / sqrt(d) + bias_h[bucket(i - j)],  P_ij = m_j exp(s_ij) / sum_j m_j exp(s_ij),  out_i = sum_j P_ij v_j
+ * i - j is the offset of their cells, numbered as in dsvt_layer_w.rel_bias; m_j = 1 (dup_mode 0: a slot repeating
+ * its predecessor's voxel is masked as a key) or the number of voxel j's slots (dup_mode 1).  A query whose keys
+ * all have the bias -infinity gets an output of zeros and no gradient; a finite bias of any size is no mask. */
+typedef struct {
+  int32_t C, heads, dtype;
+  int32_t win[3];            /* L, W, H of the window the maps were built with                          */
+  int32_t dup_mode;          /* as in dsvt_layer_w                                                       */
+  const float* rel_bias;     /* [device] [heads, n_rel]; NULL: no positional term                        */
+  const int32_t* rel_bucket; /* [device] [(2L-1)(2W-1)(2H-1)] the entry of rel_bias that an offset takes, outside
+                                0 .. n_rel - 1: none (its pairs get no term); NULL: entry u is offset u's, as in
+                                dsvt_layer_w.rel_bias, and n_rel is the number of offsets               */
+  int32_t n_rel;
+} dsvt_mha_cfg;
+
+/* Host-only: buckets for the offsets of a window, for dsvt_mha_cfg.rel_bucket.  Along an axis of window size w, with
+ * B = min(n_side, w): distances below n_exact have buckets of their own, a distance a from n_exact on has the bucket
+ * n_exact + floor((B - n_exact) log(a / n_exact) / log(w / n_exact)), none is above B - 1, and the two directions are kept
+ * apart: 2B - 1 buckets an axis.  An offset's bucket is the product of the three, x most significant.
+ * bucket [host] [(2L-1)(2W-1)(2H-1)], may be NULL; n_rel [host] the number of buckets.  0 < n_exact <= n_side. */
+int dsvt_rel_buckets(const int32_t win[3], int32_t n_exact, int32_t n_side, int32_t* bucket, int32_t* n_rel);
+
+/* qkv [device] [n_voxels, 3C] q, k, v of every voxel (the product with dsvt_layer_w.w_qkv and its bias)
+ * out [device] [n_voxels, C]  must not overlap qkv; rows of voxels that are in no set stay as they are
+ * maps: set_inds, n_sets, max_sets, tau and n_voxels are read (set slots outside 0 .. n_voxels - 1 are empty; repeats of a
+ * voxel are neighbours and every voxel is in one set, as dsvt_partition writes them).  coords as there.
+ * Supported: d a multiple of 8 up to 64, tau <= 96 (DSVT_EUNSUPPORTED otherwise), F32 and BF16; qkv, out and coords 16-byte
+ * aligned, row strides multiples of 16 bytes (DSVT_EINVAL otherwise). */
+int dsvt_set_mha(const dsvt_mha_cfg* cfg, const dsvt_maps* maps, const int32_t* coords, const void* qkv, int64_t ld_qkv,
+                 void* out, int64_t ld_out, void* stream);
+
+/* The gradients, from that of out: d_qkv [device] [n_voxels, 3C] and d_rel_bias [device] [heads, n_rel] float (NULL: not
+ * wanted), both written, not added to; rows of voxels in no set stay as they are.  Nothing but the inputs is needed from the forward
+ * call.  ws [device] 16-byte aligned, of the bytes that dsvt_set_mha_backward_workspace_size reports (none
+ * without d_rel_bias); no state is kept in it.  Supported as above, rows of d_out and d_qkv aligned likewise; d_rel_bias: at most 35,840
+ * offsets and buckets.  The results do not depend on the order in which the kernels run. */
+int dsvt_set_mha_backward_workspace_size(const dsvt_mha_cfg* cfg, const dsvt_maps* maps, size_t* bytes);
+int dsvt_set_mha_backward(const dsvt_mha_cfg* cfg, const dsvt_maps* maps, const int32_t* coords, const void* qkv, int64_t ld_qkv,
+                          const void* d_out, int64_t ld_dout, void* d_qkv, int64_t ld_dqkv, float* d_rel_bias,
+                          void* ws, size_t ws_bytes, void* stream);
+
+/* LayerNorm of a residual sum (Eq. 5): z = x + res, y = (z - mean z) / sqrt(var z + eps) * gamma + beta, row by row. */
+typedef struct {
+  int32_t C, dtype;           /* C <= DSVT_LN_MAX_C; dtype of x, res, y and their gradients                */
+  const float *gamma, *beta;  /* [C] [device]; beta is not read by the backward call                        */
+  float eps;
+} dsvt_ln_cfg;
+#define DSVT_LN_MAX_C 65536
+
+/* x, res, y [device] [n_rows, C]; res may be NULL (z = x).  y may be x or res themselves (same stride). */
+int dsvt_layer_norm(const dsvt_ln_cfg* cfg, const void* x, int64_t ld_x, const void* res, int64_t ld_res, int32_t n_rows,
+                    void* y, int64_t ld_y, void* stream);
+
+/* The gradients, from dy, that of y: dx [device] [n_rows, C] = that of z, and so of x and of res alike (dx may be dy itself, same
+ * stride); d_gamma, d_beta [device] [C] float, written, not added to.  x and res as the forward call had them.
+ * ws [device] 16-byte aligned, of the bytes that dsvt_layer_norm_backward_workspace_size reports; no state is kept in it. */
+int dsvt_layer_norm_backward_workspace_size(const dsvt_ln_cfg* cfg, int32_t n_rows, size_t* bytes);
+int dsvt_layer_norm_backward(const dsvt_ln_cfg* cfg, const void* dy, int64_t ld_dy, const void* x, int64_t ld_x, const void* res,
+                             int64_t ld_res, int32_t n_rows, void* dx, int64_t ld_dx, float* d_gamma, float* d_beta,
+                             void* ws, size_t ws_bytes, void* stream);
+
+/* ---------------------------------------------------------------------------------------
  * Instrumentation for benchmarks (not part of the method): per-kernel time from hipEvent pairs
  * recorded around every launch while enabled (launches of one kernel that follow one another on a
  * stream share a pair: begin before the first, end after the last).  Host-only; not thread-safe.

@@ -66,6 +66,15 @@ class PoolCfg(C.Structure):
                 ("mask_empty", C.c_int32), ("packed", C.c_void_p)]
 
 
+class MhaCfg(C.Structure):
+    _fields_ = [("C", C.c_int32), ("heads", C.c_int32), ("dtype", C.c_int32), ("win", I32x3), ("dup_mode", C.c_int32),
+                ("rel_bias", C.c_void_p), ("rel_bucket", C.c_void_p), ("n_rel", C.c_int32)]
+
+
+class LnCfg(C.Structure):
+    _fields_ = [("C", C.c_int32), ("dtype", C.c_int32), ("gamma", C.c_void_p), ("beta", C.c_void_p), ("eps", C.c_float)]
+
+
 _lib = None
 
 
@@ -98,6 +107,14 @@ def lib():
         L.dsvt_bev_scatter.argtypes = [vp, vp, i32, i32, i32, i32, C.POINTER(I32x3), vp, vp, vp]
         L.dsvt_vfe_workspace_size.argtypes = [C.POINTER(VfeCfg), i32, i32, C.POINTER(sz)]
         L.dsvt_vfe.argtypes = [C.POINTER(VfeCfg), vp, vp, i32, vp, vp, vp, i32, vp, sz, vp, vp]
+        i64 = C.c_int64
+        L.dsvt_rel_buckets.argtypes = [C.POINTER(I32x3), i32, i32, vp, C.POINTER(i32)]
+        L.dsvt_set_mha.argtypes = [C.POINTER(MhaCfg), C.POINTER(Maps), vp, vp, i64, vp, i64, vp]
+        L.dsvt_set_mha_backward_workspace_size.argtypes = [C.POINTER(MhaCfg), C.POINTER(Maps), C.POINTER(sz)]
+        L.dsvt_set_mha_backward.argtypes = [C.POINTER(MhaCfg), C.POINTER(Maps), vp, vp, i64, vp, i64, vp, i64, vp, vp, sz, vp]
+        L.dsvt_layer_norm.argtypes = [C.POINTER(LnCfg), vp, i64, vp, i64, i32, vp, i64, vp]
+        L.dsvt_layer_norm_backward_workspace_size.argtypes = [C.POINTER(LnCfg), i32, C.POINTER(sz)]
+        L.dsvt_layer_norm_backward.argtypes = [C.POINTER(LnCfg), vp, i64, vp, i64, vp, i64, i32, vp, i64, vp, vp, vp, sz, vp]
         L.dsvt_prof_enable.argtypes = [i32]
         L.dsvt_prof_collect.argtypes = [C.POINTER(C.c_float), C.POINTER(i32), i32]
         L.dsvt_prof_kernel_count.restype = i32
@@ -182,6 +199,19 @@ class SetMaps:
             self.tile_list = TileList(0, None, None, None, None)
         self.struct = Maps(n_voxels, self.max_sets, cfg.tau, self.set_inds.data_ptr(), self.voxel_slot.data_ptr(),
                            self.n_sets.data_ptr(), self.tile_list)
+
+    @classmethod
+    def of(cls, set_inds, n_sets, n_voxels):
+        """Maps from slot maps the caller has: set_inds int32 [max_sets, tau], n_sets int32 [1] (both on the GPU), as
+        dsvt_partition writes them.  For dsvt_set_mha and its backward call: there is no work list and no voxel_slot."""
+        assert set_inds.is_cuda and set_inds.dtype == torch.int32 and set_inds.is_contiguous() and set_inds.dim() == 2
+        assert n_sets.is_cuda and n_sets.dtype == torch.int32 and n_sets.numel() == 1
+        m = cls.__new__(cls)
+        m.cfg, m.n_voxels, m.tau, m.max_sets, m.max_tiles = None, n_voxels, set_inds.shape[1], set_inds.shape[0], 0
+        m.set_inds, m.n_sets, m.voxel_slot = set_inds, n_sets, None
+        m.tile_list = TileList(0, None, None, None, None)
+        m.struct = Maps(n_voxels, m.max_sets, m.tau, set_inds.data_ptr(), None, n_sets.data_ptr(), m.tile_list)
+        return m
 
 
 def dsvt_partition(cfg, coords, out=None, stream=None):
@@ -411,6 +441,143 @@ def dsvt_vfe(vfe, points, point_batch=None, stream=None):
                         _ptr(vfe.status), _stream(stream))
     _check("dsvt_vfe", rc)
     return vfe
+
+
+def _rows(t, shape, dtype, what):
+    """The row stride of a [rows, columns] tensor of the current device whose columns are neighbours."""
+    if t.shape != shape or t.dtype != dtype or not t.is_cuda or (t.shape[1] > 1 and t.stride(1) != 1):
+        raise ValueError(f"{what}: a {dtype} GPU tensor of shape {tuple(shape)} with neighbouring columns is wanted, got {t.dtype} "
+                         f"{tuple(t.shape)} strides {tuple(t.stride())} on {t.device}")
+    if t.device.index != torch.cuda.current_device():
+        raise ValueError(f"{what} is on {t.device}, the current device is {torch.cuda.current_device()}")
+    return t.stride(0) if t.shape[0] > 1 else max(t.stride(0), t.shape[1])
+
+
+def _vector(t, shape, dtype, what):
+    if t.shape != shape or t.dtype != dtype or not t.is_cuda or not t.is_contiguous():
+        raise ValueError(f"{what}: a contiguous {dtype} GPU tensor of shape {tuple(shape)} is wanted, got {t.dtype} {tuple(t.shape)} on {t.device}")
+
+
+def _scratch(nbytes, ws, stream):
+    """The caller's scratch, or fresh one that stays allocated until `stream` is done with it."""
+    if ws is None:
+        ws = torch.empty((max(nbytes, 1),), dtype=torch.uint8, device="cuda")
+        if stream is not None:
+            ws.record_stream(torch.cuda.ExternalStream(stream))
+    return ws
+
+
+def dsvt_rel_buckets(win, n_exact, n_side):
+    """(int32 numpy array of every offset's bucket, number of buckets) for SetMha's rel_bucket and table; see dsvt.h."""
+    n = C.c_int32(0)
+    offsets = 1
+    for w in win:
+        offsets *= max(2 * w - 1, 0)
+    bucket = np.zeros((offsets,), np.int32)
+    _check("dsvt_rel_buckets", lib().dsvt_rel_buckets(C.byref(I32x3(*win)), n_exact, n_side, bucket.ctypes.data_as(C.c_void_p), C.byref(n)))
+    return bucket, n.value
+
+
+class SetMha:
+    """Shape and relative position bias of one set attention on projected rows.  rel_bias: float32 [heads, n_rel] or None;
+    rel_bucket: int32 [(2L-1)(2W-1)(2H-1)] or None (an entry for every offset).  Both stay the caller's: the tensors
+    are read at every call."""
+
+    def __init__(self, channels, heads, dtype, win, rel_bias=None, rel_bucket=None, dup_mode=0):
+        code, self.dtype = _DT[dtype]
+        self.C, self.heads, self.rel_bias, self.rel_bucket = channels, heads, rel_bias, rel_bucket
+        offsets = (2 * win[0] - 1) * (2 * win[1] - 1) * (2 * win[2] - 1)
+        n_rel = 0
+        if rel_bias is not None:
+            n_rel = rel_bias.shape[-1]
+            _vector(rel_bias, (heads, n_rel), torch.float32, "rel_bias")
+        if rel_bucket is not None:
+            _vector(rel_bucket, (offsets,), torch.int32, "rel_bucket")
+        self.struct = MhaCfg(channels, heads, code, I32x3(*win), dup_mode, None if rel_bias is None else rel_bias.data_ptr(),
+                             None if rel_bucket is None else rel_bucket.data_ptr(), n_rel)
+
+
+def dsvt_set_mha(mha, maps, coords, qkv, out=None, stream=None):
+    """Attention inside every set of `maps` on projected rows qkv [N, 3C]; returns out [N, C]."""
+    n = maps.n_voxels
+    ld = _rows(qkv, (n, 3 * mha.C), mha.dtype, "qkv")
+    _vector(coords, (n, 4), torch.int32, "coords")
+    out = torch.empty((n, mha.C), dtype=mha.dtype, device="cuda") if out is None else out
+    rc = lib().dsvt_set_mha(C.byref(mha.struct), C.byref(maps.struct), _ptr(coords), _ptr(qkv), ld, _ptr(out),
+                            _rows(out, (n, mha.C), mha.dtype, "out"), _stream(stream))
+    _check("dsvt_set_mha", rc)
+    return out
+
+
+def dsvt_set_mha_backward_workspace_size(mha, maps):
+    b = C.c_size_t(0)
+    _check("dsvt_set_mha_backward_workspace_size",
+           lib().dsvt_set_mha_backward_workspace_size(C.byref(mha.struct), C.byref(maps.struct), C.byref(b)))
+    return b.value
+
+
+def dsvt_set_mha_backward(mha, maps, coords, qkv, d_out, d_qkv=None, d_rel_bias=None, want_rel_bias=True, ws=None, stream=None):
+    """Gradients of dsvt_set_mha: returns (d_qkv [N, 3C], d_rel_bias [heads, n_rel] float32, or None without a table or if not
+    wanted)."""
+    n = maps.n_voxels
+    ld, ld_out = _rows(qkv, (n, 3 * mha.C), mha.dtype, "qkv"), _rows(d_out, (n, mha.C), mha.dtype, "d_out")
+    _vector(coords, (n, 4), torch.int32, "coords")
+    d_qkv = torch.empty((n, 3 * mha.C), dtype=mha.dtype, device="cuda") if d_qkv is None else d_qkv
+    if d_rel_bias is not None:
+        _vector(d_rel_bias, mha.rel_bias.shape if mha.rel_bias is not None else (), torch.float32, "d_rel_bias")
+    elif want_rel_bias and mha.rel_bias is not None:
+        d_rel_bias = torch.empty_like(mha.rel_bias)
+    ws = _scratch(dsvt_set_mha_backward_workspace_size(mha, maps) if d_rel_bias is not None else 0, ws, stream)
+    rc = lib().dsvt_set_mha_backward(C.byref(mha.struct), C.byref(maps.struct), _ptr(coords), _ptr(qkv), ld, _ptr(d_out), ld_out, _ptr(d_qkv),
+                                     _rows(d_qkv, (n, 3 * mha.C), mha.dtype, "d_qkv"), _ptr(d_rel_bias), _ptr(ws), ws.numel(), _stream(stream))
+    _check("dsvt_set_mha_backward", rc)
+    return d_qkv, d_rel_bias
+
+
+class LayerNorm:
+    """Parameters of one LayerNorm of a residual sum.  gamma, beta: float32 [C]; both stay the caller's: they are read at every call."""
+
+    def __init__(self, gamma, beta, dtype, eps=1e-5):
+        code, self.dtype = _DT[dtype]
+        self.C, self.gamma, self.beta = gamma.shape[0], gamma, beta
+        _vector(gamma, (self.C,), torch.float32, "gamma")
+        _vector(beta, (self.C,), torch.float32, "beta")
+        self.struct = LnCfg(self.C, code, gamma.data_ptr(), beta.data_ptr(), eps)
+
+
+def dsvt_layer_norm(ln, x, res=None, y=None, stream=None):
+    """LayerNorm of x + res (of x without res), rows [N, C]; returns y."""
+    shape = (x.shape[0], ln.C)
+    ld_x, ld_res = _rows(x, shape, ln.dtype, "x"), 0 if res is None else _rows(res, shape, ln.dtype, "res")
+    y = torch.empty(shape, dtype=ln.dtype, device="cuda") if y is None else y
+    rc = lib().dsvt_layer_norm(C.byref(ln.struct), _ptr(x), ld_x, _ptr(res), ld_res, shape[0], _ptr(y), _rows(y, shape, ln.dtype, "y"),
+                               _stream(stream))
+    _check("dsvt_layer_norm", rc)
+    return y
+
+
+def dsvt_layer_norm_backward_workspace_size(ln, n_rows):
+    b = C.c_size_t(0)
+    _check("dsvt_layer_norm_backward_workspace_size",
+           lib().dsvt_layer_norm_backward_workspace_size(C.byref(ln.struct), n_rows, C.byref(b)))
+    return b.value
+
+
+def dsvt_layer_norm_backward(ln, dy, x, res=None, dx=None, d_gamma=None, d_beta=None, ws=None, stream=None):
+    """Gradients of dsvt_layer_norm: returns (dx, which is that of x and of res, d_gamma [C], d_beta [C])."""
+    shape = (x.shape[0], ln.C)
+    ld_dy, ld_x = _rows(dy, shape, ln.dtype, "dy"), _rows(x, shape, ln.dtype, "x")
+    ld_res = 0 if res is None else _rows(res, shape, ln.dtype, "res")
+    dx = torch.empty(shape, dtype=ln.dtype, device="cuda") if dx is None else dx
+    d_gamma = torch.empty_like(ln.gamma) if d_gamma is None else d_gamma
+    d_beta = torch.empty_like(ln.beta) if d_beta is None else d_beta
+    _vector(d_gamma, (ln.C,), torch.float32, "d_gamma")
+    _vector(d_beta, (ln.C,), torch.float32, "d_beta")
+    ws = _scratch(dsvt_layer_norm_backward_workspace_size(ln, shape[0]), ws, stream)
+    rc = lib().dsvt_layer_norm_backward(C.byref(ln.struct), _ptr(dy), ld_dy, _ptr(x), ld_x, _ptr(res), ld_res, shape[0], _ptr(dx),
+                                        _rows(dx, shape, ln.dtype, "dx"), _ptr(d_gamma), _ptr(d_beta), _ptr(ws), ws.numel(), _stream(stream))
+    _check("dsvt_layer_norm_backward", rc)
+    return dx, d_gamma, d_beta
 
 
 def prof_enable(max_launches):

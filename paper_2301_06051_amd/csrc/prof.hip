@@ -16,7 +16,8 @@ size_t g_used = 0;
 bool g_extend = false;               // the launch being marked joins the previous record
 const char* const kNames[DSVT_K_COUNT] = {
     "part_mark", "part_window_count", "part_scan_windows", "part_emit", "part_clear",
-    "part_tiles", "layer", "pool_group", "pool_attention", "bev_clear", "bev_scatter", "vfe_group", "vfe_reduce"};
+    "part_tiles", "layer", "pool_group", "pool_attention", "bev_clear", "bev_scatter", "vfe_group", "vfe_reduce",
+    "mha_forward", "mha_backward", "mha_rel_bias", "ln_forward", "ln_backward", "ln_sum"};
 }  // namespace
 
 void dsvt_prof_mark_begin(int id, hipStream_t s) {
