@@ -336,7 +336,8 @@ int dsvt_vfe(const dsvt_vfe_cfg* cfg, const float* points, const int32_t* point_
  *   s_ij = q_i.k_j / sqrt(d) + bias_h[bucket(i - j)],  P_ij = m_j exp(s_ij) / sum_j m_j exp(s_ij),  out_i = sum_j P_ij v_j
  * i - j is the offset of their cells, numbered as in dsvt_layer_w.rel_bias; m_j = 1 (dup_mode 0: a slot repeating
  * its predecessor's voxel is masked as a key) or the number of voxel j's slots (dup_mode 1).  A query whose keys
- * all have the bias -infinity gets an output of zeros and no gradient; a finite bias of any size is no mask. */
+ * all have the bias -infinity gets an output of zeros and no gradient; a finite bias is no mask (sizes above 1e37 count as 1e37).  In a
+ * set whose voxels do not fit one window (maps of another window) all pairs take the term of offset 0. */
 typedef struct {
   int32_t C, heads, dtype;
   int32_t win[3];            /* L, W, H of the window the maps were built with                          */
@@ -368,7 +369,7 @@ int dsvt_set_mha(const dsvt_mha_cfg* cfg, const dsvt_maps* maps, const int32_t* 
  * wanted), both written, not added to; rows of voxels in no set stay as they are.  Nothing but the inputs is needed from the forward
  * call.  ws [device] 16-byte aligned, of the bytes that dsvt_set_mha_backward_workspace_size reports (none
  * without d_rel_bias); no state is kept in it.  Supported as above, rows of d_out and d_qkv aligned likewise; d_rel_bias: at most 35,840
- * offsets and buckets.  The results do not depend on the order in which the kernels run. */
+ * entries a head (35,839 with buckets).  The results do not depend on the order in which the kernels run. */
 int dsvt_set_mha_backward_workspace_size(const dsvt_mha_cfg* cfg, const dsvt_maps* maps, size_t* bytes);
 int dsvt_set_mha_backward(const dsvt_mha_cfg* cfg, const dsvt_maps* maps, const int32_t* coords, const void* qkv, int64_t ld_qkv,
                           const void* d_out, int64_t ld_dout, void* d_qkv, int64_t ld_dqkv, float* d_rel_bias,

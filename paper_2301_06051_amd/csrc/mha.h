@@ -1,0 +1,348 @@
+// What the kernels of dsvt_set_mha and dsvt_set_mha_backward share (mha_forward.hip, mha_backward.hip); the entry points are
+// in mha.hip.  Multi-head attention inside every set (Eq. 5, second line) on rows that are already projected, with a learned
+// relative position bias per offset or per bucket of offsets, and its gradients.  With g = d out, sigma = 1/sqrt(d), m_j the
+// weight of voxel j as a key (1, or the number of its slots), B the bucket of an offset:
+//
+//   s_ij = sigma q_i.k_j + bias[B(c_i - c_j)]    P_ij = m_j exp(s_ij) / sum_j m_j exp(s_ij)    out_i = sum_j P_ij v_j
+//   t_ij = g_i.v_j    ds_ij = P_ij (t_ij - sum_j P_ij t_ij)
+//   dq_i = sigma sum_j ds_ij k_j    dk_j = sigma sum_i ds_ij q_i    dv_j = sum_i P_ij g_i    d bias[u] = sum of ds_ij with B = u
+//
+// A set is at most 96 voxels and every voxel is in one set, so a set's attention is a problem of its own that fits on chip: the
+// backward pass forms the probabilities again and needs nothing from the forward pass, and no two sets write one row.
+//
+// A wavefront takes one (set, head) at a time; the wavefronts of a workgroup take the heads of one set side by side, so
+// that the cache lines its heads share are fetched once.  Rows go from memory straight into matrix fragments: with the keys as
+// rows and the queries as columns of the logits, lane 16 g + m holds query m and keys 4 g .. 4 g + 3 of a tile, which is how
+// the next product wants its operand.  Operands that have to be turned round (V, and in the backward pass K, Q, g, P, ds) are
+// multiplied by the unit matrix, which is exact (one factor is 1, the others are 0; a row with an infinity or a NaN
+// becomes NaN in all of its channels).  LDS holds no tile, only what is known of the sets, and the tables.
+#pragma once
+#include "common.h"
+#include "mma.h"
+#include <cfloat>
+#include <cmath>
+
+constexpr int kSetMax = 96;                       // slots, and so voxels, of a set
+constexpr int kBatch = 8;                         // sets of a workgroup whose rows are looked up together
+constexpr float kLog2e = 1.44269504088896340736f;
+
+// Where a pair's bias is found.  By offset: LDS holds a value for every offset and head.  By bucket: LDS holds the offsets' buckets
+// (16 bits, one past the last for offsets without a bias) and a value for every bucket and head.  In memory: biases and buckets are read
+// where they lie.
+enum TableForm { kByOffset, kByBucket, kInMemory };
+
+struct MhaArgs {
+  const int32_t *set_inds, *n_sets;
+  const int4* coords;
+  const void *qkv, *d_out;
+  void* out;                                      // forward: the output rows; backward: d_qkv
+  const float* bias;                              // [heads][n_rel] or null
+  const int32_t* bucket;                          // [n_off] or null
+  float* partial;                                 // backward: [parts][heads][entries]; null: no gradient of the table
+  int64_t ld_qkv, ld_dout, ld_out;
+  int32_t n_voxels, max_sets, tau, heads, hd;
+  int32_t n_off, n_rel, entries;                  // offsets; biases of a head; values of a head in LDS
+  int32_t w[3], centre;                           // the window; the number of offset 0
+  int32_t dup, hs, slots, groups, parts;          // heads of a workgroup, sets it takes side by side, groups of heads, workgroups a group
+  float scale;
+};
+
+typedef short short4_t __attribute__((ext_vector_type(4)));
+typedef __attribute__((address_space(3))) float lds_float;
+typedef __attribute__((address_space(3))) const uint16_t lds_u16;
+
+// Matrix fragments.  A row fragment covers 4 * KL channels: lane 16 g + m holds channels KL g .. KL g + KL - 1 of row m.  A
+// tile fragment covers 16: lane 16 g + m holds elements 4 g .. 4 g + 3 of row (or column) m.
+template <typename T, int HDP> struct Frag;
+template <int HDP> struct Frag<bf16_t, HDP> {
+  static constexpr int KL = HDP == 16 ? 4 : 8, NC = HDP / (4 * KL), NT = HDP / 16, PER = KL / 4;
+  typedef bf16_t Row __attribute__((ext_vector_type(KL)));
+  typedef bf16x4 Tile;
+  static __device__ __forceinline__ f32x4 tile_mma(Tile a, Tile b, f32x4 c) {
+    return __builtin_amdgcn_mfma_f32_16x16x16bf16_1k(__builtin_bit_cast(short4_t, a), __builtin_bit_cast(short4_t, b), c, 0, 0, 0);
+  }
+  static __device__ __forceinline__ f32x4 row_mma(Row a, Row b, f32x4 c) {
+    if constexpr (KL == 8) return __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, b, c, 0, 0, 0);
+    else return tile_mma(a, b, c);
+  }
+  static __device__ __forceinline__ Tile tile(f32x4 v) { return Tile{(bf16_t)v[0], (bf16_t)v[1], (bf16_t)v[2], (bf16_t)v[3]}; }
+};
+template <int HDP> struct Frag<float, HDP> {
+  static constexpr int KL = 4, NC = HDP / 16, NT = HDP / 16, PER = 1;
+  typedef f32x4 Row;
+  typedef f32x4 Tile;
+  static __device__ __forceinline__ f32x4 tile_mma(Tile a, Tile b, f32x4 c) { return Mma<float>::mma(a, b, c); }
+  static __device__ __forceinline__ f32x4 row_mma(Row a, Row b, f32x4 c) { return Mma<float>::mma(a, b, c); }
+  static __device__ __forceinline__ Tile tile(f32x4 v) { return v; }
+};
+
+// Lanes 16 apart hold the same query's other keys: every lane gets the sum (largest) of its four.
+template <typename Op> __device__ __forceinline__ float across(float v, Op op) {
+  const auto a = __builtin_amdgcn_permlane16_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+  v = op(__uint_as_float(a[0]), __uint_as_float(a[1]));
+  const auto b = __builtin_amdgcn_permlane32_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+  return op(__uint_as_float(b[0]), __uint_as_float(b[1]));
+}
+__device__ __forceinline__ float across_sum(float v) { return across(v, [](float a, float b) { return a + b; }); }
+__device__ __forceinline__ float across_max(float v) { return across(v, [](float a, float b) { return fmaxf(a, b); }); }
+
+// The logits are formed in units of sigma, so that a bias is what the product of q and k starts from.  A finite bias stays finite.
+__device__ __forceinline__ float to_units(float b, float root) {
+  return fabsf(b) <= FLT_MAX ? fminf(fmaxf(b, -1.0e37f), 1.0e37f) * root : b;
+}
+
+// What a workgroup knows of a set, in LDS.  Row r is the set's r-th voxel; rows up to the next multiple of 16 have no voxel (-1), the
+// code of row 0 and weight 0.  code: the cell's number times the bytes of an entry, so that the difference of two codes is an
+// offset's place in a table.
+struct SetRows {
+  int32_t vox[kSetMax], code[kSetMax], weight[kSetMax];
+  int32_t n;
+};
+
+__device__ __forceinline__ int wave_max(int v) {
+#pragma unroll
+  for (int d = 1; d < 64; d *= 2) {
+    const int o = __shfl_xor(v, d, 64);
+    v = o > v ? o : v;
+  }
+  return v;
+}
+
+// A wavefront looks a set's distinct voxels up, in slot order: the first slot of every run of equal ones.  Slots outside
+// 0 .. n_voxels - 1 hold none.  Voxels that do not fit one window (the maps are another window's) all get code 0, so that
+// every offset formed from two codes is in the table.
+__device__ __forceinline__ void load_set(const MhaArgs& a, int32_t s, int entry_bytes, SetRows& rows) {
+  const int lane = threadIdx.x & 63;
+  const int32_t* inds = a.set_inds + (int64_t)s * a.tau;
+  int32_t v[2];
+  uint64_t first[2], change[2];
+  int4 c[2];
+  int32_t before = -1;
+#pragma unroll
+  for (int k = 0; k < 2; ++k) {
+    const int slot = 64 * k + lane;
+    v[k] = slot < a.tau ? inds[slot] : -1;
+    if ((uint32_t)v[k] >= (uint32_t)a.n_voxels) v[k] = -1;
+  }
+  int lo[3], hi[3];
+#pragma unroll
+  for (int x = 0; x < 3; ++x) lo[x] = hi[x] = INT32_MIN;
+#pragma unroll
+  for (int k = 0; k < 2; ++k) {
+    const int slot = 64 * k + lane;
+    int32_t prev = __shfl_up(v[k], 1, 64);
+    if (lane == 0) prev = before;
+    before = __shfl(v[k], 63, 64);
+    change[k] = __ballot(v[k] != prev || slot >= a.tau);
+    first[k] = __ballot(v[k] != prev && v[k] >= 0);
+    if (first[k] >> lane & 1) {
+      c[k] = a.coords[v[k]];
+      const int at[3] = {c[k].y, c[k].z, c[k].w};
+#pragma unroll
+      for (int x = 0; x < 3; ++x) {
+        hi[x] = at[x] > hi[x] ? at[x] : hi[x];
+        lo[x] = -1 - at[x] > lo[x] ? -1 - at[x] : lo[x];
+      }
+    }
+  }
+  // highest + 1 - lowest <= window along every axis (the lowest is kept as the highest of -1 - x), by differences that do not overflow
+  bool fits = a.bias != nullptr;
+#pragma unroll
+  for (int x = 0; x < 3; ++x) fits = fits && (int64_t)wave_max(hi[x]) + wave_max(lo[x]) + 2 <= a.w[x];
+  const int n0 = __popcll(first[0]), n = n0 + __popcll(first[1]);
+  const int w2 = 2 * a.w[1] - 1, h2 = 2 * a.w[2] - 1;
+#pragma unroll
+  for (int k = 0; k < 2; ++k)
+    if (first[k] >> lane & 1) {
+      const int r = (k ? n0 : 0) + __popcll(first[k] & ((1ull << lane) - 1));
+      const uint64_t later = lane == 63 ? 0 : change[k] >> (lane + 1);      // slots to the next change
+      int run;
+      if (later) run = 1 + __builtin_ctzll(later);
+      else if (k == 0) run = 64 - lane + (change[1] ? __builtin_ctzll(change[1]) : 64);
+      else run = 64 - lane;
+      // (unsigned: a far cell's number may pass 32 bits, the differences inside a window do not)
+      const uint32_t code = fits ? (((uint32_t)c[k].y * w2 + (uint32_t)c[k].z) * h2 + (uint32_t)c[k].w) * entry_bytes : 0;
+      rows.vox[r] = v[k];
+      rows.code[r] = (int32_t)code;
+      rows.weight[r] = a.dup ? run : 1;
+      if (r == 0) {
+        const int pad = (n + 15) & ~15;
+        for (int p = n; p < pad; ++p) rows.code[p] = (int32_t)code;
+      }
+    }
+  if (n + lane < ((n + 15) & ~15)) {
+    rows.vox[n + lane] = -1;
+    rows.weight[n + lane] = 0;
+  }
+  if (lane == 0) rows.n = n;
+}
+
+// Workgroup b takes group of heads b / 8 % groups and is part (b / 8 / groups) * 8 + b % 8 of it: workgroups that take other heads of
+// the same sets are a multiple of 8 apart and so on one XCD, whose L2 they share.
+struct Share {
+  int group, part;
+  __device__ __forceinline__ Share(const MhaArgs& a) {
+    const int r = blockIdx.x >> 3;
+    group = r % a.groups;
+    part = r / a.groups * 8 + (blockIdx.x & 7);
+  }
+};
+
+__device__ __forceinline__ int32_t sets_of(const MhaArgs& a) {
+  const int32_t n = *a.n_sets;
+  return n < 0 ? 0 : (n > a.max_sets ? a.max_sets : n);
+}
+
+// Place of the next `bytes` of dynamic LDS.
+__device__ __forceinline__ uint32_t lds_address(const void* p) { return (uint32_t)(uintptr_t)(__attribute__((address_space(3))) const void*)p; }
+
+// The heads' biases in units of sigma, and by bucket the offsets' buckets; offsets without a bias get 0.
+template <TableForm kForm> __device__ __forceinline__ void fill_tables(const MhaArgs& a, int h0, float* table, uint16_t* map) {
+  if constexpr (kForm == kInMemory) return;
+  const float root = sqrtf((float)a.hd);
+  for (int h = 0; h < a.hs; ++h)
+    for (int u = threadIdx.x; u < a.entries; u += blockDim.x) {
+      unsigned r = (unsigned)u;
+      if (kForm == kByOffset && a.bucket) r = (unsigned)a.bucket[u];
+      table[h * a.entries + u] = a.bias && r < (unsigned)a.n_rel ? to_units(a.bias[(int64_t)(h0 + h) * a.n_rel + r], root) : 0.f;
+    }
+  if constexpr (kForm == kByBucket)
+    for (int u = threadIdx.x; u < a.n_off; u += blockDim.x) {
+      const unsigned r = (unsigned)a.bucket[u];
+      map[u] = (uint16_t)(r < (unsigned)a.n_rel ? r : a.n_rel);
+    }
+}
+
+// One wavefront's head: where its rows and biases are, and its part of the matrix fragments.
+template <typename T, int HDP, TableForm kForm> struct Head {
+  typedef Frag<T, HDP> F;
+  typedef typename F::Row Row;
+  typedef typename F::Tile Tile;
+  const MhaArgs& a;
+  uint32_t table, map;                            // LDS: this head's values, the offsets' buckets
+  const float* bias;                              // memory: this head's biases
+  int m, g, h;
+  float root, scale2;                             // 1 / sigma, sigma log2 e
+
+  __device__ __forceinline__ Head(const MhaArgs& a_, const float* table_, const uint16_t* map_, int h_)
+      : a(a_), table(lds_address(table_)), map(lds_address(map_)), bias(a_.bias + (int64_t)h_ * a_.n_rel), m(threadIdx.x & 15),
+        g(threadIdx.x >> 4 & 3), h(h_), root(sqrtf((float)a_.hd)), scale2(a_.scale * kLog2e) {}
+  static constexpr int entry_bytes() { return kForm == kByBucket ? 2 : 4; }
+
+  // rows of tile t of an array of head vectors (which: 0 q, 1 k, 2 v of a qkv row; 0 of an output row)
+  __device__ __forceinline__ void load(const SetRows& rows, const void* base, int64_t ld, int which, int t, Row (&f)[F::NC]) const {
+    const int32_t v = rows.vox[16 * t + m];
+    const T* p = static_cast<const T*>(base) + (v < 0 ? 0 : v) * ld + (which * a.heads + h) * a.hd;
+#pragma unroll
+    for (int c = 0; c < F::NC; ++c) {
+      const int d = (4 * c + g) * F::KL;
+      Row zero = {};
+      f[c] = v >= 0 && d < a.hd ? *reinterpret_cast<const Row*>(p + d) : zero;
+    }
+  }
+  // tiles of the transposed result, column m = row m of tile t: a lane holds the channels that it holds of a row fragment
+  __device__ __forceinline__ void store(const SetRows& rows, void* base, int64_t ld, int which, int t, const f32x4 (&o)[F::NT], float scale) const {
+    const int32_t v = rows.vox[16 * t + m];
+    if (v < 0) return;
+    T* p = static_cast<T*>(base) + v * ld + (which * a.heads + h) * a.hd;
+#pragma unroll
+    for (int c = 0; c < F::NC; ++c) {
+      const int d = (4 * c + g) * F::KL;
+      if (d >= a.hd) continue;
+      Row r;
+#pragma unroll
+      for (int e = 0; e < F::KL; ++e) r[e] = (T)(o[c * F::PER + e / 4][e % 4] * scale);
+      *reinterpret_cast<Row*>(p + d) = r;
+    }
+  }
+  // The unit matrix that picks channels of part `half` of a row fragment: column m is channel 8 (m / 4) + 4 half + m % 4 (KL = 8) or m.
+  __device__ __forceinline__ Row unit(int half) const {
+    Row u;
+    const int d = F::KL == 8 ? 8 * (m >> 2) + 4 * half + (m & 3) : m;
+#pragma unroll
+    for (int e = 0; e < F::KL; ++e) u[e] = (T)(F::KL * g + e == d ? 1.f : 0.f);
+    return u;
+  }
+  __device__ __forceinline__ Tile tile_unit() const {
+    Tile u;
+#pragma unroll
+    for (int e = 0; e < 4; ++e) u[e] = (T)(4 * g + e == m ? 1.f : 0.f);
+    return u;
+  }
+  // rows -> NT tile fragments: lane holds channel (of tile n) m, rows 4 g .. 4 g + 3
+  __device__ __forceinline__ void turn(const Row (&f)[F::NC], Tile (&o)[F::NT]) const {
+#pragma unroll
+    for (int n = 0; n < F::NT; ++n) o[n] = F::tile(F::row_mma(f[n / F::PER], unit(n % F::PER), f32x4{0.f, 0.f, 0.f, 0.f}));
+  }
+  __device__ __forceinline__ Tile turn(Tile f) const { return F::tile(F::tile_mma(f, tile_unit(), f32x4{0.f, 0.f, 0.f, 0.f})); }
+
+  // LDS address (in memory: byte offset in the head's table) of the entry of an offset, given as the difference of two codes plus `from`
+  __device__ __forceinline__ uint32_t from() const {
+    return (uint32_t)(a.centre * entry_bytes()) + (kForm == kByOffset ? table : kForm == kByBucket ? map : 0u);
+  }
+  __device__ __forceinline__ uint32_t entry(uint32_t at) const {
+    if constexpr (kForm == kByBucket) return table + 4u * *(lds_u16*)(uintptr_t)at;
+    if constexpr (kForm == kInMemory)
+      if (a.bucket) {
+        const unsigned r = (unsigned)*reinterpret_cast<const int32_t*>(reinterpret_cast<const char*>(a.bucket) + at);
+        return 4u * (r < (unsigned)a.n_rel ? r : (unsigned)a.n_rel);
+      }
+    return at;
+  }
+  __device__ __forceinline__ float value(uint32_t entry) const {
+    if constexpr (kForm == kInMemory)
+      return entry < 4u * (unsigned)a.n_rel ? to_units(*reinterpret_cast<const float*>(reinterpret_cast<const char*>(bias) + entry), root) : 0.f;
+    return *(lds_float*)(uintptr_t)entry;
+  }
+
+  // Probabilities of one query tile before their division by the sum: p holds the logits of kTiles key tiles in units of sigma.
+  template <int kTiles> __device__ __forceinline__ float exponentials(const SetRows& rows, f32x4 (&p)[kTiles]) const {
+    float top = -INFINITY;
+#pragma unroll
+    for (int k = 0; k < kTiles; ++k)
+#pragma unroll
+      for (int i = 0; i < 4; ++i) top = fmaxf(top, p[k][i]);
+    top = across_max(top);
+    if (top == -INFINITY) top = 0.f;              // every key is masked: no probabilities
+    const float shift = top * scale2;
+    // One fma an exponent.  Its error, half a step of `shift`, is the same for all keys of the query and so falls out; it has to
+    // be small only against the range of exp2.
+    if (__any(fabsf(shift) > 16777216.f)) {
+#pragma unroll
+      for (int k = 0; k < kTiles; ++k)
+#pragma unroll
+        for (int i = 0; i < 4; ++i) p[k][i] = __builtin_amdgcn_exp2f((p[k][i] - top) * scale2);
+    } else {
+#pragma unroll
+      for (int k = 0; k < kTiles; ++k)
+#pragma unroll
+        for (int i = 0; i < 4; ++i) p[k][i] = __builtin_amdgcn_exp2f(fmaf(p[k][i], scale2, -shift));
+    }
+    if (a.dup) {
+#pragma unroll
+      for (int k = 0; k < kTiles; ++k)
+#pragma unroll
+        for (int i = 0; i < 4; ++i) p[k][i] *= (float)rows.weight[16 * k + 4 * g + i];
+    }
+    float sum = 0.f;
+#pragma unroll
+    for (int k = 0; k < kTiles; ++k)
+#pragma unroll
+      for (int i = 0; i < 4; ++i) sum += p[k][i];
+    return across_sum(sum);
+  }
+};
+
+// Launchers; `form` as the tables are laid out (mha.hip chooses it), `lds` bytes of dynamic LDS.
+int mha_forward_bf16(const MhaArgs& a, TableForm form, size_t lds, hipStream_t st);
+int mha_forward_f32(const MhaArgs& a, TableForm form, size_t lds, hipStream_t st);
+int mha_backward_bf16(const MhaArgs& a, TableForm form, size_t lds, hipStream_t st);
+int mha_backward_f32(const MhaArgs& a, TableForm form, size_t lds, hipStream_t st);
+
+// Wavefronts of a workgroup: eight; four where a wavefront needs more than half of its SIMD's registers.
+__host__ __device__ constexpr int mha_waves(bool back, int element, int padded, int tau) {
+  return padded == 64 || (padded == 32 && tau > 48 && (back || element == 4)) ? 4 : 8;
+}
+constexpr size_t kMhaLdsMax = 140 << 10;          // dynamic LDS of a workgroup, at most
+
+extern __shared__ float mha_lds[];

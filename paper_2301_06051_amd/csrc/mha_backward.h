@@ -1,0 +1,212 @@
+// The backward kernel of dsvt_set_mha_backward (see mha.h), for the two types' own files.
+#pragma once
+#include "mha.h"
+
+namespace {
+
+// The order in which a workgroup's wavefronts add to the sums of one head, so that the sums do not depend on their speed: by the
+// place of their set in the part's sequence (`slots` sets are taken side by side, each in `tiles` query tiles) -- round, then query
+// tile, then slot.  A wavefront waits until the turn is its own; it hands on the turns of tiles that its set does not
+// have.  Every wavefront takes its turns in rising order, so the one whose turn is lowest never waits for another.  With one slot a
+// head's sums belong to one wavefront and nothing waits.
+typedef volatile __attribute__((address_space(3))) int lds_turn;
+struct Turns {
+  lds_turn* next;                                 // LDS: this head's turn
+  bool wanted;                                    // more than one slot
+  int slots, slot, tiles, done;                   // done: turns of this wavefront that are over
+  __device__ __forceinline__ int turn() const { return done * slots + slot; }
+  __device__ __forceinline__ void wait() const {
+    if (!wanted) return;
+    while (*next != turn()) __builtin_amdgcn_s_sleep(1);
+    asm volatile("" ::: "memory");
+  }
+  __device__ __forceinline__ void hand_on() {
+    if (!wanted) return;
+    asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");        // this wavefront's additions are in
+    if ((threadIdx.x & 63) == 0) *next = turn() + 1;
+    ++done;
+  }
+  // up to the first turn of round r
+  __device__ __forceinline__ void skip_to(int r) {
+    if (!wanted) return;
+    while (done < r * tiles) {
+      wait();
+      hand_on();
+    }
+  }
+};
+
+// kHold: the keys' and values' fragments of all tiles stay in registers; else they are read again, from the caches, for each query tile.
+template <typename T, int HDP, int kTiles> constexpr bool hold_rows() { return HDP <= 32 && kTiles <= 3; }
+
+template <typename T, int HDP, TableForm kForm, int kTiles>
+__device__ __forceinline__ void backward_set(const Head<T, HDP, kForm>& head, const SetRows& rows, int n, int bins, Turns& turns) {
+  typedef Frag<T, HDP> F;
+  typedef typename F::Row Row;
+  typedef typename F::Tile Tile;
+  constexpr bool kHold = hold_rows<T, HDP, kTiles>();
+  constexpr int kHeld = kHold ? kTiles : 1;
+  const MhaArgs& a = head.a;
+  const int m = head.m, g = head.g;
+  const f32x4 zero = {0.f, 0.f, 0.f, 0.f};
+  Row k[kHeld][F::NC], v[kHeld][F::NC];
+  Tile turned_k[kHeld][F::NT];
+  if constexpr (kHold) {
+#pragma unroll
+    for (int t = 0; t < kTiles; ++t) {
+      head.load(rows, a.qkv, a.ld_qkv, 1, t, k[t]);
+      head.load(rows, a.qkv, a.ld_qkv, 2, t, v[t]);
+    }
+  }
+  f32x4 dk[kTiles][F::NT] = {}, dv[kTiles][F::NT] = {};
+#pragma unroll kHold ? kTiles : 1
+  for (int qt = 0; qt < kTiles; ++qt) {
+    Row q[F::NC], go[F::NC];
+    head.load(rows, a.qkv, a.ld_qkv, 0, qt, q);
+    head.load(rows, a.d_out, a.ld_dout, 0, qt, go);
+    const uint32_t at = (uint32_t)rows.code[16 * qt + m] + head.from();
+    f32x4 p[kTiles], s[kTiles];                   // p: logits, then probabilities; s: t, then ds
+    uint32_t entry[kTiles][4];
+#pragma unroll
+    for (int t = 0; t < kTiles; ++t) {
+      if constexpr (!kHold) {
+        head.load(rows, a.qkv, a.ld_qkv, 1, t, k[0]);
+        head.load(rows, a.qkv, a.ld_qkv, 2, t, v[0]);
+      }
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        entry[t][i] = head.entry(at - (uint32_t)rows.code[16 * t + 4 * g + i]);
+        p[t][i] = head.value(entry[t][i]);
+        if (t == kTiles - 1 && 16 * t + 4 * g + i >= n) p[t][i] = -INFINITY;
+      }
+      s[t] = zero;
+#pragma unroll
+      for (int c = 0; c < F::NC; ++c) {
+        p[t] = F::row_mma(k[kHold ? t : 0][c], q[c], p[t]);
+        s[t] = F::row_mma(v[kHold ? t : 0][c], go[c], s[t]);
+      }
+    }
+    const float sum = head.template exponentials<kTiles>(rows, p), inv = sum == 0.f ? 0.f : 1.f / sum;
+    float dot = 0.f;
+#pragma unroll
+    for (int t = 0; t < kTiles; ++t)
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        p[t][i] *= inv;
+        dot = fmaf(p[t][i], s[t][i], dot);
+      }
+    dot = across_sum(dot);
+#pragma unroll
+    for (int t = 0; t < kTiles; ++t)
+#pragma unroll
+      for (int i = 0; i < 4; ++i) s[t][i] = p[t][i] * (s[t][i] - dot);
+    if (a.partial) {
+      turns.wait();
+      if (qt + 1 < kTiles || 16 * qt + m < n) {
+#pragma unroll
+        for (int t = 0; t < kTiles; ++t)
+#pragma unroll
+          for (int i = 0; i < 4; ++i)
+            if (t + 1 < kTiles || 16 * t + 4 * g + i < n)
+              __hip_atomic_fetch_add((lds_float*)(uintptr_t)(entry[t][i] + bins), s[t][i], __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_WORKGROUP);
+      }
+      turns.hand_on();
+    }
+    if constexpr (kHold) {
+      if (qt == 0) {
+#pragma unroll
+        for (int t = 0; t < kTiles; ++t) head.turn(k[t], turned_k[t]);
+      }
+    }
+    f32x4 dq[F::NT] = {};
+    Tile turned_q[F::NT], turned_g[F::NT];
+    head.turn(q, turned_q);
+    head.turn(go, turned_g);
+#pragma unroll
+    for (int t = 0; t < kTiles; ++t) {
+      if constexpr (!kHold) {
+        head.load(rows, a.qkv, a.ld_qkv, 1, t, k[0]);
+        head.turn(k[0], turned_k[0]);
+      }
+      const Tile ds = F::tile(s[t]), ds_t = head.turn(ds), p_t = head.turn(F::tile(p[t]));
+#pragma unroll
+      for (int c = 0; c < F::NT; ++c) {
+        dq[c] = F::tile_mma(turned_k[kHold ? t : 0][c], ds, dq[c]);
+        dk[t][c] = F::tile_mma(turned_q[c], ds_t, dk[t][c]);
+        dv[t][c] = F::tile_mma(turned_g[c], p_t, dv[t][c]);
+      }
+    }
+    head.store(rows, a.out, a.ld_out, 0, qt, dq, a.scale);
+  }
+#pragma unroll
+  for (int t = 0; t < kTiles; ++t) {
+    head.store(rows, a.out, a.ld_out, 1, t, dk[t], a.scale);
+    head.store(rows, a.out, a.ld_out, 2, t, dv[t], 1.f);
+  }
+}
+
+// Dynamic LDS: the sums of the table's gradient [hs][entries] if they are wanted, the table [hs][entries] unless it stays in memory, the
+// offsets' buckets.
+template <typename T, int HDP, TableForm kForm, int kTilesMax>
+__global__ __launch_bounds__(64 * mha_waves(true, sizeof(T), HDP, 16 * kTilesMax)) void k_mha_backward(MhaArgs a) {
+  __shared__ SetRows sets[kBatch];
+  __shared__ int next_turn[8];
+  const Share share(a);
+  const int wave = threadIdx.x >> 6, waves = blockDim.x >> 6, h0 = share.group * a.hs, all = a.hs * a.entries;
+  float* table = mha_lds + (a.partial ? all : 0);
+  uint16_t* map = reinterpret_cast<uint16_t*>(table + all);
+  fill_tables<kForm>(a, h0, table, map);
+  if (a.partial)
+    for (int u = threadIdx.x; u < all; u += blockDim.x) mha_lds[u] = 0.f;
+  if (threadIdx.x < 8) next_turn[threadIdx.x] = 0;
+  const int slot = wave / a.hs, hl = wave - slot * a.hs;
+  const Head<T, HDP, kForm> head(a, table + hl * a.entries, map, h0 + hl);
+  // from an entry's address to its sum's
+  const int bins = kForm == kInMemory ? (int)lds_address(mha_lds + hl * a.entries) : -4 * all;
+  Turns turns = {(lds_turn*)(next_turn + hl), a.partial && a.slots > 1, a.slots, slot, (a.tau + 15) >> 4, 0};
+  const int32_t n_sets = sets_of(a);
+  int round = 0;                                  // of `slots` sets, over all batches (kBatch is a multiple of slots)
+  for (int32_t s0 = share.part; s0 < n_sets; s0 += kBatch * a.parts) {
+    __syncthreads();
+    for (int b = wave; b < kBatch && s0 + b * a.parts < n_sets; b += waves) load_set(a, s0 + b * a.parts, head.entry_bytes(), sets[b]);
+    __syncthreads();
+    for (int b = slot; b < kBatch && s0 + (b - slot) * a.parts < n_sets; b += a.slots, ++round) {
+      turns.skip_to(round);
+      if (s0 + b * a.parts >= n_sets) continue;
+      const int n = __builtin_amdgcn_readfirstlane(sets[b].n);
+      switch ((n + 15) >> 4) {
+        case 1: backward_set<T, HDP, kForm, 1>(head, sets[b], n, bins, turns); break;
+        case 2: backward_set<T, HDP, kForm, 2>(head, sets[b], n, bins, turns); break;
+        case 3: backward_set<T, HDP, kForm, 3>(head, sets[b], n, bins, turns); break;
+        case 4: if constexpr (kTilesMax > 3) backward_set<T, HDP, kForm, 4>(head, sets[b], n, bins, turns); break;
+        case 5: if constexpr (kTilesMax > 3) backward_set<T, HDP, kForm, 5>(head, sets[b], n, bins, turns); break;
+        case 6: if constexpr (kTilesMax > 3) backward_set<T, HDP, kForm, 6>(head, sets[b], n, bins, turns); break;
+      }
+    }
+    turns.skip_to(round);                         // nobody waits for this wavefront at the barrier
+  }
+  if (!a.partial) return;
+  __syncthreads();
+  if (share.part < n_sets)                        // k_mha_entries reads the parts that had a set
+    for (int u = threadIdx.x; u < all; u += blockDim.x) a.partial[((int64_t)share.part * a.heads + h0) * a.entries + u] = mha_lds[u];
+}
+
+template <typename T, int HDP, TableForm kForm, int kTilesMax> int launch(const MhaArgs& a, size_t lds, hipStream_t st) {
+  static std::atomic<uint64_t> allowed;
+  if (const int rc = dsvt_allow_lds(reinterpret_cast<const void*>(k_mha_backward<T, HDP, kForm, kTilesMax>), kMhaLdsMax, allowed)) return rc;
+  dsvt_prof_scope ps(DSVT_K_MHA_BACKWARD, st);
+  k_mha_backward<T, HDP, kForm, kTilesMax><<<(unsigned)(a.groups * a.parts), 64 * a.hs * a.slots, lds, st>>>(a);
+  return DSVT_OK;
+}
+template <typename T, int HDP> int launch(const MhaArgs& a, TableForm form, size_t lds, hipStream_t st) {
+  if (a.tau <= 48)
+    return form == kByOffset ? launch<T, HDP, kByOffset, 3>(a, lds, st) : form == kByBucket ? launch<T, HDP, kByBucket, 3>(a, lds, st)
+                                                                                            : launch<T, HDP, kInMemory, 3>(a, lds, st);
+  return form == kByOffset ? launch<T, HDP, kByOffset, 6>(a, lds, st) : form == kByBucket ? launch<T, HDP, kByBucket, 6>(a, lds, st)
+                                                                                          : launch<T, HDP, kInMemory, 6>(a, lds, st);
+}
+template <typename T> int launch(const MhaArgs& a, TableForm form, size_t lds, hipStream_t st) {
+  return a.hd <= 16 ? launch<T, 16>(a, form, lds, st) : a.hd <= 32 ? launch<T, 32>(a, form, lds, st) : launch<T, 64>(a, form, lds, st);
+}
+
+}  // namespace

@@ -1,0 +1,102 @@
+// The forward kernel of dsvt_set_mha (see mha.h), for the two types' own files.
+#pragma once
+#include "mha.h"
+
+namespace {
+
+// All of a set's rows of one head sit in registers: n voxels, kTiles tiles of 16.
+template <typename T, int HDP, TableForm kForm, int kTiles>
+__device__ __forceinline__ void forward_set(const Head<T, HDP, kForm>& head, const SetRows& rows, int n) {
+  typedef Frag<T, HDP> F;
+  const MhaArgs& a = head.a;
+  const int m = head.m, g = head.g;
+  typename F::Row k[kTiles][F::NC], v[kTiles][F::NC];
+  typename F::Tile vt[kTiles][F::NT];
+#pragma unroll
+  for (int t = 0; t < kTiles; ++t) {
+    head.load(rows, a.qkv, a.ld_qkv, 1, t, k[t]);
+    head.load(rows, a.qkv, a.ld_qkv, 2, t, v[t]);
+  }
+  typename F::Row q[2][F::NC];
+  head.load(rows, a.qkv, a.ld_qkv, 0, 0, q[0]);
+  uint32_t key[kTiles][4];
+#pragma unroll
+  for (int t = 0; t < kTiles; ++t)
+#pragma unroll
+    for (int i = 0; i < 4; ++i) key[t][i] = (uint32_t)rows.code[16 * t + 4 * g + i];
+#pragma unroll
+  for (int qt = 0; qt < kTiles; ++qt) {
+    if (qt + 1 < kTiles) head.load(rows, a.qkv, a.ld_qkv, 0, qt + 1, q[(qt + 1) & 1]);
+    const uint32_t at = (uint32_t)rows.code[16 * qt + m] + head.from();
+    f32x4 p[kTiles];
+#pragma unroll
+    for (int t = 0; t < kTiles; ++t) {
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        p[t][i] = head.value(head.entry(at - key[t][i]));
+        if (t == kTiles - 1 && 16 * t + 4 * g + i >= n) p[t][i] = -INFINITY;
+      }
+#pragma unroll
+      for (int c = 0; c < F::NC; ++c) p[t] = F::row_mma(k[t][c], q[qt & 1][c], p[t]);
+    }
+    const float sum = head.template exponentials<kTiles>(rows, p);
+    if (qt == 0) {
+#pragma unroll
+      for (int t = 0; t < kTiles; ++t) head.turn(v[t], vt[t]);
+    }
+    f32x4 o[F::NT] = {};
+#pragma unroll
+    for (int t = 0; t < kTiles; ++t)
+#pragma unroll
+      for (int c = 0; c < F::NT; ++c) o[c] = F::tile_mma(vt[t][c], F::tile(p[t]), o[c]);
+    head.store(rows, a.out, a.ld_out, 0, qt, o, sum == 0.f ? 0.f : 1.f / sum);
+  }
+}
+
+template <typename T, int HDP, TableForm kForm, int kTilesMax>
+__global__ __launch_bounds__(64 * mha_waves(false, sizeof(T), HDP, 16 * kTilesMax)) void k_mha_forward(MhaArgs a) {
+  __shared__ SetRows sets[kBatch];
+  const Share share(a);
+  const int wave = threadIdx.x >> 6, waves = blockDim.x >> 6, h0 = share.group * a.hs;
+  uint16_t* map = reinterpret_cast<uint16_t*>(mha_lds + a.hs * a.entries);
+  fill_tables<kForm>(a, h0, mha_lds, map);
+  const int slot = wave / a.hs, hl = wave - slot * a.hs;
+  const Head<T, HDP, kForm> head(a, mha_lds + hl * a.entries, map, h0 + hl);
+  const int32_t n_sets = sets_of(a);
+  for (int32_t s0 = share.part; s0 < n_sets; s0 += kBatch * a.parts) {
+    __syncthreads();
+    for (int b = wave; b < kBatch && s0 + b * a.parts < n_sets; b += waves) load_set(a, s0 + b * a.parts, head.entry_bytes(), sets[b]);
+    __syncthreads();
+    for (int b = slot; b < kBatch && s0 + b * a.parts < n_sets; b += a.slots) {
+      const int n = __builtin_amdgcn_readfirstlane(sets[b].n);
+      switch ((n + 15) >> 4) {
+        case 1: forward_set<T, HDP, kForm, 1>(head, sets[b], n); break;
+        case 2: forward_set<T, HDP, kForm, 2>(head, sets[b], n); break;
+        case 3: forward_set<T, HDP, kForm, 3>(head, sets[b], n); break;
+        case 4: if constexpr (kTilesMax > 3) forward_set<T, HDP, kForm, 4>(head, sets[b], n); break;
+        case 5: if constexpr (kTilesMax > 3) forward_set<T, HDP, kForm, 5>(head, sets[b], n); break;
+        case 6: if constexpr (kTilesMax > 3) forward_set<T, HDP, kForm, 6>(head, sets[b], n); break;
+      }
+    }
+  }
+}
+
+template <typename T, int HDP, TableForm kForm, int kTilesMax> int launch(const MhaArgs& a, size_t lds, hipStream_t st) {
+  static std::atomic<uint64_t> allowed;
+  if (const int rc = dsvt_allow_lds(reinterpret_cast<const void*>(k_mha_forward<T, HDP, kForm, kTilesMax>), kMhaLdsMax, allowed)) return rc;
+  dsvt_prof_scope ps(DSVT_K_MHA_FORWARD, st);
+  k_mha_forward<T, HDP, kForm, kTilesMax><<<(unsigned)(a.groups * a.parts), 64 * a.hs * a.slots, lds, st>>>(a);
+  return DSVT_OK;
+}
+template <typename T, int HDP> int launch(const MhaArgs& a, TableForm form, size_t lds, hipStream_t st) {
+  if (a.tau <= 48)
+    return form == kByOffset ? launch<T, HDP, kByOffset, 3>(a, lds, st) : form == kByBucket ? launch<T, HDP, kByBucket, 3>(a, lds, st)
+                                                                                            : launch<T, HDP, kInMemory, 3>(a, lds, st);
+  return form == kByOffset ? launch<T, HDP, kByOffset, 6>(a, lds, st) : form == kByBucket ? launch<T, HDP, kByBucket, 6>(a, lds, st)
+                                                                                          : launch<T, HDP, kInMemory, 6>(a, lds, st);
+}
+template <typename T> int launch(const MhaArgs& a, TableForm form, size_t lds, hipStream_t st) {
+  return a.hd <= 16 ? launch<T, 16>(a, form, lds, st) : a.hd <= 32 ? launch<T, 32>(a, form, lds, st) : launch<T, 64>(a, form, lds, st);
+}
+
+}  // namespace

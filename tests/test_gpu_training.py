@@ -185,8 +185,8 @@ def test_set_mha_buckets_outside_the_table_are_no_term():
     _run(coords, maps, win, c, heads, "bf16", qkv, d_out, table, bucket, case="buckets out of range")
 
 
-def test_set_mha_voxels_further_apart_than_a_window_have_no_term():
-    """Maps built with another window than the table's: offsets past the table give no term, and nothing is read or added outside it."""
+def test_set_mha_sets_that_fit_no_window_take_the_term_of_offset_0():
+    """Maps built with another window than the table's: nothing is read or added outside it."""
     n, c, heads, win = 200, 64, 4, (3, 3, 1)
     coords = _frame(15, (60, 60, 1), n)
     maps = gpu_maps(coords.cuda(), (60, 60, 1), (30, 30, 1), (0, 0, 0), 36, 1, 0)

@@ -62,7 +62,9 @@ def mha(qkv, sets, coords, win, heads, table, bucket, d_out=None):
             for axis, w in enumerate(win):
                 lin = lin * (2 * w - 1) + (p[:, None, axis] - p[None, :, axis]) + w - 1
                 count *= 2 * w - 1
-            index = np.where((lin >= 0) & (lin < count), lin, -1)
+            if any(np.ptp(p[:, axis]) >= w for axis, w in enumerate(win)):
+                lin[:] = count // 2                 # not one window's voxels: the term of offset 0 for all pairs
+            index = lin
             if bucket is not None:
                 e = bucket.numpy()[np.clip(index, 0, None)]
                 index = np.where((index >= 0) & (e >= 0) & (e < b_all.shape[1]), e, -1)
