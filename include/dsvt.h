@@ -361,15 +361,14 @@ int dsvt_rel_buckets(const int32_t win[3], int32_t n_exact, int32_t n_side, int3
  * maps: set_inds, n_sets, max_sets, tau and n_voxels are read (set slots outside 0 .. n_voxels - 1 are empty; repeats of a
  * voxel are neighbours and every voxel is in one set, as dsvt_partition writes them).  coords as there.
  * Supported: d a multiple of 8 up to 64, tau <= 96 (DSVT_EUNSUPPORTED otherwise), F32 and BF16; qkv, out and coords 16-byte
- * aligned, row strides multiples of 16 bytes (DSVT_EINVAL otherwise). */
+ * aligned, row strides multiples of 16 bytes and below 4 GiB (DSVT_EINVAL otherwise); fewer than 2^24 offsets and biases a head. */
 int dsvt_set_mha(const dsvt_mha_cfg* cfg, const dsvt_maps* maps, const int32_t* coords, const void* qkv, int64_t ld_qkv,
                  void* out, int64_t ld_out, void* stream);
 
 /* The gradients, from that of out: d_qkv [device] [n_voxels, 3C] and d_rel_bias [device] [heads, n_rel] float (NULL: not
  * wanted), both written, not added to; rows of voxels in no set stay as they are.  Nothing but the inputs is needed from the forward
  * call.  ws [device] 16-byte aligned, of the bytes that dsvt_set_mha_backward_workspace_size reports (none
- * without d_rel_bias); no state is kept in it.  Supported as above, rows of d_out and d_qkv aligned likewise; d_rel_bias: at most 35,840
- * entries a head (35,839 with buckets).  The results do not depend on the order in which the kernels run. */
+ * without d_rel_bias); no state is kept in it.  Supported as above, rows of d_out and d_qkv aligned likewise.  The results do not depend on the order in which the kernels run. */
 int dsvt_set_mha_backward_workspace_size(const dsvt_mha_cfg* cfg, const dsvt_maps* maps, size_t* bytes);
 int dsvt_set_mha_backward(const dsvt_mha_cfg* cfg, const dsvt_maps* maps, const int32_t* coords, const void* qkv, int64_t ld_qkv,
                           const void* d_out, int64_t ld_dout, void* d_qkv, int64_t ld_dqkv, float* d_rel_bias,

@@ -39,11 +39,12 @@ struct MhaArgs {
   const float* bias;                              // [heads][n_rel] or null
   const int32_t* bucket;                          // [n_off] or null
   float* partial;                                 // backward: [parts][heads][entries]; null: no gradient of the table
-  int64_t ld_qkv, ld_dout, ld_out;
+  uint32_t ld_qkv, ld_dout, ld_out;               // row strides in bytes
   int32_t n_voxels, max_sets, tau, heads, hd;
   int32_t n_off, n_rel, entries;                  // offsets; biases of a head; values of a head in LDS
   int32_t w[3], centre;                           // the window; the number of offset 0
   int32_t dup, hs, slots, groups, parts;          // heads of a workgroup, sets it takes side by side, groups of heads, workgroups a group
+  int32_t ranges;                                 // backward: workgroups that share a head's entries (each goes through all sets)
   float scale;
 };
 
@@ -65,7 +66,7 @@ template <int HDP> struct Frag<bf16_t, HDP> {
     if constexpr (KL == 8) return __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, b, c, 0, 0, 0);
     else return tile_mma(a, b, c);
   }
-  static __device__ __forceinline__ Tile tile(f32x4 v) { return Tile{(bf16_t)v[0], (bf16_t)v[1], (bf16_t)v[2], (bf16_t)v[3]}; }
+  static __device__ __forceinline__ Tile tile(f32x4 v) { return __builtin_convertvector(v, Tile); }
 };
 template <int HDP> struct Frag<float, HDP> {
   static constexpr int KL = 4, NC = HDP / 16, NT = HDP / 16, PER = 1;
@@ -91,9 +92,9 @@ __device__ __forceinline__ float to_units(float b, float root) {
   return fabsf(b) <= FLT_MAX ? fminf(fmaxf(b, -1.0e37f), 1.0e37f) * root : b;
 }
 
-// What a workgroup knows of a set, in LDS.  Row r is the set's r-th voxel; rows up to the next multiple of 16 have no voxel (-1), the
-// code of row 0 and weight 0.  code: the cell's number times the bytes of an entry, so that the difference of two codes is an
-// offset's place in a table.
+// What a workgroup knows of a set, in LDS.  Row r is the set's r-th voxel; rows up to the next multiple of 16 repeat row 0 with
+// weight 0: they are read like others, and masked where they would count.  code: the cell's number times the bytes of an entry, so that the
+// difference of two codes is an offset's place in a table.
 struct SetRows {
   int32_t vox[kSetMax], code[kSetMax], weight[kSetMax];
   int32_t n;
@@ -116,7 +117,7 @@ __device__ __forceinline__ void load_set(const MhaArgs& a, int32_t s, int entry_
   const int32_t* inds = a.set_inds + (int64_t)s * a.tau;
   int32_t v[2];
   uint64_t first[2], change[2];
-  int4 c[2];
+  int4 c[2] = {};
   int32_t before = -1;
 #pragma unroll
   for (int k = 0; k < 2; ++k) {
@@ -150,9 +151,14 @@ __device__ __forceinline__ void load_set(const MhaArgs& a, int32_t s, int entry_
 #pragma unroll
   for (int x = 0; x < 3; ++x) fits = fits && (int64_t)wave_max(hi[x]) + wave_max(lo[x]) + 2 <= a.w[x];
   const int n0 = __popcll(first[0]), n = n0 + __popcll(first[1]);
-  const int w2 = 2 * a.w[1] - 1, h2 = 2 * a.w[2] - 1;
+  if (lane == 0) rows.n = n;
+  if (n == 0) return;
+  const uint32_t w2 = 2 * a.w[1] - 1, h2 = 2 * a.w[2] - 1;
+  uint32_t code[2];
 #pragma unroll
-  for (int k = 0; k < 2; ++k)
+  for (int k = 0; k < 2; ++k) {
+    // (unsigned: a far cell's number may pass 32 bits, the differences inside a window do not)
+    code[k] = fits ? (((uint32_t)c[k].y * w2 + (uint32_t)c[k].z) * h2 + (uint32_t)c[k].w) * entry_bytes : 0;
     if (first[k] >> lane & 1) {
       const int r = (k ? n0 : 0) + __popcll(first[k] & ((1ull << lane) - 1));
       const uint64_t later = lane == 63 ? 0 : change[k] >> (lane + 1);      // slots to the next change
@@ -160,21 +166,18 @@ __device__ __forceinline__ void load_set(const MhaArgs& a, int32_t s, int entry_
       if (later) run = 1 + __builtin_ctzll(later);
       else if (k == 0) run = 64 - lane + (change[1] ? __builtin_ctzll(change[1]) : 64);
       else run = 64 - lane;
-      // (unsigned: a far cell's number may pass 32 bits, the differences inside a window do not)
-      const uint32_t code = fits ? (((uint32_t)c[k].y * w2 + (uint32_t)c[k].z) * h2 + (uint32_t)c[k].w) * entry_bytes : 0;
       rows.vox[r] = v[k];
-      rows.code[r] = (int32_t)code;
+      rows.code[r] = (int32_t)code[k];
       rows.weight[r] = a.dup ? run : 1;
-      if (r == 0) {
-        const int pad = (n + 15) & ~15;
-        for (int p = n; p < pad; ++p) rows.code[p] = (int32_t)code;
-      }
     }
+  }
+  const int k0 = first[0] ? 0 : 1, l0 = __builtin_ctzll(first[k0]);
+  const int32_t vox0 = __shfl(k0 ? v[1] : v[0], l0, 64), code0 = __shfl((int32_t)(k0 ? code[1] : code[0]), l0, 64);
   if (n + lane < ((n + 15) & ~15)) {
-    rows.vox[n + lane] = -1;
+    rows.vox[n + lane] = vox0;
+    rows.code[n + lane] = code0;
     rows.weight[n + lane] = 0;
   }
-  if (lane == 0) rows.n = n;
 }
 
 // Workgroup b takes group of heads b / 8 % groups and is part (b / 8 / groups) * 8 + b % 8 of it: workgroups that take other heads of
@@ -229,30 +232,38 @@ template <typename T, int HDP, TableForm kForm> struct Head {
         g(threadIdx.x >> 4 & 3), h(h_), root(sqrtf((float)a_.hd)), scale2(a_.scale * kLog2e) {}
   static constexpr int entry_bytes() { return kForm == kByBucket ? 2 : 4; }
 
-  // rows of tile t of an array of head vectors (which: 0 q, 1 k, 2 v of a qkv row; 0 of an output row)
-  __device__ __forceinline__ void load(const SetRows& rows, const void* base, int64_t ld, int which, int t, Row (&f)[F::NC]) const {
-    const int32_t v = rows.vox[16 * t + m];
-    const T* p = static_cast<const T*>(base) + (v < 0 ? 0 : v) * ld + (which * a.heads + h) * a.hd;
+  // A lane's first channel of part c of a row fragment; lanes past the head's last channel take its first ones.
+  __device__ __forceinline__ int channel(int c) const {
+    const int d = (4 * c + g) * F::KL;
+    return d < a.hd ? d : 0;
+  }
+  __device__ __forceinline__ const char* row(const SetRows& rows, const void* base, uint32_t ld, int which, int t) const {
+    return static_cast<const char*>(base) + (int64_t)(which * a.heads + h) * a.hd * (int)sizeof(T) + (uint64_t)(uint32_t)rows.vox[16 * t + m] * ld;
+  }
+  // Rows of tile t of an array of head vectors (which: 0 q, 1 k, 2 v of a qkv row; 0 of an output row).  Of two operands whose product
+  // runs over the channels one has zeros past the last (kZero).
+  template <bool kZero> __device__ __forceinline__ void load(const SetRows& rows, const void* base, uint32_t ld, int which, int t, Row (&f)[F::NC]) const {
+    const char* p = row(rows, base, ld, which, t);
 #pragma unroll
     for (int c = 0; c < F::NC; ++c) {
-      const int d = (4 * c + g) * F::KL;
-      Row zero = {};
-      f[c] = v >= 0 && d < a.hd ? *reinterpret_cast<const Row*>(p + d) : zero;
+      f[c] = *reinterpret_cast<const Row*>(p + channel(c) * (int)sizeof(T));
+      if constexpr (kZero) {
+        const Row zero = {};
+        f[c] = (4 * c + g) * F::KL < a.hd ? f[c] : zero;
+      }
     }
   }
-  // tiles of the transposed result, column m = row m of tile t: a lane holds the channels that it holds of a row fragment
-  __device__ __forceinline__ void store(const SetRows& rows, void* base, int64_t ld, int which, int t, const f32x4 (&o)[F::NT], float scale) const {
-    const int32_t v = rows.vox[16 * t + m];
-    if (v < 0) return;
-    T* p = static_cast<T*>(base) + v * ld + (which * a.heads + h) * a.hd;
+  // tiles of the transposed result, column m = row m of tile t, if `there`: a lane holds the channels that it holds of a row fragment
+  __device__ __forceinline__ void store(const SetRows& rows, void* base, uint32_t ld, int which, int t, bool there, const f32x4 (&o)[F::NT],
+                                        float scale) const {
+    char* p = const_cast<char*>(row(rows, base, ld, which, t));
 #pragma unroll
     for (int c = 0; c < F::NC; ++c) {
-      const int d = (4 * c + g) * F::KL;
-      if (d >= a.hd) continue;
-      Row r;
+      typedef float Wide __attribute__((ext_vector_type(F::KL)));
+      Wide r;
 #pragma unroll
-      for (int e = 0; e < F::KL; ++e) r[e] = (T)(o[c * F::PER + e / 4][e % 4] * scale);
-      *reinterpret_cast<Row*>(p + d) = r;
+      for (int e = 0; e < F::KL; ++e) r[e] = o[c * F::PER + e / 4][e % 4] * scale;
+      if (there && (4 * c + g) * F::KL < a.hd) *reinterpret_cast<Row*>(p + channel(c) * (int)sizeof(T)) = __builtin_convertvector(r, Row);
     }
   }
   // The unit matrix that picks channels of part `half` of a row fragment: column m is channel 8 (m / 4) + 4 half + m % 4 (KL = 8) or m.
@@ -345,4 +356,4 @@ __host__ __device__ constexpr int mha_waves(bool back, int element, int padded, 
 }
 constexpr size_t kMhaLdsMax = 140 << 10;          // dynamic LDS of a workgroup, at most
 
-extern __shared__ float mha_lds[];
+extern __shared__ double mha_lds[];

@@ -5,7 +5,6 @@
 namespace {
 
 constexpr int kGroups = 512;                      // workgroups that a launch aims at: two a compute unit
-constexpr int kSetsPerPart = 256;                 // sets of a backward workgroup, at most: more would cost its 32-bit sums digits
 
 // The parts' sums of the table's gradient added in their order: 64 columns of [heads * entries] a workgroup, 16 slices of the parts.  Entries
 // from n_out on (offsets without a bias) are dropped.
@@ -32,10 +31,11 @@ __global__ __launch_bounds__(1024) void k_mha_entries(const float* __restrict__ 
 // copies are added in theirs.
 __global__ __launch_bounds__(1024) void k_mha_buckets(const float* __restrict__ by_offset, const int32_t* __restrict__ bucket, int32_t n_off,
                                                       int32_t n_rel, float* __restrict__ d_bias) {
+  float* buckets = reinterpret_cast<float*>(mha_lds);
   const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63, waves = blockDim.x >> 6;
-  for (int u = threadIdx.x; u < waves * n_rel; u += blockDim.x) mha_lds[u] = 0.f;
+  for (int u = threadIdx.x; u < waves * n_rel; u += blockDim.x) buckets[u] = 0.f;
   __syncthreads();
-  float* mine = mha_lds + wave * n_rel;
+  float* mine = buckets + wave * n_rel;
   const int per = ((n_off + waves - 1) / waves + 63) & ~63, end = (wave + 1) * per < n_off ? (wave + 1) * per : n_off;
   for (int u = wave * per + lane; u < end; u += 64) {
     const unsigned b = (unsigned)bucket[u];
@@ -44,7 +44,7 @@ __global__ __launch_bounds__(1024) void k_mha_buckets(const float* __restrict__ 
   __syncthreads();
   for (int u = threadIdx.x; u < n_rel; u += blockDim.x) {
     double v = 0.;
-    for (int w = 0; w < waves; ++w) v += (double)mha_lds[w * n_rel + u];
+    for (int w = 0; w < waves; ++w) v += (double)buckets[w * n_rel + u];
     d_bias[(int64_t)blockIdx.x * n_rel + u] = (float)v;
   }
 }
@@ -56,7 +56,7 @@ __global__ void k_mha_zero(float* __restrict__ p, int64_t n) {
 
 struct Plan {
   TableForm form;
-  int32_t hs, slots, parts, n_off, entries;
+  int32_t hs, slots, ranges, parts, n_off, entries;
   size_t lds, ws;
 };
 
@@ -64,10 +64,9 @@ int64_t offsets_of(const dsvt_mha_cfg* c) {
   return (2 * (int64_t)c->win[0] - 1) * (2 * (int64_t)c->win[1] - 1) * (2 * (int64_t)c->win[2] - 1);
 }
 
-// LDS of a workgroup of hs heads with its table in this form.
-size_t lds_bytes(TableForm form, int hs, bool bins, int64_t entries, int64_t n_off) {
-  const size_t values = (size_t)hs * entries * 4;
-  return (bins ? values : 0) + (form == kInMemory ? 0 : values) + (form == kByBucket ? dsvt_align_up((size_t)n_off * 2, 4) : 0);
+// LDS of a workgroup of hs heads with its table in this form; bins: sums of this many entries a head.
+size_t lds_bytes(TableForm form, int hs, int64_t bins, int64_t entries, int64_t n_off) {
+  return (size_t)hs * bins * 8 + (form == kInMemory ? 0 : (size_t)hs * entries * 4) + (form == kByBucket ? dsvt_align_up((size_t)n_off * 2, 4) : 0);
 }
 
 int make_plan(const dsvt_mha_cfg* c, int32_t max_sets, int32_t tau, bool back, bool d_bias, Plan* p) {
@@ -93,23 +92,26 @@ int make_plan(const dsvt_mha_cfg* c, int32_t max_sets, int32_t tau, bool back, b
     const int64_t entries = f == kByOffset || !by_bucket ? n_off : (int64_t)c->n_rel + 1;
     int hs = 0;
     for (int h = 1; h <= waves; ++h)
-      if (c->heads % h == 0 && lds_bytes(f, h, d_bias, entries, n_off) <= kMhaLdsMax) hs = h;
-    if (hs <= p->hs) continue;
+      if (c->heads % h == 0 && lds_bytes(f, h, d_bias ? entries : 0, entries, n_off) <= kMhaLdsMax) hs = h;
+    if (hs <= p->hs && (p->hs > 0 || f != kInMemory)) continue;
     p->form = f;
     p->hs = hs;
     p->entries = (int32_t)entries;
   }
-  if (p->hs == 0) return DSVT_EUNSUPPORTED;
+  // Sums that the LDS of a workgroup does not hold for one head: workgroups of a head share its entries, and each goes through all sets.
+  p->ranges = 1;
+  if (p->hs == 0) {
+    p->hs = 1;
+    p->ranges = (int32_t)dsvt_ceil_div((int64_t)p->entries * 8, kMhaLdsMax);
+  }
   const bool fold = d_bias && by_bucket && p->form == kByOffset;
   if (fold && (size_t)c->n_rel * 4 > kMhaLdsMax) return DSVT_EUNSUPPORTED;
   p->n_off = (int32_t)n_off;
-  p->lds = lds_bytes(p->form, p->hs, d_bias, p->entries, n_off);
+  p->lds = lds_bytes(p->form, p->hs, d_bias ? dsvt_ceil_div(p->entries, p->ranges) : 0, p->entries, n_off);
   p->slots = 1;
   while (2 * p->slots * p->hs <= waves) p->slots *= 2;
   static_assert(kBatch % 8 == 0, "a batch is a whole number of rounds");
-  const int32_t groups = c->heads / p->hs;
-  int64_t parts = dsvt_ceil_div(kGroups, groups);
-  if (back && parts < dsvt_ceil_div(max_sets, kSetsPerPart)) parts = dsvt_ceil_div(max_sets, kSetsPerPart);
+  int64_t parts = dsvt_ceil_div(kGroups, c->heads / p->hs * p->ranges);
   if (parts > max_sets) parts = max_sets;
   p->parts = (int32_t)dsvt_align_up((size_t)(parts > 0 ? parts : 1), 8);
   p->ws = d_bias ? ((size_t)p->parts + fold) * c->heads * (size_t)p->entries * 4 : 0;
@@ -117,7 +119,7 @@ int make_plan(const dsvt_mha_cfg* c, int32_t max_sets, int32_t tau, bool back, b
 }
 
 bool bad_rows(const void* p, int64_t ld, int64_t width, int e) {
-  return !p || ((uintptr_t)p & 15u) != 0 || ld < width || (ld * e) % 16 != 0;
+  return !p || ((uintptr_t)p & 15u) != 0 || ld < width || ld > UINT32_MAX / e || (ld * e) % 16 != 0;
 }
 
 int check_maps(const dsvt_maps* maps) {
@@ -134,7 +136,7 @@ MhaArgs make_args(const dsvt_mha_cfg* c, const dsvt_maps* maps, const int32_t* c
   a.n_off = p.n_off; a.n_rel = c->rel_bias ? c->n_rel : 0; a.entries = p.entries;
   for (int i = 0; i < 3; ++i) a.w[i] = c->win[i];
   a.centre = c->rel_bias ? ((c->win[0] - 1) * (2 * c->win[1] - 1) + c->win[1] - 1) * (2 * c->win[2] - 1) + c->win[2] - 1 : 0;
-  a.dup = c->dup_mode; a.hs = p.hs; a.slots = p.slots; a.groups = c->heads / p.hs; a.parts = p.parts;
+  a.dup = c->dup_mode; a.hs = p.hs; a.slots = p.slots; a.groups = c->heads / p.hs * p.ranges; a.ranges = p.ranges; a.parts = p.parts;
   a.scale = 1.f / sqrtf((float)a.hd);
   return a;
 }
@@ -177,7 +179,7 @@ extern "C" int dsvt_set_mha(const dsvt_mha_cfg* cfg, const dsvt_maps* maps, cons
   const int e = cfg->dtype == DSVT_BF16 ? 2 : 4;
   if (!coords || ((uintptr_t)coords & 15u) || bad_rows(qkv, ld_qkv, 3 * (int64_t)cfg->C, e) || bad_rows(out, ld_out, cfg->C, e)) return DSVT_EINVAL;
   MhaArgs a = make_args(cfg, maps, coords, p);
-  a.qkv = qkv; a.ld_qkv = ld_qkv; a.out = out; a.ld_out = ld_out;
+  a.qkv = qkv; a.ld_qkv = (uint32_t)(ld_qkv * e); a.out = out; a.ld_out = (uint32_t)(ld_out * e);
   hipStream_t st = (hipStream_t)stream;
   if (const int rc = cfg->dtype == DSVT_BF16 ? mha_forward_bf16(a, p.form, p.lds, st) : mha_forward_f32(a, p.form, p.lds, st)) return rc;
   DSVT_HIP_TRY(hipGetLastError());
@@ -215,7 +217,7 @@ extern "C" int dsvt_set_mha_backward(const dsvt_mha_cfg* cfg, const dsvt_maps* m
   if (p.ws > 0 && (!ws || ((uintptr_t)ws & 15u))) return DSVT_EINVAL;
   if (ws_bytes < p.ws) return DSVT_ENOSPC;
   MhaArgs a = make_args(cfg, maps, coords, p);
-  a.qkv = qkv; a.ld_qkv = ld_qkv; a.d_out = d_out; a.ld_dout = ld_dout; a.out = d_qkv; a.ld_out = ld_dqkv;
+  a.qkv = qkv; a.ld_qkv = (uint32_t)(ld_qkv * e); a.d_out = d_out; a.ld_dout = (uint32_t)(ld_dout * e); a.out = d_qkv; a.ld_out = (uint32_t)(ld_dqkv * e);
   a.partial = d_rel_bias ? static_cast<float*>(ws) : nullptr;
   const bool fold = d_rel_bias && cfg->rel_bucket && p.form == kByOffset;
   static std::atomic<uint64_t> allowed;

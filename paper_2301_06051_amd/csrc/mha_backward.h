@@ -36,11 +36,27 @@ struct Turns {
   }
 };
 
+// A head's sums of the table's gradient in LDS, 64 bits each: the additions of a wavefront take 9 to 26 clocks of the LDS, those of
+// 32-bit floats take 193 (1 lane in three clocks), read with 64 lanes on consecutive up to random entries.
+struct Bins {
+  uint32_t base;                                  // LDS address of the sum of entry address 0 (modulo 2^32)
+  uint32_t lo, span;                              // kInMemory: the entries' bytes that this workgroup adds up
+  bool rows_too;                                  // this workgroup writes the rows
+  template <TableForm kForm> __device__ __forceinline__ void add(uint32_t entry, float v) const {
+    typedef __attribute__((address_space(3))) double lds_double;
+    if constexpr (kForm == kInMemory) {
+      entry -= lo;
+      if (entry >= span) return;
+    }
+    __hip_atomic_fetch_add((lds_double*)(uintptr_t)(base + 2 * entry), (double)v, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_WORKGROUP);
+  }
+};
+
 // kHold: the keys' and values' fragments of all tiles stay in registers; else they are read again, from the caches, for each query tile.
-template <typename T, int HDP, int kTiles> constexpr bool hold_rows() { return HDP <= 32 && kTiles <= 3; }
+template <typename T, int HDP, int kTiles> constexpr bool hold_rows() { return HDP * sizeof(T) <= 64 && kTiles <= 3; }
 
 template <typename T, int HDP, TableForm kForm, int kTiles>
-__device__ __forceinline__ void backward_set(const Head<T, HDP, kForm>& head, const SetRows& rows, int n, int bins, Turns& turns) {
+__device__ __forceinline__ void backward_set(const Head<T, HDP, kForm>& head, const SetRows& rows, int n, const Bins& bins, Turns& turns) {
   typedef Frag<T, HDP> F;
   typedef typename F::Row Row;
   typedef typename F::Tile Tile;
@@ -54,24 +70,24 @@ __device__ __forceinline__ void backward_set(const Head<T, HDP, kForm>& head, co
   if constexpr (kHold) {
 #pragma unroll
     for (int t = 0; t < kTiles; ++t) {
-      head.load(rows, a.qkv, a.ld_qkv, 1, t, k[t]);
-      head.load(rows, a.qkv, a.ld_qkv, 2, t, v[t]);
+      head.template load<false>(rows, a.qkv, a.ld_qkv, 1, t, k[t]);
+      head.template load<false>(rows, a.qkv, a.ld_qkv, 2, t, v[t]);
     }
   }
   f32x4 dk[kTiles][F::NT] = {}, dv[kTiles][F::NT] = {};
 #pragma unroll kHold ? kTiles : 1
   for (int qt = 0; qt < kTiles; ++qt) {
     Row q[F::NC], go[F::NC];
-    head.load(rows, a.qkv, a.ld_qkv, 0, qt, q);
-    head.load(rows, a.d_out, a.ld_dout, 0, qt, go);
+    head.template load<true>(rows, a.qkv, a.ld_qkv, 0, qt, q);
+    head.template load<true>(rows, a.d_out, a.ld_dout, 0, qt, go);
     const uint32_t at = (uint32_t)rows.code[16 * qt + m] + head.from();
     f32x4 p[kTiles], s[kTiles];                   // p: logits, then probabilities; s: t, then ds
     uint32_t entry[kTiles][4];
 #pragma unroll
     for (int t = 0; t < kTiles; ++t) {
       if constexpr (!kHold) {
-        head.load(rows, a.qkv, a.ld_qkv, 1, t, k[0]);
-        head.load(rows, a.qkv, a.ld_qkv, 2, t, v[0]);
+        head.template load<false>(rows, a.qkv, a.ld_qkv, 1, t, k[0]);
+        head.template load<false>(rows, a.qkv, a.ld_qkv, 2, t, v[0]);
       }
 #pragma unroll
       for (int i = 0; i < 4; ++i) {
@@ -86,7 +102,8 @@ __device__ __forceinline__ void backward_set(const Head<T, HDP, kForm>& head, co
         s[t] = F::row_mma(v[kHold ? t : 0][c], go[c], s[t]);
       }
     }
-    const float sum = head.template exponentials<kTiles>(rows, p), inv = sum == 0.f ? 0.f : 1.f / sum;
+    const bool query = qt + 1 < kTiles || 16 * qt + m < n;
+    const float sum = head.template exponentials<kTiles>(rows, p), inv = sum == 0.f || !query ? 0.f : 1.f / sum;
     float dot = 0.f;
 #pragma unroll
     for (int t = 0; t < kTiles; ++t)
@@ -102,15 +119,15 @@ __device__ __forceinline__ void backward_set(const Head<T, HDP, kForm>& head, co
       for (int i = 0; i < 4; ++i) s[t][i] = p[t][i] * (s[t][i] - dot);
     if (a.partial) {
       turns.wait();
-      if (qt + 1 < kTiles || 16 * qt + m < n) {
+      if (query) {
 #pragma unroll
         for (int t = 0; t < kTiles; ++t)
 #pragma unroll
           for (int i = 0; i < 4; ++i)
-            if (t + 1 < kTiles || 16 * t + 4 * g + i < n)
-              __hip_atomic_fetch_add((lds_float*)(uintptr_t)(entry[t][i] + bins), s[t][i], __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_WORKGROUP);
+            if (t + 1 < kTiles || 16 * t + 4 * g + i < n) bins.template add<kForm>(entry[t][i], s[t][i]);
       }
       turns.hand_on();
+      if (!bins.rows_too) continue;               // another workgroup writes the rows
     }
     if constexpr (kHold) {
       if (qt == 0) {
@@ -125,7 +142,7 @@ __device__ __forceinline__ void backward_set(const Head<T, HDP, kForm>& head, co
 #pragma unroll
     for (int t = 0; t < kTiles; ++t) {
       if constexpr (!kHold) {
-        head.load(rows, a.qkv, a.ld_qkv, 1, t, k[0]);
+        head.template load<false>(rows, a.qkv, a.ld_qkv, 1, t, k[0]);
         head.turn(k[0], turned_k[0]);
       }
       const Tile ds = F::tile(s[t]), ds_t = head.turn(ds), p_t = head.turn(F::tile(p[t]));
@@ -136,33 +153,36 @@ __device__ __forceinline__ void backward_set(const Head<T, HDP, kForm>& head, co
         dv[t][c] = F::tile_mma(turned_g[c], p_t, dv[t][c]);
       }
     }
-    head.store(rows, a.out, a.ld_out, 0, qt, dq, a.scale);
+    head.store(rows, a.out, a.ld_out, 0, qt, query, dq, a.scale);
   }
+  if (!bins.rows_too) return;
 #pragma unroll
   for (int t = 0; t < kTiles; ++t) {
-    head.store(rows, a.out, a.ld_out, 1, t, dk[t], a.scale);
-    head.store(rows, a.out, a.ld_out, 2, t, dv[t], 1.f);
+    const bool there = t + 1 < kTiles || 16 * t + m < n;
+    head.store(rows, a.out, a.ld_out, 1, t, there, dk[t], a.scale);
+    head.store(rows, a.out, a.ld_out, 2, t, there, dv[t], 1.f);
   }
 }
 
-// Dynamic LDS: the sums of the table's gradient [hs][entries] if they are wanted, the table [hs][entries] unless it stays in memory, the
-// offsets' buckets.
+// Dynamic LDS: the sums of the table's gradient [hs][entries of the range] if they are wanted, the table [hs][entries] unless it stays in
+// memory, the offsets' buckets.
 template <typename T, int HDP, TableForm kForm, int kTilesMax>
 __global__ __launch_bounds__(64 * mha_waves(true, sizeof(T), HDP, 16 * kTilesMax)) void k_mha_backward(MhaArgs a) {
   __shared__ SetRows sets[kBatch];
   __shared__ int next_turn[8];
   const Share share(a);
-  const int wave = threadIdx.x >> 6, waves = blockDim.x >> 6, h0 = share.group * a.hs, all = a.hs * a.entries;
-  float* table = mha_lds + (a.partial ? all : 0);
+  const int wave = threadIdx.x >> 6, waves = blockDim.x >> 6, range = share.group % a.ranges, h0 = share.group / a.ranges * a.hs, all = a.hs * a.entries;
+  // entries of a head that this workgroup adds up: all, or its range of them (then hs = 1)
+  const int per = (a.entries + a.ranges - 1) / a.ranges, lo = range * per, mine = lo + per < a.entries ? per : (a.entries > lo ? a.entries - lo : 0);
+  float* table = reinterpret_cast<float*>(mha_lds + (a.partial ? a.hs * per : 0));
   uint16_t* map = reinterpret_cast<uint16_t*>(table + all);
   fill_tables<kForm>(a, h0, table, map);
   if (a.partial)
-    for (int u = threadIdx.x; u < all; u += blockDim.x) mha_lds[u] = 0.f;
+    for (int u = threadIdx.x; u < a.hs * per; u += blockDim.x) mha_lds[u] = 0.;
   if (threadIdx.x < 8) next_turn[threadIdx.x] = 0;
   const int slot = wave / a.hs, hl = wave - slot * a.hs;
   const Head<T, HDP, kForm> head(a, table + hl * a.entries, map, h0 + hl);
-  // from an entry's address to its sum's
-  const int bins = kForm == kInMemory ? (int)lds_address(mha_lds + hl * a.entries) : -4 * all;
+  const Bins bins = {lds_address(mha_lds + hl * per) - (kForm == kInMemory ? 0u : 2 * lds_address(table + hl * a.entries)), 4u * lo, 4u * mine, range == 0};
   Turns turns = {(lds_turn*)(next_turn + hl), a.partial && a.slots > 1, a.slots, slot, (a.tau + 15) >> 4, 0};
   const int32_t n_sets = sets_of(a);
   int round = 0;                                  // of `slots` sets, over all batches (kBatch is a multiple of slots)
@@ -188,7 +208,8 @@ __global__ __launch_bounds__(64 * mha_waves(true, sizeof(T), HDP, 16 * kTilesMax
   if (!a.partial) return;
   __syncthreads();
   if (share.part < n_sets)                        // k_mha_entries reads the parts that had a set
-    for (int u = threadIdx.x; u < all; u += blockDim.x) a.partial[((int64_t)share.part * a.heads + h0) * a.entries + u] = mha_lds[u];
+    for (int u = threadIdx.x; u < a.hs * mine; u += blockDim.x)
+      a.partial[((int64_t)share.part * a.heads + h0) * a.entries + lo + u] = (float)mha_lds[u];
 }
 
 template <typename T, int HDP, TableForm kForm, int kTilesMax> int launch(const MhaArgs& a, size_t lds, hipStream_t st) {

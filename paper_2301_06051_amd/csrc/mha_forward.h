@@ -14,11 +14,11 @@ __device__ __forceinline__ void forward_set(const Head<T, HDP, kForm>& head, con
   typename F::Tile vt[kTiles][F::NT];
 #pragma unroll
   for (int t = 0; t < kTiles; ++t) {
-    head.load(rows, a.qkv, a.ld_qkv, 1, t, k[t]);
-    head.load(rows, a.qkv, a.ld_qkv, 2, t, v[t]);
+    head.template load<false>(rows, a.qkv, a.ld_qkv, 1, t, k[t]);
+    head.template load<false>(rows, a.qkv, a.ld_qkv, 2, t, v[t]);
   }
   typename F::Row q[2][F::NC];
-  head.load(rows, a.qkv, a.ld_qkv, 0, 0, q[0]);
+  head.template load<true>(rows, a.qkv, a.ld_qkv, 0, 0, q[0]);
   uint32_t key[kTiles][4];
 #pragma unroll
   for (int t = 0; t < kTiles; ++t)
@@ -26,7 +26,7 @@ __device__ __forceinline__ void forward_set(const Head<T, HDP, kForm>& head, con
     for (int i = 0; i < 4; ++i) key[t][i] = (uint32_t)rows.code[16 * t + 4 * g + i];
 #pragma unroll
   for (int qt = 0; qt < kTiles; ++qt) {
-    if (qt + 1 < kTiles) head.load(rows, a.qkv, a.ld_qkv, 0, qt + 1, q[(qt + 1) & 1]);
+    if (qt + 1 < kTiles) head.template load<true>(rows, a.qkv, a.ld_qkv, 0, qt + 1, q[(qt + 1) & 1]);
     const uint32_t at = (uint32_t)rows.code[16 * qt + m] + head.from();
     f32x4 p[kTiles];
 #pragma unroll
@@ -49,7 +49,7 @@ __device__ __forceinline__ void forward_set(const Head<T, HDP, kForm>& head, con
     for (int t = 0; t < kTiles; ++t)
 #pragma unroll
       for (int c = 0; c < F::NT; ++c) o[c] = F::tile_mma(vt[t][c], F::tile(p[t]), o[c]);
-    head.store(rows, a.out, a.ld_out, 0, qt, o, sum == 0.f ? 0.f : 1.f / sum);
+    head.store(rows, a.out, a.ld_out, 0, qt, qt + 1 < kTiles || 16 * qt + m < n, o, sum == 0.f ? 0.f : 1.f / sum);
   }
 }
 
@@ -58,10 +58,11 @@ __global__ __launch_bounds__(64 * mha_waves(false, sizeof(T), HDP, 16 * kTilesMa
   __shared__ SetRows sets[kBatch];
   const Share share(a);
   const int wave = threadIdx.x >> 6, waves = blockDim.x >> 6, h0 = share.group * a.hs;
-  uint16_t* map = reinterpret_cast<uint16_t*>(mha_lds + a.hs * a.entries);
-  fill_tables<kForm>(a, h0, mha_lds, map);
+  float* table = reinterpret_cast<float*>(mha_lds);
+  uint16_t* map = reinterpret_cast<uint16_t*>(table + a.hs * a.entries);
+  fill_tables<kForm>(a, h0, table, map);
   const int slot = wave / a.hs, hl = wave - slot * a.hs;
-  const Head<T, HDP, kForm> head(a, mha_lds + hl * a.entries, map, h0 + hl);
+  const Head<T, HDP, kForm> head(a, table + hl * a.entries, map, h0 + hl);
   const int32_t n_sets = sets_of(a);
   for (int32_t s0 = share.part; s0 < n_sets; s0 += kBatch * a.parts) {
     __syncthreads();
