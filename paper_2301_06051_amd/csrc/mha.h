@@ -58,15 +58,24 @@ template <typename T, int HDP> struct Frag;
 template <int HDP> struct Frag<bf16_t, HDP> {
   static constexpr int KL = HDP == 16 ? 4 : 8, NC = HDP / (4 * KL), NT = HDP / 16, PER = KL / 4;
   typedef bf16_t Row __attribute__((ext_vector_type(KL)));
-  typedef bf16x4 Tile;
-  static __device__ __forceinline__ f32x4 tile_mma(Tile a, Tile b, f32x4 c) {
-    return __builtin_amdgcn_mfma_f32_16x16x16bf16_1k(__builtin_bit_cast(short4_t, a), __builtin_bit_cast(short4_t, b), c, 0, 0, 0);
-  }
+  typedef short4_t Tile;
+  static __device__ __forceinline__ f32x4 tile_mma(Tile a, Tile b, f32x4 c) { return __builtin_amdgcn_mfma_f32_16x16x16bf16_1k(a, b, c, 0, 0, 0); }
   static __device__ __forceinline__ f32x4 row_mma(Row a, Row b, f32x4 c) {
     if constexpr (KL == 8) return __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, b, c, 0, 0, 0);
-    else return tile_mma(a, b, c);
+    else return tile_mma(__builtin_bit_cast(Tile, a), __builtin_bit_cast(Tile, b), c);
   }
-  static __device__ __forceinline__ Tile tile(f32x4 v) { return __builtin_convertvector(v, Tile); }
+  // (pairs in 32-bit words: on vectors of four that become operands the compiler converts one by one)
+  static __device__ __forceinline__ unsigned pair(float a, float b) {
+    typedef float F2 __attribute__((ext_vector_type(2)));
+    typedef bf16_t B2 __attribute__((ext_vector_type(2)));
+    return __builtin_bit_cast(unsigned, __builtin_convertvector(F2{a, b}, B2));
+  }
+  static __device__ __forceinline__ Tile tile(f32x4 v) { return __builtin_bit_cast(Tile, make_uint2(pair(v[0], v[1]), pair(v[2], v[3]))); }
+  // of values that are bf16 already: their upper halves
+  static __device__ __forceinline__ Tile exact_tile(f32x4 v) {
+    const auto upper = [](float a, float b) { return __builtin_amdgcn_perm(__float_as_uint(b), __float_as_uint(a), 0x07060302u); };
+    return __builtin_bit_cast(Tile, make_uint2(upper(v[0], v[1]), upper(v[2], v[3])));
+  }
 };
 template <int HDP> struct Frag<float, HDP> {
   static constexpr int KL = 4, NC = HDP / 16, NT = HDP / 16, PER = 1;
@@ -75,6 +84,7 @@ template <int HDP> struct Frag<float, HDP> {
   static __device__ __forceinline__ f32x4 tile_mma(Tile a, Tile b, f32x4 c) { return Mma<float>::mma(a, b, c); }
   static __device__ __forceinline__ f32x4 row_mma(Row a, Row b, f32x4 c) { return Mma<float>::mma(a, b, c); }
   static __device__ __forceinline__ Tile tile(f32x4 v) { return v; }
+  static __device__ __forceinline__ Tile exact_tile(f32x4 v) { return v; }
 };
 
 // Lanes 16 apart hold the same query's other keys: every lane gets the sum (largest) of its four.
@@ -85,7 +95,13 @@ template <typename Op> __device__ __forceinline__ float across(float v, Op op) {
   return op(__uint_as_float(b[0]), __uint_as_float(b[1]));
 }
 __device__ __forceinline__ float across_sum(float v) { return across(v, [](float a, float b) { return a + b; }); }
-__device__ __forceinline__ float across_max(float v) { return across(v, [](float a, float b) { return fmaxf(a, b); }); }
+__device__ __forceinline__ float across_max(float v) { return across(v, raw_max); }
+
+// 1 / sum of probabilities: the instruction's value and one Newton step, half a dozen instructions less than a division.  0 for 0.
+__device__ __forceinline__ float inverse(float sum) {
+  const float r = __builtin_amdgcn_rcpf(sum);
+  return sum == 0.f ? 0.f : fmaf(fmaf(-sum, r, 1.f), r, r);
+}
 
 // The logits are formed in units of sigma, so that a bias is what the product of q and k starts from.  A finite bias stays finite.
 __device__ __forceinline__ float to_units(float b, float root) {
@@ -275,17 +291,17 @@ template <typename T, int HDP, TableForm kForm> struct Head {
     return u;
   }
   __device__ __forceinline__ Tile tile_unit() const {
-    Tile u;
+    f32x4 u;
 #pragma unroll
-    for (int e = 0; e < 4; ++e) u[e] = (T)(4 * g + e == m ? 1.f : 0.f);
-    return u;
+    for (int e = 0; e < 4; ++e) u[e] = 4 * g + e == m ? 1.f : 0.f;
+    return F::exact_tile(u);
   }
   // rows -> NT tile fragments: lane holds channel (of tile n) m, rows 4 g .. 4 g + 3
   __device__ __forceinline__ void turn(const Row (&f)[F::NC], Tile (&o)[F::NT]) const {
 #pragma unroll
-    for (int n = 0; n < F::NT; ++n) o[n] = F::tile(F::row_mma(f[n / F::PER], unit(n % F::PER), f32x4{0.f, 0.f, 0.f, 0.f}));
+    for (int n = 0; n < F::NT; ++n) o[n] = F::exact_tile(F::row_mma(f[n / F::PER], unit(n % F::PER), f32x4{0.f, 0.f, 0.f, 0.f}));
   }
-  __device__ __forceinline__ Tile turn(Tile f) const { return F::tile(F::tile_mma(f, tile_unit(), f32x4{0.f, 0.f, 0.f, 0.f})); }
+  __device__ __forceinline__ Tile turn(Tile f) const { return F::exact_tile(F::tile_mma(f, tile_unit(), f32x4{0.f, 0.f, 0.f, 0.f})); }
 
   // LDS address (in memory: byte offset in the head's table) of the entry of an offset, given as the difference of two codes plus `from`
   __device__ __forceinline__ uint32_t from() const {

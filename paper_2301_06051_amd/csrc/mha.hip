@@ -4,7 +4,7 @@
 
 namespace {
 
-constexpr int kGroups = 512;                      // workgroups that a launch aims at: two a compute unit
+constexpr int kComputeUnits = 256;                // MI355X
 
 // The parts' sums of the table's gradient added in their order: 64 columns of [heads * entries] a workgroup, 16 slices of the parts.  Entries
 // from n_out on (offsets without a bias) are dropped.
@@ -15,8 +15,17 @@ __global__ __launch_bounds__(1024) void k_mha_entries(const float* __restrict__ 
   const int col = threadIdx.x & 63, slice = threadIdx.x >> 6;
   const int64_t cols = (int64_t)heads * entries, c = (int64_t)blockIdx.x * 64 + col;
   double v = 0.;
-  if (c < cols)
-    for (int k = slice; k < n; k += 16) v += (double)partial[k * cols + c];
+  if (c < cols) {
+    int k = slice;
+    for (; k + 7 * 16 < n; k += 8 * 16) {         // eight loads on their way at a time
+      float f[8];
+#pragma unroll
+      for (int j = 0; j < 8; ++j) f[j] = partial[(k + j * 16) * cols + c];
+#pragma unroll
+      for (int j = 0; j < 8; ++j) v += (double)f[j];
+    }
+    for (; k < n; k += 16) v += (double)partial[k * cols + c];
+  }
   s[slice][col] = v;
   __syncthreads();
   if (slice || c >= cols) return;
@@ -83,21 +92,25 @@ int make_plan(const dsvt_mha_cfg* c, int32_t max_sets, int32_t tau, bool back, b
   if (hd % 8 != 0 || hd > 64 || tau > kSetMax || n_off >= (1 << 24) || (c->rel_bias && c->n_rel >= (1 << 24))) return DSVT_EUNSUPPORTED;
   const bool by_bucket = c->rel_bias && c->rel_bucket;
   const int waves = mha_waves(back, c->dtype == DSVT_BF16 ? 2 : 4, hd <= 16 ? 16 : hd <= 32 ? 32 : 64, tau);
-  // The form that lets a workgroup take the most heads, of equal ones the first: heads of one set in one workgroup share cache lines.
+  // Two workgroups a compute unit where a wavefront's registers leave room for them (the forward call's smaller kernels), else one.
+  const int per_cu = !back && waves == 8 && tau <= 48 ? 2 : 1;
+  // Of the forms in LDS the one that lets a workgroup take the most heads, of equal ones the first: heads of one set in one workgroup share
+  // cache lines.  In memory if neither fits.
   p->hs = 0;
   const TableForm forms[] = {kByOffset, kByBucket, kInMemory};
-  for (const TableForm f : forms) {
-    if (f == kByBucket && (!by_bucket || c->n_rel > 65535)) continue;
-    if (f == kInMemory && !c->rel_bias) continue;
-    const int64_t entries = f == kByOffset || !by_bucket ? n_off : (int64_t)c->n_rel + 1;
-    int hs = 0;
-    for (int h = 1; h <= waves; ++h)
-      if (c->heads % h == 0 && lds_bytes(f, h, d_bias ? entries : 0, entries, n_off) <= kMhaLdsMax) hs = h;
-    if (hs <= p->hs && (p->hs > 0 || f != kInMemory)) continue;
-    p->form = f;
-    p->hs = hs;
-    p->entries = (int32_t)entries;
-  }
+  for (size_t most = per_cu == 2 ? kMhaLdsMax / 2 : kMhaLdsMax; p->hs == 0 && most <= kMhaLdsMax; most *= 2)
+    for (const TableForm f : forms) {
+      if (f == kByBucket && (!by_bucket || c->n_rel > 65535)) continue;
+      if (f == kInMemory && (!c->rel_bias || p->hs > 0 || most < kMhaLdsMax)) continue;
+      const int64_t entries = f == kByOffset || !by_bucket ? n_off : (int64_t)c->n_rel + 1;
+      int hs = 0;
+      for (int h = 1; h <= waves; ++h)
+        if (c->heads % h == 0 && lds_bytes(f, h, d_bias ? entries : 0, entries, n_off) <= most) hs = h;
+      if (hs <= p->hs && f != kInMemory) continue;
+      p->form = f;
+      p->hs = hs;
+      p->entries = (int32_t)entries;
+    }
   // Sums that the LDS of a workgroup does not hold for one head: workgroups of a head share its entries, and each goes through all sets.
   p->ranges = 1;
   if (p->hs == 0) {
@@ -111,7 +124,7 @@ int make_plan(const dsvt_mha_cfg* c, int32_t max_sets, int32_t tau, bool back, b
   p->slots = 1;
   while (2 * p->slots * p->hs <= waves) p->slots *= 2;
   static_assert(kBatch % 8 == 0, "a batch is a whole number of rounds");
-  int64_t parts = dsvt_ceil_div(kGroups, c->heads / p->hs * p->ranges);
+  int64_t parts = dsvt_ceil_div(kComputeUnits * per_cu, c->heads / p->hs * p->ranges);
   if (parts > max_sets) parts = max_sets;
   p->parts = (int32_t)dsvt_align_up((size_t)(parts > 0 ? parts : 1), 8);
   p->ws = d_bias ? ((size_t)p->parts + fold) * c->heads * (size_t)p->entries * 4 : 0;

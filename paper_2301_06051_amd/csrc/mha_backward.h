@@ -103,7 +103,7 @@ __device__ __forceinline__ void backward_set(const Head<T, HDP, kForm>& head, co
       }
     }
     const bool query = qt + 1 < kTiles || 16 * qt + m < n;
-    const float sum = head.template exponentials<kTiles>(rows, p), inv = sum == 0.f || !query ? 0.f : 1.f / sum;
+    const float sum = head.template exponentials<kTiles>(rows, p), inv = query ? inverse(sum) : 0.f;
     float dot = 0.f;
 #pragma unroll
     for (int t = 0; t < kTiles; ++t)
@@ -187,7 +187,7 @@ __global__ __launch_bounds__(64 * mha_waves(true, sizeof(T), HDP, 16 * kTilesMax
   const int32_t n_sets = sets_of(a);
   int round = 0;                                  // of `slots` sets, over all batches (kBatch is a multiple of slots)
   for (int32_t s0 = share.part; s0 < n_sets; s0 += kBatch * a.parts) {
-    __syncthreads();
+    if (s0 != share.part) __syncthreads();
     for (int b = wave; b < kBatch && s0 + b * a.parts < n_sets; b += waves) load_set(a, s0 + b * a.parts, head.entry_bytes(), sets[b]);
     __syncthreads();
     for (int b = slot; b < kBatch && s0 + (b - slot) * a.parts < n_sets; b += a.slots, ++round) {

@@ -49,7 +49,7 @@ __device__ __forceinline__ void forward_set(const Head<T, HDP, kForm>& head, con
     for (int t = 0; t < kTiles; ++t)
 #pragma unroll
       for (int c = 0; c < F::NT; ++c) o[c] = F::tile_mma(vt[t][c], F::tile(p[t]), o[c]);
-    head.store(rows, a.out, a.ld_out, 0, qt, qt + 1 < kTiles || 16 * qt + m < n, o, sum == 0.f ? 0.f : 1.f / sum);
+    head.store(rows, a.out, a.ld_out, 0, qt, qt + 1 < kTiles || 16 * qt + m < n, o, inverse(sum));
   }
 }
 
@@ -65,7 +65,7 @@ __global__ __launch_bounds__(64 * mha_waves(false, sizeof(T), HDP, 16 * kTilesMa
   const Head<T, HDP, kForm> head(a, table + hl * a.entries, map, h0 + hl);
   const int32_t n_sets = sets_of(a);
   for (int32_t s0 = share.part; s0 < n_sets; s0 += kBatch * a.parts) {
-    __syncthreads();
+    if (s0 != share.part) __syncthreads();
     for (int b = wave; b < kBatch && s0 + b * a.parts < n_sets; b += waves) load_set(a, s0 + b * a.parts, head.entry_bytes(), sets[b]);
     __syncthreads();
     for (int b = slot; b < kBatch && s0 + b * a.parts < n_sets; b += a.slots) {
