@@ -370,6 +370,11 @@ int mha_backward_f32(const MhaArgs& a, TableForm form, size_t lds, hipStream_t s
 __host__ __device__ constexpr int mha_waves(bool back, int element, int padded, int tau) {
   return padded == 64 || (padded == 32 && tau > 48 && (back || element == 4)) ? 4 : 8;
 }
+// Workgroups of a compute unit: two where a quarter of the registers does, else one.
+__host__ __device__ constexpr int mha_per_cu(bool back, int element, int padded, int tau) { return !back && padded * element <= 64 && tau <= 48 ? 2 : 1; }
+__host__ __device__ constexpr int mha_per_simd(bool back, int element, int padded, int tau) {
+  return mha_waves(back, element, padded, tau) * mha_per_cu(back, element, padded, tau) / 4;
+}
 constexpr size_t kMhaLdsMax = 140 << 10;          // dynamic LDS of a workgroup, at most
 
 extern __shared__ double mha_lds[];

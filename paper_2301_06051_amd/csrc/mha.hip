@@ -91,9 +91,8 @@ int make_plan(const dsvt_mha_cfg* c, int32_t max_sets, int32_t tau, bool back, b
   const int hd = c->C / c->heads;
   if (hd % 8 != 0 || hd > 64 || tau > kSetMax || n_off >= (1 << 24) || (c->rel_bias && c->n_rel >= (1 << 24))) return DSVT_EUNSUPPORTED;
   const bool by_bucket = c->rel_bias && c->rel_bucket;
-  const int waves = mha_waves(back, c->dtype == DSVT_BF16 ? 2 : 4, hd <= 16 ? 16 : hd <= 32 ? 32 : 64, tau);
-  // Two workgroups a compute unit where a wavefront's registers leave room for them (the forward call's smaller kernels), else one.
-  const int per_cu = !back && waves == 8 && tau <= 48 ? 2 : 1;
+  const int element = c->dtype == DSVT_BF16 ? 2 : 4, padded = hd <= 16 ? 16 : hd <= 32 ? 32 : 64;
+  const int waves = mha_waves(back, element, padded, tau), per_cu = mha_per_cu(back, element, padded, tau);
   // Of the forms in LDS the one that lets a workgroup take the most heads, of equal ones the first: heads of one set in one workgroup share
   // cache lines.  In memory if neither fits.
   p->hs = 0;

@@ -167,7 +167,7 @@ __device__ __forceinline__ void backward_set(const Head<T, HDP, kForm>& head, co
 // Dynamic LDS: the sums of the table's gradient [hs][entries of the range] if they are wanted, the table [hs][entries] unless it stays in
 // memory, the offsets' buckets.
 template <typename T, int HDP, TableForm kForm, int kTilesMax>
-__global__ __launch_bounds__(64 * mha_waves(true, sizeof(T), HDP, 16 * kTilesMax)) void k_mha_backward(MhaArgs a) {
+__global__ __launch_bounds__(64 * mha_waves(true, sizeof(T), HDP, 16 * kTilesMax), mha_per_simd(true, sizeof(T), HDP, 16 * kTilesMax)) void k_mha_backward(MhaArgs a) {
   __shared__ SetRows sets[kBatch];
   __shared__ int next_turn[8];
   const Share share(a);

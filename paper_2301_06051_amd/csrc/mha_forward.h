@@ -10,23 +10,24 @@ __device__ __forceinline__ void forward_set(const Head<T, HDP, kForm>& head, con
   typedef Frag<T, HDP> F;
   const MhaArgs& a = head.a;
   const int m = head.m, g = head.g;
-  typename F::Row k[kTiles][F::NC], v[kTiles][F::NC];
+  typename F::Row k[kTiles][F::NC], v[kTiles][F::NC], q[F::NC], next[F::NC];
   typename F::Tile vt[kTiles][F::NT];
+  head.template load<true>(rows, a.qkv, a.ld_qkv, 0, 0, q);
 #pragma unroll
   for (int t = 0; t < kTiles; ++t) {
     head.template load<false>(rows, a.qkv, a.ld_qkv, 1, t, k[t]);
     head.template load<false>(rows, a.qkv, a.ld_qkv, 2, t, v[t]);
   }
-  typename F::Row q[2][F::NC];
-  head.template load<true>(rows, a.qkv, a.ld_qkv, 0, 0, q[0]);
   uint32_t key[kTiles][4];
 #pragma unroll
   for (int t = 0; t < kTiles; ++t)
 #pragma unroll
     for (int i = 0; i < 4; ++i) key[t][i] = (uint32_t)rows.code[16 * t + 4 * g + i];
 #pragma unroll
+  for (int t = 0; t < kTiles; ++t) head.turn(v[t], vt[t]);
+#pragma unroll 1
   for (int qt = 0; qt < kTiles; ++qt) {
-    if (qt + 1 < kTiles) head.template load<true>(rows, a.qkv, a.ld_qkv, 0, qt + 1, q[(qt + 1) & 1]);
+    head.template load<true>(rows, a.qkv, a.ld_qkv, 0, qt + 1 < kTiles ? qt + 1 : qt, next);
     const uint32_t at = (uint32_t)rows.code[16 * qt + m] + head.from();
     f32x4 p[kTiles];
 #pragma unroll
@@ -37,24 +38,22 @@ __device__ __forceinline__ void forward_set(const Head<T, HDP, kForm>& head, con
         if (t == kTiles - 1 && 16 * t + 4 * g + i >= n) p[t][i] = -INFINITY;
       }
 #pragma unroll
-      for (int c = 0; c < F::NC; ++c) p[t] = F::row_mma(k[t][c], q[qt & 1][c], p[t]);
+      for (int c = 0; c < F::NC; ++c) p[t] = F::row_mma(k[t][c], q[c], p[t]);
     }
     const float sum = head.template exponentials<kTiles>(rows, p);
-    if (qt == 0) {
-#pragma unroll
-      for (int t = 0; t < kTiles; ++t) head.turn(v[t], vt[t]);
-    }
     f32x4 o[F::NT] = {};
 #pragma unroll
     for (int t = 0; t < kTiles; ++t)
 #pragma unroll
       for (int c = 0; c < F::NT; ++c) o[c] = F::tile_mma(vt[t][c], F::tile(p[t]), o[c]);
-    head.store(rows, a.out, a.ld_out, 0, qt, qt + 1 < kTiles || 16 * qt + m < n, o, inverse(sum));
+    head.store(rows, a.out, a.ld_out, 0, qt, 16 * qt + m < n, o, inverse(sum));
+#pragma unroll
+    for (int c = 0; c < F::NC; ++c) q[c] = next[c];
   }
 }
 
 template <typename T, int HDP, TableForm kForm, int kTilesMax>
-__global__ __launch_bounds__(64 * mha_waves(false, sizeof(T), HDP, 16 * kTilesMax)) void k_mha_forward(MhaArgs a) {
+__global__ __launch_bounds__(64 * mha_waves(false, sizeof(T), HDP, 16 * kTilesMax), mha_per_simd(false, sizeof(T), HDP, 16 * kTilesMax)) void k_mha_forward(MhaArgs a) {
   __shared__ SetRows sets[kBatch];
   const Share share(a);
   const int wave = threadIdx.x >> 6, waves = blockDim.x >> 6, h0 = share.group * a.hs;
