@@ -23,7 +23,7 @@
 #include <cmath>
 
 constexpr int kSetMax = 96;                       // slots, and so voxels, of a set
-constexpr int kBatch = 8;                         // sets of a workgroup whose rows are looked up together
+constexpr int kMhaWavesMax = 8;                   // wavefronts of a workgroup, and so sets that it looks up together
 constexpr float kLog2e = 1.44269504088896340736f;
 
 // Where a pair's bias is found.  By offset: LDS holds a value for every offset and head.  By bucket: LDS holds the offsets' buckets
@@ -111,8 +111,8 @@ __device__ __forceinline__ float to_units(float b, float root) {
 // What a workgroup knows of a set, in LDS.  Row r is the set's r-th voxel; rows up to the next multiple of 16 repeat row 0 with
 // weight 0: they are read like others, and masked where they would count.  code: the cell's number times the bytes of an entry, so that the
 // difference of two codes is an offset's place in a table.
-struct SetRows {
-  int32_t vox[kSetMax], code[kSetMax], weight[kSetMax];
+template <int kMax> struct SetRows {
+  int32_t vox[kMax], code[kMax], weight[kMax];
   int32_t n;
 };
 
@@ -126,75 +126,89 @@ __device__ __forceinline__ int wave_max(int v) {
 }
 
 // A wavefront looks a set's distinct voxels up, in slot order: the first slot of every run of equal ones.  Slots outside
-// 0 .. n_voxels - 1 hold none.  Voxels that do not fit one window (the maps are another window's) all get code 0, so that
-// every offset formed from two codes is in the table.
-__device__ __forceinline__ void load_set(const MhaArgs& a, int32_t s, int entry_bytes, SetRows& rows) {
-  const int lane = threadIdx.x & 63;
-  const int32_t* inds = a.set_inds + (int64_t)s * a.tau;
-  int32_t v[2];
-  uint64_t first[2], change[2];
-  int4 c[2] = {};
-  int32_t before = -1;
+// 0 .. n_voxels - 1 hold none.  In three steps, so that their loads travel while sets that were looked up before are computed: the
+// slots, the cells of the first slots, the rows in LDS.
+template <int kMax> struct Lookup {
+  static constexpr int kWords = kMax > 64 ? 2 : 1;             // slots of a lane
+  int32_t v[kWords];
+  int4 c[kWords];
+  uint64_t first[kWords], change[kWords];
+
+  __device__ __forceinline__ void slots(const MhaArgs& a, int32_t s) {
+    const int32_t* inds = a.set_inds + (int64_t)s * a.tau;
 #pragma unroll
-  for (int k = 0; k < 2; ++k) {
-    const int slot = 64 * k + lane;
-    v[k] = slot < a.tau ? inds[slot] : -1;
-    if ((uint32_t)v[k] >= (uint32_t)a.n_voxels) v[k] = -1;
+    for (int k = 0; k < kWords; ++k) {
+      const int slot = 64 * k + (int)(threadIdx.x & 63);
+      v[k] = slot < a.tau ? inds[slot] : -1;
+    }
   }
-  int lo[3], hi[3];
+  __device__ __forceinline__ void cells(const MhaArgs& a) {
+    const int lane = threadIdx.x & 63;
+    int32_t before = -1;
 #pragma unroll
-  for (int x = 0; x < 3; ++x) lo[x] = hi[x] = INT32_MIN;
+    for (int k = 0; k < kWords; ++k) {
+      if ((uint32_t)v[k] >= (uint32_t)a.n_voxels) v[k] = -1;
+      int32_t prev = __shfl_up(v[k], 1, 64);
+      if (lane == 0) prev = before;
+      before = __shfl(v[k], 63, 64);
+      change[k] = __ballot(v[k] != prev || 64 * k + lane >= a.tau);
+      first[k] = __ballot(v[k] != prev && v[k] >= 0);
+      c[k] = make_int4(0, 0, 0, 0);
+      if (first[k] >> lane & 1) c[k] = a.coords[v[k]];
+    }
+  }
+  // Voxels that do not fit one window (the maps are another window's) all get code 0, so that every offset formed from two codes is in
+  // the table.
+  __device__ __forceinline__ void rows(const MhaArgs& a, int entry_bytes, SetRows<kMax>& out) {
+    const int lane = threadIdx.x & 63;
+    int lo[3], hi[3], n = 0;
 #pragma unroll
-  for (int k = 0; k < 2; ++k) {
-    const int slot = 64 * k + lane;
-    int32_t prev = __shfl_up(v[k], 1, 64);
-    if (lane == 0) prev = before;
-    before = __shfl(v[k], 63, 64);
-    change[k] = __ballot(v[k] != prev || slot >= a.tau);
-    first[k] = __ballot(v[k] != prev && v[k] >= 0);
-    if (first[k] >> lane & 1) {
-      c[k] = a.coords[v[k]];
-      const int at[3] = {c[k].y, c[k].z, c[k].w};
+    for (int x = 0; x < 3; ++x) lo[x] = hi[x] = INT32_MIN;
 #pragma unroll
-      for (int x = 0; x < 3; ++x) {
-        hi[x] = at[x] > hi[x] ? at[x] : hi[x];
-        lo[x] = -1 - at[x] > lo[x] ? -1 - at[x] : lo[x];
+    for (int k = 0; k < kWords; ++k) {
+      n += __popcll(first[k]);
+      if (first[k] >> lane & 1) {
+        const int at[3] = {c[k].y, c[k].z, c[k].w};
+#pragma unroll
+        for (int x = 0; x < 3; ++x) {
+          hi[x] = at[x] > hi[x] ? at[x] : hi[x];
+          lo[x] = -1 - at[x] > lo[x] ? -1 - at[x] : lo[x];
+        }
       }
     }
-  }
-  // highest + 1 - lowest <= window along every axis (the lowest is kept as the highest of -1 - x), by differences that do not overflow
-  bool fits = a.bias != nullptr;
+    if (lane == 0) out.n = n;
+    if (n == 0) return;
+    // highest + 1 - lowest <= window along every axis (the lowest is kept as the highest of -1 - x)
+    bool fits = a.bias != nullptr;
 #pragma unroll
-  for (int x = 0; x < 3; ++x) fits = fits && (int64_t)wave_max(hi[x]) + wave_max(lo[x]) + 2 <= a.w[x];
-  const int n0 = __popcll(first[0]), n = n0 + __popcll(first[1]);
-  if (lane == 0) rows.n = n;
-  if (n == 0) return;
-  const uint32_t w2 = 2 * a.w[1] - 1, h2 = 2 * a.w[2] - 1;
-  uint32_t code[2];
+    for (int x = 0; x < 3; ++x) fits = fits && (int64_t)wave_max(hi[x]) + wave_max(lo[x]) + 2 <= a.w[x];
+    const uint32_t w2 = 2 * a.w[1] - 1, h2 = 2 * a.w[2] - 1;
+    uint32_t code[kWords];
+    int before = 0;
 #pragma unroll
-  for (int k = 0; k < 2; ++k) {
-    // (unsigned: a far cell's number may pass 32 bits, the differences inside a window do not)
-    code[k] = fits ? (((uint32_t)c[k].y * w2 + (uint32_t)c[k].z) * h2 + (uint32_t)c[k].w) * entry_bytes : 0;
-    if (first[k] >> lane & 1) {
-      const int r = (k ? n0 : 0) + __popcll(first[k] & ((1ull << lane) - 1));
-      const uint64_t later = lane == 63 ? 0 : change[k] >> (lane + 1);      // slots to the next change
-      int run;
-      if (later) run = 1 + __builtin_ctzll(later);
-      else if (k == 0) run = 64 - lane + (change[1] ? __builtin_ctzll(change[1]) : 64);
-      else run = 64 - lane;
-      rows.vox[r] = v[k];
-      rows.code[r] = (int32_t)code[k];
-      rows.weight[r] = a.dup ? run : 1;
+    for (int k = 0; k < kWords; ++k) {
+      // (unsigned: a far cell's number may pass 32 bits, the differences inside a window do not)
+      code[k] = fits ? (((uint32_t)c[k].y * w2 + (uint32_t)c[k].z) * h2 + (uint32_t)c[k].w) * entry_bytes : 0;
+      if (first[k] >> lane & 1) {
+        const int r = before + __popcll(first[k] & ((1ull << lane) - 1));
+        const uint64_t later = lane == 63 ? 0 : change[k] >> (lane + 1);    // slots to the next change
+        int run = later ? 1 + __builtin_ctzll(later) : 64 - lane;
+        if (kWords > 1 && k == 0 && !later) run += change[kWords - 1] ? __builtin_ctzll(change[kWords - 1]) : 64;
+        out.vox[r] = v[k];
+        out.code[r] = (int32_t)code[k];
+        out.weight[r] = a.dup ? run : 1;
+      }
+      before += __popcll(first[k]);
+    }
+    const int k0 = first[0] ? 0 : kWords - 1, l0 = __builtin_ctzll(first[k0]);
+    const int32_t vox0 = __shfl(k0 ? v[kWords - 1] : v[0], l0, 64), code0 = __shfl((int32_t)(k0 ? code[kWords - 1] : code[0]), l0, 64);
+    if (n + lane < ((n + 15) & ~15)) {
+      out.vox[n + lane] = vox0;
+      out.code[n + lane] = code0;
+      out.weight[n + lane] = 0;
     }
   }
-  const int k0 = first[0] ? 0 : 1, l0 = __builtin_ctzll(first[k0]);
-  const int32_t vox0 = __shfl(k0 ? v[1] : v[0], l0, 64), code0 = __shfl((int32_t)(k0 ? code[1] : code[0]), l0, 64);
-  if (n + lane < ((n + 15) & ~15)) {
-    rows.vox[n + lane] = vox0;
-    rows.code[n + lane] = code0;
-    rows.weight[n + lane] = 0;
-  }
-}
+};
 
 // Workgroup b takes group of heads b / 8 % groups and is part (b / 8 / groups) * 8 + b % 8 of it: workgroups that take other heads of
 // the same sets are a multiple of 8 apart and so on one XCD, whose L2 they share.
@@ -252,8 +266,9 @@ template <TableForm kForm> __device__ __forceinline__ void fill_tables(const Mha
 }
 
 // One wavefront's head: where its rows and biases are, and its part of the matrix fragments.
-template <typename T, int HDP, TableForm kForm> struct Head {
+template <typename T, int HDP, TableForm kForm, int kMax> struct Head {
   typedef Frag<T, HDP> F;
+  typedef SetRows<kMax> Rows;
   typedef typename F::Row Row;
   typedef typename F::Tile Tile;
   const MhaArgs& a;
@@ -272,12 +287,12 @@ template <typename T, int HDP, TableForm kForm> struct Head {
     const int d = (4 * c + g) * F::KL;
     return d < a.hd ? d : 0;
   }
-  __device__ __forceinline__ const char* row(const SetRows& rows, const void* base, uint32_t ld, int which, int t) const {
+  __device__ __forceinline__ const char* row(const Rows& rows, const void* base, uint32_t ld, int which, int t) const {
     return static_cast<const char*>(base) + (int64_t)(which * a.heads + h) * a.hd * (int)sizeof(T) + (uint64_t)(uint32_t)rows.vox[16 * t + m] * ld;
   }
   // Rows of tile t of an array of head vectors (which: 0 q, 1 k, 2 v of a qkv row; 0 of an output row).  Of two operands whose product
   // runs over the channels one has zeros past the last (kZero).
-  template <bool kZero> __device__ __forceinline__ void load(const SetRows& rows, const void* base, uint32_t ld, int which, int t, Row (&f)[F::NC]) const {
+  template <bool kZero> __device__ __forceinline__ void load(const Rows& rows, const void* base, uint32_t ld, int which, int t, Row (&f)[F::NC]) const {
     const char* p = row(rows, base, ld, which, t);
 #pragma unroll
     for (int c = 0; c < F::NC; ++c) {
@@ -289,7 +304,7 @@ template <typename T, int HDP, TableForm kForm> struct Head {
     }
   }
   // tiles of the transposed result, column m = row m of tile t, if `there`: a lane holds the channels that it holds of a row fragment
-  __device__ __forceinline__ void store(const SetRows& rows, void* base, uint32_t ld, int which, int t, bool there, const f32x4 (&o)[F::NT],
+  __device__ __forceinline__ void store(const Rows& rows, void* base, uint32_t ld, int which, int t, bool there, const f32x4 (&o)[F::NT],
                                         float scale) const {
     char* p = const_cast<char*>(row(rows, base, ld, which, t));
 #pragma unroll
@@ -342,7 +357,7 @@ template <typename T, int HDP, TableForm kForm> struct Head {
   }
 
   // Probabilities of one query tile before their division by the sum: p holds the logits of kTiles key tiles in units of sigma.
-  template <int kTiles> __device__ __forceinline__ float exponentials(const SetRows& rows, f32x4 (&p)[kTiles]) const {
+  template <int kTiles> __device__ __forceinline__ float exponentials(const Rows& rows, f32x4 (&p)[kTiles]) const {
     float top = -INFINITY;
 #pragma unroll
     for (int k = 0; k < kTiles; ++k)

@@ -122,7 +122,6 @@ int make_plan(const dsvt_mha_cfg* c, int32_t max_sets, int32_t tau, bool back, b
   p->lds = lds_bytes(p->form, p->hs, d_bias ? dsvt_ceil_div(p->entries, p->ranges) : 0, p->entries, n_off);
   p->slots = 1;
   while (2 * p->slots * p->hs <= waves) p->slots *= 2;
-  static_assert(kBatch % 8 == 0, "a batch is a whole number of rounds");
   int64_t parts = dsvt_ceil_div(kComputeUnits * per_cu, c->heads / p->hs * p->ranges);
   if (parts > max_sets) parts = max_sets;
   p->parts = (int32_t)dsvt_align_up((size_t)(parts > 0 ? parts : 1), 8);

@@ -55,8 +55,8 @@ struct Bins {
 // kHold: the keys' and values' fragments of all tiles stay in registers; else they are read again, from the caches, for each query tile.
 template <typename T, int HDP, int kTiles> constexpr bool hold_rows() { return HDP * sizeof(T) <= 64 && kTiles <= 3; }
 
-template <typename T, int HDP, TableForm kForm, int kTiles>
-__device__ __forceinline__ void backward_set(const Head<T, HDP, kForm>& head, const SetRows& rows, int n, const Bins& bins, Turns& turns) {
+template <int kTiles, typename T, int HDP, TableForm kForm, int kMax>
+__device__ __forceinline__ void backward_set(const Head<T, HDP, kForm, kMax>& head, const SetRows<kMax>& rows, int n, const Bins& bins, Turns& turns) {
   typedef Frag<T, HDP> F;
   typedef typename F::Row Row;
   typedef typename F::Tile Tile;
@@ -66,10 +66,13 @@ __device__ __forceinline__ void backward_set(const Head<T, HDP, kForm>& head, co
   const int m = head.m, g = head.g;
   const f32x4 zero = {0.f, 0.f, 0.f, 0.f};
   Row k[kHeld][F::NC], v[kHeld][F::NC];
+  Row query_rows[kHeld][F::NC], grad_rows[kHeld][F::NC];
   Tile turned_k[kHeld][F::NT];
   if constexpr (kHold) {
 #pragma unroll
     for (int t = 0; t < kTiles; ++t) {
+      head.template load<true>(rows, a.qkv, a.ld_qkv, 0, t, query_rows[t]);
+      head.template load<true>(rows, a.d_out, a.ld_dout, 0, t, grad_rows[t]);
       head.template load<false>(rows, a.qkv, a.ld_qkv, 1, t, k[t]);
       head.template load<false>(rows, a.qkv, a.ld_qkv, 2, t, v[t]);
     }
@@ -77,9 +80,11 @@ __device__ __forceinline__ void backward_set(const Head<T, HDP, kForm>& head, co
   f32x4 dk[kTiles][F::NT] = {}, dv[kTiles][F::NT] = {};
 #pragma unroll kHold ? kTiles : 1
   for (int qt = 0; qt < kTiles; ++qt) {
-    Row q[F::NC], go[F::NC];
-    head.template load<true>(rows, a.qkv, a.ld_qkv, 0, qt, q);
-    head.template load<true>(rows, a.d_out, a.ld_dout, 0, qt, go);
+    Row (&q)[F::NC] = query_rows[kHold ? qt : 0], (&go)[F::NC] = grad_rows[kHold ? qt : 0];
+    if constexpr (!kHold) {
+      head.template load<true>(rows, a.qkv, a.ld_qkv, 0, qt, q);
+      head.template load<true>(rows, a.d_out, a.ld_dout, 0, qt, go);
+    }
     const uint32_t at = (uint32_t)rows.code[16 * qt + m] + head.from();
     f32x4 p[kTiles], s[kTiles];                   // p: logits, then probabilities; s: t, then ds
     uint32_t entry[kTiles][4];
@@ -168,10 +173,12 @@ __device__ __forceinline__ void backward_set(const Head<T, HDP, kForm>& head, co
 // memory, the offsets' buckets.
 template <typename T, int HDP, TableForm kForm, int kTilesMax>
 __global__ __launch_bounds__(64 * mha_waves(true, sizeof(T), HDP, 16 * kTilesMax), mha_per_simd(true, sizeof(T), HDP, 16 * kTilesMax)) void k_mha_backward(MhaArgs a) {
-  __shared__ SetRows sets[kBatch];
+  constexpr int kMax = 16 * kTilesMax;
+  __shared__ SetRows<kMax> sets[2][kMhaWavesMax];
   __shared__ int next_turn[8];
   const Share share(a);
-  const int wave = threadIdx.x >> 6, waves = blockDim.x >> 6, range = share.group % a.ranges, h0 = share.group / a.ranges * a.hs, all = a.hs * a.entries;
+  const int32_t n_sets = sets_of(a);
+  const int wave = threadIdx.x >> 6, range = share.group % a.ranges, h0 = share.group / a.ranges * a.hs, all = a.hs * a.entries;
   // entries of a head that this workgroup adds up: all, or its range of them (then hs = 1)
   const int per = (a.entries + a.ranges - 1) / a.ranges, lo = range * per, mine = lo + per < a.entries ? per : (a.entries > lo ? a.entries - lo : 0);
   float* table = reinterpret_cast<float*>(mha_lds + (a.partial ? a.hs * per : 0));
@@ -181,28 +188,46 @@ __global__ __launch_bounds__(64 * mha_waves(true, sizeof(T), HDP, 16 * kTilesMax
     for (int u = threadIdx.x; u < a.hs * per; u += blockDim.x) mha_lds[u] = 0.;
   if (threadIdx.x < 8) next_turn[threadIdx.x] = 0;
   const int slot = wave / a.hs, hl = wave - slot * a.hs;
-  const Head<T, HDP, kForm> head(a, table + hl * a.entries, map, h0 + hl);
+  const Head<T, HDP, kForm, kMax> head(a, table + hl * a.entries, map, h0 + hl);
   const Bins bins = {lds_address(mha_lds + hl * per) - (kForm == kInMemory ? 0u : 2 * lds_address(table + hl * a.entries)), 4u * lo, 4u * mine, range == 0};
   Turns turns = {(lds_turn*)(next_turn + hl), a.partial && a.slots > 1, a.slots, slot, (a.tau + 15) >> 4, 0};
-  const int32_t n_sets = sets_of(a);
-  int round = 0;                                  // of `slots` sets, over all batches (kBatch is a multiple of slots)
-  for (int32_t s0 = share.part; s0 < n_sets; s0 += kBatch * a.parts) {
-    if (s0 != share.part) __syncthreads();
-    for (int b = wave; b < kBatch && s0 + b * a.parts < n_sets; b += waves) load_set(a, s0 + b * a.parts, head.entry_bytes(), sets[b]);
+  int round = 0;                                  // of `slots` sets, over all batches (a batch is a whole number of rounds)
+  Lookup<kMax> lookup;
+  // A batch is as many sets as there are wavefronts, each looked up by one.  The look-up of the next batch runs beside this one's sets where
+  // registers allow it.
+  constexpr bool kBeside = kTilesMax <= 3;
+  const int waves = blockDim.x >> 6;
+  const auto number = [&](int32_t batch, int b) { return share.part + (batch * waves + b) * a.parts; };       // a set's
+  const auto looks = [&](int32_t batch) { return number(batch, wave) < n_sets; };
+  if (looks(0)) {
+    lookup.slots(a, number(0, wave));
+    lookup.cells(a);
+    lookup.rows(a, head.entry_bytes(), sets[0][wave]);
+  }
+  for (int32_t batch = 0; number(batch, 0) < n_sets; ++batch) {
     __syncthreads();
-    for (int b = slot; b < kBatch && s0 + (b - slot) * a.parts < n_sets; b += a.slots, ++round) {
+    const bool more = looks(batch + 1);
+    if (kBeside && more) lookup.slots(a, number(batch + 1, wave));
+    for (int b = slot; b < waves && number(batch, b - slot) < n_sets; b += a.slots, ++round) {
       turns.skip_to(round);
-      if (s0 + b * a.parts >= n_sets) continue;
-      const int n = __builtin_amdgcn_readfirstlane(sets[b].n);
+      const bool there = number(batch, b) < n_sets;
+      const SetRows<kMax>& rows = sets[batch & 1][there ? b : b - slot];
+      const int n = there ? __builtin_amdgcn_readfirstlane(rows.n) : 0;
       switch ((n + 15) >> 4) {
-        case 1: backward_set<T, HDP, kForm, 1>(head, sets[b], n, bins, turns); break;
-        case 2: backward_set<T, HDP, kForm, 2>(head, sets[b], n, bins, turns); break;
-        case 3: backward_set<T, HDP, kForm, 3>(head, sets[b], n, bins, turns); break;
-        case 4: if constexpr (kTilesMax > 3) backward_set<T, HDP, kForm, 4>(head, sets[b], n, bins, turns); break;
-        case 5: if constexpr (kTilesMax > 3) backward_set<T, HDP, kForm, 5>(head, sets[b], n, bins, turns); break;
-        case 6: if constexpr (kTilesMax > 3) backward_set<T, HDP, kForm, 6>(head, sets[b], n, bins, turns); break;
+        case 1: backward_set<1>(head, rows, n, bins, turns); break;
+        case 2: backward_set<2>(head, rows, n, bins, turns); break;
+        case 3: backward_set<3>(head, rows, n, bins, turns); break;
+        case 4: if constexpr (kTilesMax > 3) backward_set<4>(head, rows, n, bins, turns); break;
+        case 5: if constexpr (kTilesMax > 3) backward_set<5>(head, rows, n, bins, turns); break;
+        case 6: if constexpr (kTilesMax > 3) backward_set<6>(head, rows, n, bins, turns); break;
       }
+      if (kBeside && b == slot && more) lookup.cells(a);
     }
+    if (!kBeside && more) {
+      lookup.slots(a, number(batch + 1, wave));
+      lookup.cells(a);
+    }
+    if (more) lookup.rows(a, head.entry_bytes(), sets[(batch + 1) & 1][wave]);
     turns.skip_to(round);                         // nobody waits for this wavefront at the barrier
   }
   if (!a.partial) return;

@@ -5,8 +5,8 @@
 namespace {
 
 // All of a set's rows of one head sit in registers: n voxels, kTiles tiles of 16.
-template <typename T, int HDP, TableForm kForm, int kTiles>
-__device__ __forceinline__ void forward_set(const Head<T, HDP, kForm>& head, const SetRows& rows, int n) {
+template <int kTiles, typename T, int HDP, TableForm kForm, int kMax>
+__device__ __forceinline__ void forward_set(const Head<T, HDP, kForm, kMax>& head, const SetRows<kMax>& rows, int n) {
   typedef Frag<T, HDP> F;
   const MhaArgs& a = head.a;
   const int m = head.m, g = head.g;
@@ -54,30 +54,50 @@ __device__ __forceinline__ void forward_set(const Head<T, HDP, kForm>& head, con
 
 template <typename T, int HDP, TableForm kForm, int kTilesMax>
 __global__ __launch_bounds__(64 * mha_waves(false, sizeof(T), HDP, 16 * kTilesMax), mha_per_simd(false, sizeof(T), HDP, 16 * kTilesMax)) void k_mha_forward(MhaArgs a) {
-  __shared__ SetRows sets[kBatch];
+  constexpr int kMax = 16 * kTilesMax;
+  __shared__ SetRows<kMax> sets[2][kMhaWavesMax];
   const Share share(a);
-  const int wave = threadIdx.x >> 6, waves = blockDim.x >> 6, h0 = share.group * a.hs;
+  const int32_t n_sets = sets_of(a);
+  const int wave = threadIdx.x >> 6, h0 = share.group * a.hs;
   float* table = reinterpret_cast<float*>(mha_lds);
   uint16_t* map = reinterpret_cast<uint16_t*>(table + a.hs * a.entries);
   fill_tables<kForm>(a, h0, table, map);
   const int slot = wave / a.hs, hl = wave - slot * a.hs;
-  const Head<T, HDP, kForm> head(a, table + hl * a.entries, map, h0 + hl);
-  const int32_t n_sets = sets_of(a);
-  for (int32_t s0 = share.part; s0 < n_sets; s0 += kBatch * a.parts) {
-    if (s0 != share.part) __syncthreads();
-    for (int b = wave; b < kBatch && s0 + b * a.parts < n_sets; b += waves) load_set(a, s0 + b * a.parts, head.entry_bytes(), sets[b]);
+  const Head<T, HDP, kForm, kMax> head(a, table + hl * a.entries, map, h0 + hl);
+  Lookup<kMax> lookup;
+  // A batch is as many sets as there are wavefronts, each looked up by one.  The look-up of the next batch runs beside this one's sets where
+  // registers allow it.
+  constexpr bool kBeside = kTilesMax <= 3;
+  const int waves = blockDim.x >> 6;
+  const auto number = [&](int32_t batch, int b) { return share.part + (batch * waves + b) * a.parts; };       // a set's
+  const auto looks = [&](int32_t batch) { return number(batch, wave) < n_sets; };
+  if (looks(0)) {
+    lookup.slots(a, number(0, wave));
+    lookup.cells(a);
+    lookup.rows(a, head.entry_bytes(), sets[0][wave]);
+  }
+  for (int32_t batch = 0; number(batch, 0) < n_sets; ++batch) {
     __syncthreads();
-    for (int b = slot; b < kBatch && s0 + b * a.parts < n_sets; b += a.slots) {
-      const int n = __builtin_amdgcn_readfirstlane(sets[b].n);
+    const bool more = looks(batch + 1);
+    if (kBeside && more) lookup.slots(a, number(batch + 1, wave));
+    for (int b = slot; b < waves && number(batch, b) < n_sets; b += a.slots) {
+      const SetRows<kMax>& rows = sets[batch & 1][b];
+      const int n = __builtin_amdgcn_readfirstlane(rows.n);
       switch ((n + 15) >> 4) {
-        case 1: forward_set<T, HDP, kForm, 1>(head, sets[b], n); break;
-        case 2: forward_set<T, HDP, kForm, 2>(head, sets[b], n); break;
-        case 3: forward_set<T, HDP, kForm, 3>(head, sets[b], n); break;
-        case 4: if constexpr (kTilesMax > 3) forward_set<T, HDP, kForm, 4>(head, sets[b], n); break;
-        case 5: if constexpr (kTilesMax > 3) forward_set<T, HDP, kForm, 5>(head, sets[b], n); break;
-        case 6: if constexpr (kTilesMax > 3) forward_set<T, HDP, kForm, 6>(head, sets[b], n); break;
+        case 1: forward_set<1>(head, rows, n); break;
+        case 2: forward_set<2>(head, rows, n); break;
+        case 3: forward_set<3>(head, rows, n); break;
+        case 4: if constexpr (kTilesMax > 3) forward_set<4>(head, rows, n); break;
+        case 5: if constexpr (kTilesMax > 3) forward_set<5>(head, rows, n); break;
+        case 6: if constexpr (kTilesMax > 3) forward_set<6>(head, rows, n); break;
       }
+      if (kBeside && b == slot && more) lookup.cells(a);
     }
+    if (!kBeside && more) {
+      lookup.slots(a, number(batch + 1, wave));
+      lookup.cells(a);
+    }
+    if (more) lookup.rows(a, head.entry_bytes(), sets[(batch + 1) & 1][wave]);
   }
 }
 
