@@ -116,13 +116,16 @@ template <int kMax> struct SetRows {
   int32_t n;
 };
 
+// Largest of the wavefront's values, by shifts over 1, 2, 4, 8 lanes of a row and row broadcasts; in the last lane, from where all get it.
 __device__ __forceinline__ int wave_max(int v) {
-#pragma unroll
-  for (int d = 1; d < 64; d *= 2) {
-    const int o = __shfl_xor(v, d, 64);
-    v = o > v ? o : v;
-  }
-  return v;
+  const auto step = [](int a, int b) { return a > b ? a : b; };
+  v = step(v, __builtin_amdgcn_update_dpp(INT32_MIN, v, 0x111, 0xF, 0xF, false));
+  v = step(v, __builtin_amdgcn_update_dpp(INT32_MIN, v, 0x112, 0xF, 0xF, false));
+  v = step(v, __builtin_amdgcn_update_dpp(INT32_MIN, v, 0x114, 0xF, 0xF, false));
+  v = step(v, __builtin_amdgcn_update_dpp(INT32_MIN, v, 0x118, 0xF, 0xF, false));
+  v = step(v, __builtin_amdgcn_update_dpp(INT32_MIN, v, 0x142, 0xA, 0xF, false));
+  v = step(v, __builtin_amdgcn_update_dpp(INT32_MIN, v, 0x143, 0xC, 0xF, false));
+  return __builtin_amdgcn_readlane(v, 63);
 }
 
 // A wavefront looks a set's distinct voxels up, in slot order: the first slot of every run of equal ones.  Slots outside
@@ -290,18 +293,17 @@ template <typename T, int HDP, TableForm kForm, int kMax> struct Head {
   __device__ __forceinline__ const char* row(const Rows& rows, const void* base, uint32_t ld, int which, int t) const {
     return static_cast<const char*>(base) + (int64_t)(which * a.heads + h) * a.hd * (int)sizeof(T) + (uint64_t)(uint32_t)rows.vox[16 * t + m] * ld;
   }
-  // Rows of tile t of an array of head vectors (which: 0 q, 1 k, 2 v of a qkv row; 0 of an output row).  Of two operands whose product
-  // runs over the channels one has zeros past the last (kZero).
-  template <bool kZero> __device__ __forceinline__ void load(const Rows& rows, const void* base, uint32_t ld, int which, int t, Row (&f)[F::NC]) const {
+  // Rows of tile t of an array of head vectors (which: 0 q, 1 k, 2 v of a qkv row; 0 of an output row).
+  __device__ __forceinline__ void load(const Rows& rows, const void* base, uint32_t ld, int which, int t, Row (&f)[F::NC]) const {
     const char* p = row(rows, base, ld, which, t);
 #pragma unroll
-    for (int c = 0; c < F::NC; ++c) {
-      f[c] = *reinterpret_cast<const Row*>(p + channel(c) * (int)sizeof(T));
-      if constexpr (kZero) {
-        const Row zero = {};
-        f[c] = (4 * c + g) * F::KL < a.hd ? f[c] : zero;
-      }
-    }
+    for (int c = 0; c < F::NC; ++c) f[c] = *reinterpret_cast<const Row*>(p + channel(c) * (int)sizeof(T));
+  }
+  // Zeros past the head's last channel: in one of two operands whose product runs over the channels.
+  __device__ __forceinline__ void clear_past_last(Row (&f)[F::NC]) const {
+    const Row zero = {};
+#pragma unroll
+    for (int c = 0; c < F::NC; ++c) f[c] = (4 * c + g) * F::KL < a.hd ? f[c] : zero;
   }
   // tiles of the transposed result, column m = row m of tile t, if `there`: a lane holds the channels that it holds of a row fragment
   __device__ __forceinline__ void store(const Rows& rows, void* base, uint32_t ld, int which, int t, bool there, const f32x4 (&o)[F::NT],
@@ -409,6 +411,6 @@ __host__ __device__ constexpr int mha_per_cu(bool back, int element, int padded,
 __host__ __device__ constexpr int mha_per_simd(bool back, int element, int padded, int tau) {
   return mha_waves(back, element, padded, tau) * mha_per_cu(back, element, padded, tau) / 4;
 }
-constexpr size_t kMhaLdsMax = 140 << 10;          // dynamic LDS of a workgroup, at most
+constexpr size_t kMhaLdsMax = 130 << 10;          // dynamic LDS of a workgroup, at most: 160 KB less what its sets take (28 KB)
 
 extern __shared__ double mha_lds[];

@@ -17,12 +17,12 @@ struct Turns {
   __device__ __forceinline__ int turn() const { return done * slots + slot; }
   __device__ __forceinline__ void wait() const {
     if (!wanted) return;
-    while (*next != turn()) __builtin_amdgcn_s_sleep(1);
+    while (*next != turn()) {}
     asm volatile("" ::: "memory");
   }
   __device__ __forceinline__ void hand_on() {
     if (!wanted) return;
-    asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");        // this wavefront's additions are in
+    asm volatile("" ::: "memory");                // (LDS does a wavefront's operations in their order: the additions before this)
     if ((threadIdx.x & 63) == 0) *next = turn() + 1;
     ++done;
   }
@@ -52,47 +52,59 @@ struct Bins {
   }
 };
 
-// kHold: the keys' and values' fragments of all tiles stay in registers; else they are read again, from the caches, for each query tile.
-template <typename T, int HDP, int kTiles> constexpr bool hold_rows() { return HDP * sizeof(T) <= 64 && kTiles <= 3; }
+// A set's rows of one head as fragments.  Of sets of up to three tiles of narrow heads they all sit in registers, and the next set's are
+// fetched as soon as this one's are used up, before its last results are written; else they are read as they are needed, again for each query
+// tile, from the caches.
+template <typename T, int HDP, int kMax> constexpr bool hold_rows() { return HDP * sizeof(T) <= 64 && kMax <= 48; }
+template <typename T, int HDP, int kMax> struct Held {
+  static constexpr int kTiles = hold_rows<T, HDP, kMax>() ? kMax / 16 : 1;
+  typename Frag<T, HDP>::Row q[kTiles][Frag<T, HDP>::NC], k[kTiles][Frag<T, HDP>::NC], v[kTiles][Frag<T, HDP>::NC], g[kTiles][Frag<T, HDP>::NC];
+  template <TableForm kForm> __device__ __forceinline__ void fetch(const Head<T, HDP, kForm, kMax>& head, const SetRows<kMax>& rows) {
+    if constexpr (hold_rows<T, HDP, kMax>()) {
+      const MhaArgs& a = head.a;
+      const int tiles = (__builtin_amdgcn_readfirstlane(rows.n) + 15) >> 4;
+#pragma unroll
+      for (int t = 0; t < kTiles; ++t)
+        if (t < tiles) {
+          head.load(rows, a.qkv, a.ld_qkv, 0, t, q[t]);
+          head.load(rows, a.qkv, a.ld_qkv, 1, t, k[t]);
+          head.load(rows, a.qkv, a.ld_qkv, 2, t, v[t]);
+          head.load(rows, a.d_out, a.ld_dout, 0, t, g[t]);
+        }
+    }
+  }
+};
 
 template <int kTiles, typename T, int HDP, TableForm kForm, int kMax>
-__device__ __forceinline__ void backward_set(const Head<T, HDP, kForm, kMax>& head, const SetRows<kMax>& rows, int n, const Bins& bins, Turns& turns) {
+__device__ __forceinline__ void backward_set(const Head<T, HDP, kForm, kMax>& head, const SetRows<kMax>& rows, int n, const Bins& bins, Turns& turns,
+                                             Held<T, HDP, kMax>& held, const SetRows<kMax>* next) {
   typedef Frag<T, HDP> F;
   typedef typename F::Row Row;
   typedef typename F::Tile Tile;
-  constexpr bool kHold = hold_rows<T, HDP, kTiles>();
-  constexpr int kHeld = kHold ? kTiles : 1;
+  constexpr bool kHold = hold_rows<T, HDP, kMax>();
   const MhaArgs& a = head.a;
   const int m = head.m, g = head.g;
   const f32x4 zero = {0.f, 0.f, 0.f, 0.f};
-  Row k[kHeld][F::NC], v[kHeld][F::NC];
-  Row query_rows[kHeld][F::NC], grad_rows[kHeld][F::NC];
-  Tile turned_k[kHeld][F::NT];
-  if constexpr (kHold) {
-#pragma unroll
-    for (int t = 0; t < kTiles; ++t) {
-      head.template load<true>(rows, a.qkv, a.ld_qkv, 0, t, query_rows[t]);
-      head.template load<true>(rows, a.d_out, a.ld_dout, 0, t, grad_rows[t]);
-      head.template load<false>(rows, a.qkv, a.ld_qkv, 1, t, k[t]);
-      head.template load<false>(rows, a.qkv, a.ld_qkv, 2, t, v[t]);
-    }
-  }
+  auto &k = held.k, &v = held.v;
+  Tile turned_k[kHold ? kTiles : 1][F::NT];
   f32x4 dk[kTiles][F::NT] = {}, dv[kTiles][F::NT] = {};
 #pragma unroll kHold ? kTiles : 1
   for (int qt = 0; qt < kTiles; ++qt) {
-    Row (&q)[F::NC] = query_rows[kHold ? qt : 0], (&go)[F::NC] = grad_rows[kHold ? qt : 0];
+    Row (&q)[F::NC] = held.q[kHold ? qt : 0], (&go)[F::NC] = held.g[kHold ? qt : 0];
     if constexpr (!kHold) {
-      head.template load<true>(rows, a.qkv, a.ld_qkv, 0, qt, q);
-      head.template load<true>(rows, a.d_out, a.ld_dout, 0, qt, go);
+      head.load(rows, a.qkv, a.ld_qkv, 0, qt, q);
+      head.load(rows, a.d_out, a.ld_dout, 0, qt, go);
     }
+    head.clear_past_last(q);
+    head.clear_past_last(go);
     const uint32_t at = (uint32_t)rows.code[16 * qt + m] + head.from();
     f32x4 p[kTiles], s[kTiles];                   // p: logits, then probabilities; s: t, then ds
     uint32_t entry[kTiles][4];
 #pragma unroll
     for (int t = 0; t < kTiles; ++t) {
       if constexpr (!kHold) {
-        head.template load<false>(rows, a.qkv, a.ld_qkv, 1, t, k[0]);
-        head.template load<false>(rows, a.qkv, a.ld_qkv, 2, t, v[0]);
+        head.load(rows, a.qkv, a.ld_qkv, 1, t, k[0]);
+        head.load(rows, a.qkv, a.ld_qkv, 2, t, v[0]);
       }
 #pragma unroll
       for (int i = 0; i < 4; ++i) {
@@ -147,7 +159,7 @@ __device__ __forceinline__ void backward_set(const Head<T, HDP, kForm, kMax>& he
 #pragma unroll
     for (int t = 0; t < kTiles; ++t) {
       if constexpr (!kHold) {
-        head.template load<false>(rows, a.qkv, a.ld_qkv, 1, t, k[0]);
+        head.load(rows, a.qkv, a.ld_qkv, 1, t, k[0]);
         head.turn(k[0], turned_k[0]);
       }
       const Tile ds = F::tile(s[t]), ds_t = head.turn(ds), p_t = head.turn(F::tile(p[t]));
@@ -160,6 +172,7 @@ __device__ __forceinline__ void backward_set(const Head<T, HDP, kForm, kMax>& he
     }
     head.store(rows, a.out, a.ld_out, 0, qt, query, dq, a.scale);
   }
+  if (next) held.fetch(head, *next);
   if (!bins.rows_too) return;
 #pragma unroll
   for (int t = 0; t < kTiles; ++t) {
@@ -174,7 +187,7 @@ __device__ __forceinline__ void backward_set(const Head<T, HDP, kForm, kMax>& he
 template <typename T, int HDP, TableForm kForm, int kTilesMax>
 __global__ __launch_bounds__(64 * mha_waves(true, sizeof(T), HDP, 16 * kTilesMax), mha_per_simd(true, sizeof(T), HDP, 16 * kTilesMax)) void k_mha_backward(MhaArgs a) {
   constexpr int kMax = 16 * kTilesMax;
-  __shared__ SetRows<kMax> sets[2][kMhaWavesMax];
+  __shared__ SetRows<kMax> sets[3][kMhaWavesMax];
   __shared__ int next_turn[8];
   const Share share(a);
   const int32_t n_sets = sets_of(a);
@@ -193,45 +206,53 @@ __global__ __launch_bounds__(64 * mha_waves(true, sizeof(T), HDP, 16 * kTilesMax
   Turns turns = {(lds_turn*)(next_turn + hl), a.partial && a.slots > 1, a.slots, slot, (a.tau + 15) >> 4, 0};
   int round = 0;                                  // of `slots` sets, over all batches (a batch is a whole number of rounds)
   Lookup<kMax> lookup;
-  // A batch is as many sets as there are wavefronts, each looked up by one.  The look-up of the next batch runs beside this one's sets where
-  // registers allow it.
+  // A batch is as many sets as there are wavefronts, each looked up by one, two batches ahead: beside this batch's sets where registers
+  // allow it, else after them.
   constexpr bool kBeside = kTilesMax <= 3;
   const int waves = blockDim.x >> 6;
   const auto number = [&](int32_t batch, int b) { return share.part + (batch * waves + b) * a.parts; };       // a set's
-  const auto looks = [&](int32_t batch) { return number(batch, wave) < n_sets; };
-  if (looks(0)) {
-    lookup.slots(a, number(0, wave));
-    lookup.cells(a);
-    lookup.rows(a, head.entry_bytes(), sets[0][wave]);
-  }
+  for (int batch = 0; batch < 2; ++batch)
+    if (number(batch, wave) < n_sets) {
+      lookup.slots(a, number(batch, wave));
+      lookup.cells(a);
+      lookup.rows(a, head.entry_bytes(), sets[batch][wave]);
+    }
+  __syncthreads();
+  Held<T, HDP, kMax> held;
+  if (number(0, slot) < n_sets) held.fetch(head, sets[0][slot]);
+  int now = 0;                                    // batch modulo 3
   for (int32_t batch = 0; number(batch, 0) < n_sets; ++batch) {
-    __syncthreads();
-    const bool more = looks(batch + 1);
-    if (kBeside && more) lookup.slots(a, number(batch + 1, wave));
+    const int after = now == 2 ? 0 : now + 1, last = after == 2 ? 0 : after + 1;
+    const bool more = number(batch + 2, wave) < n_sets;
+    if (kBeside && more) lookup.slots(a, number(batch + 2, wave));
     for (int b = slot; b < waves && number(batch, b - slot) < n_sets; b += a.slots, ++round) {
       turns.skip_to(round);
       const bool there = number(batch, b) < n_sets;
-      const SetRows<kMax>& rows = sets[batch & 1][there ? b : b - slot];
+      const SetRows<kMax>& rows = sets[now][there ? b : b - slot];
       const int n = there ? __builtin_amdgcn_readfirstlane(rows.n) : 0;
+      const SetRows<kMax>* next = b + a.slots < waves ? (number(batch, b + a.slots) < n_sets ? &sets[now][b + a.slots] : nullptr)
+                                                      : (number(batch + 1, slot) < n_sets ? &sets[after][slot] : nullptr);
       switch ((n + 15) >> 4) {
-        case 1: backward_set<1>(head, rows, n, bins, turns); break;
-        case 2: backward_set<2>(head, rows, n, bins, turns); break;
-        case 3: backward_set<3>(head, rows, n, bins, turns); break;
-        case 4: if constexpr (kTilesMax > 3) backward_set<4>(head, rows, n, bins, turns); break;
-        case 5: if constexpr (kTilesMax > 3) backward_set<5>(head, rows, n, bins, turns); break;
-        case 6: if constexpr (kTilesMax > 3) backward_set<6>(head, rows, n, bins, turns); break;
+        case 0: if (next) held.fetch(head, *next); break;
+        case 1: backward_set<1>(head, rows, n, bins, turns, held, next); break;
+        case 2: backward_set<2>(head, rows, n, bins, turns, held, next); break;
+        case 3: backward_set<3>(head, rows, n, bins, turns, held, next); break;
+        case 4: if constexpr (kTilesMax > 3) backward_set<4>(head, rows, n, bins, turns, held, next); break;
+        case 5: if constexpr (kTilesMax > 3) backward_set<5>(head, rows, n, bins, turns, held, next); break;
+        case 6: if constexpr (kTilesMax > 3) backward_set<6>(head, rows, n, bins, turns, held, next); break;
       }
       if (kBeside && b == slot && more) lookup.cells(a);
     }
     if (!kBeside && more) {
-      lookup.slots(a, number(batch + 1, wave));
+      lookup.slots(a, number(batch + 2, wave));
       lookup.cells(a);
     }
-    if (more) lookup.rows(a, head.entry_bytes(), sets[(batch + 1) & 1][wave]);
+    if (more) lookup.rows(a, head.entry_bytes(), sets[last][wave]);
     turns.skip_to(round);                         // nobody waits for this wavefront at the barrier
+    __syncthreads();
+    now = after;
   }
   if (!a.partial) return;
-  __syncthreads();
   if (share.part < n_sets)                        // k_mha_entries reads the parts that had a set
     for (int u = threadIdx.x; u < a.hs * mine; u += blockDim.x)
       a.partial[((int64_t)share.part * a.heads + h0) * a.entries + lo + u] = (float)mha_lds[u];

@@ -12,11 +12,11 @@ __device__ __forceinline__ void forward_set(const Head<T, HDP, kForm, kMax>& hea
   const int m = head.m, g = head.g;
   typename F::Row k[kTiles][F::NC], v[kTiles][F::NC], q[F::NC], next[F::NC];
   typename F::Tile vt[kTiles][F::NT];
-  head.template load<true>(rows, a.qkv, a.ld_qkv, 0, 0, q);
+  head.load(rows, a.qkv, a.ld_qkv, 0, 0, q);
 #pragma unroll
   for (int t = 0; t < kTiles; ++t) {
-    head.template load<false>(rows, a.qkv, a.ld_qkv, 1, t, k[t]);
-    head.template load<false>(rows, a.qkv, a.ld_qkv, 2, t, v[t]);
+    head.load(rows, a.qkv, a.ld_qkv, 1, t, k[t]);
+    head.load(rows, a.qkv, a.ld_qkv, 2, t, v[t]);
   }
   uint32_t key[kTiles][4];
 #pragma unroll
@@ -27,8 +27,9 @@ __device__ __forceinline__ void forward_set(const Head<T, HDP, kForm, kMax>& hea
   for (int t = 0; t < kTiles; ++t) head.turn(v[t], vt[t]);
 #pragma unroll 1
   for (int qt = 0; qt < kTiles; ++qt) {
-    head.template load<true>(rows, a.qkv, a.ld_qkv, 0, qt + 1 < kTiles ? qt + 1 : qt, next);
+    head.load(rows, a.qkv, a.ld_qkv, 0, qt + 1 < kTiles ? qt + 1 : qt, next);
     const uint32_t at = (uint32_t)rows.code[16 * qt + m] + head.from();
+    head.clear_past_last(q);
     f32x4 p[kTiles];
 #pragma unroll
     for (int t = 0; t < kTiles; ++t) {
