@@ -53,25 +53,40 @@ struct Bins {
 };
 
 // A set's rows of one head as fragments.  Of sets of up to three tiles of narrow heads they all sit in registers, and the next set's are
-// fetched as soon as this one's are used up, before its last results are written; else they are read as they are needed, again for each query
+// fetched as soon as this one's are used up; else they are read as they are needed, again for each query
 // tile, from the caches.
 template <typename T, int HDP, int kMax> constexpr bool hold_rows() { return HDP * sizeof(T) <= 64 && kMax <= 48; }
 template <typename T, int HDP, int kMax> struct Held {
   static constexpr int kTiles = hold_rows<T, HDP, kMax>() ? kMax / 16 : 1;
   typename Frag<T, HDP>::Row q[kTiles][Frag<T, HDP>::NC], k[kTiles][Frag<T, HDP>::NC], v[kTiles][Frag<T, HDP>::NC], g[kTiles][Frag<T, HDP>::NC];
-  template <TableForm kForm> __device__ __forceinline__ void fetch(const Head<T, HDP, kForm, kMax>& head, const SetRows<kMax>& rows) {
+  template <TableForm kForm> __device__ __forceinline__ void fetch_kv(const Head<T, HDP, kForm, kMax>& head, const SetRows<kMax>& rows) {
     if constexpr (hold_rows<T, HDP, kMax>()) {
       const MhaArgs& a = head.a;
       const int tiles = (__builtin_amdgcn_readfirstlane(rows.n) + 15) >> 4;
 #pragma unroll
       for (int t = 0; t < kTiles; ++t)
         if (t < tiles) {
-          head.load(rows, a.qkv, a.ld_qkv, 0, t, q[t]);
           head.load(rows, a.qkv, a.ld_qkv, 1, t, k[t]);
           head.load(rows, a.qkv, a.ld_qkv, 2, t, v[t]);
+        }
+    }
+  }
+  // tiles kFirst .. kEnd - 1
+  template <int kFirst, int kEnd, TableForm kForm> __device__ __forceinline__ void fetch_qg(const Head<T, HDP, kForm, kMax>& head, const SetRows<kMax>& rows) {
+    if constexpr (hold_rows<T, HDP, kMax>()) {
+      const MhaArgs& a = head.a;
+      const int tiles = (__builtin_amdgcn_readfirstlane(rows.n) + 15) >> 4;
+#pragma unroll
+      for (int t = kFirst; t < (kEnd < kTiles ? kEnd : kTiles); ++t)
+        if (t < tiles) {
+          head.load(rows, a.qkv, a.ld_qkv, 0, t, q[t]);
           head.load(rows, a.d_out, a.ld_dout, 0, t, g[t]);
         }
     }
+  }
+  template <TableForm kForm> __device__ __forceinline__ void fetch(const Head<T, HDP, kForm, kMax>& head, const SetRows<kMax>& rows) {
+    fetch_qg<0, kTiles>(head, rows);
+    fetch_kv(head, rows);
   }
 };
 
@@ -119,6 +134,16 @@ __device__ __forceinline__ void backward_set(const Head<T, HDP, kForm, kMax>& he
         s[t] = F::row_mma(v[kHold ? t : 0][c], go[c], s[t]);
       }
     }
+    if constexpr (kHold) {
+      if (qt == 0) {
+#pragma unroll
+        for (int t = 0; t < kTiles; ++t) head.turn(k[t], turned_k[t]);
+      }
+      if (qt == kTiles - 1 && next) {             // what this set does not need any more
+        held.fetch_kv(head, *next);
+        held.template fetch_qg<0, kTiles - 1>(head, *next);
+      }
+    }
     const bool query = qt + 1 < kTiles || 16 * qt + m < n;
     const float sum = head.template exponentials<kTiles>(rows, p), inv = query ? inverse(sum) : 0.f;
     float dot = 0.f;
@@ -146,12 +171,6 @@ __device__ __forceinline__ void backward_set(const Head<T, HDP, kForm, kMax>& he
       turns.hand_on();
       if (!bins.rows_too) continue;               // another workgroup writes the rows
     }
-    if constexpr (kHold) {
-      if (qt == 0) {
-#pragma unroll
-        for (int t = 0; t < kTiles; ++t) head.turn(k[t], turned_k[t]);
-      }
-    }
     f32x4 dq[F::NT] = {};
     Tile turned_q[F::NT], turned_g[F::NT];
     head.turn(q, turned_q);
@@ -172,7 +191,7 @@ __device__ __forceinline__ void backward_set(const Head<T, HDP, kForm, kMax>& he
     }
     head.store(rows, a.out, a.ld_out, 0, qt, query, dq, a.scale);
   }
-  if (next) held.fetch(head, *next);
+  if (next) held.template fetch_qg<kTiles - 1, kMax>(head, *next);
   if (!bins.rows_too) return;
 #pragma unroll
   for (int t = 0; t < kTiles; ++t) {
