@@ -240,8 +240,7 @@ template <TableForm kForm> __device__ __forceinline__ void fill_tables(const Mha
   const float root = sqrtf((float)a.hd);
   const float* bias = a.bias + (int64_t)h0 * a.n_rel;
   for (int u = threadIdx.x; u < a.entries; u += blockDim.x) {
-    unsigned r = (unsigned)u;
-    if (kForm == kByOffset && a.bucket) r = (unsigned)a.bucket[u];
+    const unsigned r = (unsigned)u;
     const bool there = a.bias && r < (unsigned)a.n_rel;
     float f[kHeads];
 #pragma unroll

@@ -7,7 +7,7 @@ namespace {
 constexpr int kComputeUnits = 256;                // MI355X
 
 // The parts' sums of the table's gradient added in their order: 64 columns of [heads * entries] a workgroup, 16 slices of the parts.  Entries
-// from n_out on (offsets without a bias) are dropped.
+// from n_out on (pairs without a bias) are dropped.
 __global__ __launch_bounds__(1024) void k_mha_entries(const float* __restrict__ partial, const int32_t* __restrict__ n_sets, int32_t parts,
                                                       int32_t heads, int32_t entries, int32_t n_out, float* __restrict__ out) {
   __shared__ double s[16][64];
@@ -34,28 +34,6 @@ __global__ __launch_bounds__(1024) void k_mha_entries(const float* __restrict__ 
   for (int k = 0; k < 16; ++k) v += s[k][col];
   const int32_t h = (int32_t)(c / entries), u = (int32_t)(c - (int64_t)h * entries);
   if (u < n_out) out[(int64_t)h * n_out + u] = (float)v;
-}
-
-// From offsets to buckets: a wavefront adds a stretch of a head's offsets to a copy of its buckets in LDS, in their order, and the
-// copies are added in theirs.
-__global__ __launch_bounds__(1024) void k_mha_buckets(const float* __restrict__ by_offset, const int32_t* __restrict__ bucket, int32_t n_off,
-                                                      int32_t n_rel, float* __restrict__ d_bias) {
-  float* buckets = reinterpret_cast<float*>(mha_lds);
-  const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63, waves = blockDim.x >> 6;
-  for (int u = threadIdx.x; u < waves * n_rel; u += blockDim.x) buckets[u] = 0.f;
-  __syncthreads();
-  float* mine = buckets + wave * n_rel;
-  const int per = ((n_off + waves - 1) / waves + 63) & ~63, end = (wave + 1) * per < n_off ? (wave + 1) * per : n_off;
-  for (int u = wave * per + lane; u < end; u += 64) {
-    const unsigned b = (unsigned)bucket[u];
-    if (b < (unsigned)n_rel) unsafeAtomicAdd(&mine[b], by_offset[(int64_t)blockIdx.x * n_off + u]);
-  }
-  __syncthreads();
-  for (int u = threadIdx.x; u < n_rel; u += blockDim.x) {
-    double v = 0.;
-    for (int w = 0; w < waves; ++w) v += (double)buckets[w * n_rel + u];
-    d_bias[(int64_t)blockIdx.x * n_rel + u] = (float)v;
-  }
 }
 
 __global__ void k_mha_zero(float* __restrict__ p, int64_t n) {
@@ -93,31 +71,32 @@ int make_plan(const dsvt_mha_cfg* c, int32_t max_sets, int32_t tau, bool back, b
   const bool by_bucket = c->rel_bias && c->rel_bucket;
   const int element = c->dtype == DSVT_BF16 ? 2 : 4, padded = hd <= 16 ? 16 : hd <= 32 ? 32 : 64;
   const int waves = mha_waves(back, element, padded, tau), per_cu = mha_per_cu(back, element, padded, tau);
-  // Of the forms in LDS the one that lets a workgroup take the most heads, of equal ones the first: heads of one set in one workgroup share
-  // cache lines.  In memory if neither fits.
+  // In LDS if it fits there for one head, for as many heads as fit: heads of one set in one workgroup share cache lines.  (Buckets could also be
+  // summed up by offset and folded afterwards: 30,000 pillars, 81 buckets, backward 38.9 us where by bucket takes 37.3, 2,000 voxels 19.6
+  // and 17.1; two lookups a pair cost less than larger tables and one more kernel.)
   p->hs = 0;
-  const TableForm forms[] = {kByOffset, kByBucket, kInMemory};
-  for (size_t most = per_cu == 2 ? kMhaLdsMax / 2 : kMhaLdsMax; p->hs == 0 && most <= kMhaLdsMax; most *= 2)
-    for (const TableForm f : forms) {
-      if (f == kByBucket && (!by_bucket || c->n_rel > 65535)) continue;
-      if (f == kInMemory && (!c->rel_bias || p->hs > 0 || most < kMhaLdsMax)) continue;
-      const int64_t entries = f == kByOffset || !by_bucket ? n_off : (int64_t)c->n_rel + 1;
-      int hs = 0;
-      for (int h = 1; h <= waves; ++h)
-        if (c->heads % h == 0 && lds_bytes(f, h, d_bias ? entries : 0, entries, n_off) <= most) hs = h;
-      if (hs <= p->hs && f != kInMemory) continue;
-      p->form = f;
-      p->hs = hs;
-      p->entries = (int32_t)entries;
-    }
+  p->form = by_bucket ? kByBucket : kByOffset;
+  const int64_t entries = by_bucket ? (int64_t)c->n_rel + 1 : n_off;
+  const auto most_heads = [&](size_t most) {
+    int hs = 0;
+    for (int h = 1; h <= waves; ++h)
+      if (c->heads % h == 0 && lds_bytes(p->form, h, d_bias ? entries : 0, entries, n_off) <= most) hs = h;
+    return hs;
+  };
+  if (by_bucket && c->n_rel > 65535) p->form = kInMemory;
+  p->hs = most_heads(kMhaLdsMax / per_cu);
+  if (p->hs == 0) p->hs = most_heads(kMhaLdsMax);
+  if (p->hs == 0) {
+    p->form = kInMemory;
+    p->hs = most_heads(kMhaLdsMax);
+  }
+  p->entries = (int32_t)entries;
   // Sums that the LDS of a workgroup does not hold for one head: workgroups of a head share its entries, and each goes through all sets.
   p->ranges = 1;
   if (p->hs == 0) {
     p->hs = 1;
     p->ranges = (int32_t)dsvt_ceil_div((int64_t)p->entries * 8, kMhaLdsMax);
   }
-  const bool fold = d_bias && by_bucket && p->form == kByOffset;
-  if (fold && (size_t)c->n_rel * 4 > kMhaLdsMax) return DSVT_EUNSUPPORTED;
   p->n_off = (int32_t)n_off;
   p->lds = lds_bytes(p->form, p->hs, d_bias ? dsvt_ceil_div(p->entries, p->ranges) : 0, p->entries, n_off);
   p->slots = 1;
@@ -125,7 +104,7 @@ int make_plan(const dsvt_mha_cfg* c, int32_t max_sets, int32_t tau, bool back, b
   int64_t parts = dsvt_ceil_div(kComputeUnits * per_cu, c->heads / p->hs * p->ranges);
   if (parts > max_sets) parts = max_sets;
   p->parts = (int32_t)dsvt_align_up((size_t)(parts > 0 ? parts : 1), 8);
-  p->ws = d_bias ? ((size_t)p->parts + fold) * c->heads * (size_t)p->entries * 4 : 0;
+  p->ws = d_bias ? (size_t)p->parts * c->heads * (size_t)p->entries * 4 : 0;
   return DSVT_OK;
 }
 
@@ -230,22 +209,12 @@ extern "C" int dsvt_set_mha_backward(const dsvt_mha_cfg* cfg, const dsvt_maps* m
   MhaArgs a = make_args(cfg, maps, coords, p);
   a.qkv = qkv; a.ld_qkv = (uint32_t)(ld_qkv * e); a.d_out = d_out; a.ld_dout = (uint32_t)(ld_dout * e); a.out = d_qkv; a.ld_out = (uint32_t)(ld_dqkv * e);
   a.partial = d_rel_bias ? static_cast<float*>(ws) : nullptr;
-  const bool fold = d_rel_bias && cfg->rel_bucket && p.form == kByOffset;
-  static std::atomic<uint64_t> allowed;
-  if (fold)
-    if (const int rc = dsvt_allow_lds(reinterpret_cast<const void*>(k_mha_buckets), kMhaLdsMax, allowed)) return rc;
   if (const int rc = cfg->dtype == DSVT_BF16 ? mha_backward_bf16(a, p.form, p.lds, st) : mha_backward_f32(a, p.form, p.lds, st)) return rc;
   if (d_rel_bias) {
     const int64_t cols = (int64_t)cfg->heads * p.entries;
-    float* sums = fold ? a.partial + p.parts * cols : d_rel_bias;
     dsvt_prof_scope ps(DSVT_K_MHA_REL, st);
     k_mha_entries<<<(unsigned)dsvt_ceil_div(cols, 64), 1024, 0, st>>>(a.partial, maps->n_sets, p.parts < maps->max_sets ? p.parts : maps->max_sets, cfg->heads,
-                                                                     p.entries, fold ? p.entries : cfg->n_rel, sums);
-    if (fold) {
-      size_t waves = kMhaLdsMax / ((size_t)cfg->n_rel * 4);
-      waves = waves > 16 ? 16 : waves;
-      k_mha_buckets<<<(unsigned)cfg->heads, (unsigned)(64 * waves), waves * cfg->n_rel * 4, st>>>(sums, cfg->rel_bucket, p.n_off, cfg->n_rel, d_rel_bias);
-    }
+                                                                     p.entries, cfg->n_rel, d_rel_bias);
   }
   DSVT_HIP_TRY(hipGetLastError());
   return DSVT_OK;
