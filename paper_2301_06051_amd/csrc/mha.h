@@ -357,7 +357,8 @@ template <typename T, int HDP, TableForm kForm, int kMax> struct Head {
     return *(lds_float*)(uintptr_t)entry;
   }
 
-  // Probabilities of one query tile before their division by the sum: p holds the logits of kTiles key tiles in units of sigma.
+  // Probabilities of one query tile before their division by the sum: p holds the logits of kTiles key tiles in units of sigma.  Returns
+  // this lane's part of the sum.
   template <int kTiles> __device__ __forceinline__ float exponentials(const Rows& rows, f32x4 (&p)[kTiles]) const {
     float top = -INFINITY;
 #pragma unroll
@@ -391,7 +392,7 @@ template <typename T, int HDP, TableForm kForm, int kMax> struct Head {
     for (int k = 0; k < kTiles; ++k)
 #pragma unroll
       for (int i = 0; i < 4; ++i) sum += p[k][i];
-    return across_sum(sum);
+    return sum;
   }
 };
 

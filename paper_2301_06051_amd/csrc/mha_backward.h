@@ -145,20 +145,21 @@ __device__ __forceinline__ void backward_set(const Head<T, HDP, kForm, kMax>& he
       }
     }
     const bool query = qt + 1 < kTiles || 16 * qt + m < n;
-    const float sum = head.template exponentials<kTiles>(rows, p), inv = query ? inverse(sum) : 0.f;
-    float dot = 0.f;
+    float sum = head.template exponentials<kTiles>(rows, p), dot = 0.f;
+#pragma unroll
+    for (int t = 0; t < kTiles; ++t)
+#pragma unroll
+      for (int i = 0; i < 4; ++i) dot = fmaf(p[t][i], s[t][i], dot);
+    sum = across_sum(sum);
+    const float inv = query ? inverse(sum) : 0.f;
+    dot = across_sum(dot) * inv;
 #pragma unroll
     for (int t = 0; t < kTiles; ++t)
 #pragma unroll
       for (int i = 0; i < 4; ++i) {
         p[t][i] *= inv;
-        dot = fmaf(p[t][i], s[t][i], dot);
+        s[t][i] = p[t][i] * (s[t][i] - dot);
       }
-    dot = across_sum(dot);
-#pragma unroll
-    for (int t = 0; t < kTiles; ++t)
-#pragma unroll
-      for (int i = 0; i < 4; ++i) s[t][i] = p[t][i] * (s[t][i] - dot);
     if (a.partial) {
       turns.wait();
       if (query) {
@@ -209,16 +210,11 @@ __global__ __launch_bounds__(64 * mha_waves(true, sizeof(T), HDP, 16 * kTilesMax
   __shared__ SetRows<kMax> sets[3][kMhaWavesMax];
   __shared__ int next_turn[8];
   const Share share(a);
-  const int32_t n_sets = sets_of(a);
   const int wave = threadIdx.x >> 6, range = share.group % a.ranges, h0 = share.group / a.ranges * a.hs, all = a.hs * a.entries;
   // entries of a head that this workgroup adds up: all, or its range of them (then hs = 1)
   const int per = (a.entries + a.ranges - 1) / a.ranges, lo = range * per, mine = lo + per < a.entries ? per : (a.entries > lo ? a.entries - lo : 0);
   float* table = reinterpret_cast<float*>(mha_lds + (a.partial ? a.hs * per : 0));
   uint16_t* map = reinterpret_cast<uint16_t*>(table + all);
-  fill_tables<kForm>(a, h0, table, map);
-  if (a.partial)
-    for (int u = threadIdx.x; u < a.hs * per; u += blockDim.x) mha_lds[u] = 0.;
-  if (threadIdx.x < 8) next_turn[threadIdx.x] = 0;
   const int slot = wave / a.hs, hl = wave - slot * a.hs;
   const Head<T, HDP, kForm, kMax> head(a, table + hl * a.entries, map, h0 + hl);
   const Bins bins = {lds_address(mha_lds + hl * per) - (kForm == kInMemory ? 0u : 2 * lds_address(table + hl * a.entries)), 4u * lo, 4u * mine, range == 0};
@@ -230,12 +226,19 @@ __global__ __launch_bounds__(64 * mha_waves(true, sizeof(T), HDP, 16 * kTilesMax
   constexpr bool kBeside = kTilesMax <= 3;
   const int waves = blockDim.x >> 6;
   const auto number = [&](int32_t batch, int b) { return share.part + (batch * waves + b) * a.parts; };       // a set's
-  for (int batch = 0; batch < 2; ++batch)
-    if (number(batch, wave) < n_sets) {
-      lookup.slots(a, number(batch, wave));
-      lookup.cells(a);
-      lookup.rows(a, head.entry_bytes(), sets[batch][wave]);
-    }
+  // (slots of sets past n_sets may be fetched, not used: their loads do not wait for n_sets, nor the tables' for them)
+  Lookup<kMax> second;
+  if (number(0, wave) < a.max_sets) lookup.slots(a, number(0, wave));
+  if (number(1, wave) < a.max_sets) second.slots(a, number(1, wave));
+  fill_tables<kForm>(a, h0, table, map);
+  if (a.partial)
+    for (int u = threadIdx.x; u < a.hs * per; u += blockDim.x) mha_lds[u] = 0.;
+  if (threadIdx.x < 8) next_turn[threadIdx.x] = 0;
+  const int32_t n_sets = sets_of(a);
+  if (number(0, wave) < n_sets) lookup.cells(a);
+  if (number(1, wave) < n_sets) second.cells(a);
+  if (number(0, wave) < n_sets) lookup.rows(a, head.entry_bytes(), sets[0][wave]);
+  if (number(1, wave) < n_sets) second.rows(a, head.entry_bytes(), sets[1][wave]);
   __syncthreads();
   Held<T, HDP, kMax> held;
   if (number(0, slot) < n_sets) held.fetch(head, sets[0][slot]);

@@ -41,7 +41,7 @@ __device__ __forceinline__ void forward_set(const Head<T, HDP, kForm, kMax>& hea
 #pragma unroll
       for (int c = 0; c < F::NC; ++c) p[t] = F::row_mma(k[t][c], q[c], p[t]);
     }
-    const float sum = head.template exponentials<kTiles>(rows, p);
+    const float sum = across_sum(head.template exponentials<kTiles>(rows, p));
     f32x4 o[F::NT] = {};
 #pragma unroll
     for (int t = 0; t < kTiles; ++t)
@@ -58,11 +58,9 @@ __global__ __launch_bounds__(64 * mha_waves(false, sizeof(T), HDP, 16 * kTilesMa
   constexpr int kMax = 16 * kTilesMax;
   __shared__ SetRows<kMax> sets[2][kMhaWavesMax];
   const Share share(a);
-  const int32_t n_sets = sets_of(a);
   const int wave = threadIdx.x >> 6, h0 = share.group * a.hs;
   float* table = reinterpret_cast<float*>(mha_lds);
   uint16_t* map = reinterpret_cast<uint16_t*>(table + a.hs * a.entries);
-  fill_tables<kForm>(a, h0, table, map);
   const int slot = wave / a.hs, hl = wave - slot * a.hs;
   const Head<T, HDP, kForm, kMax> head(a, table + hl * a.entries, map, h0 + hl);
   Lookup<kMax> lookup;
@@ -71,9 +69,12 @@ __global__ __launch_bounds__(64 * mha_waves(false, sizeof(T), HDP, 16 * kTilesMa
   constexpr bool kBeside = kTilesMax <= 3;
   const int waves = blockDim.x >> 6;
   const auto number = [&](int32_t batch, int b) { return share.part + (batch * waves + b) * a.parts; };       // a set's
+  // (slots of sets past n_sets may be fetched, not used: their loads do not wait for n_sets, nor the tables' for them)
+  if (number(0, wave) < a.max_sets) lookup.slots(a, number(0, wave));
+  fill_tables<kForm>(a, h0, table, map);
+  const int32_t n_sets = sets_of(a);
   const auto looks = [&](int32_t batch) { return number(batch, wave) < n_sets; };
   if (looks(0)) {
-    lookup.slots(a, number(0, wave));
     lookup.cells(a);
     lookup.rows(a, head.entry_bytes(), sets[0][wave]);
   }
