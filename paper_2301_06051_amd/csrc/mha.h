@@ -232,22 +232,30 @@ __device__ __forceinline__ int32_t sets_of(const MhaArgs& a) {
 // Place of the next `bytes` of dynamic LDS.
 __device__ __forceinline__ uint32_t lds_address(const void* p) { return (uint32_t)(uintptr_t)(__attribute__((address_space(3))) const void*)p; }
 
-// The heads' biases in units of sigma, and by bucket the offsets' buckets; offsets without a bias get 0.  A thread fetches an entry of all
+// The heads' biases in units of sigma, and by bucket the offsets' buckets; offsets without a bias get 0.  A thread fetches two entries of all
 // heads, or eight buckets, before it stores any: one after the other they were half of a forward call on 30,000 voxels.
 template <TableForm kForm> __device__ __forceinline__ void fill_tables(const MhaArgs& a, int h0, float* table, uint16_t* map) {
   if constexpr (kForm == kInMemory) return;
-  constexpr int kHeads = 8;                       // of a workgroup, at most
+  constexpr int kHeads = kMhaWavesMax, kEntries = 2;
   const float root = sqrtf((float)a.hd);
   const float* bias = a.bias + (int64_t)h0 * a.n_rel;
-  for (int u = threadIdx.x; u < a.entries; u += blockDim.x) {
-    const unsigned r = (unsigned)u;
-    const bool there = a.bias && r < (unsigned)a.n_rel;
-    float f[kHeads];
+  for (int u = threadIdx.x; u < a.entries; u += kEntries * (int)blockDim.x) {
+    float f[kEntries][kHeads] = {};
+    if (a.bias) {
 #pragma unroll
-    for (int h = 0; h < kHeads; ++h) f[h] = there && h < a.hs ? bias[(int64_t)h * a.n_rel + r] : 0.f;
+      for (int j = 0; j < kEntries; ++j) {
+        const int at = u + j * (int)blockDim.x, r = at < a.n_rel ? at : a.n_rel - 1;       // (fetched where there is none, and cleared below)
 #pragma unroll
-    for (int h = 0; h < kHeads; ++h)
-      if (h < a.hs) table[h * a.entries + u] = to_units(f[h], root);
+        for (int h = 0; h < kHeads; ++h) f[j][h] = bias[(int64_t)(h < a.hs ? h : 0) * a.n_rel + r];
+      }
+    }
+#pragma unroll
+    for (int j = 0; j < kEntries; ++j) {
+      const int at = u + j * (int)blockDim.x;
+#pragma unroll
+      for (int h = 0; h < kHeads; ++h)
+        if (h < a.hs && at < a.entries) table[h * a.entries + at] = at < a.n_rel ? to_units(f[j][h], root) : 0.f;
+    }
   }
   if constexpr (kForm == kByBucket) {
     constexpr int kAtOnce = 8;
