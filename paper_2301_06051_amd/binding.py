@@ -443,29 +443,23 @@ def dsvt_vfe(vfe, points, point_batch=None, stream=None):
     return vfe
 
 
-# The current device and the handle of its current stream, without the objects that torch.cuda puts around them: a call of a small
-# operator is mostly host time.
-def _current_device():
-    return torch._C._cuda_getDevice()
+# The current device and the handle of its current stream come without the objects that torch.cuda puts around them, and workspace
+# sizes are asked for once per shape: a call of a small operator is mostly host time.
+_current_device, _current_stream = torch._C._cuda_getDevice, torch._C._cuda_getCurrentRawStream
 
 
-def _current_stream(device):
-    return torch._C._cuda_getCurrentRawStream(device)
-
-
-def _rows(t, shape, dtype, what):
-    """The row stride of a [rows, columns] tensor of the current device whose columns are neighbours."""
-    if t.shape != shape or t.dtype is not dtype or not t.is_cuda or (shape[1] > 1 and t.stride(1) != 1):
-        raise ValueError(f"{what}: a {dtype} GPU tensor of shape {tuple(shape)} with neighbouring columns is wanted, got {t.dtype} "
-                         f"{tuple(t.shape)} strides {tuple(t.stride())} on {t.device}")
-    if t.get_device() != _current_device():
-        raise ValueError(f"{what} is on {t.device}, the current device is {_current_device()}")
+def _rows(t, shape, dtype, device, what):
+    """The row stride of a [rows, columns] tensor of the current device (`device`) whose columns are neighbours."""
+    if t.shape != shape or t.dtype is not dtype or t.get_device() != device or (shape[1] > 1 and t.stride(1) != 1):
+        raise ValueError(f"{what}: a {dtype} tensor of shape {tuple(shape)} with neighbouring columns on the current device, cuda:{device}, is wanted; "
+                         f"got {t.dtype} {tuple(t.shape)}, strides {tuple(t.stride())}, on {t.device}")
     return t.stride(0) if shape[0] > 1 else max(t.stride(0), shape[1])
 
 
-def _vector(t, shape, dtype, what):
-    if t.shape != shape or t.dtype is not dtype or not t.is_cuda or not t.is_contiguous():
-        raise ValueError(f"{what}: a contiguous {dtype} GPU tensor of shape {tuple(shape)} is wanted, got {t.dtype} {tuple(t.shape)} on {t.device}")
+def _vector(t, shape, dtype, device, what):
+    if t.shape != shape or t.dtype is not dtype or t.get_device() != device or not t.is_contiguous():
+        raise ValueError(f"{what}: a contiguous {dtype} tensor of shape {tuple(shape)} on the current device, cuda:{device}, is wanted; got {t.dtype} "
+                         f"{tuple(t.shape)} on {t.device}")
 
 
 def _scratch(nbytes, ws, stream, like):
@@ -475,11 +469,6 @@ def _scratch(nbytes, ws, stream, like):
         if stream is not None:
             ws.record_stream(torch.cuda.ExternalStream(stream))
     return ws
-
-
-def _on(stream, device):
-    """The stream to launch on: the one given by its handle, or the current one of the device."""
-    return _current_stream(device) if stream is None else stream
 
 
 def dsvt_rel_buckets(win, n_exact, n_side):
@@ -505,54 +494,60 @@ class SetMha:
         n_rel = 0
         if rel_bias is not None:
             n_rel = rel_bias.shape[-1]
-            _vector(rel_bias, (heads, n_rel), torch.float32, "rel_bias")
+            _vector(rel_bias, (heads, n_rel), torch.float32, _current_device(), "rel_bias")
         if rel_bucket is not None:
-            _vector(rel_bucket, (offsets,), torch.int32, "rel_bucket")
+            _vector(rel_bucket, (offsets,), torch.int32, _current_device(), "rel_bucket")
         self.struct = MhaCfg(channels, heads, code, I32x3(*win), dup_mode, None if rel_bias is None else rel_bias.data_ptr(),
                              None if rel_bucket is None else rel_bucket.data_ptr(), n_rel)
-        self.ref = C.byref(self.struct)
+        self.ref, self.sizes = C.byref(self.struct), {}      # sizes: workspace bytes by shape
 
 
 def dsvt_set_mha(mha, maps, coords, qkv, out=None, stream=None):
     """Attention inside every set of `maps` on projected rows qkv [N, 3C]; returns out [N, C]."""
-    n, c, dtype = maps.n_voxels, mha.C, mha.dtype
-    ld = _rows(qkv, (n, 3 * c), dtype, "qkv")
-    _vector(coords, (n, 4), torch.int32, "coords")
+    n, c, dtype, dev = maps.n_voxels, mha.C, mha.dtype, _current_device()
+    ld = _rows(qkv, (n, 3 * c), dtype, dev, "qkv")
+    _vector(coords, (n, 4), torch.int32, dev, "coords")
     if out is None:
         out, ld_out = qkv.new_empty((n, c)), c
     else:
-        ld_out = _rows(out, (n, c), dtype, "out")
+        ld_out = _rows(out, (n, c), dtype, dev, "out")
     rc = lib().dsvt_set_mha(mha.ref, C.byref(maps.struct), coords.data_ptr(), qkv.data_ptr(), ld, out.data_ptr(), ld_out,
-                            _on(stream, qkv.get_device()))
+                            _current_stream(dev) if stream is None else stream)
     if rc:
         _check("dsvt_set_mha", rc)
     return out
 
 
 def dsvt_set_mha_backward_workspace_size(mha, maps):
-    b = C.c_size_t(0)
-    _check("dsvt_set_mha_backward_workspace_size", lib().dsvt_set_mha_backward_workspace_size(mha.ref, C.byref(maps.struct), C.byref(b)))
-    return b.value
+    shape = (maps.max_sets, maps.tau)
+    size = mha.sizes.get(shape)
+    if size is None:
+        b = C.c_size_t(0)
+        _check("dsvt_set_mha_backward_workspace_size", lib().dsvt_set_mha_backward_workspace_size(mha.ref, C.byref(maps.struct), C.byref(b)))
+        size = mha.sizes[shape] = b.value
+    return size
 
 
 def dsvt_set_mha_backward(mha, maps, coords, qkv, d_out, d_qkv=None, d_rel_bias=None, want_rel_bias=True, ws=None, stream=None):
     """Gradients of dsvt_set_mha: returns (d_qkv [N, 3C], d_rel_bias [heads, n_rel] float32, or None without a table or if not
     wanted)."""
-    n, c, dtype = maps.n_voxels, mha.C, mha.dtype
-    ld, ld_out = _rows(qkv, (n, 3 * c), dtype, "qkv"), _rows(d_out, (n, c), dtype, "d_out")
-    _vector(coords, (n, 4), torch.int32, "coords")
+    n, c, dtype, dev = maps.n_voxels, mha.C, mha.dtype, _current_device()
+    ld, ld_out = _rows(qkv, (n, 3 * c), dtype, dev, "qkv"), _rows(d_out, (n, c), dtype, dev, "d_out")
+    _vector(coords, (n, 4), torch.int32, dev, "coords")
     if d_qkv is None:
         d_qkv, ld_d = qkv.new_empty((n, 3 * c)), 3 * c
     else:
-        ld_d = _rows(d_qkv, (n, 3 * c), dtype, "d_qkv")
+        ld_d = _rows(d_qkv, (n, 3 * c), dtype, dev, "d_qkv")
     if d_rel_bias is not None:
-        _vector(d_rel_bias, mha.rel_bias.shape if mha.rel_bias is not None else (), torch.float32, "d_rel_bias")
+        _vector(d_rel_bias, mha.rel_bias.shape if mha.rel_bias is not None else (), torch.float32, dev, "d_rel_bias")
     elif want_rel_bias and mha.rel_bias is not None:
         d_rel_bias = torch.empty_like(mha.rel_bias)
-    ws = _scratch(dsvt_set_mha_backward_workspace_size(mha, maps) if d_rel_bias is not None and ws is None else 0, ws, stream, qkv)
+    p_ws, ws_bytes, p_rel = None, 0, None
+    if d_rel_bias is not None:
+        ws = _scratch(dsvt_set_mha_backward_workspace_size(mha, maps) if ws is None else 0, ws, stream, qkv)
+        p_ws, ws_bytes, p_rel = ws.data_ptr(), ws.numel(), d_rel_bias.data_ptr()
     rc = lib().dsvt_set_mha_backward(mha.ref, C.byref(maps.struct), coords.data_ptr(), qkv.data_ptr(), ld, d_out.data_ptr(), ld_out,
-                                     d_qkv.data_ptr(), ld_d, None if d_rel_bias is None else d_rel_bias.data_ptr(), ws.data_ptr(), ws.numel(),
-                                     _on(stream, qkv.get_device()))
+                                     d_qkv.data_ptr(), ld_d, p_rel, p_ws, ws_bytes, _current_stream(dev) if stream is None else stream)
     if rc:
         _check("dsvt_set_mha_backward", rc)
     return d_qkv, d_rel_bias
@@ -564,53 +559,56 @@ class LayerNorm:
     def __init__(self, gamma, beta, dtype, eps=1e-5):
         code, self.dtype = _DT[dtype]
         self.C, self.gamma, self.beta = gamma.shape[0], gamma, beta
-        _vector(gamma, (self.C,), torch.float32, "gamma")
-        _vector(beta, (self.C,), torch.float32, "beta")
+        _vector(gamma, (self.C,), torch.float32, _current_device(), "gamma")
+        _vector(beta, (self.C,), torch.float32, _current_device(), "beta")
         self.struct = LnCfg(self.C, code, gamma.data_ptr(), beta.data_ptr(), eps)
-        self.ref = C.byref(self.struct)
+        self.ref, self.sizes = C.byref(self.struct), {}      # sizes: workspace bytes by shape
 
 
 def dsvt_layer_norm(ln, x, res=None, y=None, stream=None):
     """LayerNorm of x + res (of x without res), rows [N, C]; returns y."""
-    shape, dtype = (x.shape[0], ln.C), ln.dtype
-    ld_x = _rows(x, shape, dtype, "x")
-    ld_res, p_res = (0, None) if res is None else (_rows(res, shape, dtype, "res"), res.data_ptr())
+    n, c, dtype, dev = x.shape[0], ln.C, ln.dtype, _current_device()
+    ld_x = _rows(x, (n, c), dtype, dev, "x")
+    ld_res, p_res = (0, None) if res is None else (_rows(res, (n, c), dtype, dev, "res"), res.data_ptr())
     if y is None:
-        y, ld_y = x.new_empty(shape), ln.C
+        y, ld_y = x.new_empty((n, c)), c
     else:
-        ld_y = _rows(y, shape, dtype, "y")
-    rc = lib().dsvt_layer_norm(ln.ref, x.data_ptr(), ld_x, p_res, ld_res, shape[0], y.data_ptr(), ld_y, _on(stream, x.get_device()))
+        ld_y = _rows(y, (n, c), dtype, dev, "y")
+    rc = lib().dsvt_layer_norm(ln.ref, x.data_ptr(), ld_x, p_res, ld_res, n, y.data_ptr(), ld_y, _current_stream(dev) if stream is None else stream)
     if rc:
         _check("dsvt_layer_norm", rc)
     return y
 
 
 def dsvt_layer_norm_backward_workspace_size(ln, n_rows):
-    b = C.c_size_t(0)
-    _check("dsvt_layer_norm_backward_workspace_size", lib().dsvt_layer_norm_backward_workspace_size(ln.ref, n_rows, C.byref(b)))
-    return b.value
+    size = ln.sizes.get(n_rows)
+    if size is None:
+        b = C.c_size_t(0)
+        _check("dsvt_layer_norm_backward_workspace_size", lib().dsvt_layer_norm_backward_workspace_size(ln.ref, n_rows, C.byref(b)))
+        size = ln.sizes[n_rows] = b.value
+    return size
 
 
 def dsvt_layer_norm_backward(ln, dy, x, res=None, dx=None, d_gamma=None, d_beta=None, ws=None, stream=None):
     """Gradients of dsvt_layer_norm: returns (dx, which is that of x and of res, d_gamma [C], d_beta [C])."""
-    shape, dtype = (x.shape[0], ln.C), ln.dtype
-    ld_dy, ld_x = _rows(dy, shape, dtype, "dy"), _rows(x, shape, dtype, "x")
-    ld_res, p_res = (0, None) if res is None else (_rows(res, shape, dtype, "res"), res.data_ptr())
+    n, c, dtype, dev = x.shape[0], ln.C, ln.dtype, _current_device()
+    ld_dy, ld_x = _rows(dy, (n, c), dtype, dev, "dy"), _rows(x, (n, c), dtype, dev, "x")
+    ld_res, p_res = (0, None) if res is None else (_rows(res, (n, c), dtype, dev, "res"), res.data_ptr())
     if dx is None:
-        dx, ld_dx = x.new_empty(shape), ln.C
+        dx, ld_dx = x.new_empty((n, c)), c
     else:
-        ld_dx = _rows(dx, shape, dtype, "dx")
+        ld_dx = _rows(dx, (n, c), dtype, dev, "dx")
     if d_gamma is None:
         d_gamma = torch.empty_like(ln.gamma)
     else:
-        _vector(d_gamma, (ln.C,), torch.float32, "d_gamma")
+        _vector(d_gamma, (c,), torch.float32, dev, "d_gamma")
     if d_beta is None:
         d_beta = torch.empty_like(ln.gamma)
     else:
-        _vector(d_beta, (ln.C,), torch.float32, "d_beta")
-    ws = _scratch(dsvt_layer_norm_backward_workspace_size(ln, shape[0]) if ws is None else 0, ws, stream, x)
-    rc = lib().dsvt_layer_norm_backward(ln.ref, dy.data_ptr(), ld_dy, x.data_ptr(), ld_x, p_res, ld_res, shape[0], dx.data_ptr(), ld_dx,
-                                        d_gamma.data_ptr(), d_beta.data_ptr(), ws.data_ptr(), ws.numel(), _on(stream, x.get_device()))
+        _vector(d_beta, (c,), torch.float32, dev, "d_beta")
+    ws = _scratch(dsvt_layer_norm_backward_workspace_size(ln, n) if ws is None else 0, ws, stream, x)
+    rc = lib().dsvt_layer_norm_backward(ln.ref, dy.data_ptr(), ld_dy, x.data_ptr(), ld_x, p_res, ld_res, n, dx.data_ptr(), ld_dx, d_gamma.data_ptr(),
+                                        d_beta.data_ptr(), ws.data_ptr(), ws.numel(), _current_stream(dev) if stream is None else stream)
     if rc:
         _check("dsvt_layer_norm_backward", rc)
     return dx, d_gamma, d_beta
