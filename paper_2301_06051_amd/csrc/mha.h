@@ -21,6 +21,7 @@
 #include "mma.h"
 #include <cfloat>
 #include <cmath>
+#include <type_traits>
 
 constexpr int kSetMax = 96;                       // slots, and so voxels, of a set
 constexpr int kMhaWavesMax = 8;                   // wavefronts of a workgroup, and so sets that it looks up together
@@ -233,30 +234,37 @@ __device__ __forceinline__ int32_t sets_of(const MhaArgs& a) {
 __device__ __forceinline__ uint32_t lds_address(const void* p) { return (uint32_t)(uintptr_t)(__attribute__((address_space(3))) const void*)p; }
 
 // The heads' biases in units of sigma, and by bucket the offsets' buckets; offsets without a bias get 0.  A thread fetches two entries of all
-// heads, or eight buckets, before it stores any: one after the other they were half of a forward call on 30,000 voxels.
+// heads, 16 of one head, or eight buckets, before it stores any: one after the other they were half of a forward call on 30,000 voxels.
 template <TableForm kForm> __device__ __forceinline__ void fill_tables(const MhaArgs& a, int h0, float* table, uint16_t* map) {
   if constexpr (kForm == kInMemory) return;
-  constexpr int kHeads = kMhaWavesMax, kEntries = 2;
   const float root = sqrtf((float)a.hd);
   const float* bias = a.bias + (int64_t)h0 * a.n_rel;
-  for (int u = threadIdx.x; u < a.entries; u += kEntries * (int)blockDim.x) {
-    float f[kEntries][kHeads] = {};
-    if (a.bias) {
+  const int step = blockDim.x;
+  // kHeads heads from h1 on, kEntries entries of each
+  const auto fetch = [&](auto heads, auto entries, int h1) {
+    constexpr int kHeads = decltype(heads)::value, kEntries = decltype(entries)::value;
+    for (int u = threadIdx.x; u < a.entries; u += kEntries * step) {
+      float f[kEntries][kHeads] = {};
+      if (a.bias) {
+#pragma unroll
+        for (int j = 0; j < kEntries; ++j) {
+          const int at = u + j * step, r = at < a.n_rel ? at : a.n_rel - 1;                // (fetched where there is none, and cleared below)
+#pragma unroll
+          for (int h = 0; h < kHeads; ++h) f[j][h] = bias[(int64_t)(h1 + h < a.hs ? h1 + h : 0) * a.n_rel + r];
+        }
+      }
 #pragma unroll
       for (int j = 0; j < kEntries; ++j) {
-        const int at = u + j * (int)blockDim.x, r = at < a.n_rel ? at : a.n_rel - 1;       // (fetched where there is none, and cleared below)
+        const int at = u + j * step;
 #pragma unroll
-        for (int h = 0; h < kHeads; ++h) f[j][h] = bias[(int64_t)(h < a.hs ? h : 0) * a.n_rel + r];
+        for (int h = 0; h < kHeads; ++h)
+          if (h1 + h < a.hs && at < a.entries) table[(h1 + h) * a.entries + at] = at < a.n_rel ? to_units(f[j][h], root) : 0.f;
       }
     }
-#pragma unroll
-    for (int j = 0; j < kEntries; ++j) {
-      const int at = u + j * (int)blockDim.x;
-#pragma unroll
-      for (int h = 0; h < kHeads; ++h)
-        if (h < a.hs && at < a.entries) table[h * a.entries + at] = at < a.n_rel ? to_units(f[j][h], root) : 0.f;
-    }
-  }
+  };
+  if (a.hs > 2) fetch(std::integral_constant<int, kMhaWavesMax>(), std::integral_constant<int, 2>(), 0);
+  else
+    for (int h = 0; h < a.hs; ++h) fetch(std::integral_constant<int, 1>(), std::integral_constant<int, 16>(), h);
   if constexpr (kForm == kByBucket) {
     constexpr int kAtOnce = 8;
     for (int u = threadIdx.x; u < a.n_off; u += kAtOnce * blockDim.x) {
