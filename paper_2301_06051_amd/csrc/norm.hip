@@ -7,8 +7,8 @@
 // z, its mean and its variance are formed again in the backward pass instead of being kept: x and res hold the sum
 // exactly, where a z kept in bf16 would not, and one more row read is one row less written by the forward pass.
 //
-// Both passes are bound by the bytes of their rows.  A row sits in the registers of kLanes neighbouring lanes (8 to 64, up to
-// four 16-byte pieces each), so it is read once, and its sums take three to six steps across lanes.  Workgroups stay and
+// Both passes are bound by the bytes of their rows.  A row sits in the registers of kLanes neighbouring lanes (8 to 64, or a workgroup's
+// 256, up to four 16-byte pieces each), so it is read once, and its sums take three to eight steps across lanes.  Workgroups stay and
 // take rows in turn: gamma and beta are read once a workgroup, and the backward pass adds d_gamma and d_beta up in
 // registers, then in LDS and in one row of partial sums a workgroup, which k_ln_sum adds in their order.  All sums are
 // held in 32 bits or more, and none depends on the order in which workgroups run.
@@ -18,7 +18,7 @@
 namespace {
 
 constexpr int kThreads = 256;
-constexpr int kVectors = 4;                       // pieces of a row in one lane, at most
+constexpr int kVectors = 4, kNarrow = 16;         // pieces of a row in one lane, at most: 16-byte ones, smaller ones
 constexpr int kBackwardGroups = 512;              // workgroups of a backward pass, at most: two a compute unit
 constexpr int kForwardGroups = 2048;
 
@@ -52,10 +52,18 @@ template <typename T, int V> __device__ __forceinline__ typename Piece<T, V>::ty
   return p;
 }
 
-// Sum over kLanes neighbouring lanes; every lane gets it.
-template <int kLanes> __device__ __forceinline__ float lane_sum(float v) {
+// Sum over kLanes neighbouring lanes, or over the workgroup (kLanes = kThreads, `s` holds a value per wavefront); every lane gets it.
+template <int kLanes> __device__ __forceinline__ float lane_sum(float v, float* s) {
 #pragma unroll
-  for (int d = 1; d < kLanes; d *= 2) v += __shfl_xor(v, d, 64);
+  for (int d = 1; d < (kLanes < 64 ? kLanes : 64); d *= 2) v += __shfl_xor(v, d, 64);
+  if constexpr (kLanes > 64) {
+    __syncthreads();
+    if ((threadIdx.x & 63) == 0) s[threadIdx.x >> 6] = v;
+    __syncthreads();
+    v = 0.f;
+#pragma unroll
+    for (int k = 0; k < kThreads / 64; ++k) v += s[k];
+  }
   return v;
 }
 
@@ -76,7 +84,7 @@ template <typename T, int V, int kLanes, int R> struct RowPieces {
 // z = x + res in 32 bits, normed in place: returns rsqrt(var + eps).  The mean is subtracted before the squares are summed.
 template <typename T, int V, int kLanes, int R>
 __device__ __forceinline__ float norm_row(const RowPieces<T, V, kLanes, R>& x, const RowPieces<T, V, kLanes, R>& res, bool with_res, int part,
-                                          int pieces, float inv_c, float eps, float (&z)[R][V]) {
+                                          int pieces, float inv_c, float eps, float (&z)[R][V], float* s) {
   float sum = 0.f;
 #pragma unroll
   for (int r = 0; r < R; ++r) {
@@ -90,7 +98,7 @@ __device__ __forceinline__ float norm_row(const RowPieces<T, V, kLanes, R>& x, c
 #pragma unroll
     for (int i = 0; i < V; ++i) sum += z[r][i];
   }
-  const float mean = lane_sum<kLanes>(sum) * inv_c;
+  const float mean = lane_sum<kLanes>(sum, s) * inv_c;
   float sq = 0.f;
 #pragma unroll
   for (int r = 0; r < R; ++r) {
@@ -101,7 +109,7 @@ __device__ __forceinline__ float norm_row(const RowPieces<T, V, kLanes, R>& x, c
       sq = fmaf(z[r][i], z[r][i], sq);
     }
   }
-  const float rs = 1.f / sqrtf(lane_sum<kLanes>(sq) * inv_c + eps);
+  const float rs = 1.f / sqrtf(lane_sum<kLanes>(sq, s) * inv_c + eps);
 #pragma unroll
   for (int r = 0; r < R; ++r)
 #pragma unroll
@@ -120,6 +128,7 @@ __device__ __forceinline__ void load_vector(const float* v, int part, int pieces
 template <typename T, int V, int kLanes, int R>
 __global__ __launch_bounds__(kThreads) void k_ln_forward(LnArgs a) {
   constexpr int kRows = kThreads / kLanes;
+  __shared__ float s[kThreads / 64];
   const int part = threadIdx.x % kLanes, pieces = a.C / V;
   const float inv_c = 1.f / (float)a.C;
   float gamma[R][V], beta[R][V];
@@ -131,7 +140,7 @@ __global__ __launch_bounds__(kThreads) void k_ln_forward(LnArgs a) {
     x.load(a.x, row * a.ld_x, part, pieces, true);
     if (a.res) res.load(a.res, row * a.ld_res, part, pieces, true);
     float z[R][V];
-    norm_row<T, V, kLanes, R>(x, res, a.res != nullptr, part, pieces, inv_c, a.eps, z);
+    norm_row<T, V, kLanes, R>(x, res, a.res != nullptr, part, pieces, inv_c, a.eps, z, s);
     P* out = reinterpret_cast<P*>(static_cast<T*>(a.out) + row * a.ld_out);
 #pragma unroll
     for (int r = 0; r < R; ++r) {
@@ -145,6 +154,7 @@ __global__ __launch_bounds__(kThreads) void k_ln_forward(LnArgs a) {
 template <typename T, int V, int kLanes, int R>
 __global__ __launch_bounds__(kThreads) void k_ln_backward(LnArgs a) {
   constexpr int kRows = kThreads / kLanes;
+  __shared__ float s[kThreads / 64];
   const int part = threadIdx.x % kLanes, pieces = a.C / V;
   const float inv_c = 1.f / (float)a.C;
   float gamma[R][V], dg[R][V] = {}, db[R][V] = {};
@@ -156,7 +166,7 @@ __global__ __launch_bounds__(kThreads) void k_ln_backward(LnArgs a) {
     if (a.res) res.load(a.res, row * a.ld_res, part, pieces, true);
     dy.load(a.dy, row * a.ld_dy, part, pieces, true);
     float z[R][V], w[R][V];
-    const float rs = norm_row<T, V, kLanes, R>(x, res, a.res != nullptr, part, pieces, inv_c, a.eps, z);
+    const float rs = norm_row<T, V, kLanes, R>(x, res, a.res != nullptr, part, pieces, inv_c, a.eps, z, s);
     float sum_w = 0.f, sum_wn = 0.f;
 #pragma unroll
     for (int r = 0; r < R; ++r) {
@@ -170,7 +180,7 @@ __global__ __launch_bounds__(kThreads) void k_ln_backward(LnArgs a) {
         sum_wn = fmaf(w[r][i], z[r][i], sum_wn);
       }
     }
-    const float mean_w = lane_sum<kLanes>(sum_w) * inv_c, mean_wn = lane_sum<kLanes>(sum_wn) * inv_c;
+    const float mean_w = lane_sum<kLanes>(sum_w, s) * inv_c, mean_wn = lane_sum<kLanes>(sum_wn, s) * inv_c;
     P* out = reinterpret_cast<P*>(static_cast<T*>(a.out) + row * a.ld_out);
 #pragma unroll
     for (int r = 0; r < R; ++r) {
@@ -180,8 +190,9 @@ __global__ __launch_bounds__(kThreads) void k_ln_backward(LnArgs a) {
     }
   }
   // the workgroup's sums: over the rows of a wavefront across lanes, over its wavefronts in LDS
-  __shared__ float sums[kThreads / 64][2][kLanes * R * V];
-  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  constexpr int kCopies = kLanes > 64 ? 1 : kThreads / 64;
+  __shared__ float sums[kCopies][2][kLanes * R * V];
+  const int lane = threadIdx.x & 63, copy = kLanes > 64 ? 0 : threadIdx.x >> 6;
 #pragma unroll
   for (int r = 0; r < R; ++r)
 #pragma unroll
@@ -192,31 +203,19 @@ __global__ __launch_bounds__(kThreads) void k_ln_backward(LnArgs a) {
         db[r][i] += __shfl_xor(db[r][i], d, 64);
       }
       if (lane < kLanes) {
-        sums[wave][0][(r * kLanes + part) * V + i] = dg[r][i];
-        sums[wave][1][(r * kLanes + part) * V + i] = db[r][i];
+        sums[copy][0][(r * kLanes + part) * V + i] = dg[r][i];
+        sums[copy][1][(r * kLanes + part) * V + i] = db[r][i];
       }
     }
   __syncthreads();
   for (int c = threadIdx.x; c < 2 * a.C; c += kThreads) {
     const int which = c >= a.C, col = c - which * a.C;
-    float s = 0.f;
+    float v = 0.f;
 #pragma unroll
-    for (int k = 0; k < kThreads / 64; ++k) s += sums[k][which][col];
-    if (a.d_gamma) (which ? a.d_beta : a.d_gamma)[col] = s;
-    else a.partial[(int64_t)blockIdx.x * 2 * a.C + c] = s;
+    for (int k = 0; k < kCopies; ++k) v += sums[k][which][col];
+    if (a.d_gamma) (which ? a.d_beta : a.d_gamma)[col] = v;
+    else a.partial[(int64_t)blockIdx.x * 2 * a.C + c] = v;
   }
-}
-
-// Sum of one value per thread over a workgroup, the same in every thread; `s` holds a value per wavefront.
-__device__ __forceinline__ float group_sum(float v, float* s) {
-  v = lane_sum<64>(v);
-  __syncthreads();
-  if ((threadIdx.x & 63) == 0) s[threadIdx.x >> 6] = v;
-  __syncthreads();
-  v = 0.f;
-#pragma unroll
-  for (int k = 0; k < kThreads / 64; ++k) v += s[k];
-  return v;
 }
 
 template <typename T> __device__ __forceinline__ float sum_at(const LnArgs& a, int64_t row, int c) {
@@ -225,8 +224,8 @@ template <typename T> __device__ __forceinline__ float sum_at(const LnArgs& a, i
   return z;
 }
 
-// Rows that the registers of a wavefront do not hold (more than 64 * kVectors pieces): a workgroup a row, which is read again,
-// from the caches, for each of its sums.  Workgroups take consecutive rows, `rows` of them.
+// Rows that registers do not hold: a workgroup a row, which is read again, from the caches, for each of its sums.  Workgroups take
+// consecutive rows, `rows` of them.
 template <typename T, bool kBackward>
 __global__ __launch_bounds__(kThreads) void k_ln_long(LnArgs a, int32_t rows) {
   __shared__ float s[kThreads / 64];
@@ -237,13 +236,13 @@ __global__ __launch_bounds__(kThreads) void k_ln_long(LnArgs a, int32_t rows) {
   for (int64_t row = first; row < last; ++row) {
     float v = 0.f;
     for (int c = threadIdx.x; c < a.C; c += kThreads) v += sum_at<T>(a, row, c);
-    const float mean = group_sum(v, s) * inv_c;
+    const float mean = lane_sum<kThreads>(v, s) * inv_c;
     v = 0.f;
     for (int c = threadIdx.x; c < a.C; c += kThreads) {
       const float z = sum_at<T>(a, row, c) - mean;
       v = fmaf(z, z, v);
     }
-    const float rs = 1.f / sqrtf(group_sum(v, s) * inv_c + a.eps);
+    const float rs = 1.f / sqrtf(lane_sum<kThreads>(v, s) * inv_c + a.eps);
     T* out = static_cast<T*>(a.out) + row * a.ld_out;
     if (!kBackward) {
       for (int c = threadIdx.x; c < a.C; c += kThreads) out[c] = (T)fmaf((sum_at<T>(a, row, c) - mean) * rs, a.gamma[c], a.beta[c]);
@@ -256,7 +255,7 @@ __global__ __launch_bounds__(kThreads) void k_ln_long(LnArgs a, int32_t rows) {
       sum_w += w;
       sum_wn = fmaf(w, (sum_at<T>(a, row, c) - mean) * rs, sum_wn);
     }
-    const float mean_w = group_sum(sum_w, s) * inv_c, mean_wn = group_sum(sum_wn, s) * inv_c;
+    const float mean_w = lane_sum<kThreads>(sum_w, s) * inv_c, mean_wn = lane_sum<kThreads>(sum_wn, s) * inv_c;
     for (int c = threadIdx.x; c < a.C; c += kThreads) {
       const float d = (float)dy[c], n = (sum_at<T>(a, row, c) - mean) * rs;
       out[c] = (T)(rs * (d * a.gamma[c] - mean_w - n * mean_wn));
@@ -284,18 +283,20 @@ __global__ __launch_bounds__(1024) void k_ln_sum(const float* __restrict__ parti
   (c < C ? d_gamma : d_beta)[c < C ? c : c - C] = v;
 }
 
-// 16-byte pieces where every row of every array starts on one and C is a whole number of them, else single values; then the
-// fewest lanes a row that hold it in kVectors pieces.  0: no such number.
+// 16-byte pieces where every row of every array starts on one and C is a whole number of them, else pairs of bf16 likewise, else single
+// values; then the fewest lanes a row that hold it.  0: none do.
 int piece_elems(const LnArgs& a, int32_t dtype) {
-  const int v = dtype == DSVT_BF16 ? 8 : 4, e = dtype == DSVT_BF16 ? 2 : 4;
+  const int e = dtype == DSVT_BF16 ? 2 : 4;
   uintptr_t all = (uintptr_t)a.x | (uintptr_t)a.res | (uintptr_t)a.dy | (uintptr_t)a.out;
   all |= (uintptr_t)((a.ld_x | a.ld_res | a.ld_dy | a.ld_out) * e);
-  return a.C % v == 0 && (all & 15) == 0 ? v : 1;
+  for (int bytes = 16; bytes > e; bytes = bytes == 16 && e == 2 ? 4 : e)
+    if (a.C % (bytes / e) == 0 && (all & (uintptr_t)(bytes - 1)) == 0) return bytes / e;
+  return 1;
 }
-int row_lanes(int32_t pieces) {
+int row_lanes(int32_t pieces, bool wide) {
   for (int l = 8; l <= 64; l *= 2)
     if (pieces <= l * kVectors) return l;
-  return 0;
+  return wide ? (pieces <= kThreads * kVectors ? kThreads : 0) : (pieces <= 64 * kNarrow ? 64 : 0);
 }
 
 template <typename T, int V, int kLanes, int R> void launch_rows(const LnArgs& a, bool back, unsigned groups, hipStream_t st) {
@@ -315,9 +316,17 @@ template <typename T, int V> void launch_pieces(const LnArgs& a, bool back, int 
   } else if (lanes == 32) {
     if (r == 3) launch_rows<T, V, 32, 3>(a, back, groups, st);
     else launch_rows<T, V, 32, 4>(a, back, groups, st);
-  } else {
+  } else if (lanes == 64) {
     if (r == 3) launch_rows<T, V, 64, 3>(a, back, groups, st);
-    else launch_rows<T, V, 64, 4>(a, back, groups, st);
+    else if (r == 4) launch_rows<T, V, 64, 4>(a, back, groups, st);
+    else if constexpr (V * sizeof(T) < 16) {
+      if (r <= 8) launch_rows<T, V, 64, 8>(a, back, groups, st);
+      else if (r <= 12) launch_rows<T, V, 64, 12>(a, back, groups, st);
+      else launch_rows<T, V, 64, kNarrow>(a, back, groups, st);
+    }
+  } else if constexpr (V * sizeof(T) == 16) {
+    if (r <= 2) launch_rows<T, V, kThreads, 2>(a, back, groups, st);
+    else launch_rows<T, V, kThreads, kVectors>(a, back, groups, st);
   }
 }
 template <typename T> void launch(const LnArgs& a, bool back, int v, int lanes, unsigned groups, int32_t rows, hipStream_t st) {
@@ -325,6 +334,7 @@ template <typename T> void launch(const LnArgs& a, bool back, int v, int lanes, 
     if (back) k_ln_long<T, true><<<groups, kThreads, 0, st>>>(a, rows);
     else k_ln_long<T, false><<<groups, kThreads, 0, st>>>(a, rows);
   } else if (v == 1) launch_pieces<T, 1>(a, back, lanes, groups, st);
+  else if (v == 2) launch_pieces<T, sizeof(T) == 2 ? 2 : 1>(a, back, lanes, groups, st);
   else launch_pieces<T, 16 / (int)sizeof(T)>(a, back, lanes, groups, st);
 }
 
@@ -352,7 +362,7 @@ extern "C" int dsvt_layer_norm(const dsvt_ln_cfg* cfg, const void* x, int64_t ld
   LnArgs a = {};
   a.x = x; a.res = res; a.out = y; a.gamma = cfg->gamma; a.beta = cfg->beta;
   a.ld_x = ld_x; a.ld_res = res ? ld_res : 0; a.ld_out = ld_y; a.n = n_rows; a.C = cfg->C; a.eps = cfg->eps;
-  const int v = piece_elems(a, cfg->dtype), lanes = row_lanes(cfg->C / v);
+  const int v = piece_elems(a, cfg->dtype), lanes = row_lanes(cfg->C / v, v * (cfg->dtype == DSVT_BF16 ? 2 : 4) == 16);
   const int64_t per = lanes ? kThreads / lanes : 1, all = dsvt_ceil_div(n_rows, per);
   const unsigned groups = (unsigned)(all < kForwardGroups ? all : kForwardGroups);
   const int32_t rows = (int32_t)dsvt_ceil_div(n_rows, groups);
@@ -391,7 +401,7 @@ extern "C" int dsvt_layer_norm_backward(const dsvt_ln_cfg* cfg, const void* dy, 
     a.x = x; a.res = res; a.dy = dy; a.out = dx; a.gamma = cfg->gamma;
     a.ld_x = ld_x; a.ld_res = res ? ld_res : 0; a.ld_dy = ld_dy; a.ld_out = ld_dx; a.n = n_rows; a.C = cfg->C; a.eps = cfg->eps;
     a.partial = static_cast<float*>(ws);
-    const int v = piece_elems(a, cfg->dtype), lanes = row_lanes(cfg->C / v);
+    const int v = piece_elems(a, cfg->dtype), lanes = row_lanes(cfg->C / v, v * (cfg->dtype == DSVT_BF16 ? 2 : 4) == 16);
     const int64_t per = lanes ? kThreads / lanes : 1, all = dsvt_ceil_div(n_rows, per);
     groups = (int32_t)(all < kBackwardGroups ? all : kBackwardGroups);
     const int32_t rows = (int32_t)dsvt_ceil_div(n_rows, groups);

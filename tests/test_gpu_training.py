@@ -284,7 +284,9 @@ def test_set_mha_backward_repeats_bit_for_bit(win, c, heads, buckets):
 LN_CASES = [(1, 192, "bf16", True), (2000, 64, "f32", True), (333, 192, "bf16", True), (777, 128, "bf16", False), (513, 256, "f32", False),
             (100, 99, "f32", True), (100, 99, "bf16", False), (33, 1, "f32", True), (65, 7, "bf16", True), (40, 320, "bf16", True),
             (40, 600, "f32", True), (20, 1000, "bf16", False), (19, 2048, "bf16", True), (9, 2056, "bf16", True), (9, 1500, "f32", True),
-            (600, 257, "f32", True), (5, 5001, "bf16", True), (3, 65536, "f32", False), (40000, 64, "bf16", True), (16, 48, "f32", True), (700, 24, "bf16", True)]
+            (600, 257, "f32", True), (5, 5001, "bf16", True), (3, 65536, "f32", False), (40000, 64, "bf16", True), (16, 48, "f32", True), (700, 24, "bf16", True), (70, 700, "bf16", True),
+            (70, 701, "bf16", False), (70, 401, "bf16", True), (50, 1023, "f32", True), (30, 1900, "bf16", True), (30, 4096, "bf16", True), (30, 8192, "bf16", True),
+            (30, 4096, "f32", False), (700, 2056, "f32", True), (600, 1025, "bf16", True)]
 
 
 @pytest.mark.parametrize("n,c,dtype,with_res", LN_CASES)
