@@ -18,7 +18,8 @@
 namespace {
 
 constexpr int kThreads = 256;
-constexpr int kVectors = 4, kNarrow = 16;         // pieces of a row in one lane, at most: 16-byte ones, smaller ones
+constexpr int kVectors = 4;                       // 16-byte pieces of a row in one lane, at most
+constexpr int narrow_max(int bytes) { return bytes == 8 ? 8 : 16; }      // and smaller ones
 constexpr int kBackwardGroups = 512;              // workgroups of a backward pass, at most: two a compute unit
 constexpr int kForwardGroups = 2048;
 
@@ -283,20 +284,20 @@ __global__ __launch_bounds__(1024) void k_ln_sum(const float* __restrict__ parti
   (c < C ? d_gamma : d_beta)[c < C ? c : c - C] = v;
 }
 
-// 16-byte pieces where every row of every array starts on one and C is a whole number of them, else pairs of bf16 likewise, else single
-// values; then the fewest lanes a row that hold it.  0: none do.
+// The widest pieces of 16, 8, 4 or 2 bytes on which every row of every array starts and of which C is a whole number; then the fewest lanes
+// a row that hold it.  0: none do.
 int piece_elems(const LnArgs& a, int32_t dtype) {
   const int e = dtype == DSVT_BF16 ? 2 : 4;
   uintptr_t all = (uintptr_t)a.x | (uintptr_t)a.res | (uintptr_t)a.dy | (uintptr_t)a.out;
   all |= (uintptr_t)((a.ld_x | a.ld_res | a.ld_dy | a.ld_out) * e);
-  for (int bytes = 16; bytes > e; bytes = bytes == 16 && e == 2 ? 4 : e)
+  for (int bytes = 16; bytes > e; bytes /= 2)
     if (a.C % (bytes / e) == 0 && (all & (uintptr_t)(bytes - 1)) == 0) return bytes / e;
   return 1;
 }
-int row_lanes(int32_t pieces, bool wide) {
+int row_lanes(int32_t pieces, int bytes) {
   for (int l = 8; l <= 64; l *= 2)
     if (pieces <= l * kVectors) return l;
-  return wide ? (pieces <= kThreads * kVectors ? kThreads : 0) : (pieces <= 64 * kNarrow ? 64 : 0);
+  return bytes == 16 ? (pieces <= kThreads * kVectors ? kThreads : 0) : (pieces <= 64 * narrow_max(bytes) ? 64 : 0);
 }
 
 template <typename T, int V, int kLanes, int R> void launch_rows(const LnArgs& a, bool back, unsigned groups, hipStream_t st) {
@@ -320,9 +321,12 @@ template <typename T, int V> void launch_pieces(const LnArgs& a, bool back, int 
     if (r == 3) launch_rows<T, V, 64, 3>(a, back, groups, st);
     else if (r == 4) launch_rows<T, V, 64, 4>(a, back, groups, st);
     else if constexpr (V * sizeof(T) < 16) {
-      if (r <= 8) launch_rows<T, V, 64, 8>(a, back, groups, st);
-      else if (r <= 12) launch_rows<T, V, 64, 12>(a, back, groups, st);
-      else launch_rows<T, V, 64, kNarrow>(a, back, groups, st);
+      if (r <= 6) launch_rows<T, V, 64, 6>(a, back, groups, st);
+      else if (r <= 8) launch_rows<T, V, 64, 8>(a, back, groups, st);
+      else if constexpr (V * sizeof(T) < 8) {
+        if (r <= 12) launch_rows<T, V, 64, 12>(a, back, groups, st);
+        else launch_rows<T, V, 64, 16>(a, back, groups, st);
+      }
     }
   } else if constexpr (V * sizeof(T) == 16) {
     if (r <= 2) launch_rows<T, V, kThreads, 2>(a, back, groups, st);
@@ -334,7 +338,8 @@ template <typename T> void launch(const LnArgs& a, bool back, int v, int lanes, 
     if (back) k_ln_long<T, true><<<groups, kThreads, 0, st>>>(a, rows);
     else k_ln_long<T, false><<<groups, kThreads, 0, st>>>(a, rows);
   } else if (v == 1) launch_pieces<T, 1>(a, back, lanes, groups, st);
-  else if (v == 2) launch_pieces<T, sizeof(T) == 2 ? 2 : 1>(a, back, lanes, groups, st);
+  else if (v == 2) launch_pieces<T, 2>(a, back, lanes, groups, st);
+  else if (v * sizeof(T) == 8) launch_pieces<T, 8 / (int)sizeof(T)>(a, back, lanes, groups, st);
   else launch_pieces<T, 16 / (int)sizeof(T)>(a, back, lanes, groups, st);
 }
 
@@ -362,7 +367,7 @@ extern "C" int dsvt_layer_norm(const dsvt_ln_cfg* cfg, const void* x, int64_t ld
   LnArgs a = {};
   a.x = x; a.res = res; a.out = y; a.gamma = cfg->gamma; a.beta = cfg->beta;
   a.ld_x = ld_x; a.ld_res = res ? ld_res : 0; a.ld_out = ld_y; a.n = n_rows; a.C = cfg->C; a.eps = cfg->eps;
-  const int v = piece_elems(a, cfg->dtype), lanes = row_lanes(cfg->C / v, v * (cfg->dtype == DSVT_BF16 ? 2 : 4) == 16);
+  const int v = piece_elems(a, cfg->dtype), lanes = row_lanes(cfg->C / v, v * e);
   const int64_t per = lanes ? kThreads / lanes : 1, all = dsvt_ceil_div(n_rows, per);
   const unsigned groups = (unsigned)(all < kForwardGroups ? all : kForwardGroups);
   const int32_t rows = (int32_t)dsvt_ceil_div(n_rows, groups);
@@ -401,7 +406,7 @@ extern "C" int dsvt_layer_norm_backward(const dsvt_ln_cfg* cfg, const void* dy, 
     a.x = x; a.res = res; a.dy = dy; a.out = dx; a.gamma = cfg->gamma;
     a.ld_x = ld_x; a.ld_res = res ? ld_res : 0; a.ld_dy = ld_dy; a.ld_out = ld_dx; a.n = n_rows; a.C = cfg->C; a.eps = cfg->eps;
     a.partial = static_cast<float*>(ws);
-    const int v = piece_elems(a, cfg->dtype), lanes = row_lanes(cfg->C / v, v * (cfg->dtype == DSVT_BF16 ? 2 : 4) == 16);
+    const int v = piece_elems(a, cfg->dtype), lanes = row_lanes(cfg->C / v, v * e);
     const int64_t per = lanes ? kThreads / lanes : 1, all = dsvt_ceil_div(n_rows, per);
     groups = (int32_t)(all < kBackwardGroups ? all : kBackwardGroups);
     const int32_t rows = (int32_t)dsvt_ceil_div(n_rows, groups);
