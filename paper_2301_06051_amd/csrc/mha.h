@@ -112,10 +112,12 @@ __device__ __forceinline__ float to_units(float b, float root) {
 // What a workgroup knows of a set, in LDS.  Row r is the set's r-th voxel; rows up to the next multiple of 16 repeat row 0 with
 // weight 0: they are read like others, and masked where they would count.  code: the cell's number times the bytes of an entry, so that the
 // difference of two codes is an offset's place in a table.
-template <int kMax> struct SetRows {
+template <int kMax> struct alignas(16) SetRows {
   int32_t vox[kMax], code[kMax], weight[kMax];
   int32_t n;
 };
+// four neighbouring values from the `at`-th on, a multiple of four
+__device__ __forceinline__ int4 four(const int32_t* values, int at) { return *reinterpret_cast<const int4*>(values + at); }
 
 // Largest of the wavefront's values, by shifts over 1, 2, 4, 8 lanes of a row and row broadcasts; in the last lane, from where all get it.
 __device__ __forceinline__ int wave_max(int v) {
@@ -358,6 +360,14 @@ template <typename T, int HDP, TableForm kForm, int kMax> struct Head {
   __device__ __forceinline__ uint32_t from() const {
     return (uint32_t)(a.centre * entry_bytes()) + (kForm == kByOffset ? table : kForm == kByBucket ? map : 0u);
   }
+  // entry of the four pairs of query code `at` (plus from()) and the keys 16 t + 4 g .. + 3
+  __device__ __forceinline__ void entries(const Rows& rows, uint32_t at, int t, uint32_t (&e)[4]) const {
+    const int4 key = four(rows.code, 16 * t + 4 * g);
+    e[0] = entry(at - (uint32_t)key.x);
+    e[1] = entry(at - (uint32_t)key.y);
+    e[2] = entry(at - (uint32_t)key.z);
+    e[3] = entry(at - (uint32_t)key.w);
+  }
   __device__ __forceinline__ uint32_t entry(uint32_t at) const {
     if constexpr (kForm == kByBucket) return table + 4u * *(lds_u16*)(uintptr_t)at;
     if constexpr (kForm == kInMemory)
@@ -399,9 +409,10 @@ template <typename T, int HDP, TableForm kForm, int kMax> struct Head {
     }
     if (a.dup) {
 #pragma unroll
-      for (int k = 0; k < kTiles; ++k)
-#pragma unroll
-        for (int i = 0; i < 4; ++i) p[k][i] *= (float)rows.weight[16 * k + 4 * g + i];
+      for (int k = 0; k < kTiles; ++k) {
+        const int4 w = four(rows.weight, 16 * k + 4 * g);
+        p[k] *= f32x4{(float)w.x, (float)w.y, (float)w.z, (float)w.w};
+      }
     }
     float sum = 0.f;
 #pragma unroll

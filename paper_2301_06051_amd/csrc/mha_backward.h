@@ -121,9 +121,9 @@ __device__ __forceinline__ void backward_set(const Head<T, HDP, kForm, kMax>& he
         head.load(rows, a.qkv, a.ld_qkv, 1, t, k[0]);
         head.load(rows, a.qkv, a.ld_qkv, 2, t, v[0]);
       }
+      head.entries(rows, at, t, entry[t]);
 #pragma unroll
       for (int i = 0; i < 4; ++i) {
-        entry[t][i] = head.entry(at - (uint32_t)rows.code[16 * t + 4 * g + i]);
         p[t][i] = head.value(entry[t][i]);
         if (t == kTiles - 1 && 16 * t + 4 * g + i >= n) p[t][i] = -INFINITY;
       }

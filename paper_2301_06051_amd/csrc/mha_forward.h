@@ -18,11 +18,6 @@ __device__ __forceinline__ void forward_set(const Head<T, HDP, kForm, kMax>& hea
     head.load(rows, a.qkv, a.ld_qkv, 1, t, k[t]);
     head.load(rows, a.qkv, a.ld_qkv, 2, t, v[t]);
   }
-  uint32_t key[kTiles][4];
-#pragma unroll
-  for (int t = 0; t < kTiles; ++t)
-#pragma unroll
-    for (int i = 0; i < 4; ++i) key[t][i] = (uint32_t)rows.code[16 * t + 4 * g + i];
 #pragma unroll
   for (int t = 0; t < kTiles; ++t) head.turn(v[t], vt[t]);
 #pragma unroll 1
@@ -33,9 +28,11 @@ __device__ __forceinline__ void forward_set(const Head<T, HDP, kForm, kMax>& hea
     f32x4 p[kTiles];
 #pragma unroll
     for (int t = 0; t < kTiles; ++t) {
+      uint32_t entry[4];
+      head.entries(rows, at, t, entry);
 #pragma unroll
       for (int i = 0; i < 4; ++i) {
-        p[t][i] = head.value(head.entry(at - key[t][i]));
+        p[t][i] = head.value(entry[i]);
         if (t == kTiles - 1 && 16 * t + 4 * g + i >= n) p[t][i] = -INFINITY;
       }
 #pragma unroll
