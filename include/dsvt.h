@@ -353,7 +353,8 @@ typedef struct {
  * B = min(n_side, w): distances below n_exact have buckets of their own, a distance a from n_exact on has the bucket
  * n_exact + floor((B - n_exact) log(a / n_exact) / log(w / n_exact)), none is above B - 1, and the two directions are kept
  * apart: 2B - 1 buckets an axis.  An offset's bucket is the product of the three, x most significant.
- * bucket [host] [(2L-1)(2W-1)(2H-1)], may be NULL; n_rel [host] the number of buckets.  0 < n_exact <= n_side. */
+ * bucket [host] [(2L-1)(2W-1)(2H-1)], may be NULL; n_rel [host] the number of buckets.  0 < n_exact <= n_side;
+ * fewer than 2^24 offsets (DSVT_EUNSUPPORTED otherwise). */
 int dsvt_rel_buckets(const int32_t win[3], int32_t n_exact, int32_t n_side, int32_t* bucket, int32_t* n_rel);
 
 /* qkv [device] [n_voxels, 3C] q, k, v of every voxel (the product with dsvt_layer_w.w_qkv and its bias)

@@ -456,6 +456,11 @@ def _rows(t, shape, dtype, device, what):
     return t.stride(0) if shape[0] > 1 else max(t.stride(0), shape[1])
 
 
+def _same_device(owner, device):
+    if owner.device != device:
+        raise ValueError(f"the {type(owner).__name__} was made on cuda:{owner.device}, the current device is cuda:{device}")
+
+
 def _vector(t, shape, dtype, device, what):
     if t.shape != shape or t.dtype is not dtype or t.get_device() != device or not t.is_contiguous():
         raise ValueError(f"{what}: a contiguous {dtype} tensor of shape {tuple(shape)} on the current device, cuda:{device}, is wanted; got {t.dtype} "
@@ -474,10 +479,8 @@ def _scratch(nbytes, ws, stream, like):
 def dsvt_rel_buckets(win, n_exact, n_side):
     """(int32 numpy array of every offset's bucket, number of buckets) for SetMha's rel_bucket and table; see dsvt.h."""
     n = C.c_int32(0)
-    offsets = 1
-    for w in win:
-        offsets *= max(2 * w - 1, 0)
-    bucket = np.zeros((offsets,), np.int32)
+    _check("dsvt_rel_buckets", lib().dsvt_rel_buckets(C.byref(I32x3(*win)), n_exact, n_side, None, C.byref(n)))
+    bucket = np.zeros(((2 * win[0] - 1) * (2 * win[1] - 1) * (2 * win[2] - 1),), np.int32)
     _check("dsvt_rel_buckets", lib().dsvt_rel_buckets(C.byref(I32x3(*win)), n_exact, n_side, bucket.ctypes.data_as(C.c_void_p), C.byref(n)))
     return bucket, n.value
 
@@ -499,12 +502,13 @@ class SetMha:
             _vector(rel_bucket, (offsets,), torch.int32, _current_device(), "rel_bucket")
         self.struct = MhaCfg(channels, heads, code, I32x3(*win), dup_mode, None if rel_bias is None else rel_bias.data_ptr(),
                              None if rel_bucket is None else rel_bucket.data_ptr(), n_rel)
-        self.ref, self.sizes = C.byref(self.struct), {}      # sizes: workspace bytes by shape
+        self.ref, self.sizes, self.device = C.byref(self.struct), {}, _current_device()     # sizes: workspace bytes by shape
 
 
 def dsvt_set_mha(mha, maps, coords, qkv, out=None, stream=None):
     """Attention inside every set of `maps` on projected rows qkv [N, 3C]; returns out [N, C]."""
     n, c, dtype, dev = maps.n_voxels, mha.C, mha.dtype, _current_device()
+    _same_device(mha, dev)
     ld = _rows(qkv, (n, 3 * c), dtype, dev, "qkv")
     _vector(coords, (n, 4), torch.int32, dev, "coords")
     if out is None:
@@ -532,6 +536,7 @@ def dsvt_set_mha_backward(mha, maps, coords, qkv, d_out, d_qkv=None, d_rel_bias=
     """Gradients of dsvt_set_mha: returns (d_qkv [N, 3C], d_rel_bias [heads, n_rel] float32, or None without a table or if not
     wanted)."""
     n, c, dtype, dev = maps.n_voxels, mha.C, mha.dtype, _current_device()
+    _same_device(mha, dev)
     ld, ld_out = _rows(qkv, (n, 3 * c), dtype, dev, "qkv"), _rows(d_out, (n, c), dtype, dev, "d_out")
     _vector(coords, (n, 4), torch.int32, dev, "coords")
     if d_qkv is None:
@@ -562,12 +567,13 @@ class LayerNorm:
         _vector(gamma, (self.C,), torch.float32, _current_device(), "gamma")
         _vector(beta, (self.C,), torch.float32, _current_device(), "beta")
         self.struct = LnCfg(self.C, code, gamma.data_ptr(), beta.data_ptr(), eps)
-        self.ref, self.sizes = C.byref(self.struct), {}      # sizes: workspace bytes by shape
+        self.ref, self.sizes, self.device = C.byref(self.struct), {}, _current_device()     # sizes: workspace bytes by shape
 
 
 def dsvt_layer_norm(ln, x, res=None, y=None, stream=None):
     """LayerNorm of x + res (of x without res), rows [N, C]; returns y."""
     n, c, dtype, dev = x.shape[0], ln.C, ln.dtype, _current_device()
+    _same_device(ln, dev)
     ld_x = _rows(x, (n, c), dtype, dev, "x")
     ld_res, p_res = (0, None) if res is None else (_rows(res, (n, c), dtype, dev, "res"), res.data_ptr())
     if y is None:
@@ -592,6 +598,7 @@ def dsvt_layer_norm_backward_workspace_size(ln, n_rows):
 def dsvt_layer_norm_backward(ln, dy, x, res=None, dx=None, d_gamma=None, d_beta=None, ws=None, stream=None):
     """Gradients of dsvt_layer_norm: returns (dx, which is that of x and of res, d_gamma [C], d_beta [C])."""
     n, c, dtype, dev = x.shape[0], ln.C, ln.dtype, _current_device()
+    _same_device(ln, dev)
     ld_dy, ld_x = _rows(dy, (n, c), dtype, dev, "dy"), _rows(x, (n, c), dtype, dev, "x")
     ld_res, p_res = (0, None) if res is None else (_rows(res, (n, c), dtype, dev, "res"), res.data_ptr())
     if dx is None:

@@ -438,6 +438,6 @@ __host__ __device__ constexpr int mha_per_cu(bool back, int element, int padded,
 __host__ __device__ constexpr int mha_per_simd(bool back, int element, int padded, int tau) {
   return mha_waves(back, element, padded, tau) * mha_per_cu(back, element, padded, tau) / 4;
 }
-constexpr size_t kMhaLdsMax = 130 << 10;          // dynamic LDS of a workgroup, at most: 160 KB less what its sets take (28 KB)
+constexpr size_t kMhaLdsMax = 131 << 10;          // dynamic LDS of a workgroup, at most: 160 KB less what its sets take (28 KB)
 
 extern __shared__ double mha_lds[];

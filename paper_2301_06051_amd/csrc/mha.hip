@@ -113,7 +113,7 @@ bool bad_rows(const void* p, int64_t ld, int64_t width, int e) {
 }
 
 int check_maps(const dsvt_maps* maps) {
-  if (!maps || maps->n_voxels < 0 || maps->max_sets < 0 || maps->tau <= 0) return DSVT_EINVAL;
+  if (!maps || maps->n_voxels < 0 || maps->max_sets < 0 || maps->max_sets > (1 << 30) || maps->tau <= 0) return DSVT_EINVAL;
   if (maps->n_voxels > 0 && (!maps->set_inds || !maps->n_sets)) return DSVT_EINVAL;
   return DSVT_OK;
 }
@@ -135,13 +135,14 @@ MhaArgs make_args(const dsvt_mha_cfg* c, const dsvt_maps* maps, const int32_t* c
 
 extern "C" int dsvt_rel_buckets(const int32_t win[3], int32_t n_exact, int32_t n_side, int32_t* bucket, int32_t* n_rel) {
   if (!win || !n_rel || n_exact <= 0 || n_side < n_exact) return DSVT_EINVAL;
-  int64_t total = 1, most[3];
+  int64_t total = 1, offsets = 1, most[3];
   for (int i = 0; i < 3; ++i) {
     if (win[i] <= 0 || win[i] > 4096) return DSVT_EINVAL;
     most[i] = n_side < win[i] ? n_side : win[i];
     total *= 2 * most[i] - 1;
+    offsets *= 2 * (int64_t)win[i] - 1;
   }
-  if (total >= (1 << 24)) return DSVT_EUNSUPPORTED;
+  if (offsets >= (1 << 24)) return DSVT_EUNSUPPORTED;
   *n_rel = (int32_t)total;
   if (!bucket) return DSVT_OK;
   const auto along = [&](int axis, int32_t d) {               // bucket of a signed distance, 0 .. 2 most - 2

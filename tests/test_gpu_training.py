@@ -70,6 +70,12 @@ CASES = [
     (56, 7, "bf16", (24, 24, 1), 200, 1, (9, 7, 1), 17, 1, None),
     (264, 11, "bf16", (20, 20, 1), 150, 1, (12, 12, 1), 33, 0, (1, 3)),
     (192, 12, "f32", (20, 20, 1), 150, 1, (12, 12, 1), 32, 1, (1, 1)),
+    (256, 8, "bf16", (20, 20, 1), 250, 1, (12, 12, 1), 48, 0, (3, 4)),
+    (144, 3, "bf16", (24, 24, 1), 300, 1, (12, 12, 1), 60, 1, None),
+    (96, 3, "f32", (24, 24, 1), 300, 1, (12, 12, 1), 48, 0, None),
+    (128, 4, "bf16", (24, 24, 1), 400, 1, (20, 20, 1), 96, 0, None),
+    (48, 3, "f32", (24, 24, 1), 400, 1, (20, 20, 1), 96, 1, (4, 8)),
+    (16, 2, "bf16", (30, 30, 1), 700, 1, (12, 12, 1), 16, 0, None),
 ]
 
 
@@ -97,9 +103,10 @@ def test_set_mha_without_a_positional_term(dtype, c, heads):
     _run(coords, maps, (12, 12, 1), c, heads, dtype, qkv, d_out, None, case="no table " + dtype)
 
 
-@pytest.mark.parametrize("win,buckets", [((12, 12, 32), None), ((12, 12, 32), (4, 7)), ((24, 24, 1), None), ((12, 12, 8), None)])
+@pytest.mark.parametrize("win,buckets", [((12, 12, 32), None), ((12, 12, 32), (4, 7)), ((24, 24, 1), None), ((12, 12, 8), None), ((30, 30, 20), None),
+                                         ((30, 30, 32), (2, 4))])
 def test_set_mha_large_tables(win, buckets):
-    """Tables that LDS holds for all heads, for a few, or for one."""
+    """Tables that LDS holds for all heads, for a few, for one, or not at all (their sums then shared out over workgroups)."""
     grid = (30, 30, win[2])
     n = 700
     coords = _frame(7, grid, n)
@@ -172,6 +179,67 @@ def test_set_mha_biases_that_mask(dtype, c, heads, tau, low):
         d = c // heads
         qkv[:, :d] = 0
         _run(coords, maps, win, c, heads, dtype, qkv, d_out, table, case=f"masks {low}")
+
+
+@pytest.mark.parametrize("dtype,tau", [("bf16", 36), ("f32", 36), ("bf16", 90)])
+def test_set_mha_logits_of_any_size(dtype, tau):
+    """Logits of up to 1e11: the probabilities are one key's alone wherever the largest logit stands out, and everything is finite."""
+    win, n, c, heads = (12, 12, 1), 250, 64, 4
+    coords = _frame(61, (20, 20, 1), n)
+    maps = gpu_maps(coords.cuda(), (20, 20, 1), win, (0, 0, 0), tau, 1, 0)
+    qkv, d_out, table = _inputs(62, n, c, dtype, heads, synth.weights.rel_table_size(win))
+    qkv[:, :2 * c] *= 2.0 ** 17
+    print("[case] large logits", dtype, tau, flush=True)
+    mha = dsvt.SetMha(c, heads, dtype, win, table.cuda())
+    out = dsvt.dsvt_set_mha(mha, maps, coords.cuda(), qkv.cuda()).cpu()
+    d_qkv, d_rel = dsvt.dsvt_set_mha_backward(mha, maps, coords.cuda(), qkv.cuda(), d_out.cuda())
+    assert all(bool(t.isfinite().all()) for t in (out, d_qkv, d_rel))
+    x, d, clear = qkv.double().reshape(n, 3, heads, c // heads), c // heads, 0
+    for vox, _ in ref.members(maps.set_inds[:int(maps.n_sets)].cpu(), n, 0):
+        s = torch.einsum("qhd,khd->hqk", x[vox, 0], x[vox, 1])
+        best = s.topk(min(2, len(vox)), dim=2).values
+        # sums of 16 products in 32 bits are off by 2^-20 of their sizes at most: 1e5 of a logit here
+        stands_out = (best[..., 0] - best[..., -1] > 1e6) | (len(vox) == 1)
+        want = x[vox, 2].permute(1, 0, 2).gather(1, s.argmax(2)[..., None].expand(-1, -1, d))
+        got = out.double().reshape(n, heads, d)[vox].permute(1, 0, 2)
+        assert torch.equal(got[stands_out], want[stands_out])
+        clear += int(stands_out.sum())
+    assert clear > n * heads * 0.9
+
+
+def test_set_mha_backward_without_the_tables_gradient():
+    win, n, c, heads = (12, 12, 1), 250, 192, 8
+    coords = _frame(63, (20, 20, 1), n)
+    maps = gpu_maps(coords.cuda(), (20, 20, 1), win, (0, 0, 0), 36, 1, 0)
+    qkv, d_out, table = (t.cuda() for t in _inputs(64, n, c, "bf16", heads, 529))
+    mha = dsvt.SetMha(c, heads, "bf16", win, table)
+    both, rel = dsvt.dsvt_set_mha_backward(mha, maps, coords.cuda(), qkv, d_out)
+    alone, none = dsvt.dsvt_set_mha_backward(mha, maps, coords.cuda(), qkv, d_out, want_rel_bias=False)
+    assert none is None and rel is not None and torch.equal(alone, both)
+
+
+def test_calls_refuse_tensors_that_do_not_fit():
+    coords = _frame(65, (20, 20, 1), 50).cuda()
+    maps = gpu_maps(coords, (20, 20, 1), (12, 12, 1), (0, 0, 0), 36, 1, 0)
+    qkv, d_out, table = (t.cuda() for t in _inputs(66, 50, 64, "bf16", 4, 529))
+    mha = dsvt.SetMha(64, 4, "bf16", (12, 12, 1), table)
+    ln = dsvt.LayerNorm(torch.ones(64, device="cuda"), torch.ones(64, device="cuda"), "bf16")
+    for bad in (qkv.float(), qkv[:49], qkv[:, :128], qkv.cpu(), qkv.t().contiguous().t()):
+        with pytest.raises(ValueError):
+            dsvt.dsvt_set_mha(mha, maps, coords, bad)
+        with pytest.raises(ValueError):
+            dsvt.dsvt_set_mha_backward(mha, maps, coords, bad, d_out)
+    for bad in (d_out.float(), d_out[:3], d_out.cpu()):
+        with pytest.raises(ValueError):
+            dsvt.dsvt_set_mha_backward(mha, maps, coords, qkv, bad)
+        with pytest.raises(ValueError):
+            dsvt.dsvt_layer_norm_backward(ln, bad, d_out)
+    with pytest.raises(dsvt.DsvtError):                       # a broadcast gradient: rows of stride 0
+        dsvt.dsvt_layer_norm_backward(ln, d_out[:1].expand(50, 64), d_out)
+    with pytest.raises(dsvt.DsvtError):                       # rows that do not start on 16 bytes
+        dsvt.dsvt_set_mha(mha, maps, coords, torch.zeros((50, 200), dtype=torch.bfloat16, device="cuda")[:, 4:196])
+    with pytest.raises(ValueError):
+        dsvt.SetMha(64, 4, "bf16", (12, 12, 1), table, torch.zeros(528, dtype=torch.int32, device="cuda"))
 
 
 def test_set_mha_buckets_outside_the_table_are_no_term():

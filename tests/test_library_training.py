@@ -43,13 +43,13 @@ def test_set_mha_refuses_configurations(cfg, rc):
     assert b.lib().dsvt_set_mha_backward_workspace_size(C.byref(_mha(**cfg)), C.byref(_maps()), C.byref(size)) == rc
 
 
-@pytest.mark.parametrize("maps,rc", [(dict(n_voxels=-1), EINVAL), (dict(max_sets=-1), EINVAL), (dict(tau=0), EINVAL), (dict(tau=97), EUNSUPPORTED),
+@pytest.mark.parametrize("maps,rc", [(dict(n_voxels=-1), EINVAL), (dict(max_sets=-1), EINVAL), (dict(max_sets=2 ** 30 + 1), EINVAL), (dict(tau=0), EINVAL), (dict(tau=97), EUNSUPPORTED),
                                      (dict(set_inds=None), EINVAL), (dict(n_sets=None), EINVAL)])
 def test_set_mha_refuses_maps(maps, rc):
     assert _forward(maps=_maps(**maps)) == rc and _backward(maps=_maps(**maps)) == rc
 
 
-@pytest.mark.parametrize("kw", [dict(coords=None), dict(coords=P + 4), dict(qkv=None), dict(qkv=P + 8), dict(ld=575), dict(ld=580)])
+@pytest.mark.parametrize("kw", [dict(coords=None), dict(coords=P + 4), dict(qkv=None), dict(qkv=P + 8), dict(ld=575), dict(ld=580), dict(ld=2 ** 32)])
 def test_set_mha_refuses_arrays(kw):
     assert _forward(**kw) == EINVAL and _backward(**kw) == EINVAL
 
@@ -119,6 +119,6 @@ def test_buckets_by_their_definition():
 
 
 def test_buckets_refusals():
-    for win, exact, side in (((0, 1, 1), 1, 1), ((12, 12, 1), 0, 3), ((12, 12, 1), 4, 3), ((5000, 1, 1), 2, 3)):
+    for win, exact, side in (((0, 1, 1), 1, 1), ((12, 12, 1), 0, 3), ((12, 12, 1), 4, 3), ((5000, 1, 1), 2, 3), ((1000, 1000, 5), 2, 3)):
         with pytest.raises(b.DsvtError):
             b.dsvt_rel_buckets(win, exact, side)
