@@ -273,8 +273,17 @@ __global__ __launch_bounds__(1024) void k_ln_sum(const float* __restrict__ parti
   __shared__ float s[32][33];
   const int col = threadIdx.x & 31, slice = threadIdx.x >> 5, c = blockIdx.x * 32 + col;
   float v = 0.f;
-  if (c < 2 * C)
-    for (int k = slice; k < groups; k += 32) v += partial[(int64_t)k * 2 * C + c];
+  if (c < 2 * C) {
+    int k = slice;
+    for (; k + 7 * 32 < groups; k += 8 * 32) {    // eight loads on their way at a time
+      float f[8];
+#pragma unroll
+      for (int j = 0; j < 8; ++j) f[j] = partial[(int64_t)(k + j * 32) * 2 * C + c];
+#pragma unroll
+      for (int j = 0; j < 8; ++j) v += f[j];
+    }
+    for (; k < groups; k += 32) v += partial[(int64_t)k * 2 * C + c];
+  }
   s[slice][col] = v;
   __syncthreads();
   if (threadIdx.x >= 32 || c >= 2 * C) return;
