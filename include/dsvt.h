@@ -369,7 +369,7 @@ int dsvt_set_mha(const dsvt_mha_cfg* cfg, const dsvt_maps* maps, const int32_t* 
 /* The gradients, from that of out: d_qkv [device] [n_voxels, 3C] and d_rel_bias [device] [heads, n_rel] float (NULL: not
  * wanted), both written, not added to; rows of voxels in no set stay as they are.  Nothing but the inputs is needed from the forward
  * call.  ws [device] 16-byte aligned, of the bytes that dsvt_set_mha_backward_workspace_size reports (none
- * without d_rel_bias); no state is kept in it.  Supported as above, rows of d_out and d_qkv aligned likewise.  The results do not depend on the order in which the kernels run. */
+ * without d_rel_bias); no state is kept in it, calls that may run at the same time need one each.  Supported as above, rows of d_out and d_qkv aligned likewise.  The results do not depend on the order in which the kernels run. */
 int dsvt_set_mha_backward_workspace_size(const dsvt_mha_cfg* cfg, const dsvt_maps* maps, size_t* bytes);
 int dsvt_set_mha_backward(const dsvt_mha_cfg* cfg, const dsvt_maps* maps, const int32_t* coords, const void* qkv, int64_t ld_qkv,
                           const void* d_out, int64_t ld_dout, void* d_qkv, int64_t ld_dqkv, float* d_rel_bias,
@@ -389,7 +389,8 @@ int dsvt_layer_norm(const dsvt_ln_cfg* cfg, const void* x, int64_t ld_x, const v
 
 /* The gradients, from dy, that of y: dx [device] [n_rows, C] = that of z, and so of x and of res alike (dx may be dy itself, same
  * stride); d_gamma, d_beta [device] [C] float, written, not added to.  x and res as the forward call had them.
- * ws [device] 16-byte aligned, of the bytes that dsvt_layer_norm_backward_workspace_size reports; no state is kept in it. */
+ * ws [device] 16-byte aligned, of the bytes that dsvt_layer_norm_backward_workspace_size reports; no state is kept in it, calls that
+ * may run at the same time need one each. */
 int dsvt_layer_norm_backward_workspace_size(const dsvt_ln_cfg* cfg, int32_t n_rows, size_t* bytes);
 int dsvt_layer_norm_backward(const dsvt_ln_cfg* cfg, const void* dy, int64_t ld_dy, const void* x, int64_t ld_x, const void* res,
                              int64_t ld_res, int32_t n_rows, void* dx, int64_t ld_dx, float* d_gamma, float* d_beta,
