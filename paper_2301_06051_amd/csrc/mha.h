@@ -438,6 +438,7 @@ __host__ __device__ constexpr int mha_per_cu(bool back, int element, int padded,
 __host__ __device__ constexpr int mha_per_simd(bool back, int element, int padded, int tau) {
   return mha_waves(back, element, padded, tau) * mha_per_cu(back, element, padded, tau) / 4;
 }
-constexpr size_t kMhaLdsMax = 131 << 10;          // dynamic LDS of a workgroup, at most: 160 KB less what its sets take (28 KB)
+// Dynamic LDS of a workgroup, at most: 160 KB less what its sets take (14 KB of up to 48 voxels, 28 KB of up to 96), or half of it.
+__host__ __device__ constexpr size_t mha_lds_max(int tau, int per_cu) { return (per_cu == 2 ? 65 : tau <= 48 ? 146 : 131) << 10; }
 
 extern __shared__ double mha_lds[];

@@ -84,18 +84,18 @@ int make_plan(const dsvt_mha_cfg* c, int32_t max_sets, int32_t tau, bool back, b
     return hs;
   };
   if (by_bucket && c->n_rel > 65535) p->form = kInMemory;
-  p->hs = most_heads(kMhaLdsMax / per_cu);
-  if (p->hs == 0) p->hs = most_heads(kMhaLdsMax);
+  p->hs = most_heads(mha_lds_max(tau, per_cu));
+  if (p->hs == 0) p->hs = most_heads(mha_lds_max(tau, 1));      // one workgroup a compute unit after all
   if (p->hs == 0) {
     p->form = kInMemory;
-    p->hs = most_heads(kMhaLdsMax);
+    p->hs = most_heads(mha_lds_max(tau, 1));
   }
   p->entries = (int32_t)entries;
   // Sums that the LDS of a workgroup does not hold for one head: workgroups of a head share its entries, and each goes through all sets.
   p->ranges = 1;
   if (p->hs == 0) {
     p->hs = 1;
-    p->ranges = (int32_t)dsvt_ceil_div((int64_t)p->entries * 8, kMhaLdsMax);
+    p->ranges = (int32_t)dsvt_ceil_div((int64_t)p->entries * 8, mha_lds_max(tau, 1));
   }
   p->n_off = (int32_t)n_off;
   p->lds = lds_bytes(p->form, p->hs, d_bias ? dsvt_ceil_div(p->entries, p->ranges) : 0, p->entries, n_off);

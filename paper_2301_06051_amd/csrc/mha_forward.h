@@ -106,7 +106,7 @@ __global__ __launch_bounds__(64 * mha_waves(false, sizeof(T), HDP, 16 * kTilesMa
 
 template <typename T, int HDP, TableForm kForm, int kTilesMax> int launch(const MhaArgs& a, size_t lds, hipStream_t st) {
   static std::atomic<uint64_t> allowed;
-  if (const int rc = dsvt_allow_lds(reinterpret_cast<const void*>(k_mha_forward<T, HDP, kForm, kTilesMax>), kMhaLdsMax, allowed)) return rc;
+  if (const int rc = dsvt_allow_lds(reinterpret_cast<const void*>(k_mha_forward<T, HDP, kForm, kTilesMax>), mha_lds_max(16 * kTilesMax, 1), allowed)) return rc;
   dsvt_prof_scope ps(DSVT_K_MHA_FORWARD, st);
   k_mha_forward<T, HDP, kForm, kTilesMax><<<(unsigned)(a.groups * a.parts), 64 * a.hs * a.slots, lds, st>>>(a);
   return DSVT_OK;
