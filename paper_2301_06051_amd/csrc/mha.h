@@ -1,4 +1,4 @@
-// What the kernels of dsvt_set_mha and dsvt_set_mha_backward share (mha_forward.hip, mha_backward.hip); the entry points are
+// What the kernels of dsvt_set_mha and dsvt_set_mha_backward share (mha_forward.h, mha_backward.h); the entry points are
 // in mha.hip.  Multi-head attention inside every set (Eq. 5, second line) on rows that are already projected, with a learned
 // relative position bias per offset or per bucket of offsets, and its gradients.  With g = d out, sigma = 1/sqrt(d), m_j the
 // weight of voxel j as a key (1, or the number of its slots), B the bucket of an offset:
