@@ -467,13 +467,22 @@ def _vector(t, shape, dtype, device, what):
                          f"{tuple(t.shape)} on {t.device}")
 
 
-def _scratch(nbytes, ws, stream, like):
-    """The caller's scratch, or fresh one that stays allocated until `stream` is done with it."""
-    if ws is None:
-        ws = like.new_empty(nbytes, dtype=torch.uint8)
-        if stream is not None:
-            ws.record_stream(torch.cuda.ExternalStream(stream))
-    return ws
+def _other_stream(stream, device):
+    """None if the call's kernels run on the current stream, else the stream of that handle (0: the default stream)."""
+    if stream is None or stream == _current_stream(device):
+        return None
+    return torch.cuda.ExternalStream(stream, device) if stream else torch.cuda.default_stream(device)
+
+
+def _new(like, shape, dtype, other):
+    """An uninitialised tensor for kernels that run on `other` (None: the current stream).  It is a block of that stream's, whose earlier
+    users are so ordered before them: a block of the current stream may be in use there still."""
+    if other is None:
+        return like.new_empty(shape, dtype=dtype)
+    with torch.cuda.stream(other):
+        t = like.new_empty(shape, dtype=dtype)
+    t.record_stream(torch.cuda.current_stream())       # where the caller goes on with it
+    return t
 
 
 def dsvt_rel_buckets(win, n_exact, n_side):
@@ -512,7 +521,7 @@ def dsvt_set_mha(mha, maps, coords, qkv, out=None, stream=None):
     ld = _rows(qkv, (n, 3 * c), dtype, dev, "qkv")
     _vector(coords, (n, 4), torch.int32, dev, "coords")
     if out is None:
-        out, ld_out = qkv.new_empty((n, c)), c
+        out, ld_out = _new(qkv, (n, c), dtype, _other_stream(stream, dev)), c
     else:
         ld_out = _rows(out, (n, c), dtype, dev, "out")
     rc = lib().dsvt_set_mha(mha.ref, C.byref(maps.struct), coords.data_ptr(), qkv.data_ptr(), ld, out.data_ptr(), ld_out,
@@ -539,17 +548,19 @@ def dsvt_set_mha_backward(mha, maps, coords, qkv, d_out, d_qkv=None, d_rel_bias=
     _same_device(mha, dev)
     ld, ld_out = _rows(qkv, (n, 3 * c), dtype, dev, "qkv"), _rows(d_out, (n, c), dtype, dev, "d_out")
     _vector(coords, (n, 4), torch.int32, dev, "coords")
+    other = _other_stream(stream, dev)
     if d_qkv is None:
-        d_qkv, ld_d = qkv.new_empty((n, 3 * c)), 3 * c
+        d_qkv, ld_d = _new(qkv, (n, 3 * c), dtype, other), 3 * c
     else:
         ld_d = _rows(d_qkv, (n, 3 * c), dtype, dev, "d_qkv")
     if d_rel_bias is not None:
         _vector(d_rel_bias, mha.rel_bias.shape if mha.rel_bias is not None else (), torch.float32, dev, "d_rel_bias")
     elif want_rel_bias and mha.rel_bias is not None:
-        d_rel_bias = torch.empty_like(mha.rel_bias)
+        d_rel_bias = _new(mha.rel_bias, mha.rel_bias.shape, torch.float32, other)
     p_ws, ws_bytes, p_rel = None, 0, None
     if d_rel_bias is not None:
-        ws = _scratch(dsvt_set_mha_backward_workspace_size(mha, maps) if ws is None else 0, ws, stream, qkv)
+        if ws is None:
+            ws = _new(qkv, dsvt_set_mha_backward_workspace_size(mha, maps), torch.uint8, other)
         p_ws, ws_bytes, p_rel = ws.data_ptr(), ws.numel(), d_rel_bias.data_ptr()
     rc = lib().dsvt_set_mha_backward(mha.ref, C.byref(maps.struct), coords.data_ptr(), qkv.data_ptr(), ld, d_out.data_ptr(), ld_out,
                                      d_qkv.data_ptr(), ld_d, p_rel, p_ws, ws_bytes, _current_stream(dev) if stream is None else stream)
@@ -577,7 +588,7 @@ def dsvt_layer_norm(ln, x, res=None, y=None, stream=None):
     ld_x = _rows(x, (n, c), dtype, dev, "x")
     ld_res, p_res = (0, None) if res is None else (_rows(res, (n, c), dtype, dev, "res"), res.data_ptr())
     if y is None:
-        y, ld_y = x.new_empty((n, c)), c
+        y, ld_y = _new(x, (n, c), dtype, _other_stream(stream, dev)), c
     else:
         ld_y = _rows(y, (n, c), dtype, dev, "y")
     rc = lib().dsvt_layer_norm(ln.ref, x.data_ptr(), ld_x, p_res, ld_res, n, y.data_ptr(), ld_y, _current_stream(dev) if stream is None else stream)
@@ -601,19 +612,21 @@ def dsvt_layer_norm_backward(ln, dy, x, res=None, dx=None, d_gamma=None, d_beta=
     _same_device(ln, dev)
     ld_dy, ld_x = _rows(dy, (n, c), dtype, dev, "dy"), _rows(x, (n, c), dtype, dev, "x")
     ld_res, p_res = (0, None) if res is None else (_rows(res, (n, c), dtype, dev, "res"), res.data_ptr())
+    other = _other_stream(stream, dev)
     if dx is None:
-        dx, ld_dx = x.new_empty((n, c)), c
+        dx, ld_dx = _new(x, (n, c), dtype, other), c
     else:
         ld_dx = _rows(dx, (n, c), dtype, dev, "dx")
     if d_gamma is None:
-        d_gamma = torch.empty_like(ln.gamma)
+        d_gamma = _new(ln.gamma, (c,), torch.float32, other)
     else:
         _vector(d_gamma, (c,), torch.float32, dev, "d_gamma")
     if d_beta is None:
-        d_beta = torch.empty_like(ln.gamma)
+        d_beta = _new(ln.gamma, (c,), torch.float32, other)
     else:
         _vector(d_beta, (c,), torch.float32, dev, "d_beta")
-    ws = _scratch(dsvt_layer_norm_backward_workspace_size(ln, n) if ws is None else 0, ws, stream, x)
+    if ws is None:
+        ws = _new(x, dsvt_layer_norm_backward_workspace_size(ln, n), torch.uint8, other)
     rc = lib().dsvt_layer_norm_backward(ln.ref, dy.data_ptr(), ld_dy, x.data_ptr(), ld_x, p_res, ld_res, n, dx.data_ptr(), ld_dx, d_gamma.data_ptr(),
                                         d_beta.data_ptr(), ws.data_ptr(), ws.numel(), _current_stream(dev) if stream is None else stream)
     if rc:

@@ -1,0 +1,66 @@
+"""How the training calls treat streams, memory and arguments on the GPU."""
+import pytest
+import torch
+
+pytestmark = pytest.mark.gpu
+dsvt = pytest.importorskip("paper_2301_06051_amd")
+from gpu_util import gpu_maps  # noqa: E402
+from paper_2301_06051_amd import binding  # noqa: E402
+
+N, C, HEADS, WIN = 300, 64, 4, (12, 12, 1)
+
+
+def _problem():
+    g = torch.Generator().manual_seed(1)
+    cell = torch.randperm(400, generator=g)[:N]
+    coords = torch.stack([torch.zeros_like(cell), cell // 20, cell % 20, torch.zeros_like(cell)], 1).to(torch.int32).cuda()
+    maps = gpu_maps(coords, (20, 20, 1), WIN, (0, 0, 0), 36, 1, 0)
+    qkv, d_out = (torch.randn((N, k * C), generator=g).to(torch.bfloat16).cuda() for k in (3, 1))
+    mha = dsvt.SetMha(C, HEADS, "bf16", WIN, torch.randn((HEADS, 529), generator=g).cuda())
+    ln = dsvt.LayerNorm(torch.ones(C, device="cuda"), torch.zeros(C, device="cuda"), "bf16")
+    return coords, maps, qkv, d_out, mha, ln
+
+
+def _calls(problem, **kw):
+    coords, maps, qkv, d_out, mha, ln = problem
+    return [dsvt.dsvt_set_mha(mha, maps, coords, qkv, **kw), *dsvt.dsvt_set_mha_backward(mha, maps, coords, qkv, d_out, **kw),
+            dsvt.dsvt_layer_norm(ln, d_out, **kw), *dsvt.dsvt_layer_norm_backward(ln, d_out, d_out, **kw)]
+
+
+class _Recorder:
+    """The library, keeping the arguments of its calls."""
+
+    def __init__(self, library):
+        self.library, self.calls = library, []
+
+    def __getattr__(self, name):
+        f = getattr(self.library, name)
+        return lambda *args: self.calls.append((name, args)) or f(*args)
+
+
+def _stream_of(pointer):
+    for seg in torch.cuda.memory_snapshot():
+        if seg["address"] <= pointer < seg["address"] + seg["total_size"]:
+            return seg["stream"]
+    raise AssertionError("no block of the allocator's")
+
+
+@pytest.mark.parametrize("handle", ["other", "default", "current"])
+def test_memory_of_a_call_on_another_stream_is_that_streams(handle, monkeypatch):
+    """Outputs and scratch that a call allocates are blocks of the stream its kernels run on: one of the current stream's may be in use there."""
+    problem = _problem()
+    want = _calls(problem)
+    torch.cuda.synchronize()
+    side = torch.cuda.Stream()
+    current = side if handle == "default" else torch.cuda.current_stream()
+    run_on = {"other": side, "default": torch.cuda.default_stream(), "current": current}[handle].cuda_stream
+    recorder = _Recorder(binding.lib())
+    monkeypatch.setattr(binding, "lib", lambda: recorder)
+    with torch.cuda.stream(current):
+        got = _calls(problem, stream=run_on)
+    torch.cuda.synchronize()
+    scratch = [args[-3] for name, args in recorder.calls if name in ("dsvt_set_mha_backward", "dsvt_layer_norm_backward")]
+    assert len(scratch) == 2 and all(scratch)
+    assert all(args[-1] == run_on for name, args in recorder.calls if not name.endswith("size"))
+    assert all(_stream_of(p) == run_on for p in scratch + [t.data_ptr() for t in got])
+    assert all(torch.equal(a, b) for a, b in zip(got, want))
