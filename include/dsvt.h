@@ -358,7 +358,8 @@ typedef struct {
 int dsvt_rel_buckets(const int32_t win[3], int32_t n_exact, int32_t n_side, int32_t* bucket, int32_t* n_rel);
 
 /* qkv [device] [n_voxels, 3C] q, k, v of every voxel (the product with dsvt_layer_w.w_qkv and its bias)
- * out [device] [n_voxels, C]  must not overlap qkv; rows of voxels that are in no set stay as they are
+ * out [device] [n_voxels, C]  rows of voxels that are in no set stay as they are.  Its rows must not overlap those of qkv: slices of one
+ * wider array may lie beside each other, arrays of different strides must lie apart as a whole (DSVT_EINVAL otherwise)
  * maps: set_inds, n_sets, max_sets, tau and n_voxels are read (set slots outside 0 .. n_voxels - 1 are empty; repeats of a
  * voxel are neighbours and every voxel is in one set, as dsvt_partition writes them).  coords as there.
  * Supported: d a multiple of 8 up to 64, tau <= 96 (DSVT_EUNSUPPORTED otherwise), F32 and BF16; qkv, out and coords 16-byte
@@ -367,7 +368,8 @@ int dsvt_set_mha(const dsvt_mha_cfg* cfg, const dsvt_maps* maps, const int32_t* 
                  void* out, int64_t ld_out, void* stream);
 
 /* The gradients, from that of out: d_qkv [device] [n_voxels, 3C] and d_rel_bias [device] [heads, n_rel] float (NULL: not
- * wanted), both written, not added to; rows of voxels in no set stay as they are.  Nothing but the inputs is needed from the forward
+ * wanted), both written, not added to; rows of voxels in no set stay as they are.  The rows of d_qkv must not overlap those of qkv
+ * or d_out, as above.  Nothing but the inputs is needed from the forward
  * call.  ws [device] 16-byte aligned, of the bytes that dsvt_set_mha_backward_workspace_size reports (none
  * without d_rel_bias); no state is kept in it, calls that may run at the same time need one each.  Supported as above, rows of d_out and d_qkv aligned likewise.  The results do not depend on the order in which the kernels run. */
 int dsvt_set_mha_backward_workspace_size(const dsvt_mha_cfg* cfg, const dsvt_maps* maps, size_t* bytes);

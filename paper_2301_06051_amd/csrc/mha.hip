@@ -112,6 +112,17 @@ bool bad_rows(const void* p, int64_t ld, int64_t width, int e) {
   return !p || ((uintptr_t)p & 15u) != 0 || ld < width || ld > UINT32_MAX / e || (ld * e) % 16 != 0;
 }
 
+// Whether two arrays of n rows share a byte (strides and widths in bytes).  Rows of one stride may lie between each other, as slices of a
+// wider array do; of two strides the arrays have to lie apart as a whole.
+bool overlap(const void* p, int64_t ld_p, int64_t w_p, const void* q, int64_t ld_q, int64_t w_q, int32_t n) {
+  const uint64_t a = (uintptr_t)p, b = (uintptr_t)q;
+  if (a + (uint64_t)(n - 1) * ld_p + w_p <= b || b + (uint64_t)(n - 1) * ld_q + w_q <= a) return false;
+  if (ld_p != ld_q) return true;
+  // row j of q begins d + (j - i) ld behind row i of p: r behind the one that begins before it, ld - r before the next
+  const int64_t d = (int64_t)(b - a), ld = ld_p, r = (d % ld + ld) % ld, k = (r - d) / ld;
+  return (r < w_p && k < n && k > -n) || (ld - r < w_q && k - 1 < n && k - 1 > -n);
+}
+
 int check_maps(const dsvt_maps* maps) {
   if (!maps || maps->n_voxels < 0 || maps->max_sets < 0 || maps->max_sets > (1 << 30) || maps->tau <= 0) return DSVT_EINVAL;
   if (maps->n_voxels > 0 && (!maps->set_inds || !maps->n_sets)) return DSVT_EINVAL;
@@ -169,6 +180,7 @@ extern "C" int dsvt_set_mha(const dsvt_mha_cfg* cfg, const dsvt_maps* maps, cons
   if (maps->n_voxels == 0 || maps->max_sets == 0) return DSVT_OK;
   const int e = cfg->dtype == DSVT_BF16 ? 2 : 4;
   if (!coords || ((uintptr_t)coords & 15u) || bad_rows(qkv, ld_qkv, 3 * (int64_t)cfg->C, e) || bad_rows(out, ld_out, cfg->C, e)) return DSVT_EINVAL;
+  if (overlap(out, ld_out * e, (int64_t)cfg->C * e, qkv, ld_qkv * e, 3 * (int64_t)cfg->C * e, maps->n_voxels)) return DSVT_EINVAL;
   MhaArgs a = make_args(cfg, maps, coords, p);
   a.qkv = qkv; a.ld_qkv = (uint32_t)(ld_qkv * e); a.out = out; a.ld_out = (uint32_t)(ld_out * e);
   hipStream_t st = (hipStream_t)stream;
@@ -207,6 +219,9 @@ extern "C" int dsvt_set_mha_backward(const dsvt_mha_cfg* cfg, const dsvt_maps* m
     return DSVT_EINVAL;
   if (p.ws > 0 && (!ws || ((uintptr_t)ws & 15u))) return DSVT_EINVAL;
   if (ws_bytes < p.ws) return DSVT_ENOSPC;
+  // (rows are read ahead, read again, and read by workgroups that do not write them)
+  if (overlap(d_qkv, ld_dqkv * e, 3 * C * e, qkv, ld_qkv * e, 3 * C * e, maps->n_voxels) ||
+      overlap(d_qkv, ld_dqkv * e, 3 * C * e, d_out, ld_dout * e, C * e, maps->n_voxels)) return DSVT_EINVAL;
   MhaArgs a = make_args(cfg, maps, coords, p);
   a.qkv = qkv; a.ld_qkv = (uint32_t)(ld_qkv * e); a.d_out = d_out; a.ld_dout = (uint32_t)(ld_dout * e); a.out = d_qkv; a.ld_out = (uint32_t)(ld_dqkv * e);
   a.partial = d_rel_bias ? static_cast<float*>(ws) : nullptr;

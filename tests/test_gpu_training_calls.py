@@ -64,3 +64,27 @@ def test_memory_of_a_call_on_another_stream_is_that_streams(handle, monkeypatch)
     assert all(args[-1] == run_on for name, args in recorder.calls if not name.endswith("size"))
     assert all(_stream_of(p) == run_on for p in scratch + [t.data_ptr() for t in got])
     assert all(torch.equal(a, b) for a, b in zip(got, want))
+
+
+def test_set_mha_slices_of_one_array_lie_beside_each_other():
+    """All arrays of a call as columns of one; over each other they are refused."""
+    coords, maps, qkv, d_out, mha, _ = _problem()
+    wide = torch.full((N, 8 * C + 16), 5.0, dtype=torch.bfloat16, device="cuda")
+    x, o, g, d = (wide[:, a * C:b * C] for a, b in ((0, 3), (3, 4), (4, 5), (5, 8)))
+    x.copy_(qkv)
+    g.copy_(d_out)
+    want = dsvt.dsvt_set_mha(mha, maps, coords, qkv), dsvt.dsvt_set_mha_backward(mha, maps, coords, qkv, d_out)[0]
+    dsvt.dsvt_set_mha(mha, maps, coords, x, out=o)
+    dsvt.dsvt_set_mha_backward(mha, maps, coords, x, g, d_qkv=d)
+    assert torch.equal(o, want[0]) and torch.equal(d, want[1]) and torch.equal(x, qkv) and bool((wide[:, 8 * C:] == 5).all())
+    # row by row one behind the other: of the same array, N rows on
+    both = torch.empty((2 * N, 3 * C), dtype=torch.bfloat16, device="cuda")
+    both[:N].copy_(qkv)
+    dsvt.dsvt_set_mha_backward(mha, maps, coords, both[:N], d_out, d_qkv=both[N:])
+    assert torch.equal(both[:N], qkv) and torch.equal(both[N:], want[1])
+    for out in (x[:, :C], x[:, 2 * C:], wide[:, 2 * C + 8:3 * C + 8]):
+        with pytest.raises(dsvt.DsvtError):
+            dsvt.dsvt_set_mha(mha, maps, coords, x, out=out)
+    for grad in (x, wide[:, 2 * C:5 * C], wide[:, 4 * C - 8:7 * C - 8], both[1:N + 1]):
+        with pytest.raises(dsvt.DsvtError):
+            dsvt.dsvt_set_mha_backward(mha, maps, coords, x if grad._base is wide else both[:N], g, d_qkv=grad)
