@@ -467,6 +467,15 @@ def _vector(t, shape, dtype, device, what):
                          f"{tuple(t.shape)} on {t.device}")
 
 
+def _no_graph(call, *tensors):
+    """The calls record no graph: tensors that a gradient is to pass through are refused, where it would be lost without a word."""
+    if torch.is_grad_enabled():
+        for t in tensors:
+            if t is not None and t.requires_grad:
+                raise RuntimeError(f"{call} records no graph for automatic differentiation, and a tensor of it requires gradients: call it under "
+                                   "torch.no_grad(), or within a torch.autograd.Function whose backward makes the backward call")
+
+
 def _other_stream(stream, device):
     """None if the call's kernels run on the current stream, else the stream of that handle (0: the default stream)."""
     if stream is None or stream == _current_stream(device):
@@ -516,6 +525,7 @@ class SetMha:
 
 def dsvt_set_mha(mha, maps, coords, qkv, out=None, stream=None):
     """Attention inside every set of `maps` on projected rows qkv [N, 3C]; returns out [N, C]."""
+    _no_graph("dsvt_set_mha", qkv, mha.rel_bias, out)
     n, c, dtype, dev = maps.n_voxels, mha.C, mha.dtype, _current_device()
     _same_device(mha, dev)
     ld = _rows(qkv, (n, 3 * c), dtype, dev, "qkv")
@@ -544,6 +554,7 @@ def dsvt_set_mha_backward_workspace_size(mha, maps):
 def dsvt_set_mha_backward(mha, maps, coords, qkv, d_out, d_qkv=None, d_rel_bias=None, want_rel_bias=True, ws=None, stream=None):
     """Gradients of dsvt_set_mha: returns (d_qkv [N, 3C], d_rel_bias [heads, n_rel] float32, or None without a table or if not
     wanted)."""
+    _no_graph("dsvt_set_mha_backward", qkv, d_out, mha.rel_bias, d_qkv, d_rel_bias)
     n, c, dtype, dev = maps.n_voxels, mha.C, mha.dtype, _current_device()
     _same_device(mha, dev)
     ld, ld_out = _rows(qkv, (n, 3 * c), dtype, dev, "qkv"), _rows(d_out, (n, c), dtype, dev, "d_out")
@@ -583,6 +594,7 @@ class LayerNorm:
 
 def dsvt_layer_norm(ln, x, res=None, y=None, stream=None):
     """LayerNorm of x + res (of x without res), rows [N, C]; returns y."""
+    _no_graph("dsvt_layer_norm", x, res, ln.gamma, ln.beta, y)
     n, c, dtype, dev = x.shape[0], ln.C, ln.dtype, _current_device()
     _same_device(ln, dev)
     ld_x = _rows(x, (n, c), dtype, dev, "x")
@@ -608,6 +620,7 @@ def dsvt_layer_norm_backward_workspace_size(ln, n_rows):
 
 def dsvt_layer_norm_backward(ln, dy, x, res=None, dx=None, d_gamma=None, d_beta=None, ws=None, stream=None):
     """Gradients of dsvt_layer_norm: returns (dx, which is that of x and of res, d_gamma [C], d_beta [C])."""
+    _no_graph("dsvt_layer_norm_backward", dy, x, res, ln.gamma, dx, d_gamma, d_beta)
     n, c, dtype, dev = x.shape[0], ln.C, ln.dtype, _current_device()
     _same_device(ln, dev)
     ld_dy, ld_x = _rows(dy, (n, c), dtype, dev, "dy"), _rows(x, (n, c), dtype, dev, "x")

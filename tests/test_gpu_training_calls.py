@@ -88,3 +88,44 @@ def test_set_mha_slices_of_one_array_lie_beside_each_other():
     for grad in (x, wide[:, 2 * C:5 * C], wide[:, 4 * C - 8:7 * C - 8], both[1:N + 1]):
         with pytest.raises(dsvt.DsvtError):
             dsvt.dsvt_set_mha_backward(mha, maps, coords, x if grad._base is wide else both[:N], g, d_qkv=grad)
+
+
+def test_calls_within_an_autograd_function():
+    """As part of a graph: in a Function, whose gradients are those of the calls made by hand; not twice differentiable, which is refused."""
+    coords, maps, qkv, d_out, mha, ln = _problem()
+
+    class Attention(torch.autograd.Function):
+        @staticmethod
+        def forward(ctx, x, table):
+            ctx.save_for_backward(x, table)
+            return dsvt.dsvt_set_mha(dsvt.SetMha(C, HEADS, "bf16", WIN, table), maps, coords, x)
+
+        @staticmethod
+        def backward(ctx, g):
+            x, table = ctx.saved_tensors
+            return dsvt.dsvt_set_mha_backward(dsvt.SetMha(C, HEADS, "bf16", WIN, table), maps, coords, x, g.contiguous())
+
+    class Norm(torch.autograd.Function):
+        @staticmethod
+        def forward(ctx, x, branch, gamma, beta):
+            ctx.save_for_backward(x, branch, gamma, beta)
+            return dsvt.dsvt_layer_norm(dsvt.LayerNorm(gamma, beta, "bf16"), x, branch)
+
+        @staticmethod
+        def backward(ctx, dy):
+            x, branch, gamma, beta = ctx.saved_tensors
+            dz, dg, db = dsvt.dsvt_layer_norm_backward(dsvt.LayerNorm(gamma, beta, "bf16"), dy.contiguous(), x, branch)
+            return dz, dz, dg, db
+
+    x, t, gamma, beta = (a.detach().clone().requires_grad_() for a in (qkv, mha.rel_bias, ln.gamma, ln.beta))
+    with pytest.raises(RuntimeError, match="records no graph"):
+        dsvt.dsvt_set_mha(mha, maps, coords, x)
+    o = Attention.apply(x, t)
+    y = Norm.apply(d_out, o, gamma, beta)
+    got = torch.autograd.grad(y, (x, t, gamma, beta), d_out, retain_graph=True)
+    plain = dsvt.dsvt_set_mha(mha, maps, coords, qkv)
+    dz, dg, db = dsvt.dsvt_layer_norm_backward(ln, d_out, d_out, plain)
+    assert torch.equal(y, dsvt.dsvt_layer_norm(ln, d_out, plain))
+    assert all(torch.equal(a, b) for a, b in zip(got, (*dsvt.dsvt_set_mha_backward(mha, maps, coords, qkv, dz), dg, db)))
+    with pytest.raises(RuntimeError, match="records no graph"):
+        torch.autograd.grad(y, (x, t), d_out, create_graph=True)

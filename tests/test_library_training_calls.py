@@ -1,8 +1,10 @@
 """More that the training calls refuse: host code only, no GPU (nothing is enqueued for a call that is refused)."""
 import ctypes as C
 import os
+from types import SimpleNamespace
 
 import pytest
+import torch
 
 from paper_2301_06051_amd import binding as b
 
@@ -33,3 +35,26 @@ def test_set_mha_refuses_rows_over_rows(dtype, e):
         assert L.dsvt_set_mha_backward(C.byref(cfg), C.byref(maps), P, P, ld_r, far, W, P + at, ld_w, P, P, 1 << 30, None) == b.DSVT_EINVAL
         assert L.dsvt_set_mha_backward(C.byref(cfg), C.byref(maps), P, far, 3 * W, P, ld_r, P + at, ld_w, P, P, 1 << 30, None) == (
             b.DSVT_EINVAL), (ld_r, ld_w, at)
+
+
+def test_tensors_that_require_gradients_are_refused():
+    """By every call, for every tensor of it, before anything else is looked at; not without gradients enabled."""
+    def tensors(names, needing):
+        return {k: torch.zeros((4, 4), requires_grad=k == needing) for k in names}
+
+    def calls(t):
+        mha, ln = SimpleNamespace(rel_bias=t["rel_bias"]), SimpleNamespace(gamma=t["gamma"], beta=t["beta"])
+        return {"qkv rel_bias out": lambda: b.dsvt_set_mha(mha, None, None, t["qkv"], out=t["out"]),
+                "qkv d_out rel_bias d_qkv d_rel_bias": lambda: b.dsvt_set_mha_backward(mha, None, None, t["qkv"], t["d_out"], t["d_qkv"], t["d_rel_bias"]),
+                "x res gamma beta y": lambda: b.dsvt_layer_norm(ln, t["x"], t["res"], y=t["y"]),
+                "dy x res gamma dx d_gamma d_beta": lambda: b.dsvt_layer_norm_backward(ln, t["dy"], t["x"], t["res"], t["dx"], t["d_gamma"], t["d_beta"])}
+
+    names = {k for args in calls(dict.fromkeys("qkv rel_bias out d_out d_qkv d_rel_bias x res gamma beta y dy dx d_gamma d_beta".split())) for k in args.split()}
+    for needing in names:
+        for args, call in calls(tensors(names, needing)).items():
+            if needing in args.split():
+                with pytest.raises(RuntimeError, match="records no graph"):
+                    call()
+                with torch.no_grad(), pytest.raises(Exception) as e:      # of the next check: the arguments are no call's
+                    call()
+                assert "records no graph" not in str(e.value)
