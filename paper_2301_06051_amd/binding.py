@@ -461,6 +461,19 @@ def _same_device(owner, device):
         raise ValueError(f"the {type(owner).__name__} was made on cuda:{owner.device}, the current device is cuda:{device}")
 
 
+def _maps_here(maps, device):
+    if maps.set_inds.get_device() != device or maps.n_sets.get_device() != device:
+        raise ValueError(f"the maps are on {maps.set_inds.device} and {maps.n_sets.device}, the current device is cuda:{device}")
+
+
+def _scratch(ws, device):
+    """Address and bytes of the caller's scratch."""
+    if ws.get_device() != device or not ws.is_contiguous():
+        raise ValueError(f"ws: contiguous memory on the current device, cuda:{device}, is wanted; got {tuple(ws.shape)}, strides {tuple(ws.stride())}, "
+                         f"on {ws.device}")
+    return ws.data_ptr(), ws.numel() * ws.element_size()
+
+
 def _vector(t, shape, dtype, device, what):
     if t.shape != shape or t.dtype is not dtype or t.get_device() != device or not t.is_contiguous():
         raise ValueError(f"{what}: a contiguous {dtype} tensor of shape {tuple(shape)} on the current device, cuda:{device}, is wanted; got {t.dtype} "
@@ -528,6 +541,7 @@ def dsvt_set_mha(mha, maps, coords, qkv, out=None, stream=None):
     _no_graph("dsvt_set_mha", qkv, mha.rel_bias, out)
     n, c, dtype, dev = maps.n_voxels, mha.C, mha.dtype, _current_device()
     _same_device(mha, dev)
+    _maps_here(maps, dev)
     ld = _rows(qkv, (n, 3 * c), dtype, dev, "qkv")
     _vector(coords, (n, 4), torch.int32, dev, "coords")
     if out is None:
@@ -557,6 +571,7 @@ def dsvt_set_mha_backward(mha, maps, coords, qkv, d_out, d_qkv=None, d_rel_bias=
     _no_graph("dsvt_set_mha_backward", qkv, d_out, mha.rel_bias, d_qkv, d_rel_bias)
     n, c, dtype, dev = maps.n_voxels, mha.C, mha.dtype, _current_device()
     _same_device(mha, dev)
+    _maps_here(maps, dev)
     ld, ld_out = _rows(qkv, (n, 3 * c), dtype, dev, "qkv"), _rows(d_out, (n, c), dtype, dev, "d_out")
     _vector(coords, (n, 4), torch.int32, dev, "coords")
     other = _other_stream(stream, dev)
@@ -572,7 +587,7 @@ def dsvt_set_mha_backward(mha, maps, coords, qkv, d_out, d_qkv=None, d_rel_bias=
     if d_rel_bias is not None:
         if ws is None:
             ws = _new(qkv, dsvt_set_mha_backward_workspace_size(mha, maps), torch.uint8, other)
-        p_ws, ws_bytes, p_rel = ws.data_ptr(), ws.numel(), d_rel_bias.data_ptr()
+        (p_ws, ws_bytes), p_rel = _scratch(ws, dev), d_rel_bias.data_ptr()
     rc = lib().dsvt_set_mha_backward(mha.ref, C.byref(maps.struct), coords.data_ptr(), qkv.data_ptr(), ld, d_out.data_ptr(), ld_out,
                                      d_qkv.data_ptr(), ld_d, p_rel, p_ws, ws_bytes, _current_stream(dev) if stream is None else stream)
     if rc:
@@ -640,8 +655,9 @@ def dsvt_layer_norm_backward(ln, dy, x, res=None, dx=None, d_gamma=None, d_beta=
         _vector(d_beta, (c,), torch.float32, dev, "d_beta")
     if ws is None:
         ws = _new(x, dsvt_layer_norm_backward_workspace_size(ln, n), torch.uint8, other)
+    p_ws, ws_bytes = _scratch(ws, dev)
     rc = lib().dsvt_layer_norm_backward(ln.ref, dy.data_ptr(), ld_dy, x.data_ptr(), ld_x, p_res, ld_res, n, dx.data_ptr(), ld_dx, d_gamma.data_ptr(),
-                                        d_beta.data_ptr(), ws.data_ptr(), ws.numel(), _current_stream(dev) if stream is None else stream)
+                                        d_beta.data_ptr(), p_ws, ws_bytes, _current_stream(dev) if stream is None else stream)
     if rc:
         _check("dsvt_layer_norm_backward", rc)
     return dx, d_gamma, d_beta

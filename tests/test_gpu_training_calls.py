@@ -129,3 +129,24 @@ def test_calls_within_an_autograd_function():
     assert all(torch.equal(a, b) for a, b in zip(got, (*dsvt.dsvt_set_mha_backward(mha, maps, coords, qkv, dz), dg, db)))
     with pytest.raises(RuntimeError, match="records no graph"):
         torch.autograd.grad(y, (x, t), d_out, create_graph=True)
+
+
+def test_scratch_of_the_caller():
+    """Of any type and of more bytes than needed; on the host, expanded or too small it is refused."""
+    coords, maps, qkv, d_out, mha, ln = _problem()
+    want = dsvt.dsvt_set_mha_backward(mha, maps, coords, qkv, d_out), dsvt.dsvt_layer_norm_backward(ln, d_out, d_out)
+    sizes = dsvt.dsvt_set_mha_backward_workspace_size(mha, maps), dsvt.dsvt_layer_norm_backward_workspace_size(ln, N)
+    for t in (torch.uint8, torch.float32):
+        a, b = (torch.full((s // t.itemsize + 5,), 3, dtype=t, device="cuda") for s in sizes)
+        assert all(torch.equal(x, y) for x, y in zip(dsvt.dsvt_set_mha_backward(mha, maps, coords, qkv, d_out, ws=a), want[0]))
+        assert all(torch.equal(x, y) for x, y in zip(dsvt.dsvt_layer_norm_backward(ln, d_out, d_out, ws=b), want[1]))
+        assert bool((a[-5:] == 3).all()) and bool((b[-5:] == 3).all())
+    for bad in (torch.zeros(max(sizes), dtype=torch.uint8), torch.zeros(1, dtype=torch.uint8, device="cuda").expand(max(sizes))):
+        with pytest.raises(ValueError):
+            dsvt.dsvt_set_mha_backward(mha, maps, coords, qkv, d_out, ws=bad)
+        with pytest.raises(ValueError):
+            dsvt.dsvt_layer_norm_backward(ln, d_out, d_out, ws=bad)
+    with pytest.raises(dsvt.DsvtError):
+        dsvt.dsvt_set_mha_backward(mha, maps, coords, qkv, d_out, ws=torch.zeros(sizes[0] - 1, dtype=torch.uint8, device="cuda"))
+    with pytest.raises(dsvt.DsvtError):
+        dsvt.dsvt_layer_norm_backward(ln, d_out, d_out, ws=torch.zeros(sizes[1] - 1, dtype=torch.uint8, device="cuda"))

@@ -58,3 +58,60 @@ def test_tensors_that_require_gradients_are_refused():
                 with torch.no_grad(), pytest.raises(Exception) as e:      # of the next check: the arguments are no call's
                     call()
                 assert "records no graph" not in str(e.value)
+
+
+class _Elsewhere:
+    """A tensor on another device than the current one."""
+
+    device, shape = "cuda:3", (4,)
+
+    def get_device(self):
+        return 3
+
+    def is_contiguous(self):
+        return True
+
+    def stride(self):
+        return (1,)
+
+
+class _NoLibrary:
+    """Fails the test if a call goes on to the library; sizes are asked for."""
+
+    def __getattr__(self, name):
+        if name.endswith("workspace_size"):
+            return getattr(self.library, name)
+        raise AssertionError(f"{name} was called")
+
+
+def test_scratch_and_maps_that_kernels_cannot_use_are_refused(monkeypatch):
+    """Host memory, memory of another device, and an expanded tensor, whose elements are more than its memory holds.  The current device is
+    taken to be that of the host's tensors (-1), so that everything else fits."""
+    no = _NoLibrary()
+    no.library = b.lib()
+    monkeypatch.setattr(b, "_current_device", lambda: -1)
+    monkeypatch.setattr(b, "_current_stream", lambda device: 0)
+    monkeypatch.setattr(b, "lib", lambda: no)
+    n, c, heads = 3, 64, 4
+    i32 = dict(dtype=torch.int32)
+    mha = b.SetMha(c, heads, "f32", (3, 3, 1), torch.zeros((heads, 25)))
+    ln = b.LayerNorm(torch.zeros(c), torch.zeros(c), "f32")
+    coords, qkv, d_out = torch.zeros((n, 4), **i32), torch.zeros((n, 3 * c)), torch.zeros((n, c))
+
+    def maps(inds=torch.zeros((2, 4), **i32), n_sets=torch.zeros((1,), **i32)):
+        return SimpleNamespace(n_voxels=n, max_sets=2, tau=4, set_inds=inds, n_sets=n_sets, struct=b.Maps(n, 2, 4, P, None, P, b.TileList(0, None, None, None, None)))
+
+    for bad in (_Elsewhere(), torch.zeros(1, dtype=torch.uint8).expand(1 << 20)):
+        with pytest.raises(ValueError, match="ws"):
+            b.dsvt_set_mha_backward(mha, maps(), coords, qkv, d_out, ws=bad)
+        with pytest.raises(ValueError, match="ws"):
+            b.dsvt_layer_norm_backward(ln, d_out, d_out, ws=bad)
+    for bad in (maps(inds=_Elsewhere()), maps(n_sets=_Elsewhere())):
+        with pytest.raises(ValueError, match="maps"):
+            b.dsvt_set_mha(mha, bad, coords, qkv)
+        with pytest.raises(ValueError, match="maps"):
+            b.dsvt_set_mha_backward(mha, bad, coords, qkv, d_out)
+    with pytest.raises(AssertionError, match="dsvt_set_mha was called"):                       # and nothing else was wrong
+        b.dsvt_set_mha(mha, maps(), coords, qkv)
+    with pytest.raises(AssertionError, match="dsvt_layer_norm_backward was called"):
+        b.dsvt_layer_norm_backward(ln, d_out, d_out, ws=torch.zeros(1 << 16, dtype=torch.uint8))
