@@ -444,8 +444,9 @@ def dsvt_vfe(vfe, points, point_batch=None, stream=None):
 
 
 # The current device and the handle of its current stream come without the objects that torch.cuda puts around them, and workspace
-# sizes are asked for once per shape: a call of a small operator is mostly host time.
-_current_device, _current_stream = torch._C._cuda_getDevice, torch._C._cuda_getCurrentRawStream
+# sizes are asked for once per shape: a call of a small operator is mostly host time.  (A torch built for the CPU has neither.)
+_current_device = getattr(torch._C, "_cuda_getDevice", torch.cuda.current_device)
+_current_stream = getattr(torch._C, "_cuda_getCurrentRawStream", lambda device: torch.cuda.current_stream(device).cuda_stream)
 
 
 def _rows(t, shape, dtype, device, what):

@@ -1,6 +1,8 @@
 """More that the training calls refuse: host code only, no GPU (nothing is enqueued for a call that is refused)."""
 import ctypes as C
 import os
+import subprocess
+import sys
 from types import SimpleNamespace
 
 import pytest
@@ -115,3 +117,17 @@ def test_scratch_and_maps_that_kernels_cannot_use_are_refused(monkeypatch):
         b.dsvt_set_mha(mha, maps(), coords, qkv)
     with pytest.raises(AssertionError, match="dsvt_layer_norm_backward was called"):
         b.dsvt_layer_norm_backward(ln, d_out, d_out, ws=torch.zeros(1 << 16, dtype=torch.uint8))
+
+
+def test_import_with_a_torch_for_the_cpu():
+    """Which has no torch._C._cuda_* functions: the package, its size queries and its refusals work all the same."""
+    code = """
+import torch
+for name in [n for n in dir(torch._C) if n.startswith("_cuda_")]:
+    delattr(torch._C, name)
+import paper_2301_06051_amd as dsvt
+assert dsvt.dsvt_rel_buckets((12, 12, 1), 3, 5)[1] == 81
+"""
+    root = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
+    r = subprocess.run([sys.executable, "-c", code], cwd=root, capture_output=True, text=True, timeout=300)
+    assert r.returncode == 0, r.stderr
