@@ -443,8 +443,9 @@ def dsvt_vfe(vfe, points, point_batch=None, stream=None):
     return vfe
 
 
-# The current device and the handle of its current stream come without the objects that torch.cuda puts around them, and workspace
-# sizes are asked for once per shape: a call of a small operator is mostly host time.  (A torch built for the CPU has neither.)
+# A call of a small operator is mostly host time: the current device and the handle of its current stream come without the objects that
+# torch.cuda puts around them (a torch built for the CPU has neither function), and a workspace's size is asked for only if the shape is not
+# that of the call before.
 _current_device = getattr(torch._C, "_cuda_getDevice", torch.cuda.current_device)
 _current_stream = getattr(torch._C, "_cuda_getCurrentRawStream", lambda device: torch.cuda.current_stream(device).cuda_stream)
 
@@ -534,7 +535,7 @@ class SetMha:
             _vector(rel_bucket, (offsets,), torch.int32, _current_device(), "rel_bucket")
         self.struct = MhaCfg(channels, heads, code, I32x3(*win), dup_mode, None if rel_bias is None else rel_bias.data_ptr(),
                              None if rel_bucket is None else rel_bucket.data_ptr(), n_rel)
-        self.ref, self.sizes, self.device = C.byref(self.struct), {}, _current_device()     # sizes: workspace bytes by shape
+        self.ref, self.size, self.device = C.byref(self.struct), (None, 0), _current_device()     # size: the last shape and its workspace bytes
 
 
 def dsvt_set_mha(mha, maps, coords, qkv, out=None, stream=None):
@@ -558,11 +559,12 @@ def dsvt_set_mha(mha, maps, coords, qkv, out=None, stream=None):
 
 def dsvt_set_mha_backward_workspace_size(mha, maps):
     shape = (maps.max_sets, maps.tau)
-    size = mha.sizes.get(shape)
-    if size is None:
+    last, size = mha.size
+    if shape != last:
         b = C.c_size_t(0)
         _check("dsvt_set_mha_backward_workspace_size", lib().dsvt_set_mha_backward_workspace_size(mha.ref, C.byref(maps.struct), C.byref(b)))
-        size = mha.sizes[shape] = b.value
+        size = b.value
+        mha.size = shape, size
     return size
 
 
@@ -605,7 +607,7 @@ class LayerNorm:
         _vector(gamma, (self.C,), torch.float32, _current_device(), "gamma")
         _vector(beta, (self.C,), torch.float32, _current_device(), "beta")
         self.struct = LnCfg(self.C, code, gamma.data_ptr(), beta.data_ptr(), eps)
-        self.ref, self.sizes, self.device = C.byref(self.struct), {}, _current_device()     # sizes: workspace bytes by shape
+        self.ref, self.size, self.device = C.byref(self.struct), (None, 0), _current_device()     # size: the last shape and its workspace bytes
 
 
 def dsvt_layer_norm(ln, x, res=None, y=None, stream=None):
@@ -626,11 +628,12 @@ def dsvt_layer_norm(ln, x, res=None, y=None, stream=None):
 
 
 def dsvt_layer_norm_backward_workspace_size(ln, n_rows):
-    size = ln.sizes.get(n_rows)
-    if size is None:
+    last, size = ln.size
+    if n_rows != last:
         b = C.c_size_t(0)
         _check("dsvt_layer_norm_backward_workspace_size", lib().dsvt_layer_norm_backward_workspace_size(ln.ref, n_rows, C.byref(b)))
-        size = ln.sizes[n_rows] = b.value
+        size = b.value
+        ln.size = n_rows, size
     return size
 
 

@@ -131,3 +131,22 @@ assert dsvt.dsvt_rel_buckets((12, 12, 1), 3, 5)[1] == 81
     root = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
     r = subprocess.run([sys.executable, "-c", code], cwd=root, capture_output=True, text=True, timeout=300)
     assert r.returncode == 0, r.stderr
+
+
+def test_operators_keep_nothing_of_every_shape(monkeypatch):
+    """A training run has another number of rows and sets in every step; sizes are right in any order of them."""
+    monkeypatch.setattr(b, "_current_device", lambda: -1)
+    mha, ln = b.SetMha(64, 4, "f32", (3, 3, 1), torch.zeros((4, 25))), b.LayerNorm(torch.zeros(64), torch.zeros(64), "f32")
+
+    def held(o):
+        return sum(len(v) for v in vars(o).values() if isinstance(v, (dict, list, tuple, set)))
+
+    def maps(sets, tau):
+        return SimpleNamespace(max_sets=sets, tau=tau, struct=b.Maps(9, sets, tau, P, None, P, b.TileList(0, None, None, None, None)))
+
+    first = [(b.dsvt_layer_norm_backward_workspace_size(ln, n), b.dsvt_set_mha_backward_workspace_size(mha, maps(n, 4))) for n in range(2, 600)]
+    before = held(mha), held(ln)
+    again = [(b.dsvt_layer_norm_backward_workspace_size(ln, n), b.dsvt_set_mha_backward_workspace_size(mha, maps(n, 4))) for n in range(599, 1, -1)]
+    assert first == again[::-1] and first[0][0] == 2 * 2 * 64 * 4 and first[-1][0] == 512 * 2 * 64 * 4
+    assert (held(mha), held(ln)) == before and max(before) < 10
+    assert b.dsvt_set_mha_backward_workspace_size(mha, maps(8, 4)) == b.dsvt_set_mha_backward_workspace_size(mha, maps(8, 96))
