@@ -451,11 +451,12 @@ _current_stream = getattr(torch._C, "_cuda_getCurrentRawStream", lambda device: 
 
 
 def _rows(t, shape, dtype, device, what):
-    """The row stride of a [rows, columns] tensor of the current device (`device`) whose columns are neighbours."""
+    """The row stride of a [rows, columns] tensor of the current device (`device`) whose columns are neighbours; of one row, whatever its tensor
+    says, the row's length."""
     if t.shape != shape or t.dtype is not dtype or t.get_device() != device or (shape[1] > 1 and t.stride(1) != 1):
         raise ValueError(f"{what}: a {dtype} tensor of shape {tuple(shape)} with neighbouring columns on the current device, cuda:{device}, is wanted; "
                          f"got {t.dtype} {tuple(t.shape)}, strides {tuple(t.stride())}, on {t.device}")
-    return t.stride(0) if shape[0] > 1 else max(t.stride(0), shape[1])
+    return t.stride(0) if shape[0] > 1 else shape[1]
 
 
 def _same_device(owner, device):

@@ -150,3 +150,15 @@ def test_scratch_of_the_caller():
         dsvt.dsvt_set_mha_backward(mha, maps, coords, qkv, d_out, ws=torch.zeros(sizes[0] - 1, dtype=torch.uint8, device="cuda"))
     with pytest.raises(dsvt.DsvtError):
         dsvt.dsvt_layer_norm_backward(ln, d_out, d_out, ws=torch.zeros(sizes[1] - 1, dtype=torch.uint8, device="cuda"))
+
+
+def test_one_voxel_out_of_odd_rows():
+    """A tensor of one row has a stride that nothing goes by."""
+    coords, _, qkv, d_out, mha, ln = _problem()
+    maps = dsvt.SetMaps.of(torch.zeros((1, 4), dtype=torch.int32, device="cuda"), torch.ones((1,), dtype=torch.int32, device="cuda"), 1)
+    odd = torch.zeros((2, 3 * C + 1), dtype=torch.bfloat16, device="cuda")
+    odd[:1, :3 * C] = qkv[:1]
+    x, g = odd[:1, :3 * C], d_out[:1]
+    assert torch.equal(dsvt.dsvt_set_mha(mha, maps, coords[:1].clone(), x), qkv[:1, 2 * C:])       # one key: its value
+    d_qkv, d_rel = dsvt.dsvt_set_mha_backward(mha, maps, coords[:1].clone(), x, g)
+    assert torch.equal(d_qkv[:, 2 * C:], g) and not d_qkv[:, :2 * C].any() and not d_rel.any()

@@ -150,3 +150,12 @@ def test_operators_keep_nothing_of_every_shape(monkeypatch):
     assert first == again[::-1] and first[0][0] == 2 * 2 * 64 * 4 and first[-1][0] == 512 * 2 * 64 * 4
     assert (held(mha), held(ln)) == before and max(before) < 10
     assert b.dsvt_set_mha_backward_workspace_size(mha, maps(8, 4)) == b.dsvt_set_mha_backward_workspace_size(mha, maps(8, 96))
+
+
+def test_one_row_has_no_stride():
+    """The first row of rows that lie 579 elements apart begins on 16 bytes, which is all that one row needs."""
+    for stride in (579, 3, 0, 1 << 40):
+        row = torch.empty_strided((1, 576), (stride, 1), dtype=torch.bfloat16, device="meta")
+        assert row.stride(0) == stride and b._rows(row, (1, 576), torch.bfloat16, row.get_device(), "qkv") == 576
+    assert b._rows(torch.empty((2, 579))[:, :576], (2, 576), torch.float32, -1, "qkv") == 579
+    assert b._rows(torch.empty((0, 192)), (0, 192), torch.float32, -1, "x") == 192
