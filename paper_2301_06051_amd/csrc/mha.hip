@@ -101,9 +101,11 @@ int make_plan(const dsvt_mha_cfg* c, int32_t max_sets, int32_t tau, bool back, b
   p->lds = lds_bytes(p->form, p->hs, d_bias ? dsvt_ceil_div(p->entries, p->ranges) : 0, p->entries, n_off);
   p->slots = 1;
   while (2 * p->slots * p->hs <= waves) p->slots *= 2;
-  int64_t parts = dsvt_ceil_div(kComputeUnits * per_cu, c->heads / p->hs * p->ranges);
-  if (parts > max_sets) parts = max_sets;
-  p->parts = (int32_t)dsvt_align_up((size_t)(parts > 0 ? parts : 1), 8);
+  // Parts by eights (see Share), and no more workgroups than fit the chip at once: one part too many is a second round of all of them.
+  // At least eight; one a set where there are fewer sets.
+  const int64_t fit = kComputeUnits * per_cu / (c->heads / p->hs * p->ranges) / 8 * 8, parts = fit > 8 ? fit : 8;
+  const int64_t sets = (int64_t)dsvt_align_up((size_t)(max_sets > 0 ? max_sets : 1), 8);
+  p->parts = (int32_t)(parts < sets ? parts : sets);
   p->ws = d_bias ? (size_t)p->parts * c->heads * (size_t)p->entries * 4 : 0;
   return DSVT_OK;
 }

@@ -159,3 +159,15 @@ def test_one_row_has_no_stride():
         assert row.stride(0) == stride and b._rows(row, (1, 576), torch.bfloat16, row.get_device(), "qkv") == 576
     assert b._rows(torch.empty((2, 579))[:, :576], (2, 576), torch.float32, -1, "qkv") == 579
     assert b._rows(torch.empty((0, 192)), (0, 192), torch.float32, -1, "x") == 192
+
+
+@pytest.mark.parametrize("heads,side_by_side", [(8, 8), (24, 8), (40, 8), (12, 6), (7, 7), (11, 1), (33, 3), (264, 8)])
+def test_backward_workgroups_fit_the_chip_at_once(heads, side_by_side):
+    """A row of partial sums for every part of the sets; a part has a workgroup for every group of heads, all parts together at most one a
+    compute unit (256), and at least eight parts."""
+    cfg, size = b.MhaCfg(8 * heads, heads, b.DSVT_BF16, b.I32x3(12, 12, 1), 0, P, None, 529), C.c_size_t(0)
+    for sets in (0, 1, 8, 9, 50, 100, 1 << 20):
+        assert b.lib().dsvt_set_mha_backward_workspace_size(C.byref(cfg), C.byref(b.Maps(N, sets, 36, P, None, P, b.TileList(0, None, None, None, None))), C.byref(size)) == 0
+        parts, rest = divmod(size.value, heads * 529 * 4)
+        groups = heads // side_by_side
+        assert rest == 0 and parts % 8 == 0 and parts == min(max(256 // groups // 8 * 8, 8), max((sets + 7) // 8 * 8, 8)), (sets, parts)
