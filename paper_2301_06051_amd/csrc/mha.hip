@@ -70,7 +70,8 @@ int make_plan(const dsvt_mha_cfg* c, int32_t max_sets, int32_t tau, bool back, b
   if (hd % 8 != 0 || hd > 64 || tau > kSetMax || n_off >= (1 << 24) || (c->rel_bias && c->n_rel >= (1 << 24))) return DSVT_EUNSUPPORTED;
   const bool by_bucket = c->rel_bias && c->rel_bucket;
   const int element = c->dtype == DSVT_BF16 ? 2 : 4, padded = hd <= 16 ? 16 : hd <= 32 ? 32 : 64;
-  const int waves = mha_waves(back, element, padded, tau), per_cu = mha_per_cu(back, element, padded, tau);
+  const int waves = mha_waves(back, element, padded, tau);
+  int per_cu = mha_per_cu(back, element, padded, tau);
   // In LDS if it fits there for one head, for as many heads as fit: heads of one set in one workgroup share cache lines.  (Buckets could also be
   // summed up by offset and folded afterwards: 30,000 pillars, 81 buckets, backward 38.9 us where by bucket takes 37.3, 2,000 voxels 19.6
   // and 17.1; two lookups a pair cost less than larger tables and one more kernel.)
@@ -99,6 +100,7 @@ int make_plan(const dsvt_mha_cfg* c, int32_t max_sets, int32_t tau, bool back, b
   }
   p->n_off = (int32_t)n_off;
   p->lds = lds_bytes(p->form, p->hs, d_bias ? dsvt_ceil_div(p->entries, p->ranges) : 0, p->entries, n_off);
+  if (p->lds > mha_lds_max(tau, per_cu)) per_cu = 1;
   p->slots = 1;
   while (2 * p->slots * p->hs <= waves) p->slots *= 2;
   // Parts by eights (see Share), and no more workgroups than fit the chip at once: one part too many is a second round of all of them.

@@ -1,4 +1,6 @@
 """How the training calls treat streams, memory and arguments on the GPU."""
+import ctypes
+
 import pytest
 import torch
 
@@ -162,3 +164,41 @@ def test_one_voxel_out_of_odd_rows():
     assert torch.equal(dsvt.dsvt_set_mha(mha, maps, coords[:1].clone(), x), qkv[:1, 2 * C:])       # one key: its value
     d_qkv, d_rel = dsvt.dsvt_set_mha_backward(mha, maps, coords[:1].clone(), x, g)
     assert torch.equal(d_qkv[:, 2 * C:], g) and not d_qkv[:, :2 * C].any() and not d_rel.any()
+
+
+def _launches(call):
+    """(workgroups, bytes of dynamic LDS) of the kernels that a call launches, from its captured graph, which is never run."""
+    class Params(ctypes.Structure):                  # hipKernelNodeParams
+        _fields_ = [("block", ctypes.c_uint32 * 3), ("extra", ctypes.c_void_p), ("func", ctypes.c_void_p), ("grid", ctypes.c_uint32 * 3),
+                    ("args", ctypes.c_void_p), ("lds", ctypes.c_uint32)]
+
+    with open("/proc/self/maps") as f:
+        hip = ctypes.CDLL(next(line.split()[-1] for line in f if "libamdhip64" in line))
+    graph = torch.cuda.CUDAGraph(keep_graph=True)
+    with torch.cuda.graph(graph):
+        call()
+    raw, count, kind, out = ctypes.c_void_p(graph.raw_cuda_graph()), ctypes.c_size_t(0), ctypes.c_int(0), []
+    assert hip.hipGraphGetNodes(raw, None, ctypes.byref(count)) == 0
+    nodes = (ctypes.c_void_p * count.value)()
+    assert hip.hipGraphGetNodes(raw, nodes, ctypes.byref(count)) == 0
+    for node in nodes:
+        assert hip.hipGraphNodeGetType(ctypes.c_void_p(node), ctypes.byref(kind)) == 0
+        if kind.value == 0:                          # hipGraphNodeTypeKernel
+            p = Params()
+            assert hip.hipGraphKernelNodeGetParams(ctypes.c_void_p(node), ctypes.byref(p)) == 0
+            out.append((p.grid[0], p.lds))
+    return out
+
+
+@pytest.mark.parametrize("win,heads,tau,most", [((12, 12, 1), 8, 36, 512), ((12, 12, 8), 8, 48, 512), ((12, 12, 32), 8, 36, 256), ((30, 30, 20), 8, 36, 512),
+                                                ((12, 12, 32), 24, 48, 256), ((12, 12, 1), 24, 36, 512), ((12, 12, 1), 8, 90, 256)])
+def test_set_mha_workgroups_fit_the_chip_at_once(win, heads, tau, most):
+    """A forward call fills 256 compute units once: with two workgroups each where half of the LDS and of the registers is enough, else with one."""
+    n, sets = 40, 5000
+    maps = dsvt.SetMaps.of(torch.full((sets, tau), -1, dtype=torch.int32, device="cuda"), torch.zeros((1,), dtype=torch.int32, device="cuda"), n)
+    coords, qkv = torch.zeros((n, 4), dtype=torch.int32, device="cuda"), torch.zeros((n, 24 * heads), dtype=torch.bfloat16, device="cuda")
+    mha = dsvt.SetMha(8 * heads, heads, "bf16", win, torch.zeros((heads, (2 * win[0] - 1) * (2 * win[1] - 1) * (2 * win[2] - 1)), device="cuda"))
+    out = torch.empty((n, 8 * heads), dtype=torch.bfloat16, device="cuda")
+    (grid, lds), = _launches(lambda: dsvt.dsvt_set_mha(mha, maps, coords, qkv, out=out))
+    print("[case]", win, heads, tau, grid, "workgroups", lds, "bytes", flush=True)
+    assert most * 3 // 4 <= grid <= most and lds <= (65 << 10 if most == 512 else 146 << 10)
