@@ -267,13 +267,14 @@ __global__ __launch_bounds__(kThreads) void k_ln_long(LnArgs a, int32_t rows) {
   }
 }
 
-// d_gamma and d_beta from the workgroups' partial sums: 32 columns a workgroup, 32 slices of the partial rows, added in a fixed order.
+// d_gamma and d_beta from the workgroups' partial sums: 32 columns a workgroup, 32 slices of the partial rows, added in a fixed order.  In 64
+// bits: 512 numbers added one after the other in 32 would be most of the error of these sums, and the adds are not what the kernel waits for.
 // No rows (groups == 0): zeros.
 __global__ __launch_bounds__(1024) void k_ln_sum(const float* __restrict__ partial, int32_t groups, int32_t C, float* __restrict__ d_gamma,
                                                  float* __restrict__ d_beta) {
-  __shared__ float s[32][33];
+  __shared__ double s[32][33];
   const int col = threadIdx.x & 31, slice = threadIdx.x >> 5, c = blockIdx.x * 32 + col;
-  float v = 0.f;
+  double v = 0.;
   if (c < 2 * C) {
     int k = slice;
     for (; k + 7 * 32 < groups; k += 8 * 32) {    // eight loads on their way at a time
@@ -281,17 +282,17 @@ __global__ __launch_bounds__(1024) void k_ln_sum(const float* __restrict__ parti
 #pragma unroll
       for (int j = 0; j < 8; ++j) f[j] = partial[(int64_t)(k + j * 32) * 2 * C + c];
 #pragma unroll
-      for (int j = 0; j < 8; ++j) v += f[j];
+      for (int j = 0; j < 8; ++j) v += (double)f[j];
     }
-    for (; k < groups; k += 32) v += partial[(int64_t)k * 2 * C + c];
+    for (; k < groups; k += 32) v += (double)partial[(int64_t)k * 2 * C + c];
   }
   s[slice][col] = v;
   __syncthreads();
   if (threadIdx.x >= 32 || c >= 2 * C) return;
-  v = 0.f;
+  v = 0.;
 #pragma unroll
   for (int k = 0; k < 32; ++k) v += s[k][col];
-  (c < C ? d_gamma : d_beta)[c < C ? c : c - C] = v;
+  (c < C ? d_gamma : d_beta)[c < C ? c : c - C] = (float)v;
 }
 
 // The widest pieces of 16, 8, 4 or 2 bytes on which every row of every array starts and of which C is a whole number; then the fewest lanes

@@ -202,3 +202,18 @@ def test_set_mha_workgroups_fit_the_chip_at_once(win, heads, tau, most):
     (grid, lds), = _launches(lambda: dsvt.dsvt_set_mha(mha, maps, coords, qkv, out=out))
     print("[case]", win, heads, tau, grid, "workgroups", lds, "bytes", flush=True)
     assert most * 3 // 4 <= grid <= most and lds <= (65 << 10 if most == 512 else 146 << 10)
+
+
+def test_layer_norm_adds_workgroups_in_64_bits():
+    """Gradients in rows 64 apart, each in another workgroup's sum and so alone in it: what is left of large ones that cancel is exact."""
+    n, c = 16384, 64
+    g = torch.Generator().manual_seed(5)
+    dy = torch.zeros((n, c))
+    few = torch.randint(1 << 19, 1 << 20, (256, c), generator=g).float()
+    few[1::2] = 1 / 8 - few[::2]                     # (20 bits and three behind the point)
+    dy[::64] = few
+    ln = dsvt.LayerNorm(torch.ones(c, device="cuda"), torch.zeros(c, device="cuda"), "f32")
+    x = torch.randn((n, c), generator=g)
+    _, _, d_beta = dsvt.dsvt_layer_norm_backward(ln, dy.cuda(), x.cuda())
+    want = dy.double().sum(0)
+    assert bool((want.abs() < 64).all()) and torch.equal(d_beta.cpu(), want.float())
