@@ -199,18 +199,20 @@ class SetMaps:
             self.tile_list = TileList(0, None, None, None, None)
         self.struct = Maps(n_voxels, self.max_sets, cfg.tau, self.set_inds.data_ptr(), self.voxel_slot.data_ptr(),
                            self.n_sets.data_ptr(), self.tile_list)
+        self.device = self.set_inds.get_device()
 
     @classmethod
     def of(cls, set_inds, n_sets, n_voxels):
         """Maps from slot maps the caller has: set_inds int32 [max_sets, tau], n_sets int32 [1] (both on the GPU), as
         dsvt_partition writes them.  For dsvt_set_mha and its backward call: there is no work list and no voxel_slot."""
         assert set_inds.is_cuda and set_inds.dtype == torch.int32 and set_inds.is_contiguous() and set_inds.dim() == 2
-        assert n_sets.is_cuda and n_sets.dtype == torch.int32 and n_sets.numel() == 1
+        assert n_sets.device == set_inds.device and n_sets.dtype == torch.int32 and n_sets.numel() == 1
         m = cls.__new__(cls)
         m.cfg, m.n_voxels, m.tau, m.max_sets, m.max_tiles = None, n_voxels, set_inds.shape[1], set_inds.shape[0], 0
         m.set_inds, m.n_sets, m.voxel_slot = set_inds, n_sets, None
         m.tile_list = TileList(0, None, None, None, None)
         m.struct = Maps(n_voxels, m.max_sets, m.tau, set_inds.data_ptr(), None, n_sets.data_ptr(), m.tile_list)
+        m.device = set_inds.get_device()
         return m
 
 
@@ -459,14 +461,10 @@ def _rows(t, shape, dtype, device, what):
     return t.stride(0) if shape[0] > 1 else shape[1]
 
 
-def _same_device(owner, device):
-    if owner.device != device:
-        raise ValueError(f"the {type(owner).__name__} was made on cuda:{owner.device}, the current device is cuda:{device}")
-
-
-def _maps_here(maps, device):
-    if maps.set_inds.get_device() != device or maps.n_sets.get_device() != device:
-        raise ValueError(f"the maps are on {maps.set_inds.device} and {maps.n_sets.device}, the current device is cuda:{device}")
+def _elsewhere(device, *owners):
+    for owner in owners:
+        if owner.device != device:
+            raise ValueError(f"the {type(owner).__name__} was made on cuda:{owner.device}, the current device is cuda:{device}")
 
 
 def _scratch(ws, device):
@@ -483,28 +481,23 @@ def _vector(t, shape, dtype, device, what):
                          f"{tuple(t.shape)} on {t.device}")
 
 
+# The calls record no graph: with gradients enabled, tensors that one is to pass through are refused, where it would be lost without a word.
+_recording = torch.is_grad_enabled
+
+
 def _no_graph(call, *tensors):
-    """The calls record no graph: tensors that a gradient is to pass through are refused, where it would be lost without a word."""
-    if torch.is_grad_enabled():
-        for t in tensors:
-            if t is not None and t.requires_grad:
-                raise RuntimeError(f"{call} records no graph for automatic differentiation, and a tensor of it requires gradients: call it under "
-                                   "torch.no_grad(), or within a torch.autograd.Function whose backward makes the backward call")
+    for t in tensors:
+        if t is not None and t.requires_grad:
+            raise RuntimeError(f"{call} records no graph for automatic differentiation, and a tensor of it requires gradients: call it under "
+                               "torch.no_grad(), or within a torch.autograd.Function whose backward makes the backward call")
 
 
-def _other_stream(stream, device):
-    """None if the call's kernels run on the current stream, else the stream of that handle (0: the default stream)."""
-    if stream is None or stream == _current_stream(device):
-        return None
-    return torch.cuda.ExternalStream(stream, device) if stream else torch.cuda.default_stream(device)
-
-
-def _new(like, shape, dtype, other):
-    """An uninitialised tensor for kernels that run on `other` (None: the current stream).  It is a block of that stream's, whose earlier
-    users are so ordered before them: a block of the current stream may be in use there still."""
-    if other is None:
+def _new_on(stream, device, like, shape, dtype):
+    """An uninitialised tensor for kernels that run on the stream of that handle (0: the default stream).  It is a block of that stream's, whose
+    earlier users are so ordered before them: a block of the current stream may be in use there still."""
+    if stream == _current_stream(device):
         return like.new_empty(shape, dtype=dtype)
-    with torch.cuda.stream(other):
+    with torch.cuda.stream(torch.cuda.ExternalStream(stream, device) if stream else torch.cuda.default_stream(device)):
         t = like.new_empty(shape, dtype=dtype)
     t.record_stream(torch.cuda.current_stream())       # where the caller goes on with it
     return t
@@ -541,14 +534,15 @@ class SetMha:
 
 def dsvt_set_mha(mha, maps, coords, qkv, out=None, stream=None):
     """Attention inside every set of `maps` on projected rows qkv [N, 3C]; returns out [N, C]."""
-    _no_graph("dsvt_set_mha", qkv, mha.rel_bias, out)
+    if _recording():
+        _no_graph("dsvt_set_mha", qkv, mha.rel_bias, out)
     n, c, dtype, dev = maps.n_voxels, mha.C, mha.dtype, _current_device()
-    _same_device(mha, dev)
-    _maps_here(maps, dev)
+    if mha.device != dev or maps.device != dev:
+        _elsewhere(dev, mha, maps)
     ld = _rows(qkv, (n, 3 * c), dtype, dev, "qkv")
     _vector(coords, (n, 4), torch.int32, dev, "coords")
     if out is None:
-        out, ld_out = _new(qkv, (n, c), dtype, _other_stream(stream, dev)), c
+        out, ld_out = qkv.new_empty((n, c)) if stream is None else _new_on(stream, dev, qkv, (n, c), dtype), c
     else:
         ld_out = _rows(out, (n, c), dtype, dev, "out")
     rc = lib().dsvt_set_mha(mha.ref, C.byref(maps.struct), coords.data_ptr(), qkv.data_ptr(), ld, out.data_ptr(), ld_out,
@@ -572,26 +566,30 @@ def dsvt_set_mha_backward_workspace_size(mha, maps):
 def dsvt_set_mha_backward(mha, maps, coords, qkv, d_out, d_qkv=None, d_rel_bias=None, want_rel_bias=True, ws=None, stream=None):
     """Gradients of dsvt_set_mha: returns (d_qkv [N, 3C], d_rel_bias [heads, n_rel] float32, or None without a table or if not
     wanted)."""
-    _no_graph("dsvt_set_mha_backward", qkv, d_out, mha.rel_bias, d_qkv, d_rel_bias)
+    if _recording():
+        _no_graph("dsvt_set_mha_backward", qkv, d_out, mha.rel_bias, d_qkv, d_rel_bias)
     n, c, dtype, dev = maps.n_voxels, mha.C, mha.dtype, _current_device()
-    _same_device(mha, dev)
-    _maps_here(maps, dev)
+    if mha.device != dev or maps.device != dev:
+        _elsewhere(dev, mha, maps)
     ld, ld_out = _rows(qkv, (n, 3 * c), dtype, dev, "qkv"), _rows(d_out, (n, c), dtype, dev, "d_out")
     _vector(coords, (n, 4), torch.int32, dev, "coords")
-    other = _other_stream(stream, dev)
     if d_qkv is None:
-        d_qkv, ld_d = _new(qkv, (n, 3 * c), dtype, other), 3 * c
+        d_qkv, ld_d = qkv.new_empty((n, 3 * c)) if stream is None else _new_on(stream, dev, qkv, (n, 3 * c), dtype), 3 * c
     else:
         ld_d = _rows(d_qkv, (n, 3 * c), dtype, dev, "d_qkv")
     if d_rel_bias is not None:
         _vector(d_rel_bias, mha.rel_bias.shape if mha.rel_bias is not None else (), torch.float32, dev, "d_rel_bias")
     elif want_rel_bias and mha.rel_bias is not None:
-        d_rel_bias = _new(mha.rel_bias, mha.rel_bias.shape, torch.float32, other)
+        d_rel_bias = torch.empty_like(mha.rel_bias) if stream is None else _new_on(stream, dev, qkv, mha.rel_bias.shape, torch.float32)
     p_ws, ws_bytes, p_rel = None, 0, None
     if d_rel_bias is not None:
+        p_rel = d_rel_bias.data_ptr()
         if ws is None:
-            ws = _new(qkv, dsvt_set_mha_backward_workspace_size(mha, maps), torch.uint8, other)
-        (p_ws, ws_bytes), p_rel = _scratch(ws, dev), d_rel_bias.data_ptr()
+            ws_bytes = dsvt_set_mha_backward_workspace_size(mha, maps)
+            ws = qkv.new_empty(ws_bytes, dtype=torch.uint8) if stream is None else _new_on(stream, dev, qkv, ws_bytes, torch.uint8)
+            p_ws = ws.data_ptr()
+        else:
+            p_ws, ws_bytes = _scratch(ws, dev)
     rc = lib().dsvt_set_mha_backward(mha.ref, C.byref(maps.struct), coords.data_ptr(), qkv.data_ptr(), ld, d_out.data_ptr(), ld_out,
                                      d_qkv.data_ptr(), ld_d, p_rel, p_ws, ws_bytes, _current_stream(dev) if stream is None else stream)
     if rc:
@@ -613,13 +611,15 @@ class LayerNorm:
 
 def dsvt_layer_norm(ln, x, res=None, y=None, stream=None):
     """LayerNorm of x + res (of x without res), rows [N, C]; returns y."""
-    _no_graph("dsvt_layer_norm", x, res, ln.gamma, ln.beta, y)
+    if _recording():
+        _no_graph("dsvt_layer_norm", x, res, ln.gamma, ln.beta, y)
     n, c, dtype, dev = x.shape[0], ln.C, ln.dtype, _current_device()
-    _same_device(ln, dev)
+    if ln.device != dev:
+        _elsewhere(dev, ln)
     ld_x = _rows(x, (n, c), dtype, dev, "x")
     ld_res, p_res = (0, None) if res is None else (_rows(res, (n, c), dtype, dev, "res"), res.data_ptr())
     if y is None:
-        y, ld_y = _new(x, (n, c), dtype, _other_stream(stream, dev)), c
+        y, ld_y = x.new_empty((n, c)) if stream is None else _new_on(stream, dev, x, (n, c), dtype), c
     else:
         ld_y = _rows(y, (n, c), dtype, dev, "y")
     rc = lib().dsvt_layer_norm(ln.ref, x.data_ptr(), ld_x, p_res, ld_res, n, y.data_ptr(), ld_y, _current_stream(dev) if stream is None else stream)
@@ -640,27 +640,31 @@ def dsvt_layer_norm_backward_workspace_size(ln, n_rows):
 
 def dsvt_layer_norm_backward(ln, dy, x, res=None, dx=None, d_gamma=None, d_beta=None, ws=None, stream=None):
     """Gradients of dsvt_layer_norm: returns (dx, which is that of x and of res, d_gamma [C], d_beta [C])."""
-    _no_graph("dsvt_layer_norm_backward", dy, x, res, ln.gamma, dx, d_gamma, d_beta)
+    if _recording():
+        _no_graph("dsvt_layer_norm_backward", dy, x, res, ln.gamma, dx, d_gamma, d_beta)
     n, c, dtype, dev = x.shape[0], ln.C, ln.dtype, _current_device()
-    _same_device(ln, dev)
+    if ln.device != dev:
+        _elsewhere(dev, ln)
     ld_dy, ld_x = _rows(dy, (n, c), dtype, dev, "dy"), _rows(x, (n, c), dtype, dev, "x")
     ld_res, p_res = (0, None) if res is None else (_rows(res, (n, c), dtype, dev, "res"), res.data_ptr())
-    other = _other_stream(stream, dev)
     if dx is None:
-        dx, ld_dx = _new(x, (n, c), dtype, other), c
+        dx, ld_dx = x.new_empty((n, c)) if stream is None else _new_on(stream, dev, x, (n, c), dtype), c
     else:
         ld_dx = _rows(dx, (n, c), dtype, dev, "dx")
     if d_gamma is None:
-        d_gamma = _new(ln.gamma, (c,), torch.float32, other)
+        d_gamma = torch.empty_like(ln.gamma) if stream is None else _new_on(stream, dev, x, (c,), torch.float32)
     else:
         _vector(d_gamma, (c,), torch.float32, dev, "d_gamma")
     if d_beta is None:
-        d_beta = _new(ln.gamma, (c,), torch.float32, other)
+        d_beta = torch.empty_like(ln.gamma) if stream is None else _new_on(stream, dev, x, (c,), torch.float32)
     else:
         _vector(d_beta, (c,), torch.float32, dev, "d_beta")
     if ws is None:
-        ws = _new(x, dsvt_layer_norm_backward_workspace_size(ln, n), torch.uint8, other)
-    p_ws, ws_bytes = _scratch(ws, dev)
+        ws_bytes = dsvt_layer_norm_backward_workspace_size(ln, n)
+        ws = x.new_empty(ws_bytes, dtype=torch.uint8) if stream is None else _new_on(stream, dev, x, ws_bytes, torch.uint8)
+        p_ws = ws.data_ptr()
+    else:
+        p_ws, ws_bytes = _scratch(ws, dev)
     rc = lib().dsvt_layer_norm_backward(ln.ref, dy.data_ptr(), ld_dy, x.data_ptr(), ld_x, p_res, ld_res, n, dx.data_ptr(), ld_dx, d_gamma.data_ptr(),
                                         d_beta.data_ptr(), p_ws, ws_bytes, _current_stream(dev) if stream is None else stream)
     if rc:

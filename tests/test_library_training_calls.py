@@ -100,19 +100,20 @@ def test_scratch_and_maps_that_kernels_cannot_use_are_refused(monkeypatch):
     ln = b.LayerNorm(torch.zeros(c), torch.zeros(c), "f32")
     coords, qkv, d_out = torch.zeros((n, 4), **i32), torch.zeros((n, 3 * c)), torch.zeros((n, c))
 
-    def maps(inds=torch.zeros((2, 4), **i32), n_sets=torch.zeros((1,), **i32)):
-        return SimpleNamespace(n_voxels=n, max_sets=2, tau=4, set_inds=inds, n_sets=n_sets, struct=b.Maps(n, 2, 4, P, None, P, b.TileList(0, None, None, None, None)))
+    def maps(device=-1):
+        return SimpleNamespace(n_voxels=n, max_sets=2, tau=4, device=device, struct=b.Maps(n, 2, 4, P, None, P, b.TileList(0, None, None, None, None)))
 
     for bad in (_Elsewhere(), torch.zeros(1, dtype=torch.uint8).expand(1 << 20)):
         with pytest.raises(ValueError, match="ws"):
             b.dsvt_set_mha_backward(mha, maps(), coords, qkv, d_out, ws=bad)
         with pytest.raises(ValueError, match="ws"):
             b.dsvt_layer_norm_backward(ln, d_out, d_out, ws=bad)
-    for bad in (maps(inds=_Elsewhere()), maps(n_sets=_Elsewhere())):
-        with pytest.raises(ValueError, match="maps"):
-            b.dsvt_set_mha(mha, bad, coords, qkv)
-        with pytest.raises(ValueError, match="maps"):
-            b.dsvt_set_mha_backward(mha, bad, coords, qkv, d_out)
+    with pytest.raises(ValueError, match="SimpleNamespace was made on cuda:3"):
+        b.dsvt_set_mha(mha, maps(3), coords, qkv)
+    with pytest.raises(ValueError, match="SimpleNamespace was made on cuda:3"):
+        b.dsvt_set_mha_backward(mha, maps(3), coords, qkv, d_out)
+    with pytest.raises(AssertionError):
+        b.SetMaps.of(torch.zeros((2, 4), **i32), torch.zeros((1,), **i32), n)                  # of the host
     with pytest.raises(AssertionError, match="dsvt_set_mha was called"):                       # and nothing else was wrong
         b.dsvt_set_mha(mha, maps(), coords, qkv)
     with pytest.raises(AssertionError, match="dsvt_layer_norm_backward was called"):
