@@ -326,9 +326,10 @@ int dsvt_vfe(const dsvt_vfe_cfg* cfg, const float* points, const int32_t* point_
              int32_t* status, void* stream);
 
 /* ---------------------------------------------------------------------------------------
- * Training a layer: the parts of a DSVT layer that are no matrix product (Eq. 5), each as a call of
- * its own with its gradients.  The caller's matrix products (projections, MLP) go in between.  Rows
- * have strides in elements (ld >= row length), so that slices of wider arrays can be passed; n may be 0.
+ * Training a layer: two parts of a DSVT layer (Eq. 5), the attention inside its sets and the
+ * LayerNorm of its residual sums, as calls of their own with their gradients.  The rest is the
+ * caller's: matrix products and their bias sums, the MLP's activation.  Rows have strides in elements
+ * (ld >= row length), so that slices of wider arrays can be passed; n may be 0.
  * ------------------------------------------------------------------------------------ */
 
 /* Multi-head attention inside every set on projected rows, with a learned relative position bias.
@@ -337,7 +338,11 @@ int dsvt_vfe(const dsvt_vfe_cfg* cfg, const float* points, const int32_t* point_
  * i - j is the offset of their cells, numbered as in dsvt_layer_w.rel_bias; m_j = 1 (dup_mode 0: a slot repeating
  * its predecessor's voxel is masked as a key) or the number of voxel j's slots (dup_mode 1).  A query whose keys
  * all have the bias -infinity gets an output of zeros and no gradient; a finite bias is no mask (sizes above 1e37 count as 1e37).  In a
- * set whose voxels do not fit one window (maps of another window) all pairs take the term of offset 0. */
+ * set whose voxels do not fit one window (maps of another window) all pairs take the term of offset 0.
+ * Logits, softmax and all sums are held in 32 bits.  BF16: P, and in the backward call the gradients of the logits, are rounded to
+ * bf16 as operands of the products with v, k and q, beside the rounding of the results (relative to their norm 2.0e-3 in all where the
+ * rounding of the results alone is 1.7e-3; gradients 2.4e-3).  A row of q, k, v or d_out with an infinity or a NaN can make all
+ * channels of its head NaN in the results of its set. */
 typedef struct {
   int32_t C, heads, dtype;
   int32_t win[3];            /* L, W, H of the window the maps were built with                          */
@@ -369,9 +374,11 @@ int dsvt_set_mha(const dsvt_mha_cfg* cfg, const dsvt_maps* maps, const int32_t* 
 
 /* The gradients, from that of out: d_qkv [device] [n_voxels, 3C] and d_rel_bias [device] [heads, n_rel] float (NULL: not
  * wanted), both written, not added to; rows of voxels in no set stay as they are.  The rows of d_qkv must not overlap those of qkv
- * or d_out, as above.  Nothing but the inputs is needed from the forward
- * call.  ws [device] 16-byte aligned, of the bytes that dsvt_set_mha_backward_workspace_size reports (none
- * without d_rel_bias); no state is kept in it, calls that may run at the same time need one each.  Supported as above, rows of d_out and d_qkv aligned likewise.  The results do not depend on the order in which the kernels run. */
+ * or d_out, as above.  Nothing but the inputs is needed from the forward call.  d_rel_bias is added up in 64 bits by every
+ * workgroup, rounded to 32 once, and added up in 64 over the workgroups.
+ * ws [device] 16-byte aligned, of the bytes that dsvt_set_mha_backward_workspace_size reports (none without d_rel_bias); no state is
+ * kept in it, calls that may run at the same time need one each.  Supported as above, rows of d_out and d_qkv aligned likewise.  The
+ * results do not depend on the order in which the kernels run. */
 int dsvt_set_mha_backward_workspace_size(const dsvt_mha_cfg* cfg, const dsvt_maps* maps, size_t* bytes);
 int dsvt_set_mha_backward(const dsvt_mha_cfg* cfg, const dsvt_maps* maps, const int32_t* coords, const void* qkv, int64_t ld_qkv,
                           const void* d_out, int64_t ld_dout, void* d_qkv, int64_t ld_dqkv, float* d_rel_bias,
@@ -385,12 +392,14 @@ typedef struct {
 } dsvt_ln_cfg;
 #define DSVT_LN_MAX_C 65536
 
-/* x, res, y [device] [n_rows, C]; res may be NULL (z = x).  y may be x or res themselves (same stride). */
+/* x, res, y [device] [n_rows, C]; res may be NULL (z = x).  y may be x or res themselves (same stride), and overlaps them in no
+ * other way. */
 int dsvt_layer_norm(const dsvt_ln_cfg* cfg, const void* x, int64_t ld_x, const void* res, int64_t ld_res, int32_t n_rows,
                     void* y, int64_t ld_y, void* stream);
 
 /* The gradients, from dy, that of y: dx [device] [n_rows, C] = that of z, and so of x and of res alike (dx may be dy itself, same
- * stride); d_gamma, d_beta [device] [C] float, written, not added to.  x and res as the forward call had them.
+ * stride, and overlaps the others in no other way); d_gamma, d_beta [device] [C] float, written, not added to: sums of 32 bits over the
+ * rows that a lane and a workgroup take (at most 512 workgroups), of 64 over the workgroups.  x and res as the forward call had them.
  * ws [device] 16-byte aligned, of the bytes that dsvt_layer_norm_backward_workspace_size reports; no state is kept in it, calls that
  * may run at the same time need one each. */
 int dsvt_layer_norm_backward_workspace_size(const dsvt_ln_cfg* cfg, int32_t n_rows, size_t* bytes);

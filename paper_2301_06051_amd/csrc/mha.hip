@@ -86,7 +86,7 @@ int make_plan(const dsvt_mha_cfg* c, int32_t max_sets, int32_t tau, bool back, b
   };
   if (by_bucket && c->n_rel > 65535) p->form = kInMemory;
   p->hs = most_heads(mha_lds_max(tau, per_cu));
-  if (p->hs == 0) p->hs = most_heads(mha_lds_max(tau, 1));      // one workgroup a compute unit after all
+  if (p->hs == 0) p->hs = most_heads(mha_lds_max(tau, 1));      // (one workgroup a compute unit after all, see below)
   if (p->hs == 0) {
     p->form = kInMemory;
     p->hs = most_heads(mha_lds_max(tau, 1));
@@ -100,11 +100,12 @@ int make_plan(const dsvt_mha_cfg* c, int32_t max_sets, int32_t tau, bool back, b
   }
   p->n_off = (int32_t)n_off;
   p->lds = lds_bytes(p->form, p->hs, d_bias ? dsvt_ceil_div(p->entries, p->ranges) : 0, p->entries, n_off);
+  // (120,000 voxels, 12 x 12 x 32 windows with an entry an offset, 133 KB: forward 92 us, 99 with workgroups for two a compute unit)
   if (p->lds > mha_lds_max(tau, per_cu)) per_cu = 1;
   p->slots = 1;
   while (2 * p->slots * p->hs <= waves) p->slots *= 2;
   // Parts by eights (see Share), and no more workgroups than fit the chip at once: one part too many is a second round of all of them.
-  // At least eight; one a set where there are fewer sets.
+  // (120,000 voxels, 24 heads of 16, three groups: backward 248 us, 403 rounded up.)  At least eight; one a set where there are fewer sets.
   const int64_t fit = kComputeUnits * per_cu / (c->heads / p->hs * p->ranges) / 8 * 8, parts = fit > 8 ? fit : 8;
   const int64_t sets = (int64_t)dsvt_align_up((size_t)(max_sets > 0 ? max_sets : 1), 8);
   p->parts = (int32_t)(parts < sets ? parts : sets);

@@ -3,8 +3,8 @@
 // With the queries as columns, P and ds of one query tile and all keys are in registers; dq comes from them as they are, dk and dv, which
 // run over the queries, from P and ds turned round, summed up over the query tiles in registers.  That takes half of a SIMD's registers, so two
 // wavefronts share it, and what bounds a large call is a set's chain of steps at that: C = 192, 8 heads, bf16, 800,000 voxels in full sets of
-// 36 with 2,197 buckets 1,002 us (2.15 GB: 2.1 TB/s); 708 with all rows in the caches and additions in any order, 488 without additions and
-// stores.  30,000 voxels 27 us and 5 for the last step of the table's gradient.
+// 36 with 2,197 buckets 1,005 us (2.15 GB: 2.1 TB/s); 708 with all rows in the caches and additions in any order, 488 without additions and
+// stores.  30,000 voxels 33.5 us a pass, 4.5 of them the last step of the table's gradient.
 #pragma once
 #include "mha.h"
 
