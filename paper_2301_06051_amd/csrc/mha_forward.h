@@ -1,8 +1,8 @@
 // The forward kernel of dsvt_set_mha (see mha.h), for the two types' own files.
 //
 // Bound by latency: of a set's chain (rows, logits, probabilities, product), which four wavefronts a SIMD (128 registers) hide in part, and of
-// the first look-ups.  C = 192, 8 heads, bf16: 30,000 voxels in sets of up to 36 take 16.5 us (46 MB: 2.8 TB/s;
-// of a workgroup's 24 k clocks 7.4 k until its first sets), 120,000 in sets of up to 48 with 2,475 buckets 74 us (187 MB: 2.5 TB/s; 17 of 131 k).
+// the first look-ups.  C = 192, 8 heads, bf16: 30,000 voxels in sets of up to 36 take 16.5 us (46 MB: 2.8 TB/s; of a
+// workgroup's 24 k clocks 7.4 k until its first sets), 120,000 in sets of up to 48 with 2,475 buckets 74 us (187 MB: 2.5 TB/s; 17 of 131 k).
 #pragma once
 #include "mha.h"
 

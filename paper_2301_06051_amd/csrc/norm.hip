@@ -11,8 +11,8 @@
 // 256, up to four 16-byte pieces each), so it is read once, and its sums take three to eight steps across lanes.  Workgroups stay and
 // take rows in turn: gamma and beta are read once a workgroup, and the backward pass adds d_gamma and d_beta up in
 // registers, then in LDS and in one row of partial sums a workgroup, which k_ln_sum adds in their order.  All sums are
-// held in 32 bits, that over the workgroups in 64, and none depends on the order in which workgroups run.  800,000 rows of 192 bf16 with a branch: forward 175 us,
-// backward 233 (5.3 TB/s each; a copy of 2 GiB reaches 4.8 on the same card).
+// held in 32 bits, that over the workgroups in 64, and none depends on the order in which workgroups run.  800,000 rows of 192 bf16 with a
+// branch: forward 175 us, backward 233 (5.3 TB/s each; a copy of 2 GiB reaches 4.8 on the same card).
 #include "common.h"
 #include "mma.h"
 
