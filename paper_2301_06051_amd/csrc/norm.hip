@@ -10,77 +10,21 @@
 // Both passes are bound by the bytes of their rows.  A row sits in the registers of kLanes neighbouring lanes (8 to 64, or a workgroup's
 // 256, up to four 16-byte pieces each), so it is read once, and its sums take three to eight steps across lanes.  Workgroups stay and
 // take rows in turn: gamma and beta are read once a workgroup, and the backward pass adds d_gamma and d_beta up in
-// registers, then in LDS and in one row of partial sums a workgroup, which k_ln_sum adds in their order.  All sums are
+// registers, then in LDS and in one row of partial sums a workgroup, which k_sum_parts adds in their order.  All sums are
 // held in 32 bits, that over the workgroups in 64, and none depends on the order in which workgroups run.  800,000 rows of 192 bf16 with a
 // branch: forward 175 us, backward 233 (5.3 TB/s each; a copy of 2 GiB reaches 4.8 on the same card).
-#include "common.h"
-#include "mma.h"
+#include "rows.h"
 
 namespace {
-
-constexpr int kThreads = 256;
-constexpr int kVectors = 4;                       // 16-byte pieces of a row in one lane, at most
-constexpr int narrow_max(int bytes) { return bytes == 8 ? 8 : 16; }      // and smaller ones
-constexpr int kBackwardGroups = 512;              // workgroups of a backward pass, at most: two a compute unit
-constexpr int kForwardGroups = 2048;
 
 struct LnArgs {
   const void *x, *res, *dy;                       // res: may be null; dy: backward only
   void* out;                                      // y or dx
   const float *gamma, *beta;
-  float *partial, *d_gamma, *d_beta;              // [groups][2][C]; d_*: null when partial sums are to be added up by k_ln_sum
+  float *partial, *d_gamma, *d_beta;              // [groups][2][C]; d_*: null when partial sums are to be added up by k_sum_parts
   int64_t ld_x, ld_res, ld_dy, ld_out;
   int32_t n, C;
   float eps;
-};
-
-template <typename T, int V> struct Piece { typedef T type __attribute__((ext_vector_type(V))); };
-template <typename T> struct Piece<T, 1> { typedef T type; };
-
-template <typename T, int V> __device__ __forceinline__ void widen(const typename Piece<T, V>::type& p, float (&f)[V]) {
-  if constexpr (V == 1) f[0] = (float)p;
-  else {
-#pragma unroll
-    for (int i = 0; i < V; ++i) f[i] = (float)p[i];
-  }
-}
-template <typename T, int V> __device__ __forceinline__ typename Piece<T, V>::type narrow(const float (&f)[V]) {
-  typename Piece<T, V>::type p;
-  if constexpr (V == 1) p = (T)f[0];
-  else {
-#pragma unroll
-    for (int i = 0; i < V; ++i) p[i] = (T)f[i];
-  }
-  return p;
-}
-
-// Sum over kLanes neighbouring lanes, or over the workgroup (kLanes = kThreads, `s` holds a value per wavefront); every lane gets it.
-template <int kLanes> __device__ __forceinline__ float lane_sum(float v, float* s) {
-#pragma unroll
-  for (int d = 1; d < (kLanes < 64 ? kLanes : 64); d *= 2) v += __shfl_xor(v, d, 64);
-  if constexpr (kLanes > 64) {
-    __syncthreads();
-    if ((threadIdx.x & 63) == 0) s[threadIdx.x >> 6] = v;
-    __syncthreads();
-    v = 0.f;
-#pragma unroll
-    for (int k = 0; k < kThreads / 64; ++k) v += s[k];
-  }
-  return v;
-}
-
-// The pieces of one row that a lane holds: piece r is number r * kLanes + lane, past the row's end zero.
-template <typename T, int V, int kLanes, int R> struct RowPieces {
-  typedef typename Piece<T, V>::type P;
-  P p[R];
-  __device__ __forceinline__ void load(const void* base, int64_t at, int part, int pieces, bool there) {
-    const P* row = reinterpret_cast<const P*>(static_cast<const T*>(base) + at);
-#pragma unroll
-    for (int r = 0; r < R; ++r) {
-      P zero = {};
-      p[r] = there && r * kLanes + part < pieces ? row[r * kLanes + part] : zero;
-    }
-  }
 };
 
 // z = x + res in 32 bits, normed in place: returns rsqrt(var + eps).  The mean is subtracted before the squares are summed.
@@ -117,14 +61,6 @@ __device__ __forceinline__ float norm_row(const RowPieces<T, V, kLanes, R>& x, c
 #pragma unroll
     for (int i = 0; i < V; ++i) z[r][i] *= rs;
   return rs;
-}
-
-template <int V, int kLanes, int R>
-__device__ __forceinline__ void load_vector(const float* v, int part, int pieces, float (&f)[R][V]) {
-#pragma unroll
-  for (int r = 0; r < R; ++r)
-#pragma unroll
-    for (int i = 0; i < V; ++i) f[r][i] = r * kLanes + part < pieces ? v[(r * kLanes + part) * V + i] : 0.f;
 }
 
 template <typename T, int V, int kLanes, int R>
@@ -267,91 +203,27 @@ __global__ __launch_bounds__(kThreads) void k_ln_long(LnArgs a, int32_t rows) {
   }
 }
 
-// d_gamma and d_beta from the workgroups' partial sums: 32 columns a workgroup, 32 slices of the partial rows, added in a fixed order.  In 64
-// bits: 512 numbers added one after the other in 32 would be most of the error of these sums, and the adds are not what the kernel waits for.
-// No rows (groups == 0): zeros.
-__global__ __launch_bounds__(1024) void k_ln_sum(const float* __restrict__ partial, int32_t groups, int32_t C, float* __restrict__ d_gamma,
-                                                 float* __restrict__ d_beta) {
-  __shared__ double s[32][33];
-  const int col = threadIdx.x & 31, slice = threadIdx.x >> 5, c = blockIdx.x * 32 + col;
-  double v = 0.;
-  if (c < 2 * C) {
-    int k = slice;
-    for (; k + 7 * 32 < groups; k += 8 * 32) {    // eight loads on their way at a time
-      float f[8];
-#pragma unroll
-      for (int j = 0; j < 8; ++j) f[j] = partial[(int64_t)(k + j * 32) * 2 * C + c];
-#pragma unroll
-      for (int j = 0; j < 8; ++j) v += (double)f[j];
-    }
-    for (; k < groups; k += 32) v += (double)partial[(int64_t)k * 2 * C + c];
-  }
-  s[slice][col] = v;
-  __syncthreads();
-  if (threadIdx.x >= 32 || c >= 2 * C) return;
-  v = 0.;
-#pragma unroll
-  for (int k = 0; k < 32; ++k) v += s[k][col];
-  (c < C ? d_gamma : d_beta)[c < C ? c : c - C] = (float)v;
+// All of a row's arrays, as piece_elems wants them.
+uintptr_t starts(const LnArgs& a, int e) {
+  return (uintptr_t)a.x | (uintptr_t)a.res | (uintptr_t)a.dy | (uintptr_t)a.out | (uintptr_t)((a.ld_x | a.ld_res | a.ld_dy | a.ld_out) * e);
 }
 
-// The widest pieces of 16, 8, 4 or 2 bytes on which every row of every array starts and of which C is a whole number; then the fewest lanes
-// a row that hold it.  0: none do.
-int piece_elems(const LnArgs& a, int32_t dtype) {
-  const int e = dtype == DSVT_BF16 ? 2 : 4;
-  uintptr_t all = (uintptr_t)a.x | (uintptr_t)a.res | (uintptr_t)a.dy | (uintptr_t)a.out;
-  all |= (uintptr_t)((a.ld_x | a.ld_res | a.ld_dy | a.ld_out) * e);
-  for (int bytes = 16; bytes > e; bytes /= 2)
-    if (a.C % (bytes / e) == 0 && (all & (uintptr_t)(bytes - 1)) == 0) return bytes / e;
-  return 1;
-}
-int row_lanes(int32_t pieces, int bytes) {
-  for (int l = 8; l <= 64; l *= 2)
-    if (pieces <= l * kVectors) return l;
-  return bytes == 16 ? (pieces <= kThreads * kVectors ? kThreads : 0) : (pieces <= 64 * narrow_max(bytes) ? 64 : 0);
-}
-
-template <typename T, int V, int kLanes, int R> void launch_rows(const LnArgs& a, bool back, unsigned groups, hipStream_t st) {
-  if (back) k_ln_backward<T, V, kLanes, R><<<groups, kThreads, 0, st>>>(a);
-  else k_ln_forward<T, V, kLanes, R><<<groups, kThreads, 0, st>>>(a);
-}
-template <typename T, int V> void launch_pieces(const LnArgs& a, bool back, int lanes, unsigned groups, hipStream_t st) {
-  const int r = (int)dsvt_ceil_div(a.C / V, lanes);
-  if (lanes == 8) {
-    if (r == 1) launch_rows<T, V, 8, 1>(a, back, groups, st);
-    else if (r == 2) launch_rows<T, V, 8, 2>(a, back, groups, st);
-    else if (r == 3) launch_rows<T, V, 8, 3>(a, back, groups, st);
-    else launch_rows<T, V, 8, 4>(a, back, groups, st);
-  } else if (lanes == 16) {                       // more than 4 * 8 pieces: three or four of 16 lanes, and so on
-    if (r == 3) launch_rows<T, V, 16, 3>(a, back, groups, st);
-    else launch_rows<T, V, 16, 4>(a, back, groups, st);
-  } else if (lanes == 32) {
-    if (r == 3) launch_rows<T, V, 32, 3>(a, back, groups, st);
-    else launch_rows<T, V, 32, 4>(a, back, groups, st);
-  } else if (lanes == 64) {
-    if (r == 3) launch_rows<T, V, 64, 3>(a, back, groups, st);
-    else if (r == 4) launch_rows<T, V, 64, 4>(a, back, groups, st);
-    else if constexpr (V * sizeof(T) < 16) {
-      if (r <= 6) launch_rows<T, V, 64, 6>(a, back, groups, st);
-      else if (r <= 8) launch_rows<T, V, 64, 8>(a, back, groups, st);
-      else if constexpr (V * sizeof(T) < 8) {
-        if (r <= 12) launch_rows<T, V, 64, 12>(a, back, groups, st);
-        else launch_rows<T, V, 64, 16>(a, back, groups, st);
-      }
-    }
-  } else if constexpr (V * sizeof(T) == 16) {
-    if (r <= 2) launch_rows<T, V, kThreads, 2>(a, back, groups, st);
-    else launch_rows<T, V, kThreads, kVectors>(a, back, groups, st);
+struct Forward {
+  template <typename T, int V, int kLanes, int R> static void rows(const LnArgs& a, unsigned groups, hipStream_t st) {
+    k_ln_forward<T, V, kLanes, R><<<groups, kThreads, 0, st>>>(a);
   }
-}
+};
+struct Backward {
+  template <typename T, int V, int kLanes, int R> static void rows(const LnArgs& a, unsigned groups, hipStream_t st) {
+    k_ln_backward<T, V, kLanes, R><<<groups, kThreads, 0, st>>>(a);
+  }
+};
 template <typename T> void launch(const LnArgs& a, bool back, int v, int lanes, unsigned groups, int32_t rows, hipStream_t st) {
   if (lanes == 0) {
     if (back) k_ln_long<T, true><<<groups, kThreads, 0, st>>>(a, rows);
     else k_ln_long<T, false><<<groups, kThreads, 0, st>>>(a, rows);
-  } else if (v == 1) launch_pieces<T, 1>(a, back, lanes, groups, st);
-  else if (v == 2) launch_pieces<T, 2>(a, back, lanes, groups, st);
-  else if (v * sizeof(T) == 8) launch_pieces<T, 8 / (int)sizeof(T)>(a, back, lanes, groups, st);
-  else launch_pieces<T, 16 / (int)sizeof(T)>(a, back, lanes, groups, st);
+  } else if (back) launch_rows<Backward, T>(a, v, lanes, groups, st);
+  else launch_rows<Forward, T>(a, v, lanes, groups, st);
 }
 
 int check(const dsvt_ln_cfg* cfg, int32_t n_rows) {
@@ -363,8 +235,6 @@ int check(const dsvt_ln_cfg* cfg, int32_t n_rows) {
 }
 // Workgroups of a backward pass, and so rows of partial sums: bounded by the rows alone, so that the workspace goes by n_rows and C only.
 int32_t backward_groups(int32_t n_rows) { return n_rows < kBackwardGroups ? n_rows : kBackwardGroups; }
-
-bool bad_rows(const void* p, int64_t ld, int32_t C, int e) { return !p || ((uintptr_t)p % (uintptr_t)e) != 0 || ld < C; }
 
 }  // namespace
 
@@ -378,7 +248,7 @@ extern "C" int dsvt_layer_norm(const dsvt_ln_cfg* cfg, const void* x, int64_t ld
   LnArgs a = {};
   a.x = x; a.res = res; a.out = y; a.gamma = cfg->gamma; a.beta = cfg->beta;
   a.ld_x = ld_x; a.ld_res = res ? ld_res : 0; a.ld_out = ld_y; a.n = n_rows; a.C = cfg->C; a.eps = cfg->eps;
-  const int v = piece_elems(a, cfg->dtype), lanes = row_lanes(cfg->C / v, v * e);
+  const int v = piece_elems(starts(a, e), a.C, e), lanes = row_lanes(cfg->C / v, v * e);
   const int64_t per = lanes ? kThreads / lanes : 1, all = dsvt_ceil_div(n_rows, per);
   const unsigned groups = (unsigned)(all < kForwardGroups ? all : kForwardGroups);
   const int32_t rows = (int32_t)dsvt_ceil_div(n_rows, groups);
@@ -417,7 +287,7 @@ extern "C" int dsvt_layer_norm_backward(const dsvt_ln_cfg* cfg, const void* dy, 
     a.x = x; a.res = res; a.dy = dy; a.out = dx; a.gamma = cfg->gamma;
     a.ld_x = ld_x; a.ld_res = res ? ld_res : 0; a.ld_dy = ld_dy; a.ld_out = ld_dx; a.n = n_rows; a.C = cfg->C; a.eps = cfg->eps;
     a.partial = static_cast<float*>(ws);
-    const int v = piece_elems(a, cfg->dtype), lanes = row_lanes(cfg->C / v, v * e);
+    const int v = piece_elems(starts(a, e), a.C, e), lanes = row_lanes(cfg->C / v, v * e);
     const int64_t per = lanes ? kThreads / lanes : 1, all = dsvt_ceil_div(n_rows, per);
     groups = (int32_t)(all < kBackwardGroups ? all : kBackwardGroups);
     const int32_t rows = (int32_t)dsvt_ceil_div(n_rows, groups);
@@ -429,7 +299,8 @@ extern "C" int dsvt_layer_norm_backward(const dsvt_ln_cfg* cfg, const void* dy, 
   }
   if (groups != 1) {
     dsvt_prof_scope ps(DSVT_K_LN_SUM, st);
-    k_ln_sum<<<(unsigned)dsvt_ceil_div(2 * (int64_t)cfg->C, 32), 1024, 0, st>>>(static_cast<const float*>(ws), groups, cfg->C, d_gamma, d_beta);
+    k_sum_parts<<<(unsigned)dsvt_ceil_div(2 * (int64_t)cfg->C, 32), 1024, 0, st>>>(static_cast<const float*>(ws), groups, 2 * cfg->C, cfg->C, d_gamma,
+                                                                                   d_beta);
   }
   DSVT_HIP_TRY(hipGetLastError());
   return DSVT_OK;
