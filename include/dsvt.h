@@ -408,6 +408,70 @@ int dsvt_layer_norm_backward(const dsvt_ln_cfg* cfg, const void* dy, int64_t ld_
                              void* ws, size_t ws_bytes, void* stream);
 
 /* ---------------------------------------------------------------------------------------
+ * Rows in 8 bits: a layer's projections served in 8 bits, and its activations kept in 8 bits for the backward pass.  One format for
+ * both, and for weights (a row is then an output's): C codes from -127 to 127 and a scale; code * scale is the value.  With m the largest size in the
+ * row, in 32 bits and every operation rounded once: scale = m / 127 (or the float below it, should 127 times it pass 32 bits), code = v * (127 / m)
+ * rounded to the nearest whole number, ties to the even one.  m < 2^-118: scale and codes 0.  An infinity or a NaN in the row: scale NaN, codes 0; what is made of such a row is NaN.
+ * Arrays that a call writes must not overlap others of it, except where a call says so.  C and out <= DSVT_LN_MAX_C (DSVT_EUNSUPPORTED
+ * otherwise); n_rows may be 0.  Rows of the type have strides in elements, as in the training calls.
+ * ------------------------------------------------------------------------------------ */
+typedef struct {
+  int8_t* codes;  /* [device] rows of ld bytes, ld >= C; 16-byte aligned, ld a multiple of 16.  Bytes past a row's C-th are not written, and may
+                     be read (ld bytes of every row are the array's) but do not count                          */
+  int64_t ld;
+  float* scale;   /* [device] [n_rows]                                                                          */
+} dsvt_rows8;
+
+/* kept [n_rows, C] in 8 bits of x [device] [n_rows, C]; and back, rounded to the type. */
+int dsvt_keep_rows8(int32_t C, int32_t dtype, const void* x, int64_t ld_x, int32_t n_rows, const dsvt_rows8* kept, void* stream);
+int dsvt_read_rows8(int32_t C, int32_t dtype, const dsvt_rows8* rows, int32_t n_rows, void* x, int64_t ld_x, void* stream);
+
+/* Root-mean-square norm of a residual sum: z = x + res, y = z / sqrt(mean z^2 + eps) * gamma, row by row. */
+typedef struct {
+  int32_t C, dtype;           /* dtype of x, res, z, y and their gradients                                  */
+  const float* gamma;         /* [C] [device]                                                               */
+  float eps;
+} dsvt_rms_cfg;
+
+/* x, res, z, y [device] [n_rows, C]; res may be NULL (z = x), z and one of y and rows8 too: NULL is not wanted.  y and rows8 are of the sum in
+ * 32 bits, not of the z that is rounded to the type.  z and y may each be x or res themselves (same stride). */
+int dsvt_rms_norm(const dsvt_rms_cfg* cfg, const void* x, int64_t ld_x, const void* res, int64_t ld_res, int32_t n_rows, void* z, int64_t ld_z,
+                  void* y, int64_t ld_y, const dsvt_rows8* rows8, void* stream);
+
+/* The gradients, from dy, that of y, and d_sum, that of z (NULL: there is none): dx [device] [n_rows, C] = that of x and of res alike (dx may
+ * be dy or d_sum themselves, same stride); d_gamma [device] [C] float, written, not added to, summed up as by dsvt_layer_norm_backward.
+ * ws [device] 16-byte aligned, of the bytes that dsvt_rms_norm_backward_workspace_size reports; no state is kept in it, calls that may run at
+ * the same time need one each. */
+int dsvt_rms_norm_backward_workspace_size(const dsvt_rms_cfg* cfg, int32_t n_rows, size_t* bytes);
+int dsvt_rms_norm_backward(const dsvt_rms_cfg* cfg, const void* dy, int64_t ld_dy, const void* x, int64_t ld_x, const void* res, int64_t ld_res,
+                           const void* d_sum, int64_t ld_dsum, int32_t n_rows, void* dx, int64_t ld_dx, float* d_gamma, void* ws, size_t ws_bytes,
+                           void* stream);
+
+/* The MLP's activation, GELU(h) = h Phi(h), of h [device] [n_rows, C], in 8 bits, and h itself in 8 bits (either may be NULL); and its gradient, dh =
+ * dy (Phi(k) + k phi(k)) with k = code * scale of the kept rows (dh may be dy itself, same stride).  Phi is off by at most 2e-7. */
+int dsvt_gelu_rows8(int32_t C, int32_t dtype, const void* h, int64_t ld_h, int32_t n_rows, const dsvt_rows8* out, const dsvt_rows8* kept, void* stream);
+int dsvt_gelu_rows8_backward(int32_t C, int32_t dtype, const dsvt_rows8* kept, const void* dy, int64_t ld_dy, int32_t n_rows, void* dh,
+                             int64_t ld_dh, void* stream);
+
+/* A linear layer on rows and weights in 8 bits: y[n][o] = act(s_n t_o (sum over c of x[n][c] w[o][c]) + bias[o]), x and w the codes, s and t
+ * their scales.  The sum over c is exact. */
+enum { DSVT_ACT_NONE = 0, DSVT_ACT_GELU = 1 };
+typedef struct {
+  int32_t C, out, dtype, act; /* dtype of y                                                                  */
+  dsvt_rows8 w;               /* [out, C]                                                                    */
+  const float* bias;          /* [out] [device] or NULL                                                      */
+} dsvt_linear8_cfg;
+int dsvt_linear_rows8(const dsvt_linear8_cfg* cfg, const dsvt_rows8* x, int32_t n_rows, void* y, int64_t ld_y, void* stream);
+
+/* The gradients of a linear layer's weights and bias, from dy [device] [n_rows, out] and the layer's input as it was kept: d_w [device] [out, C] of
+ * dtype (dy's) = sum over n of dy[n][o] s_n x[n][c], d_b [device] [out] float = sum of dy (NULL: not wanted); both written, not added to.
+ * All sums are of 32 bits or more and do not depend on the order in which the kernels run.
+ * ws [device] as for dsvt_rms_norm_backward. */
+int dsvt_linear_rows8_weight_grad_workspace_size(int32_t C, int32_t out, int32_t dtype, int32_t n_rows, size_t* bytes);
+int dsvt_linear_rows8_weight_grad(int32_t C, int32_t out, int32_t dtype, const dsvt_rows8* x, const void* dy, int64_t ld_dy, int32_t n_rows,
+                                  void* d_w, int64_t ld_dw, float* d_b, void* ws, size_t ws_bytes, void* stream);
+
+/* ---------------------------------------------------------------------------------------
  * Instrumentation for benchmarks (not part of the method): per-kernel time from hipEvent pairs
  * recorded around every launch while enabled (launches of one kernel that follow one another on a
  * stream share a pair: begin before the first, end after the last).  Host-only; not thread-safe.

@@ -75,6 +75,18 @@ class LnCfg(C.Structure):
     _fields_ = [("C", C.c_int32), ("dtype", C.c_int32), ("gamma", C.c_void_p), ("beta", C.c_void_p), ("eps", C.c_float)]
 
 
+class Rows8S(C.Structure):
+    _fields_ = [("codes", C.c_void_p), ("ld", C.c_int64), ("scale", C.c_void_p)]
+
+
+class RmsCfg(C.Structure):
+    _fields_ = [("C", C.c_int32), ("dtype", C.c_int32), ("gamma", C.c_void_p), ("eps", C.c_float)]
+
+
+class Linear8Cfg(C.Structure):
+    _fields_ = [("C", C.c_int32), ("out", C.c_int32), ("dtype", C.c_int32), ("act", C.c_int32), ("w", Rows8S), ("bias", C.c_void_p)]
+
+
 _lib = None
 
 
@@ -115,6 +127,17 @@ def lib():
         L.dsvt_layer_norm.argtypes = [C.POINTER(LnCfg), vp, i64, vp, i64, i32, vp, i64, vp]
         L.dsvt_layer_norm_backward_workspace_size.argtypes = [C.POINTER(LnCfg), i32, C.POINTER(sz)]
         L.dsvt_layer_norm_backward.argtypes = [C.POINTER(LnCfg), vp, i64, vp, i64, vp, i64, i32, vp, i64, vp, vp, vp, sz, vp]
+        r8 = C.POINTER(Rows8S)
+        L.dsvt_keep_rows8.argtypes = [i32, i32, vp, i64, i32, r8, vp]
+        L.dsvt_read_rows8.argtypes = [i32, i32, r8, i32, vp, i64, vp]
+        L.dsvt_rms_norm.argtypes = [C.POINTER(RmsCfg), vp, i64, vp, i64, i32, vp, i64, vp, i64, r8, vp]
+        L.dsvt_rms_norm_backward_workspace_size.argtypes = [C.POINTER(RmsCfg), i32, C.POINTER(sz)]
+        L.dsvt_rms_norm_backward.argtypes = [C.POINTER(RmsCfg), vp, i64, vp, i64, vp, i64, vp, i64, i32, vp, i64, vp, vp, sz, vp]
+        L.dsvt_gelu_rows8.argtypes = [i32, i32, vp, i64, i32, r8, r8, vp]
+        L.dsvt_gelu_rows8_backward.argtypes = [i32, i32, r8, vp, i64, i32, vp, i64, vp]
+        L.dsvt_linear_rows8.argtypes = [C.POINTER(Linear8Cfg), r8, i32, vp, i64, vp]
+        L.dsvt_linear_rows8_weight_grad_workspace_size.argtypes = [i32, i32, i32, i32, C.POINTER(sz)]
+        L.dsvt_linear_rows8_weight_grad.argtypes = [i32, i32, i32, r8, vp, i64, i32, vp, i64, vp, vp, sz, vp]
         L.dsvt_prof_enable.argtypes = [i32]
         L.dsvt_prof_collect.argtypes = [C.POINTER(C.c_float), C.POINTER(i32), i32]
         L.dsvt_prof_kernel_count.restype = i32
@@ -670,6 +693,311 @@ def dsvt_layer_norm_backward(ln, dy, x, res=None, dx=None, d_gamma=None, d_beta=
     if rc:
         _check("dsvt_layer_norm_backward", rc)
     return dx, d_gamma, d_beta
+
+
+_CODE = {torch.float32: DSVT_F32, torch.bfloat16: DSVT_BF16}
+
+
+def _type_of(t, what):
+    if t.dtype not in _CODE or t.dim() != 2:
+        raise ValueError(f"{what}: a two-dimensional tensor of float32 or bfloat16 is wanted; got {t.dtype} {tuple(t.shape)}")
+    return t.dtype
+
+
+def _new(stream, device, like, shape, dtype):
+    return like.new_empty(shape, dtype=dtype) if stream is None else _new_on(stream, device, like, shape, dtype)
+
+
+class Rows8:
+    """Rows in 8 bits (dsvt_rows8 in dsvt.h): codes int8 [n, C], whose rows begin on 16 bytes and are whole multiples of 16 bytes apart, and
+    scale float32 [n]; a row stands for its codes times its scale.  Made by the calls that write rows, or of tensors the caller has."""
+
+    __slots__ = ("codes", "scale", "n", "C", "struct", "ref", "device", "__weakref__")
+
+    def __init__(self, codes, scale):
+        self.codes, self.scale, (self.n, self.C) = codes, scale, codes.shape
+        self.device = codes.get_device()
+        self.struct = Rows8S(codes.data_ptr(), codes.stride(0) if self.n > 1 else (self.C + 15) // 16 * 16, scale.data_ptr())
+        self.ref = C.byref(self.struct)
+
+    @classmethod
+    def of(cls, codes, scale):
+        """Of an int8 tensor [n, C] whose memory holds every row to its full stride, and its scales.  Both stay the caller's: they are read at
+        every call."""
+        if codes.dtype is not torch.int8 or codes.dim() != 2 or codes.shape[1] < 1 or (codes.shape[1] > 1 and codes.stride(1) != 1):
+            raise ValueError(f"codes: an int8 tensor [n, C] with neighbouring columns is wanted; got {codes.dtype} {tuple(codes.shape)}, strides "
+                             f"{tuple(codes.stride())}")
+        n, c = codes.shape
+        ld = codes.stride(0) if n > 1 else (c + 15) // 16 * 16
+        if codes.data_ptr() % 16 or ld % 16 or ld < c:
+            raise ValueError(f"codes: rows that begin on 16 bytes and lie a multiple of 16 bytes apart are wanted; got a stride of {ld} bytes, address "
+                             f"{codes.data_ptr():#x}")
+        if codes.untyped_storage().nbytes() < codes.storage_offset() + n * ld:
+            raise ValueError(f"codes: memory of {n} rows of {ld} bytes is wanted, the last one's {ld} too")
+        _vector(scale, (n,), torch.float32, codes.get_device(), "scale")
+        return cls(codes, scale)
+
+    @classmethod
+    def empty(cls, n, channels, device="cuda"):
+        return cls(torch.empty((n, (channels + 15) // 16 * 16), dtype=torch.int8, device=device)[:, :channels],
+                   torch.empty((n,), dtype=torch.float32, device=device))
+
+    @classmethod
+    def _like(cls, stream, device, like, n, channels):
+        ld = (channels + 15) // 16 * 16
+        codes = _new(stream, device, like, (n, ld), torch.int8)
+        return cls(codes if ld == channels else codes[:, :channels], _new(stream, device, like, (n,), torch.float32))
+
+
+def _rows8(rows, n, channels, device, what):
+    if (n is not None and rows.n != n) or (channels is not None and rows.C != channels) or rows.device != device:
+        raise ValueError(f"{what}: {'' if n is None else n} rows of {'' if channels is None else channels} codes on the current device, cuda:{device}, are "
+                         f"wanted; got {rows.n} of {rows.C} on cuda:{rows.device}")
+    return rows.ref
+
+
+def dsvt_keep_rows8(x, out=None, stream=None):
+    """Rows x [N, C] in 8 bits; returns Rows8."""
+    if _recording():
+        _no_graph("dsvt_keep_rows8", x)
+    dtype, dev = _type_of(x, "x"), _current_device()
+    n, c = x.shape
+    ld = _rows(x, (n, c), dtype, dev, "x")
+    if out is None:
+        out = Rows8._like(stream, dev, x, n, c)
+    else:
+        _rows8(out, n, c, dev, "out")
+    rc = lib().dsvt_keep_rows8(c, _CODE[dtype], x.data_ptr(), ld, n, out.ref, _current_stream(dev) if stream is None else stream)
+    if rc:
+        _check("dsvt_keep_rows8", rc)
+    return out
+
+
+def dsvt_read_rows8(rows, dtype, x=None, stream=None):
+    """What Rows8 stand for, as rows [N, C] of "bf16" or "f32"."""
+    if _recording():
+        _no_graph("dsvt_read_rows8", rows.scale, x)
+    code, dtype = _DT[dtype]
+    n, c, dev = rows.n, rows.C, _current_device()
+    ref = _rows8(rows, None, None, dev, "rows")
+    if x is None:
+        x, ld = _new(stream, dev, rows.codes, (n, c), dtype), c
+    else:
+        ld = _rows(x, (n, c), dtype, dev, "x")
+    rc = lib().dsvt_read_rows8(c, code, ref, n, x.data_ptr(), ld, _current_stream(dev) if stream is None else stream)
+    if rc:
+        _check("dsvt_read_rows8", rc)
+    return x
+
+
+class RmsNorm:
+    """Parameters of one root-mean-square norm of a residual sum.  gamma: float32 [C]; it stays the caller's: it is read at every call."""
+
+    def __init__(self, gamma, dtype, eps=1e-5):
+        code, self.dtype = _DT[dtype]
+        self.C, self.gamma = gamma.shape[0], gamma
+        _vector(gamma, (self.C,), torch.float32, _current_device(), "gamma")
+        self.struct = RmsCfg(self.C, code, gamma.data_ptr(), eps)
+        self.ref, self.size, self.device = C.byref(self.struct), (None, 0), _current_device()     # size: the last shape and its workspace bytes
+
+
+def _rms_norm(call, rms, x, res, z, y, rows, want_sum, stream, dev):
+    """What dsvt_rms_norm and dsvt_rms_norm_rows8 share; returns z."""
+    n, c, dtype = x.shape[0], rms.C, rms.dtype
+    ld_x = _rows(x, (n, c), dtype, dev, "x")
+    ld_res, p_res = (0, None) if res is None else (_rows(res, (n, c), dtype, dev, "res"), res.data_ptr())
+    ld_y, p_y = (0, None) if y is None else (_rows(y, (n, c), dtype, dev, "y"), y.data_ptr())
+    if z is None and want_sum:
+        z = _new(stream, dev, x, (n, c), dtype)
+    ld_z, p_z = (0, None) if z is None else (_rows(z, (n, c), dtype, dev, "z"), z.data_ptr())
+    rc = lib().dsvt_rms_norm(rms.ref, x.data_ptr(), ld_x, p_res, ld_res, n, p_z, ld_z, p_y, ld_y, None if rows is None else rows.ref,
+                             _current_stream(dev) if stream is None else stream)
+    if rc:
+        _check(call, rc)
+    return z
+
+
+def dsvt_rms_norm(rms, x, res=None, y=None, z=None, want_sum=False, stream=None):
+    """Root-mean-square norm of x + res (of x without res), rows [N, C]; returns y, or (y, z) with the sum z as rows if it is wanted or given."""
+    if _recording():
+        _no_graph("dsvt_rms_norm", x, res, rms.gamma, y, z)
+    dev = _current_device()
+    if rms.device != dev:
+        _elsewhere(dev, rms)
+    if y is None:
+        y = _new(stream, dev, x, (x.shape[0], rms.C), rms.dtype)
+    z = _rms_norm("dsvt_rms_norm", rms, x, res, z, y, None, want_sum, stream, dev)
+    return y if z is None else (y, z)
+
+
+def dsvt_rms_norm_rows8(rms, x, res=None, out=None, z=None, want_sum=False, stream=None):
+    """The same with its output in 8 bits: returns Rows8, or (Rows8, z)."""
+    if _recording():
+        _no_graph("dsvt_rms_norm_rows8", x, res, rms.gamma, z)
+    dev = _current_device()
+    if rms.device != dev:
+        _elsewhere(dev, rms)
+    if out is None:
+        out = Rows8._like(stream, dev, x, x.shape[0], rms.C)
+    else:
+        _rows8(out, x.shape[0], rms.C, dev, "out")
+    z = _rms_norm("dsvt_rms_norm_rows8", rms, x, res, z, None, out, want_sum, stream, dev)
+    return out if z is None else (out, z)
+
+
+def dsvt_rms_norm_backward_workspace_size(rms, n_rows):
+    last, size = rms.size
+    if n_rows != last:
+        b = C.c_size_t(0)
+        _check("dsvt_rms_norm_backward_workspace_size", lib().dsvt_rms_norm_backward_workspace_size(rms.ref, n_rows, C.byref(b)))
+        size = b.value
+        rms.size = n_rows, size
+    return size
+
+
+def dsvt_rms_norm_backward(rms, dy, x, res=None, d_sum=None, dx=None, d_gamma=None, ws=None, stream=None):
+    """Gradients of dsvt_rms_norm from those of y and, if its sum was used too, of z (d_sum): returns (dx, which is that of x and of res,
+    d_gamma [C])."""
+    if _recording():
+        _no_graph("dsvt_rms_norm_backward", dy, x, res, d_sum, rms.gamma, dx, d_gamma)
+    n, c, dtype, dev = x.shape[0], rms.C, rms.dtype, _current_device()
+    if rms.device != dev:
+        _elsewhere(dev, rms)
+    ld_dy, ld_x = _rows(dy, (n, c), dtype, dev, "dy"), _rows(x, (n, c), dtype, dev, "x")
+    ld_res, p_res = (0, None) if res is None else (_rows(res, (n, c), dtype, dev, "res"), res.data_ptr())
+    ld_sum, p_sum = (0, None) if d_sum is None else (_rows(d_sum, (n, c), dtype, dev, "d_sum"), d_sum.data_ptr())
+    if dx is None:
+        dx, ld_dx = _new(stream, dev, x, (n, c), dtype), c
+    else:
+        ld_dx = _rows(dx, (n, c), dtype, dev, "dx")
+    if d_gamma is None:
+        d_gamma = _new(stream, dev, x, (c,), torch.float32)
+    else:
+        _vector(d_gamma, (c,), torch.float32, dev, "d_gamma")
+    if ws is None:
+        ws_bytes = dsvt_rms_norm_backward_workspace_size(rms, n)
+        ws = _new(stream, dev, x, ws_bytes, torch.uint8)
+        p_ws = ws.data_ptr()
+    else:
+        p_ws, ws_bytes = _scratch(ws, dev)
+    rc = lib().dsvt_rms_norm_backward(rms.ref, dy.data_ptr(), ld_dy, x.data_ptr(), ld_x, p_res, ld_res, p_sum, ld_sum, n, dx.data_ptr(), ld_dx,
+                                      d_gamma.data_ptr(), p_ws, ws_bytes, _current_stream(dev) if stream is None else stream)
+    if rc:
+        _check("dsvt_rms_norm_backward", rc)
+    return dx, d_gamma
+
+
+def dsvt_gelu_rows8(h, out=None, kept=None, want_kept=True, stream=None):
+    """GELU of rows h [N, C] in 8 bits, and h itself in 8 bits for the backward call: returns (Rows8, Rows8, or None if it is not wanted)."""
+    if _recording():
+        _no_graph("dsvt_gelu_rows8", h)
+    dtype, dev = _type_of(h, "h"), _current_device()
+    n, c = h.shape
+    ld = _rows(h, (n, c), dtype, dev, "h")
+    if out is None:
+        out = Rows8._like(stream, dev, h, n, c)
+    else:
+        _rows8(out, n, c, dev, "out")
+    if kept is not None:
+        _rows8(kept, n, c, dev, "kept")
+    elif want_kept:
+        kept = Rows8._like(stream, dev, h, n, c)
+    rc = lib().dsvt_gelu_rows8(c, _CODE[dtype], h.data_ptr(), ld, n, out.ref, None if kept is None else kept.ref,
+                               _current_stream(dev) if stream is None else stream)
+    if rc:
+        _check("dsvt_gelu_rows8", rc)
+    return out, kept
+
+
+def dsvt_gelu_rows8_backward(kept, dy, dh=None, stream=None):
+    """Gradient of GELU's input from that of its output, dy [N, C], at the kept rows."""
+    if _recording():
+        _no_graph("dsvt_gelu_rows8_backward", kept.scale, dy, dh)
+    dtype, dev = _type_of(dy, "dy"), _current_device()
+    n, c = dy.shape
+    ref, ld = _rows8(kept, n, c, dev, "kept"), _rows(dy, (n, c), dtype, dev, "dy")
+    if dh is None:
+        dh, ld_dh = _new(stream, dev, dy, (n, c), dtype), c
+    else:
+        ld_dh = _rows(dh, (n, c), dtype, dev, "dh")
+    rc = lib().dsvt_gelu_rows8_backward(c, _CODE[dtype], ref, dy.data_ptr(), ld, n, dh.data_ptr(), ld_dh,
+                                        _current_stream(dev) if stream is None else stream)
+    if rc:
+        _check("dsvt_gelu_rows8_backward", rc)
+    return dh
+
+
+class Linear8:
+    """One linear layer in 8 bits: weight Rows8 [out, C], a scale an output (dsvt_keep_rows8 of the weights makes them); bias float32 [out] or
+    None.  dtype of the output; gelu: its activation is part of the call.  All stay the caller's: they are read at every call."""
+
+    def __init__(self, weight, dtype, bias=None, gelu=False):
+        code, self.dtype = _DT[dtype]
+        self.out, self.C, self.weight, self.bias, self.device = weight.n, weight.C, weight, bias, _current_device()
+        _rows8(weight, None, None, self.device, "weight")
+        if bias is not None:
+            _vector(bias, (self.out,), torch.float32, self.device, "bias")
+        self.struct = Linear8Cfg(self.C, self.out, code, int(gelu), weight.struct, None if bias is None else bias.data_ptr())
+        self.ref = C.byref(self.struct)
+
+
+def dsvt_linear_rows8(linear, rows, y=None, stream=None):
+    """The layer on Rows8 [N, C]; returns y [N, out]."""
+    if _recording():
+        _no_graph("dsvt_linear_rows8", rows.scale, linear.weight.scale, linear.bias, y)
+    n, dev = rows.n, _current_device()
+    if linear.device != dev:
+        _elsewhere(dev, linear)
+    ref = _rows8(rows, None, linear.C, dev, "rows")
+    if y is None:
+        y, ld = _new(stream, dev, rows.codes, (n, linear.out), linear.dtype), linear.out
+    else:
+        ld = _rows(y, (n, linear.out), linear.dtype, dev, "y")
+    rc = lib().dsvt_linear_rows8(linear.ref, ref, n, y.data_ptr(), ld, _current_stream(dev) if stream is None else stream)
+    if rc:
+        _check("dsvt_linear_rows8", rc)
+    return y
+
+
+def dsvt_linear_rows8_weight_grad_workspace_size(channels, out, dtype, n_rows):
+    b = C.c_size_t(0)
+    _check("dsvt_linear_rows8_weight_grad_workspace_size",
+           lib().dsvt_linear_rows8_weight_grad_workspace_size(channels, out, _DT[dtype][0], n_rows, C.byref(b)))
+    return b.value
+
+
+def dsvt_linear_rows8_weight_grad(rows, dy, d_w=None, d_b=None, want_bias=True, ws=None, stream=None):
+    """Gradients of a linear layer's weight and bias, from that of its output, dy [N, out], and its input as Rows8 [N, C]: returns (d_w [out, C] of
+    dy's type, d_b float32 [out], or None if it is not wanted)."""
+    if _recording():
+        _no_graph("dsvt_linear_rows8_weight_grad", rows.scale, dy, d_w, d_b)
+    dtype, dev = _type_of(dy, "dy"), _current_device()
+    n, c, o = rows.n, rows.C, dy.shape[1]
+    ref, ld = _rows8(rows, None, None, dev, "rows"), _rows(dy, (n, o), dtype, dev, "dy")
+    if d_w is None:
+        d_w, ld_w = _new(stream, dev, dy, (o, c), dtype), c
+    else:
+        ld_w = _rows(d_w, (o, c), dtype, dev, "d_w")
+    if d_b is not None:
+        _vector(d_b, (o,), torch.float32, dev, "d_b")
+    elif want_bias:
+        d_b = _new(stream, dev, dy, (o,), torch.float32)
+    code = _CODE[dtype]
+    if ws is None:
+        b = C.c_size_t(0)
+        rc = lib().dsvt_linear_rows8_weight_grad_workspace_size(c, o, code, n, C.byref(b))
+        if rc:
+            _check("dsvt_linear_rows8_weight_grad", rc)
+        ws_bytes = b.value
+        ws = _new(stream, dev, dy, ws_bytes, torch.uint8)
+        p_ws = ws.data_ptr()
+    else:
+        p_ws, ws_bytes = _scratch(ws, dev)
+    rc = lib().dsvt_linear_rows8_weight_grad(c, o, code, ref, dy.data_ptr(), ld, n, d_w.data_ptr(), ld_w, None if d_b is None else d_b.data_ptr(),
+                                             p_ws, ws_bytes, _current_stream(dev) if stream is None else stream)
+    if rc:
+        _check("dsvt_linear_rows8_weight_grad", rc)
+    return d_w, d_b
 
 
 def prof_enable(max_launches):

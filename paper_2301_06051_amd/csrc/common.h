@@ -37,7 +37,8 @@ enum {
   DSVT_K_PART_MARK = 0, DSVT_K_PART_COUNT, DSVT_K_PART_SCAN, DSVT_K_PART_EMIT, DSVT_K_PART_CLEAR,
   DSVT_K_PART_TILES, DSVT_K_LAYER, DSVT_K_POOL_GROUP, DSVT_K_POOL_ATTN, DSVT_K_BEV_CLEAR, DSVT_K_BEV_SCATTER,
   DSVT_K_VFE_GROUP, DSVT_K_VFE_REDUCE, DSVT_K_MHA_FORWARD, DSVT_K_MHA_BACKWARD, DSVT_K_MHA_REL, DSVT_K_LN_FORWARD,
-  DSVT_K_LN_BACKWARD, DSVT_K_LN_SUM, DSVT_K_COUNT
+  DSVT_K_LN_BACKWARD, DSVT_K_LN_SUM, DSVT_K_RMS_FORWARD, DSVT_K_RMS_BACKWARD, DSVT_K_RMS_SUM, DSVT_K_ROWS8_WRITE,
+  DSVT_K_ROWS8_READ, DSVT_K_LINEAR8, DSVT_K_LINEAR8_GRAD, DSVT_K_LINEAR8_JOIN, DSVT_K_COUNT
 };
 struct dsvt_prof_scope {
   int id; hipStream_t s;

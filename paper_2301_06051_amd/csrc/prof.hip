@@ -17,7 +17,8 @@ bool g_extend = false;               // the launch being marked joins the previo
 const char* const kNames[DSVT_K_COUNT] = {
     "part_mark", "part_window_count", "part_scan_windows", "part_emit", "part_clear",
     "part_tiles", "layer", "pool_group", "pool_attention", "bev_clear", "bev_scatter", "vfe_group", "vfe_reduce",
-    "mha_forward", "mha_backward", "mha_rel_bias", "ln_forward", "ln_backward", "ln_sum"};
+    "mha_forward", "mha_backward", "mha_rel_bias", "ln_forward", "ln_backward", "ln_sum",
+    "rms_forward", "rms_backward", "rms_sum", "rows8_write", "rows8_read", "linear8", "linear8_grad", "linear8_join"};
 }  // namespace
 
 void dsvt_prof_mark_begin(int id, hipStream_t s) {

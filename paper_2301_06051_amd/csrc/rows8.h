@@ -1,0 +1,110 @@
+// Rows in 8 bits (dsvt_rows8): a row of C values v is C codes from -127 to 127 and a scale.  With m the largest |v| of the row, in 32 bits and
+// every operation rounded once:
+//   scale = m / 127 (or the float below it, should 127 times it pass 32 bits), code = v * (127 / m) rounded to the nearest whole number, ties to the even one; the row stands for code * scale.
+// m < 2^-118: scale and codes 0 (127 / m would pass 32 bits).  An infinity or a NaN in the row: scale NaN, codes 0, so that nothing that is made
+// of the row is finite.
+#pragma once
+#include "rows.h"
+
+namespace {
+
+constexpr float kSmallestTop = 0x1p-118f;
+constexpr float kLargestScale = 0x1.020406p+121f; // the largest whose product with 127 is a number
+
+template <int V> struct Codes { typedef uint32_t type __attribute__((ext_vector_type(V / 4))); };
+template <> struct Codes<4> { typedef uint32_t type; };
+template <> struct Codes<2> { typedef uint16_t type; };
+template <> struct Codes<1> { typedef uint8_t type; };
+
+template <int V> __device__ __forceinline__ typename Codes<V>::type pack_codes(const int (&q)[V]) {
+  const auto word = [&](int at) { return (uint32_t)(q[at] & 255) | (uint32_t)(q[at + 1] & 255) << 8 | (uint32_t)(q[at + 2] & 255) << 16 | (uint32_t)q[at + 3] << 24; };
+  typename Codes<V>::type p;
+  if constexpr (V == 1) p = (uint8_t)q[0];
+  else if constexpr (V == 2) p = (uint16_t)((q[0] & 255) | (q[1] & 255) << 8);
+  else if constexpr (V == 4) p = word(0);
+  else {
+#pragma unroll
+    for (int k = 0; k < V / 4; ++k) p[k] = word(4 * k);
+  }
+  return p;
+}
+template <int V> __device__ __forceinline__ void widen_codes(typename Codes<V>::type p, float (&f)[V]) {
+  if constexpr (V <= 4) {
+#pragma unroll
+    for (int i = 0; i < V; ++i) f[i] = (float)(int8_t)(p >> (8 * i));
+  } else {
+#pragma unroll
+    for (int i = 0; i < V; ++i) f[i] = (float)(int8_t)(p[i / 4] >> (8 * (i % 4)));
+  }
+}
+
+// Sizes as whole numbers: of infinities above those of numbers, of NaN above all.
+__device__ __forceinline__ uint32_t size_bits(float v) { return __float_as_uint(v) & 0x7fffffffu; }
+
+struct RowScale {
+  float scale, to_codes;                          // codes are v * to_codes, rounded; of a row without a scale 0
+  bool plain;                                     // the row is numbers that are not too small
+  __device__ __forceinline__ explicit RowScale(uint32_t top_bits) {
+    const float top = __uint_as_float(top_bits);
+    const bool numbers = top_bits < 0x7f800000u;
+    plain = numbers && top >= kSmallestTop;
+    scale = plain ? fminf(top / 127.f, kLargestScale) : numbers ? 0.f : __uint_as_float(0x7fc00000u);
+    to_codes = plain ? 127.f / top : 0.f;
+  }
+  // (the product is rounded, then the whole number is taken: not one fma, which could decide a tie otherwise)
+  __device__ __forceinline__ int code(float v) const { return plain ? (int)rintf(v * to_codes) : 0; }
+};
+
+// The row's pieces v in 8 bits: what its kLanes lanes hold of it goes to `codes`, its scale to *scale.
+template <int V, int kLanes, int R>
+__device__ __forceinline__ void store_codes(const float (&v)[R][V], int part, int pieces, int8_t* codes, float* scale, uint32_t* s) {
+  uint32_t top = 0;
+#pragma unroll
+  for (int r = 0; r < R; ++r)
+#pragma unroll
+    for (int i = 0; i < V; ++i) {
+      const uint32_t b = size_bits(v[r][i]);
+      top = b > top ? b : top;
+    }
+  const RowScale by(lane_join<kLanes>(top, s, [](uint32_t a, uint32_t b) { return a > b ? a : b; }));
+  if (part == 0) *scale = by.scale;
+  typedef typename Codes<V>::type P;
+  P* row = reinterpret_cast<P*>(codes);
+#pragma unroll
+  for (int r = 0; r < R; ++r) {
+    int q[V];
+#pragma unroll
+    for (int i = 0; i < V; ++i) q[i] = by.code(v[r][i]);
+    if (r * kLanes + part < pieces) row[r * kLanes + part] = pack_codes<V>(q);
+  }
+}
+
+// GELU, x Phi(x), and its slope Phi(x) + x phi(x).  Phi(-|x|) = phi-like exponential times a polynomial of 1 / (1 + p z), z = |x| / sqrt 2
+// (Abramowitz & Stegun 7.1.26, off by at most 1.5e-7 in erf and so 7.5e-8 in Phi); the slope needs the same exponential.
+struct Normal {
+  float cdf, density;
+  __device__ __forceinline__ explicit Normal(float x) {
+    const float e = __builtin_amdgcn_exp2f(x * x * -0.72134752044448170368f);             // exp(-x^2 / 2)
+    const float t = __builtin_amdgcn_rcpf(fmaf(fabsf(x), 0.3275911f * 0.70710678118654752440f, 1.f));
+    float p = fmaf(t, 0.5f * 1.061405429f, 0.5f * -1.453152027f);
+    p = fmaf(t, p, 0.5f * 1.421413741f);
+    p = fmaf(t, p, 0.5f * -0.284496736f);
+    p = fmaf(t, p, 0.5f * 0.254829592f);
+    const float below = t * p * e;                // Phi(-|x|)
+    cdf = x < 0.f ? below : 1.f - below;
+    density = e * 0.39894228040143267794f;
+  }
+};
+__device__ __forceinline__ float gelu(float x) { return x * Normal(x).cdf; }
+__device__ __forceinline__ float gelu_slope(float x) {
+  const Normal n(x);
+  return fmaf(x, n.density, n.cdf);
+}
+
+// n rows of C codes and their scales.  Rows of `ld` bytes, begin on 16.
+inline bool bad_rows8(const dsvt_rows8* r, int32_t C) {
+  return !r || !r->codes || !r->scale || ((uintptr_t)r->codes & 15u) != 0 || ((uintptr_t)r->scale & 3u) != 0 || r->ld < C || r->ld % 16 != 0;
+}
+// Pieces of 16 bf16 or fp32 values do not exist, so codes, whose rows begin on 16 bytes, never make pieces narrower.
+
+}  // namespace

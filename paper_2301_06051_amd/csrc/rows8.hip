@@ -1,0 +1,184 @@
+// Rows in 8 bits (rows8.h): dsvt_keep_rows8 writes them, dsvt_read_rows8 reads them back; dsvt_gelu_rows8 and dsvt_gelu_rows8_backward
+// are the activation of an MLP whose input is kept in 8 bits for the backward pass.
+//
+//   forward   out = codes of gelu(h), kept = codes of h          gelu(h) = h Phi(h)
+//   backward  dh = dy (Phi(k) + k phi(k)), k = code * scale
+//
+// All are bound by the bytes of their rows: writers hold a row in registers (rows.h), as its largest value is wanted before its first code.
+#include "rows8.h"
+
+namespace {
+
+struct Rows8Args {
+  const void *x, *dy;                             // rows of the type: writers' input; dy of the backward pass
+  void* y;                                        // readers' output
+  int8_t *out, *kept;                             // writers: codes of gelu(x) (or of x itself) and of x; either may be null.  Readers: kept
+  float *out_scale, *kept_scale;
+  int64_t ld_x, ld_dy, ld_y, ld_out, ld_kept;
+  int32_t n, C;
+};
+
+template <bool kGelu, typename T, int V, int kLanes, int R>
+__global__ __launch_bounds__(kThreads) void k_write_rows8(Rows8Args a) {
+  constexpr int kRows = kThreads / kLanes;
+  __shared__ uint32_t s[kThreads / 64];
+  const int part = threadIdx.x % kLanes, pieces = a.C / V;
+  for (int64_t row = (int64_t)blockIdx.x * kRows + threadIdx.x / kLanes; row < a.n; row += (int64_t)gridDim.x * kRows) {
+    RowPieces<T, V, kLanes, R> x;
+    x.load(a.x, row * a.ld_x, part, pieces, true);
+    float v[R][V];
+#pragma unroll
+    for (int r = 0; r < R; ++r) widen<T, V>(x.p[r], v[r]);
+    if (a.kept) store_codes<V, kLanes, R>(v, part, pieces, a.kept + row * a.ld_kept, a.kept_scale + row, s);
+    if constexpr (kGelu) {
+      if (!a.out) continue;
+#pragma unroll
+      for (int r = 0; r < R; ++r)
+#pragma unroll
+        for (int i = 0; i < V; ++i) v[r][i] = gelu(v[r][i]);
+      store_codes<V, kLanes, R>(v, part, pieces, a.out + row * a.ld_out, a.out_scale + row, s);
+    }
+  }
+}
+
+// Rows that registers do not hold: a workgroup a row, read twice.
+template <bool kGelu, typename T> __global__ __launch_bounds__(kThreads) void k_write_rows8_long(Rows8Args a) {
+  __shared__ uint32_t s[2][kThreads / 64];
+  for (int64_t row = blockIdx.x; row < a.n; row += gridDim.x) {
+    const T* x = static_cast<const T*>(a.x) + row * a.ld_x;
+    uint32_t top = 0, top_out = 0;
+    const auto larger = [](uint32_t p, uint32_t q) { return p > q ? p : q; };
+    for (int c = threadIdx.x; c < a.C; c += kThreads) {
+      const float v = (float)x[c];
+      top = larger(top, size_bits(v));
+      if constexpr (kGelu) top_out = larger(top_out, size_bits(gelu(v)));
+    }
+    const RowScale by(lane_join<kThreads>(top, s[0], larger)), by_out(lane_join<kThreads>(top_out, s[1], larger));
+    if (threadIdx.x == 0) {
+      if (a.kept) a.kept_scale[row] = by.scale;
+      if (kGelu && a.out) a.out_scale[row] = by_out.scale;
+    }
+    for (int c = threadIdx.x; c < a.C; c += kThreads) {
+      const float v = (float)x[c];
+      if (a.kept) a.kept[row * a.ld_kept + c] = (int8_t)by.code(v);
+      if (kGelu && a.out) a.out[row * a.ld_out + c] = (int8_t)by_out.code(gelu(v));
+    }
+  }
+}
+
+// kLanes lanes go along a row of any length.
+template <bool kGelu, typename T, int V, int kLanes> __global__ __launch_bounds__(kThreads) void k_read_rows8(Rows8Args a) {
+  constexpr int kRows = kThreads / kLanes;
+  const int part = threadIdx.x % kLanes, pieces = a.C / V;
+  typedef typename Piece<T, V>::type P;
+  typedef typename Codes<V>::type Q;
+  for (int64_t row = (int64_t)blockIdx.x * kRows + threadIdx.x / kLanes; row < a.n; row += (int64_t)gridDim.x * kRows) {
+    const Q* codes = reinterpret_cast<const Q*>(a.kept + row * a.ld_kept);
+    const float scale = a.kept_scale[row];
+    P* out = reinterpret_cast<P*>(static_cast<T*>(a.y) + row * a.ld_y);
+    const P* dy = kGelu ? reinterpret_cast<const P*>(static_cast<const T*>(a.dy) + row * a.ld_dy) : nullptr;
+    for (int p = part; p < pieces; p += kLanes) {
+      float f[V];
+      widen_codes<V>(codes[p], f);
+#pragma unroll
+      for (int i = 0; i < V; ++i) f[i] *= scale;
+      if constexpr (kGelu) {
+        float d[V];
+        widen<T, V>(dy[p], d);
+#pragma unroll
+        for (int i = 0; i < V; ++i) f[i] = d[i] * gelu_slope(f[i]);
+      }
+      out[p] = narrow<T, V>(f);
+    }
+  }
+}
+
+template <bool kGelu> struct Write {
+  template <typename T, int V, int kLanes, int R> static void rows(const Rows8Args& a, unsigned groups, hipStream_t st) {
+    k_write_rows8<kGelu, T, V, kLanes, R><<<groups, kThreads, 0, st>>>(a);
+  }
+};
+template <bool kGelu, typename T> void launch_write(const Rows8Args& a, int v, int lanes, unsigned groups, hipStream_t st) {
+  if (lanes == 0) k_write_rows8_long<kGelu, T><<<groups, kThreads, 0, st>>>(a);
+  else launch_rows<Write<kGelu>, T>(a, v, lanes, groups, st);
+}
+template <bool kGelu, typename T, int V> void launch_read(const Rows8Args& a, hipStream_t st) {
+  int lanes = 8;
+  while (lanes < 64 && lanes * 4 < a.C / V) lanes *= 2;
+  const int64_t all = dsvt_ceil_div(a.n, kThreads / lanes);
+  const unsigned groups = (unsigned)(all < 2 * kForwardGroups ? all : 2 * kForwardGroups);
+  if (lanes == 8) k_read_rows8<kGelu, T, V, 8><<<groups, kThreads, 0, st>>>(a);
+  else if (lanes == 16) k_read_rows8<kGelu, T, V, 16><<<groups, kThreads, 0, st>>>(a);
+  else if (lanes == 32) k_read_rows8<kGelu, T, V, 32><<<groups, kThreads, 0, st>>>(a);
+  else k_read_rows8<kGelu, T, V, 64><<<groups, kThreads, 0, st>>>(a);
+}
+template <bool kGelu, typename T> void launch_read(const Rows8Args& a, int v, hipStream_t st) {
+  if (v == 1) launch_read<kGelu, T, 1>(a, st);
+  else if (v == 2) launch_read<kGelu, T, 2>(a, st);
+  else if (v * sizeof(T) == 8) launch_read<kGelu, T, 8 / (int)sizeof(T)>(a, st);
+  else launch_read<kGelu, T, 16 / (int)sizeof(T)>(a, st);
+}
+
+int check(int32_t C, int32_t dtype, int32_t n_rows) {
+  if (C <= 0 || n_rows < 0 || (dtype != DSVT_F32 && dtype != DSVT_BF16)) return DSVT_EINVAL;
+  return C > DSVT_LN_MAX_C ? DSVT_EUNSUPPORTED : DSVT_OK;
+}
+
+int write(bool with_gelu, int32_t C, int32_t dtype, const void* x, int64_t ld_x, int32_t n_rows, const dsvt_rows8* out, const dsvt_rows8* kept,
+          void* stream) {
+  if (const int rc = check(C, dtype, n_rows)) return rc;
+  if (n_rows == 0) return DSVT_OK;
+  const int e = dtype == DSVT_BF16 ? 2 : 4;
+  if (bad_rows(x, ld_x, C, e) || (!out && !kept) || (out && bad_rows8(out, C)) || (kept && bad_rows8(kept, C))) return DSVT_EINVAL;
+  Rows8Args a = {};
+  a.x = x; a.ld_x = ld_x; a.n = n_rows; a.C = C;
+  if (out) { a.out = out->codes; a.out_scale = out->scale; a.ld_out = out->ld; }
+  if (kept) { a.kept = kept->codes; a.kept_scale = kept->scale; a.ld_kept = kept->ld; }
+  const int v = piece_elems((uintptr_t)x | (uintptr_t)(ld_x * e), C, e), lanes = row_lanes(C / v, v * e);
+  const int64_t all = dsvt_ceil_div(n_rows, lanes ? kThreads / lanes : 1);
+  const unsigned groups = (unsigned)(all < kForwardGroups ? all : kForwardGroups);
+  hipStream_t st = (hipStream_t)stream;
+  {
+    dsvt_prof_scope ps(DSVT_K_ROWS8_WRITE, st);
+    if (dtype == DSVT_BF16) with_gelu ? launch_write<true, bf16_t>(a, v, lanes, groups, st) : launch_write<false, bf16_t>(a, v, lanes, groups, st);
+    else with_gelu ? launch_write<true, float>(a, v, lanes, groups, st) : launch_write<false, float>(a, v, lanes, groups, st);
+  }
+  DSVT_HIP_TRY(hipGetLastError());
+  return DSVT_OK;
+}
+
+int read(bool with_gelu, int32_t C, int32_t dtype, const dsvt_rows8* kept, const void* dy, int64_t ld_dy, int32_t n_rows, void* y, int64_t ld_y,
+         void* stream) {
+  if (const int rc = check(C, dtype, n_rows)) return rc;
+  if (n_rows == 0) return DSVT_OK;
+  const int e = dtype == DSVT_BF16 ? 2 : 4;
+  if (bad_rows8(kept, C) || bad_rows(y, ld_y, C, e) || (with_gelu && bad_rows(dy, ld_dy, C, e))) return DSVT_EINVAL;
+  Rows8Args a = {};
+  a.dy = dy; a.ld_dy = ld_dy; a.y = y; a.ld_y = ld_y; a.kept = kept->codes; a.kept_scale = kept->scale; a.ld_kept = kept->ld; a.n = n_rows; a.C = C;
+  const int v = piece_elems((uintptr_t)dy | (uintptr_t)y | (uintptr_t)((ld_dy | ld_y) * e), C, e);
+  hipStream_t st = (hipStream_t)stream;
+  {
+    dsvt_prof_scope ps(DSVT_K_ROWS8_READ, st);
+    if (dtype == DSVT_BF16) with_gelu ? launch_read<true, bf16_t>(a, v, st) : launch_read<false, bf16_t>(a, v, st);
+    else with_gelu ? launch_read<true, float>(a, v, st) : launch_read<false, float>(a, v, st);
+  }
+  DSVT_HIP_TRY(hipGetLastError());
+  return DSVT_OK;
+}
+
+}  // namespace
+
+extern "C" int dsvt_keep_rows8(int32_t C, int32_t dtype, const void* x, int64_t ld_x, int32_t n_rows, const dsvt_rows8* kept, void* stream) {
+  return write(false, C, dtype, x, ld_x, n_rows, nullptr, kept, stream);
+}
+extern "C" int dsvt_gelu_rows8(int32_t C, int32_t dtype, const void* h, int64_t ld_h, int32_t n_rows, const dsvt_rows8* out,
+                               const dsvt_rows8* kept, void* stream) {
+  return write(true, C, dtype, h, ld_h, n_rows, out, kept, stream);
+}
+extern "C" int dsvt_read_rows8(int32_t C, int32_t dtype, const dsvt_rows8* rows, int32_t n_rows, void* x, int64_t ld_x, void* stream) {
+  return read(false, C, dtype, rows, nullptr, 0, n_rows, x, ld_x, stream);
+}
+extern "C" int dsvt_gelu_rows8_backward(int32_t C, int32_t dtype, const dsvt_rows8* kept, const void* dy, int64_t ld_dy, int32_t n_rows, void* dh,
+                                        int64_t ld_dh, void* stream) {
+  return read(true, C, dtype, kept, dy, ld_dy, n_rows, dh, ld_dh, stream);
+}
