@@ -97,24 +97,20 @@ template <typename T, int kRowsT, int kOutsT, int kM, int kN> __global__ __launc
     const int r = tid / kPieces + kPer * (i < PX ? i : i - PX), last = i < PX ? last_x : last_w;
     off[i] = (uint32_t)(r < last ? r : last) * (uint32_t)(i < PX ? a.ld_x : a.ld_w) + 16u * piece;
   }
+  // What is fetched does not hang on a condition, which would have to wait for it: pieces past a row's end are its last one.
   i32x4 stage[PX + PW];
+  const int last_piece = (a.C - 1) >> 4 << 4;
   const auto fetch = [&](int k0) {
-    const int left = a.C - k0 - 16 * piece;
-    if (k0 + kColumns <= a.C) {
+    const int back = k0 + 16 * piece > last_piece ? k0 + 16 * piece - last_piece : 0;
 #pragma unroll
-      for (int i = 0; i < PX + PW; ++i) stage[i] = *reinterpret_cast<const i32x4*>((i < PX ? x : w) + k0 + off[i]);
-    } else {
-#pragma unroll
-      for (int i = 0; i < PX + PW; ++i) {
-        const i32x4 zero = {};
-        stage[i] = zero;
-        if (left > 0) stage[i] = *reinterpret_cast<const i32x4*>((i < PX ? x : w) + k0 + off[i]);
-        if (i >= PX) stage[i] = first_bytes(stage[i], left);              // what lies past a row's end may be anything; zeros in one operand do
-      }
-    }
+    for (int i = 0; i < PX + PW; ++i) stage[i] = *reinterpret_cast<const i32x4*>((i < PX ? x : w) + k0 + (int64_t)off[i] - back);
   };
   i32x4* const mine = lds + tid / kPieces * kPieces;
-  const auto put = [&](int buffer) {
+  const auto put = [&](int buffer, int k0) {
+    if (k0 + kColumns > a.C) {                    // what lies past a row's end may be anything; zeros in one operand do
+#pragma unroll
+      for (int i = PX; i < PX + PW; ++i) stage[i] = first_bytes(stage[i], a.C - k0 - 16 * piece);
+    }
 #pragma unroll
     for (int i = 0; i < PX + PW; ++i) {
       const int r = tid / kPieces;                // (kPer is a multiple of 16, so the permutation is that of row r)
@@ -127,83 +123,108 @@ template <typename T, int kRowsT, int kOutsT, int kM, int kN> __global__ __launc
   const int turn = m >> 1 & 7, out_m = (m >> 2 & 1) * 16 + (m >> 3) * 4 + (m & 3), out_turn = out_m >> 1 & 7;
   const i32x4* const xs = lds + (wm * TM * 32 + m) * kPieces;
   const i32x4* const ws = lds + (kRowsT + wn * TN * 32 + out_m) * kPieces;
-  const auto multiply = [&](int buffer, int k) {
-    i32x4 p[TN], q[TM];
+  struct Frags { i32x4 p[TN], q[TM]; } now, next;
+  const auto read = [&](Frags& f, int buffer, int k) {
 #pragma unroll
-    for (int t = 0; t < TN; ++t) p[t] = ws[buffer * (kRowsT + kOutsT) * kPieces + t * 32 * kPieces + ((2 * k + h) ^ out_turn)];
+    for (int t = 0; t < TN; ++t) f.p[t] = ws[buffer * (kRowsT + kOutsT) * kPieces + t * 32 * kPieces + ((2 * k + h) ^ out_turn)];
 #pragma unroll
-    for (int t = 0; t < TM; ++t) q[t] = xs[buffer * (kRowsT + kOutsT) * kPieces + t * 32 * kPieces + ((2 * k + h) ^ turn)];
+    for (int t = 0; t < TM; ++t) f.q[t] = xs[buffer * (kRowsT + kOutsT) * kPieces + t * 32 * kPieces + ((2 * k + h) ^ turn)];
+  };
+  const auto multiply = [&](const Frags& f) {
 #pragma unroll
     for (int i = 0; i < TM; ++i)
 #pragma unroll
-      for (int j = 0; j < TN; ++j) acc[i][j] = __builtin_amdgcn_mfma_i32_32x32x32_i8(p[j], q[i], acc[i][j], 0, 0, 0);
+      for (int j = 0; j < TN; ++j) acc[i][j] = __builtin_amdgcn_mfma_i32_32x32x32_i8(f.p[j], f.q[i], acc[i][j], 0, 0, 0);
   };
 
+  // The fragments of a product are read while the one before is under way, the first ones of a buffer behind the barrier that the other
+  // wavefronts' part of it is waited for at, during the last product of the buffer before.
   fetch(0);
-  put(0);
-  if (kColumns < a.C) fetch(kColumns);
+  put(0, 0);
+  fetch(kColumns);
   lds_barrier();
+  read(now, 0, 0);
   int buffer = 0;
   int k0 = 0;
   for (; k0 + kColumns < a.C; k0 += kColumns, buffer ^= 1) {
-    multiply(buffer, 0);
-    multiply(buffer, 1);
-    put(buffer ^ 1);
-    if (k0 + 2 * kColumns < a.C) fetch(k0 + 2 * kColumns);
-    multiply(buffer, 2);
-    multiply(buffer, 3);
+    read(next, buffer, 1);
+    multiply(now);
+    put(buffer ^ 1, k0 + kColumns);
+    fetch(k0 + 2 * kColumns);
+    read(now, buffer, 2);
+    multiply(next);
+    read(next, buffer, 3);
+    multiply(now);
     lds_barrier();
+    read(now, buffer ^ 1, 0);
+    multiply(next);
   }
-  for (int k = 0; k < 4 && k0 + 32 * k < a.C; ++k) multiply(buffer, k);
+  for (int k = 0; k < 4 && k0 + 32 * k < a.C; ++k) {
+    if (k) read(now, buffer, k);
+    multiply(now);
+  }
 
-  const bool wide = ((uintptr_t)a.y & 15u) == 0 && a.ld_y * (int64_t)sizeof(T) % 16 == 0;
+  // Results go through LDS, 32 rows of a wavefront at a time, so that a row's are written side by side: as they come out of the product, a store would
+  // write 32 pieces of 64 bytes.
+  constexpr int kWide = TN * 32, V = 16 / (int)sizeof(T), PR = kWide / V;
+  static_assert(PR == 4 || PR == 8 || PR == 16, "pieces of a row are permuted within 4 or 8");
+  const auto spot = [](int row, int p) { return row * PR + (p ^ (PR == 4 ? row >> 1 & 3 : row & 7)); };
+  typedef typename Piece<T, V>::type P;
+  static_assert(kM * kN * 32 * PR <= 2 * (kRowsT + kOutsT) * kPieces, "the results of all wavefronts fit the buffers");
+  P* const out = reinterpret_cast<P*>(lds) + wave * 32 * PR;
+  const int first_out = out0 + wn * kWide, outs = a.O - first_out < kWide ? a.O - first_out : kWide;
+  const bool wide = outs % V == 0 && ((uintptr_t)a.y & 15u) == 0 && a.ld_y * (int64_t)sizeof(T) % 16 == 0;
+  float t[TN][16], bias[TN][16];
 #pragma unroll
-  for (int j = 0; j < TN; ++j) {
-    const int out = out0 + (wn * TN + j) * 32 + 16 * h;
-    if (out >= a.O) continue;
-    float t[16], b[16];
-    if (out + 16 <= a.O) {
+  for (int j = 0; j < TN; ++j)
 #pragma unroll
-      for (int e = 0; e < 16; ++e) {
-        t[e] = a.t[out + e];
-        b[e] = a.bias ? a.bias[out + e] : 0.f;
+    for (int e = 0; e < 16; ++e) {
+      const int at = j * 32 + 16 * h + e, there = first_out + (at < outs ? at : 0);
+      t[j][e] = outs > 0 ? a.t[there] : 0.f;
+      bias[j][e] = outs > 0 && a.bias ? a.bias[there] : 0.f;
+    }
+  lds_barrier();                                  // all wavefronts are done with the buffers
+  if (outs <= 0) return;
+#pragma unroll
+  for (int i = 0; i < TM; ++i) {
+    const int64_t from = row0 + (wm * TM + i) * 32;
+    const int rows = (int)(a.n - from < 32 ? a.n - from : 32);
+    if (rows <= 0) break;
+    const float s = a.s[from + (m < rows ? m : 0)];
+#pragma unroll
+    for (int j = 0; j < TN; ++j)
+#pragma unroll
+      for (int e = 0; e < 16; e += V) {
+        float f[V];
+#pragma unroll
+        for (int k = 0; k < V; ++k) {
+          f[k] = (float)acc[i][j][e + k] * s * t[j][e + k];
+          if (a.bias) f[k] += bias[j][e + k];
+          if (a.act) f[k] = gelu(f[k]);
+        }
+        out[spot(m, (32 * j + 16 * h + e) / V)] = narrow<T, V>(f);
+      }
+    __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
+    __builtin_amdgcn_wave_barrier();
+    __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
+    T* y = static_cast<T*>(a.y) + from * a.ld_y + first_out;
+    if (wide) {
+      constexpr int kAtOnce = 64 / PR;            // rows of a store
+#pragma unroll
+      for (int r = 0; r < 32; r += kAtOnce) {
+        const int row = r + lane / PR, p = lane % PR;
+        if (row < rows && p * V < outs) *reinterpret_cast<P*>(y + row * a.ld_y + p * V) = out[spot(row, p)];
       }
     } else {
-#pragma unroll
-      for (int e = 0; e < 16; ++e) {
-        t[e] = out + e < a.O ? a.t[out + e] : 0.f;
-        b[e] = out + e < a.O && a.bias ? a.bias[out + e] : 0.f;
+      constexpr int kAtOnce = 64 / kWide;
+      for (int r = 0; r < 32; r += kAtOnce) {
+        const int row = r + lane / kWide, c = lane % kWide;
+        if (row < rows && c < outs) y[row * a.ld_y + c] = reinterpret_cast<const T*>(out + spot(row, c / V))[c % V];
       }
     }
-#pragma unroll
-    for (int i = 0; i < TM; ++i) {
-      const int64_t row = row0 + (wm * TM + i) * 32 + m;
-      if (row >= a.n) continue;
-      const float s = a.s[row];
-      T* y = static_cast<T*>(a.y) + row * a.ld_y + out;
-      float v[16];
-#pragma unroll
-      for (int e = 0; e < 16; ++e) {
-        v[e] = (float)acc[i][j][e] * s * t[e];
-        if (a.bias) v[e] += b[e];
-        if (a.act) v[e] = gelu(v[e]);
-      }
-      if (wide && out + 16 <= a.O) {
-        constexpr int V = 16 / sizeof(T);
-        typedef typename Piece<T, V>::type P;
-#pragma unroll
-        for (int e = 0; e < 16; e += V) {
-          float f[V];
-#pragma unroll
-          for (int k = 0; k < V; ++k) f[k] = v[e + k];
-          reinterpret_cast<P*>(y)[e / V] = narrow<T, V>(f);
-        }
-      } else {
-#pragma unroll
-        for (int e = 0; e < 16; ++e)
-          if (out + e < a.O) y[e] = (T)v[e];
-      }
-    }
+    __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
+    __builtin_amdgcn_wave_barrier();
+    __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
   }
 }
 

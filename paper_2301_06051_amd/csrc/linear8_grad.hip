@@ -7,6 +7,7 @@
 // LDS, the kept ones as s_n x[n][c]; in bf16 that is rounded to bf16, as an operand of the product (products of 32-bit operands run at a sixteenth of
 // the rate; the result, itself rounded, is off by 2.3e-3 of its norm instead of 1.7e-3).
 #include "rows8.h"
+#include <cstdlib>
 
 namespace {
 
@@ -54,7 +55,7 @@ template <> struct Columns<float> {
 };
 
 // kO outputs and kC columns, shared by kWO x kWC wavefronts; kN rows at a time.
-template <typename T, int kO, int kC, int kWO, int kWC, int kN> struct Tile {
+template <typename T, int kO, int kC, int kWO, int kWC, int kN, int kAhead> struct Tile {
   static constexpr int kAll = 64 * kWO * kWC, TO = kO / kWO / 32, TC = kC / kWC / 32, V = 16 / (int)sizeof(T);
   static constexpr int kPitchO = kO * (int)sizeof(T) + Columns<T>::kPad, kPitchC = kC * (int)sizeof(T) + Columns<T>::kPad;
   static constexpr int kBuffer = kN * (kPitchO + kPitchC);
@@ -66,8 +67,8 @@ template <typename T, int kO, int kC, int kWO, int kWC, int kN> struct Tile {
 
 extern __shared__ __attribute__((aligned(16))) char grad_lds[];
 
-template <typename T, int kO, int kC, int kWO, int kWC, int kN> __global__ __launch_bounds__(64 * kWO * kWC) void k_linear8_grad(Grad8Args a) {
-  typedef Tile<T, kO, kC, kWO, kWC, kN> S;
+template <typename T, int kO, int kC, int kWO, int kWC, int kN, int kAhead> __global__ __launch_bounds__(64 * kWO * kWC) void k_linear8_grad(Grad8Args a) {
+  typedef Tile<T, kO, kC, kWO, kWC, kN, kAhead> S;
   typedef Columns<T> F;
   constexpr int V = S::V, TO = S::TO, TC = S::TC, PO = S::PO, PC = S::PC;
   typedef typename Piece<T, V>::type P;
@@ -80,61 +81,78 @@ template <typename T, int kO, int kC, int kWO, int kWC, int kN> __global__ __lau
   const int64_t first = (int64_t)slice * a.slice, last = first + a.slice < a.n ? first + a.slice : a.n;
   const bool sums = a.d_b && c0 == 0;
 
+  // Threads past the last output or column fetch the first ones of the tile.  A step whose rows would pass the slice's last takes the last kN ones,
+  // of which those of the step before count as zeros: what is fetched, and from where, hangs on no condition, which would have to wait for it.
   const int piece_o = tid % (kO / V), row_o = tid / (kO / V), piece_c = tid % (kC / 8), row_c = tid / (kC / 8);
-  const int o = o0 + V * piece_o, c = c0 + 8 * piece_c;
-  const bool aligned = ((uintptr_t)a.dy & 15u) == 0 && a.ld_dy * (int64_t)sizeof(T) % 16 == 0;
-  P dy[PO];
-  uint2 x[PC];
-  float s[PC];
-  const auto fetch = [&](int64_t n0) {
+  const int o = V * piece_o < a.O - o0 ? V * piece_o : 0, c = 8 * piece_c < a.C - c0 ? 8 * piece_c : 0;
+  const bool cut = a.O % V != 0 && o0 + kO > a.O;             // a piece of this tile's outputs does not end within them
+  const int rows = (int)(last - first < kN ? last - first : kN);
+  const int64_t last_step = last - rows;
+  uint32_t off_o[PO], off_c[PC], off_s[PC];
 #pragma unroll
-    for (int i = 0; i < PO; ++i) {
-      const int64_t row = n0 + row_o + i * S::kRowsO;
-      const P zero = {};
-      dy[i] = zero;
-      if (row >= last) continue;
-      const T* p = static_cast<const T*>(a.dy) + row * a.ld_dy + o;
-      if (aligned && o + V <= a.O) dy[i] = *reinterpret_cast<const P*>(p);
-      else {
+  for (int i = 0; i < PO; ++i) {
+    const int r = row_o + i * S::kRowsO;
+    off_o[i] = (uint32_t)(r < rows ? r : rows - 1) * (uint32_t)a.ld_dy + o;
+  }
 #pragma unroll
-        for (int e = 0; e < V; ++e) if (o + e < a.O) dy[i][e] = p[e];
-      }
-    }
+  for (int i = 0; i < PC; ++i) {
+    const int r = row_c + i * S::kRowsC;
+    off_s[i] = r < rows ? r : rows - 1;
+    off_c[i] = off_s[i] * (uint32_t)a.ld_x + c;
+  }
+  struct Stage {                                  // what this thread has fetched of the rows of one step
+    P dy[PO];
+    uint2 x[PC];
+    float s[PC];
+  } stages[kAhead];
+  const auto fetch = [&](Stage& g, int64_t n0) {
+    const int64_t from = n0 < last_step ? n0 : last_step;
+    const int8_t* x = a.x + from * a.ld_x + c0;
+    const float* s = a.s + from;
+    const T* dy = static_cast<const T*>(a.dy) + from * a.ld_dy + o0;
 #pragma unroll
     for (int i = 0; i < PC; ++i) {
-      const int64_t row = n0 + row_c + i * S::kRowsC;
-      x[i] = make_uint2(0, 0);
-      s[i] = 0.f;
-      if (row >= last || c >= a.C) continue;
-      x[i] = *reinterpret_cast<const uint2*>(a.x + row * a.ld_x + c);
-      s[i] = a.s[row];
+      g.x[i] = *reinterpret_cast<const uint2*>(x + off_c[i]);
+      g.s[i] = s[off_s[i]];
+    }
+#pragma unroll
+    for (int i = 0; i < PO; ++i) {
+      const T* p = dy + off_o[i];
+      if (cut) {
+#pragma unroll
+        for (int e = 0; e < V; ++e) g.dy[i][e] = p[o0 + o + e < a.O ? e : 0];
+      } else __builtin_memcpy(&g.dy[i], p, 16);   // (on any element)
     }
   };
   float db[V] = {};
-  const auto put = [&](int buffer) {
+  const auto put = [&](const Stage& g, int64_t n0, int buffer) {
     char* to = grad_lds + buffer * S::kBuffer;
-#pragma unroll
-    for (int i = 0; i < PO; ++i) {
-      *reinterpret_cast<P*>(to + (row_o + i * S::kRowsO) * S::kPitchO + 16 * piece_o) = dy[i];
-      if (sums) {
-        float f[V];
-        widen<T, V>(dy[i], f);
-#pragma unroll
-        for (int e = 0; e < V; ++e) db[e] += f[e];
-      }
-    }
-    to += kN * S::kPitchO;
+    const int before = n0 > last_step ? (int)(n0 - last_step < kN ? n0 - last_step : kN) : 0;     // rows of the step before
 #pragma unroll
     for (int i = 0; i < PC; ++i) {
       typename Codes<8>::type codes;
-      codes[0] = x[i].x;
-      codes[1] = x[i].y;
+      codes[0] = g.x[i].x;
+      codes[1] = g.x[i].y;
       float f[8];
       widen_codes<8>(codes, f);
+      const int r = row_c + i * S::kRowsC;
+      const float s = r >= before && r < rows ? g.s[i] : 0.f;
 #pragma unroll
-      for (int e = 0; e < 8; ++e) f[e] *= s[i];
+      for (int e = 0; e < 8; ++e) f[e] *= s;
       typedef typename Piece<T, 8>::type P8;
-      *reinterpret_cast<P8*>(to + (row_c + i * S::kRowsC) * S::kPitchC + 8 * (int)sizeof(T) * piece_c) = narrow<T, 8>(f);
+      *reinterpret_cast<P8*>(to + kN * S::kPitchO + r * S::kPitchC + 8 * (int)sizeof(T) * piece_c) = narrow<T, 8>(f);
+    }
+#pragma unroll
+    for (int i = 0; i < PO; ++i) {
+      const int r = row_o + i * S::kRowsO;
+      const P zero = {}, p = r >= before && r < rows ? g.dy[i] : zero;
+      *reinterpret_cast<P*>(to + r * S::kPitchO + 16 * piece_o) = p;
+      if (sums) {
+        float f[V];
+        widen<T, V>(p, f);
+#pragma unroll
+        for (int e = 0; e < V; ++e) db[e] += f[e];
+      }
     }
   };
 
@@ -154,21 +172,24 @@ template <typename T, int kO, int kC, int kWO, int kWC, int kN> __global__ __lau
   };
 
   constexpr int kSteps = kN / F::kStep;
-  fetch(first);
-  put(0);
-  if (first + kN < last) fetch(first + kN);
+#pragma unroll
+  for (int k = 0; k < kAhead; ++k) fetch(stages[k], first + k * kN);
+  put(stages[0], first, 0);
+  fetch(stages[0], first + kAhead * kN);
   lds_barrier();
   int buffer = 0;
-  for (int64_t n0 = first; n0 < last; n0 += kN, buffer ^= 1) {
+  for (int64_t n0 = first; n0 < last; n0 += kAhead * kN) {
 #pragma unroll
-    for (int k = 0; k < kSteps / 2; ++k) multiply(buffer, k);
-    if (n0 + kN < last) {
-      put(buffer ^ 1);
-      if (n0 + 2 * kN < last) fetch(n0 + 2 * kN);
+    for (int d = 0; d < kAhead; ++d) {            // the rows from n0 + d kN on; those of the next kAhead steps are on their way
+#pragma unroll
+      for (int k = 0; k < kSteps / 2; ++k) multiply(buffer, k);
+      put(stages[(d + 1) % kAhead], n0 + (d + 1) * kN, buffer ^ 1);
+      fetch(stages[(d + 1) % kAhead], n0 + (d + 1 + kAhead) * kN);
+#pragma unroll
+      for (int k = kSteps / 2; k < kSteps; ++k) multiply(buffer, k);
+      lds_barrier();
+      buffer ^= 1;
     }
-#pragma unroll
-    for (int k = kSteps / 2; k < kSteps; ++k) multiply(buffer, k);
-    lds_barrier();
   }
 
 #pragma unroll
@@ -250,6 +271,7 @@ Plan make_plan(int32_t C, int32_t O, int32_t dtype, int32_t n) {
   } else {
     slices = dsvt_ceil_div(512, tiles(64));
   }
+  if (getenv("G8_FORM")) { p.form = atoi(getenv("G8_FORM")); const int fo[] = {64, 128, 256, 192, 192, 192, 64, 64, 96}, fc[] = {64, 128, 256, 192, 64, 96, 192, 64, 192}; slices = atoi(getenv("G8_WGS")) / (dsvt_ceil_div(O, fo[p.form]) * dsvt_ceil_div(C, fc[p.form])); if (slices < 1) slices = 1; }
   const int64_t most = dsvt_ceil_div(steps, 4);
   slices = slices < most ? slices : most;
   const int64_t per = dsvt_ceil_div(steps, slices);
@@ -258,10 +280,10 @@ Plan make_plan(int32_t C, int32_t O, int32_t dtype, int32_t n) {
   return p;
 }
 
-template <typename T, int kO, int kC, int kWO, int kWC, int kN> int launch_tile(const Grad8Args& a, hipStream_t st) {
-  typedef Tile<T, kO, kC, kWO, kWC, kN> S;
+template <typename T, int kO, int kC, int kWO, int kWC, int kN, int kAhead> int launch_tile(const Grad8Args& a, hipStream_t st) {
+  typedef Tile<T, kO, kC, kWO, kWC, kN, kAhead> S;
   static std::atomic<uint64_t> allowed;
-  const auto kernel = k_linear8_grad<T, kO, kC, kWO, kWC, kN>;
+  const auto kernel = k_linear8_grad<T, kO, kC, kWO, kWC, kN, kAhead>;
   if (const int rc = dsvt_allow_lds(reinterpret_cast<const void*>(kernel), S::lds(), allowed)) return rc;
   const int64_t all = dsvt_ceil_div(a.O, kO) * dsvt_ceil_div(a.C, kC) * a.slices;
   dsvt_prof_scope ps(DSVT_K_LINEAR8_GRAD, st);
@@ -272,9 +294,14 @@ template <typename T> int launch(const Grad8Args& a, int form, hipStream_t st) {
   if (a.slices > 0) {
     int rc;
     if constexpr (sizeof(T) == 2) {
-      rc = form == 2 ? launch_tile<T, 256, 256, 2, 4, 64>(a, st) : form == 1 ? launch_tile<T, 128, 128, 2, 2, 64>(a, st) : launch_tile<T, 64, 64, 2, 2, 64>(a, st);
+      const int dd = getenv("G8_D") ? atoi(getenv("G8_D")) : 1;
+      if (form == 2) rc = dd == 1 ? launch_tile<T, 256, 256, 2, 4, 64, 1>(a, st) : dd == 4 ? launch_tile<T, 256, 256, 2, 4, 32, 2>(a, st) : dd == 3 ? launch_tile<T, 256, 256, 2, 4, 32, 3>(a, st) : launch_tile<T, 256, 256, 2, 4, 32, 1>(a, st);
+      else if (form == 0) rc = dd == 1 ? launch_tile<T, 64, 64, 2, 2, 64, 1>(a, st) : dd == 2 ? launch_tile<T, 64, 64, 2, 2, 64, 2>(a, st) : dd == 3 ? launch_tile<T, 64, 64, 2, 2, 64, 3>(a, st) : launch_tile<T, 64, 64, 2, 2, 64, 4>(a, st);
+      else if (form == 3) rc = dd == 1 ? launch_tile<T, 192, 192, 3, 2, 32, 1>(a, st) : dd == 2 ? launch_tile<T, 192, 192, 3, 2, 32, 2>(a, st) : launch_tile<T, 192, 192, 3, 2, 32, 3>(a, st);
+      else if (form == 4) rc = dd == 1 ? launch_tile<T, 192, 64, 3, 2, 48, 1>(a, st) : dd == 2 ? launch_tile<T, 192, 64, 3, 2, 48, 2>(a, st) : launch_tile<T, 192, 64, 3, 2, 48, 3>(a, st);
+      else rc = dd == 1 ? launch_tile<T, 128, 128, 2, 2, 64, 1>(a, st) : dd == 2 ? launch_tile<T, 128, 128, 2, 2, 64, 2>(a, st) : launch_tile<T, 128, 128, 2, 2, 32, 3>(a, st);
     } else {
-      rc = form == 1 ? launch_tile<T, 128, 128, 2, 2, 32>(a, st) : launch_tile<T, 64, 64, 2, 2, 32>(a, st);
+      rc = form == 1 ? launch_tile<T, 128, 128, 2, 2, 32, 1>(a, st) : launch_tile<T, 64, 64, 2, 2, 32, 1>(a, st);
     }
     if (rc) return rc;
   }
