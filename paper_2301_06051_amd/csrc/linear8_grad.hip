@@ -7,7 +7,7 @@
 // LDS, the kept ones as s_n x[n][c]; in bf16 that is rounded to bf16, as an operand of the product (products of 32-bit operands run at a sixteenth of
 // the rate; the result, itself rounded, is off by 2.3e-3 of its norm instead of 1.7e-3).
 #include "rows8.h"
-#include <cstdlib>
+#include <cmath>
 
 namespace {
 
@@ -54,6 +54,10 @@ template <> struct Columns<float> {
   }
 };
 
+// How rows of dy end: with a whole piece of 16 bytes; within one, which is then fetched so that it ends there, and shifted; or before the first one
+// does, in which case values are fetched one by one.
+enum Ends { kWhole, kShifted, kSingly };
+
 // kO outputs and kC columns, shared by kWO x kWC wavefronts; kN rows at a time.
 template <typename T, int kO, int kC, int kWO, int kWC, int kN, int kAhead> struct Tile {
   static constexpr int kAll = 64 * kWO * kWC, TO = kO / kWO / 32, TC = kC / kWC / 32, V = 16 / (int)sizeof(T);
@@ -65,9 +69,18 @@ template <typename T, int kO, int kC, int kWO, int kWC, int kN, int kAhead> stru
   static constexpr size_t lds() { return 2 * (size_t)kBuffer > (size_t)kRowsO * kO * 4 ? 2 * (size_t)kBuffer : (size_t)kRowsO * kO * 4; }
 };
 
+// 16 bytes less their first `bits` bits, zeros behind them.
+template <typename P> __device__ __forceinline__ P shifted(P p, int bits) {
+  typedef uint64_t Two __attribute__((ext_vector_type(2)));
+  Two v = __builtin_bit_cast(Two, p);
+  if (bits >= 64) v = Two{v.y >> (bits - 64), 0};
+  else if (bits > 0) v = Two{v.x >> bits | v.y << (64 - bits), v.y >> bits};
+  return __builtin_bit_cast(P, v);
+}
+
 extern __shared__ __attribute__((aligned(16))) char grad_lds[];
 
-template <typename T, int kO, int kC, int kWO, int kWC, int kN, int kAhead> __global__ __launch_bounds__(64 * kWO * kWC) void k_linear8_grad(Grad8Args a) {
+template <typename T, int kO, int kC, int kWO, int kWC, int kN, int kAhead, Ends kEnds> __global__ __launch_bounds__(64 * kWO * kWC) void k_linear8_grad(Grad8Args a) {
   typedef Tile<T, kO, kC, kWO, kWC, kN, kAhead> S;
   typedef Columns<T> F;
   constexpr int V = S::V, TO = S::TO, TC = S::TC, PO = S::PO, PC = S::PC;
@@ -84,15 +97,16 @@ template <typename T, int kO, int kC, int kWO, int kWC, int kN, int kAhead> __gl
   // Threads past the last output or column fetch the first ones of the tile.  A step whose rows would pass the slice's last takes the last kN ones,
   // of which those of the step before count as zeros: what is fetched, and from where, hangs on no condition, which would have to wait for it.
   const int piece_o = tid % (kO / V), row_o = tid / (kO / V), piece_c = tid % (kC / 8), row_c = tid / (kC / 8);
-  const int o = V * piece_o < a.O - o0 ? V * piece_o : 0, c = 8 * piece_c < a.C - c0 ? 8 * piece_c : 0;
-  const bool cut = a.O % V != 0 && o0 + kO > a.O;             // a piece of this tile's outputs does not end within them
+  // (a piece that would pass a row's end is fetched so that it ends there, and shifted when it is put into LDS)
+  const int want_o = V * piece_o < a.O - o0 ? V * piece_o : 0, most_o = a.O - o0 - V, o = kEnds != kShifted || want_o < most_o ? want_o : most_o;
+  const int shift = 8 * (int)sizeof(T) * (want_o - o), c = 8 * piece_c < a.C - c0 ? 8 * piece_c : 0;
   const int rows = (int)(last - first < kN ? last - first : kN);
   const int64_t last_step = last - rows;
   uint32_t off_o[PO], off_c[PC], off_s[PC];
 #pragma unroll
   for (int i = 0; i < PO; ++i) {
     const int r = row_o + i * S::kRowsO;
-    off_o[i] = (uint32_t)(r < rows ? r : rows - 1) * (uint32_t)a.ld_dy + o;
+    off_o[i] = (uint32_t)(r < rows ? r : rows - 1) * (uint32_t)a.ld_dy + (uint32_t)o;
   }
 #pragma unroll
   for (int i = 0; i < PC; ++i) {
@@ -117,39 +131,43 @@ template <typename T, int kO, int kC, int kWO, int kWC, int kN, int kAhead> __gl
     }
 #pragma unroll
     for (int i = 0; i < PO; ++i) {
-      const T* p = dy + off_o[i];
-      if (cut) {
+      const T* p = dy + (int32_t)off_o[i];
+      if constexpr (kEnds == kSingly) {
 #pragma unroll
-        for (int e = 0; e < V; ++e) g.dy[i][e] = p[o0 + o + e < a.O ? e : 0];
+        for (int e = 0; e < V; ++e) g.dy[i][e] = p[o + e < a.O ? e : 0];
       } else __builtin_memcpy(&g.dy[i], p, 16);   // (on any element)
     }
   };
+  // Of what was fetched, part k of kSteps goes to LDS.
+  constexpr int kSteps = kN / F::kStep;
   float db[V] = {};
-  const auto put = [&](const Stage& g, int64_t n0, int buffer) {
+  const auto put = [&](Stage& g, int64_t n0, int buffer, int k) {
     char* to = grad_lds + buffer * S::kBuffer;
     const int before = n0 > last_step ? (int)(n0 - last_step < kN ? n0 - last_step : kN) : 0;     // rows of the step before
 #pragma unroll
-    for (int i = 0; i < PC; ++i) {
-      typename Codes<8>::type codes;
-      codes[0] = g.x[i].x;
-      codes[1] = g.x[i].y;
-      float f[8];
-      widen_codes<8>(codes, f);
+    for (int i = k; i < PC; i += kSteps) {
+      // (the compiler would take the bytes apart, and wait for them, where they are fetched)
+      asm volatile("" : "+v"(g.x[i].x), "+v"(g.x[i].y), "+v"(g.s[i]));
       const int r = row_c + i * S::kRowsC;
-      const float s = r >= before && r < rows ? g.s[i] : 0.f;
-#pragma unroll
-      for (int e = 0; e < 8; ++e) f[e] *= s;
+      const typename Codes<8>::type codes = {g.x[i].x, g.x[i].y};
+      float f[8];
+      values_of<8>(codes, r >= before && r < rows ? g.s[i] : 0.f, f);
       typedef typename Piece<T, 8>::type P8;
       *reinterpret_cast<P8*>(to + kN * S::kPitchO + r * S::kPitchC + 8 * (int)sizeof(T) * piece_c) = narrow<T, 8>(f);
     }
 #pragma unroll
-    for (int i = 0; i < PO; ++i) {
+    for (int i = k; i < PO; i += kSteps) {
       const int r = row_o + i * S::kRowsO;
-      const P zero = {}, p = r >= before && r < rows ? g.dy[i] : zero;
-      *reinterpret_cast<P*>(to + r * S::kPitchO + 16 * piece_o) = p;
-      if (sums) {
+      const P zero = {};
+      g.dy[i] = r >= before && r < rows ? g.dy[i] : zero;
+      if constexpr (kEnds == kShifted) g.dy[i] = shifted<P>(g.dy[i], shift);
+      *reinterpret_cast<P*>(to + r * S::kPitchO + 16 * piece_o) = g.dy[i];
+    }
+    if (k == kSteps - 1 && sums) {
+#pragma unroll
+      for (int i = 0; i < PO; ++i) {
         float f[V];
-        widen<T, V>(p, f);
+        widen<T, V>(g.dy[i], f);
 #pragma unroll
         for (int e = 0; e < V; ++e) db[e] += f[e];
       }
@@ -157,40 +175,51 @@ template <typename T, int kO, int kC, int kWO, int kWC, int kN, int kAhead> __gl
   };
 
   f32x16 acc[TO][TC] = {};
-  const auto multiply = [&](int buffer, int step) {
-    const char* from = grad_lds + buffer * S::kBuffer + wo * TO * 32 * (int)sizeof(T) + step * F::kStep * S::kPitchO;
+  struct Frags { typename F::Frag p[TC], q[TO]; } frags[2];
+  const auto read = [&](Frags& f, int buffer, int step) {
+    const char* dys = grad_lds + buffer * S::kBuffer + wo * TO * 32 * (int)sizeof(T) + step * F::kStep * S::kPitchO;
     const char* xs = grad_lds + buffer * S::kBuffer + kN * S::kPitchO + wc * TC * 32 * (int)sizeof(T) + step * F::kStep * S::kPitchC;
-    typename F::Frag p[TC], q[TO];
 #pragma unroll
-    for (int t = 0; t < TC; ++t) p[t] = F::template load<true>(xs + t * 32 * (int)sizeof(T), S::kPitchC);
+    for (int t = 0; t < TC; ++t) f.p[t] = F::template load<true>(xs + t * 32 * (int)sizeof(T), S::kPitchC);
 #pragma unroll
-    for (int t = 0; t < TO; ++t) q[t] = F::template load<false>(from + t * 32 * (int)sizeof(T), S::kPitchO);
+    for (int t = 0; t < TO; ++t) f.q[t] = F::template load<false>(dys + t * 32 * (int)sizeof(T), S::kPitchO);
+  };
+  const auto multiply = [&](const Frags& f) {
 #pragma unroll
     for (int i = 0; i < TO; ++i)
 #pragma unroll
-      for (int j = 0; j < TC; ++j) acc[i][j] = F::mma(p[j], q[i], acc[i][j]);
+      for (int j = 0; j < TC; ++j) acc[i][j] = F::mma(f.p[j], f.q[i], acc[i][j]);
   };
 
-  constexpr int kSteps = kN / F::kStep;
+  // The fragments of a product are read while the one before is under way, and so goes what was fetched to LDS; the first fragments of a
+  // buffer are read behind the barrier that all wavefronts' parts of it are waited for at, during the last product of the buffer before.
+  static_assert(kSteps % 2 == 0, "fragments change places");
 #pragma unroll
   for (int k = 0; k < kAhead; ++k) fetch(stages[k], first + k * kN);
-  put(stages[0], first, 0);
+#pragma unroll
+  for (int k = 0; k < kSteps; ++k) put(stages[0], first, 0, k);
   fetch(stages[0], first + kAhead * kN);
   lds_barrier();
+  read(frags[0], 0, 0);
   int buffer = 0;
   for (int64_t n0 = first; n0 < last; n0 += kAhead * kN) {
 #pragma unroll
     for (int d = 0; d < kAhead; ++d) {            // the rows from n0 + d kN on; those of the next kAhead steps are on their way
+      Stage& g = stages[(d + 1) % kAhead];
 #pragma unroll
-      for (int k = 0; k < kSteps / 2; ++k) multiply(buffer, k);
-      put(stages[(d + 1) % kAhead], n0 + (d + 1) * kN, buffer ^ 1);
-      fetch(stages[(d + 1) % kAhead], n0 + (d + 1 + kAhead) * kN);
-#pragma unroll
-      for (int k = kSteps / 2; k < kSteps; ++k) multiply(buffer, k);
+      for (int k = 0; k < kSteps; ++k) {
+        if (k < kSteps - 1) read(frags[(k + 1) & 1], buffer, k + 1);
+        put(g, n0 + (d + 1) * kN, buffer ^ 1, k);
+        if (k < kSteps - 1) multiply(frags[k & 1]);
+      }
+      fetch(g, n0 + (d + 1 + kAhead) * kN);
       lds_barrier();
       buffer ^= 1;
+      read(frags[0], buffer, 0);
+      multiply(frags[1]);
     }
   }
+  lds_barrier();
 
 #pragma unroll
   for (int i = 0; i < TO; ++i) {
@@ -218,7 +247,7 @@ template <typename T, int kO, int kC, int kWO, int kWC, int kN, int kAhead> __gl
     }
   }
   if (!sums) return;
-  float* red = reinterpret_cast<float*>(grad_lds);            // (the last barrier is behind all reads)
+  float* red = reinterpret_cast<float*>(grad_lds);
 #pragma unroll
   for (int e = 0; e < V; ++e) red[row_o * kO + V * piece_o + e] = db[e];
   __syncthreads();
@@ -250,41 +279,50 @@ template <typename T> __global__ __launch_bounds__(256) void k_linear8_grad_join
   }
 }
 
-constexpr int kRowsStep = 64;                     // of every form's rows at a time a multiple
+// What tiles a call takes and how many slices.  A form's steps of 64 rows take `step` us with all its workgroups on the chip (`at_once`), and a slice
+// costs the writing and reading of its partial sums, at 3 TB/s; the form and number of slices of the smallest sum are taken.  Measured, each
+// form at its best, bf16, tiles of 64, 128, 192 and 256: 30,000 rows of 192 -> 576 26.5 us, 30, 34, 38; 800,000 512, 466, 335, 403; 16,384 of 1,024 -> 1,024 93,
+// 72, 84, 80; 65,536 of 1,024 -> 2,048 713, 433, 538, 340; fp32, tiles of 64 and 128: 30,000 of 192 -> 576 75, 106; 65,536 of 1,024 -> 2,048 2,831, 2,340.
+constexpr int kRowsStep = 64, kLongest = 16384;   // rows of fp32 that one slice adds up at most: each sum is a chain of additions
+struct Form { int tile, at_once; float step; };
+constexpr Form kForms[2][4] = {{{64, 768, 1.13f}, {128, 512, 1.75f}, {192, 256, 2.2f}, {256, 256, 2.55f}}, {{64, 768, 3.8f}, {128, 512, 9.1f}, {}, {}}};
 
 struct Plan {
-  int form;                                       // 0: tiles of 64, 1: of 128, 2: of 256
+  int form;                                       // of kForms
   int32_t slices, slice;
 };
 Plan make_plan(int32_t C, int32_t O, int32_t dtype, int32_t n) {
-  const auto tiles = [&](int t) { return dsvt_ceil_div(O, t) * dsvt_ceil_div(C, t); };
-  const int64_t steps = dsvt_ceil_div(n, kRowsStep);
   Plan p = {0, 0, kRowsStep};
   if (n <= 0) return p;
-  int64_t slices;
-  if (dtype == DSVT_BF16 && tiles(256) * steps >= 256 * 16 && tiles(256) >= 8) {
-    p.form = 2;
-    slices = dsvt_ceil_div(256, tiles(256));
-  } else if (tiles(128) >= 8 && tiles(128) * steps >= 512 * 8) {
-    p.form = 1;
-    slices = dsvt_ceil_div(512, tiles(128));
-  } else {
-    slices = dsvt_ceil_div(512, tiles(64));
+  const bool narrow = dtype == DSVT_BF16;
+  const int64_t steps = dsvt_ceil_div(n, kRowsStep), least = narrow ? 1 : dsvt_ceil_div(n, kLongest);
+  const double slice_us = (double)O * C * 8. / 3e6;
+  double best = 0.;
+  for (int f = 0; f < (narrow ? 4 : 2); ++f) {
+    const Form& form = kForms[!narrow][f];
+    const int64_t tiles = dsvt_ceil_div(O, form.tile) * dsvt_ceil_div(C, form.tile);
+    int64_t most = form.at_once / tiles, slices = (int64_t)sqrt((double)steps * form.step / slice_us);
+    most = most < steps / 4 ? most : steps / 4;    // (a slice of fewer steps is mostly its beginning and end)
+    slices = slices < most ? slices : most;
+    slices = slices > least ? slices : least;      // (one at least)
+    const int64_t per = dsvt_ceil_div(steps, slices);
+    slices = dsvt_ceil_div(steps, per);
+    const double us = (double)per * form.step * (tiles * slices > form.at_once ? (double)(tiles * slices) / form.at_once : 1.) + (slices > 1 ? slices * slice_us + 4. : 0.);
+    if (f > 0 && us >= best) continue;
+    best = us;
+    p = {f, (int32_t)slices, (int32_t)(per * kRowsStep)};
   }
-  if (getenv("G8_FORM")) { p.form = atoi(getenv("G8_FORM")); const int fo[] = {64, 128, 256, 192, 192, 192, 64, 64, 96}, fc[] = {64, 128, 256, 192, 64, 96, 192, 64, 192}; slices = atoi(getenv("G8_WGS")) / (dsvt_ceil_div(O, fo[p.form]) * dsvt_ceil_div(C, fc[p.form])); if (slices < 1) slices = 1; }
-  const int64_t most = dsvt_ceil_div(steps, 4);
-  slices = slices < most ? slices : most;
-  const int64_t per = dsvt_ceil_div(steps, slices);
-  p.slice = (int32_t)(per * kRowsStep);
-  p.slices = (int32_t)dsvt_ceil_div(steps, per);
   return p;
 }
 
 template <typename T, int kO, int kC, int kWO, int kWC, int kN, int kAhead> int launch_tile(const Grad8Args& a, hipStream_t st) {
   typedef Tile<T, kO, kC, kWO, kWC, kN, kAhead> S;
-  static std::atomic<uint64_t> allowed;
-  const auto kernel = k_linear8_grad<T, kO, kC, kWO, kWC, kN, kAhead>;
-  if (const int rc = dsvt_allow_lds(reinterpret_cast<const void*>(kernel), S::lds(), allowed)) return rc;
+  static std::atomic<uint64_t> allowed[3];
+  const Ends ends = a.O % S::V == 0 ? kWhole : a.O > S::V ? kShifted : kSingly;
+  const auto kernel = ends == kWhole     ? k_linear8_grad<T, kO, kC, kWO, kWC, kN, kAhead, kWhole>
+                      : ends == kShifted ? k_linear8_grad<T, kO, kC, kWO, kWC, kN, kAhead, kShifted>
+                                         : k_linear8_grad<T, kO, kC, kWO, kWC, kN, kAhead, kSingly>;
+  if (const int rc = dsvt_allow_lds(reinterpret_cast<const void*>(kernel), S::lds(), allowed[ends])) return rc;
   const int64_t all = dsvt_ceil_div(a.O, kO) * dsvt_ceil_div(a.C, kC) * a.slices;
   dsvt_prof_scope ps(DSVT_K_LINEAR8_GRAD, st);
   kernel<<<(unsigned)(dsvt_ceil_div(all, 8) * 8), S::kAll, S::lds(), st>>>(a);
@@ -292,14 +330,12 @@ template <typename T, int kO, int kC, int kWO, int kWC, int kN, int kAhead> int 
 }
 template <typename T> int launch(const Grad8Args& a, int form, hipStream_t st) {
   if (a.slices > 0) {
-    int rc;
+    int rc = DSVT_OK;
     if constexpr (sizeof(T) == 2) {
-      const int dd = getenv("G8_D") ? atoi(getenv("G8_D")) : 1;
-      if (form == 2) rc = dd == 1 ? launch_tile<T, 256, 256, 2, 4, 64, 1>(a, st) : dd == 4 ? launch_tile<T, 256, 256, 2, 4, 32, 2>(a, st) : dd == 3 ? launch_tile<T, 256, 256, 2, 4, 32, 3>(a, st) : launch_tile<T, 256, 256, 2, 4, 32, 1>(a, st);
-      else if (form == 0) rc = dd == 1 ? launch_tile<T, 64, 64, 2, 2, 64, 1>(a, st) : dd == 2 ? launch_tile<T, 64, 64, 2, 2, 64, 2>(a, st) : dd == 3 ? launch_tile<T, 64, 64, 2, 2, 64, 3>(a, st) : launch_tile<T, 64, 64, 2, 2, 64, 4>(a, st);
-      else if (form == 3) rc = dd == 1 ? launch_tile<T, 192, 192, 3, 2, 32, 1>(a, st) : dd == 2 ? launch_tile<T, 192, 192, 3, 2, 32, 2>(a, st) : launch_tile<T, 192, 192, 3, 2, 32, 3>(a, st);
-      else if (form == 4) rc = dd == 1 ? launch_tile<T, 192, 64, 3, 2, 48, 1>(a, st) : dd == 2 ? launch_tile<T, 192, 64, 3, 2, 48, 2>(a, st) : launch_tile<T, 192, 64, 3, 2, 48, 3>(a, st);
-      else rc = dd == 1 ? launch_tile<T, 128, 128, 2, 2, 64, 1>(a, st) : dd == 2 ? launch_tile<T, 128, 128, 2, 2, 64, 2>(a, st) : launch_tile<T, 128, 128, 2, 2, 32, 3>(a, st);
+      rc = form == 3   ? launch_tile<T, 256, 256, 2, 4, 32, 2>(a, st)
+           : form == 2 ? launch_tile<T, 192, 192, 3, 2, 32, 2>(a, st)
+           : form == 1 ? launch_tile<T, 128, 128, 2, 2, 64, 1>(a, st)
+                       : launch_tile<T, 64, 64, 2, 2, 64, 1>(a, st);
     } else {
       rc = form == 1 ? launch_tile<T, 128, 128, 2, 2, 32, 1>(a, st) : launch_tile<T, 64, 64, 2, 2, 32, 1>(a, st);
     }
@@ -334,6 +370,7 @@ extern "C" int dsvt_linear_rows8_weight_grad(int32_t C, int32_t out, int32_t dty
   const int e = dtype == DSVT_BF16 ? 2 : 4;
   if (bad_rows(d_w, ld_dw, C, e) || ((uintptr_t)d_b & 3u) != 0) return DSVT_EINVAL;
   if (n_rows > 0 && (bad_rows8(x, C) || bad_rows(dy, ld_dy, out, e))) return DSVT_EINVAL;
+  if (n_rows > 0 && (x->ld >= (1 << 24) || ld_dy >= (1 << 24))) return DSVT_EUNSUPPORTED;        // (the rows of a step are less than 2^31 apart)
   if (need > 0 && (!ws || ((uintptr_t)ws & 15u))) return DSVT_EINVAL;
   if (ws_bytes < need) return DSVT_ENOSPC;
   const Plan p = make_plan(C, out, dtype, n_rows);

@@ -28,13 +28,32 @@ template <int V> __device__ __forceinline__ typename Codes<V>::type pack_codes(c
   }
   return p;
 }
-template <int V> __device__ __forceinline__ void widen_codes(typename Codes<V>::type p, float (&f)[V]) {
+// One code of four as a float, in one instruction (the compiler takes two: it cuts the byte out first).
+template <int kByte> __device__ __forceinline__ float code_of(uint32_t four) {
+  float f;
+  if constexpr (kByte == 0) asm("v_cvt_f32_i32_sdwa %0, sext(%1) dst_sel:DWORD dst_unused:UNUSED_PAD src0_sel:BYTE_0" : "=v"(f) : "v"(four));
+  else if constexpr (kByte == 1) asm("v_cvt_f32_i32_sdwa %0, sext(%1) dst_sel:DWORD dst_unused:UNUSED_PAD src0_sel:BYTE_1" : "=v"(f) : "v"(four));
+  else if constexpr (kByte == 2) asm("v_cvt_f32_i32_sdwa %0, sext(%1) dst_sel:DWORD dst_unused:UNUSED_PAD src0_sel:BYTE_2" : "=v"(f) : "v"(four));
+  else asm("v_cvt_f32_i32_sdwa %0, sext(%1) dst_sel:DWORD dst_unused:UNUSED_PAD src0_sel:BYTE_3" : "=v"(f) : "v"(four));
+  return f;
+}
+// codes times scale
+template <int V> __device__ __forceinline__ void values_of(typename Codes<V>::type p, float scale, float (&f)[V]) {
   if constexpr (V <= 4) {
-#pragma unroll
-    for (int i = 0; i < V; ++i) f[i] = (float)(int8_t)(p >> (8 * i));
+    f[0] = code_of<0>(p) * scale;
+    if constexpr (V > 1) f[1] = code_of<1>(p) * scale;
+    if constexpr (V > 2) {
+      f[2] = code_of<2>(p) * scale;
+      f[3] = code_of<3>(p) * scale;
+    }
   } else {
 #pragma unroll
-    for (int i = 0; i < V; ++i) f[i] = (float)(int8_t)(p[i / 4] >> (8 * (i % 4)));
+    for (int i = 0; i < V; i += 4) {
+      float four[4];
+      values_of<4>(p[i / 4], scale, four);
+#pragma unroll
+      for (int k = 0; k < 4; ++k) f[i + k] = four[k];
+    }
   }
 }
 

@@ -79,9 +79,7 @@ template <bool kGelu, typename T, int V, int kLanes> __global__ __launch_bounds_
     const P* dy = kGelu ? reinterpret_cast<const P*>(static_cast<const T*>(a.dy) + row * a.ld_dy) : nullptr;
     for (int p = part; p < pieces; p += kLanes) {
       float f[V];
-      widen_codes<V>(codes[p], f);
-#pragma unroll
-      for (int i = 0; i < V; ++i) f[i] *= scale;
+      values_of<V>(codes[p], scale, f);
       if constexpr (kGelu) {
         float d[V];
         widen<T, V>(dy[p], d);

@@ -378,7 +378,7 @@ def test_mlp_step_in_a_graph_and_on_other_streams():
 
 def test_arguments():
     """Scratch and outputs of the caller; what does not fit is refused."""
-    n, c, o = 300, 192, 130
+    n, c, o = 3000, 192, 130
     g = _gen(2)
     x, dy = _rows(g, n, c, "bf16").cuda(), torch.randn((n, o), generator=g).to(torch.bfloat16).cuda()
     norm = dsvt.RmsNorm(torch.ones(c, device="cuda"), "bf16")
