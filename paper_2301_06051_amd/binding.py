@@ -708,17 +708,15 @@ def _new(stream, device, like, shape, dtype):
     return like.new_empty(shape, dtype=dtype) if stream is None else _new_on(stream, device, like, shape, dtype)
 
 
+def _new_of(stream, device, rows, shape, dtype):
+    return _new(stream, device, rows._codes if rows._memory is None else rows._memory, shape, dtype)
+
+
 class Rows8:
     """Rows in 8 bits (dsvt_rows8 in dsvt.h): codes int8 [n, C], whose rows begin on 16 bytes and are whole multiples of 16 bytes apart, and
     scale float32 [n]; a row stands for its codes times its scale.  Made by the calls that write rows, or of tensors the caller has."""
 
-    __slots__ = ("codes", "scale", "n", "C", "struct", "ref", "device", "__weakref__")
-
-    def __init__(self, codes, scale):
-        self.codes, self.scale, (self.n, self.C) = codes, scale, codes.shape
-        self.device = codes.get_device()
-        self.struct = Rows8S(codes.data_ptr(), codes.stride(0) if self.n > 1 else (self.C + 15) // 16 * 16, scale.data_ptr())
-        self.ref = C.byref(self.struct)
+    __slots__ = ("n", "C", "device", "given", "struct", "ref", "_memory", "_codes", "_scale", "__weakref__")
 
     @classmethod
     def of(cls, codes, scale):
@@ -735,18 +733,45 @@ class Rows8:
         if codes.untyped_storage().nbytes() < codes.storage_offset() + n * ld:
             raise ValueError(f"codes: memory of {n} rows of {ld} bytes is wanted, the last one's {ld} too")
         _vector(scale, (n,), torch.float32, codes.get_device(), "scale")
-        return cls(codes, scale)
+        self = cls.__new__(cls)
+        self.n, self.C, self.device, self.given = n, c, codes.get_device(), scale
+        self._codes, self._scale, self._memory = codes, scale, None
+        self.struct = Rows8S(codes.data_ptr(), ld, scale.data_ptr())
+        self.ref = C.byref(self.struct)
+        return self
 
     @classmethod
     def empty(cls, n, channels, device="cuda"):
-        return cls(torch.empty((n, (channels + 15) // 16 * 16), dtype=torch.int8, device=device)[:, :channels],
-                   torch.empty((n,), dtype=torch.float32, device=device))
+        ld = (channels + 15) & ~15
+        return cls._in(torch.empty((n * (ld + 4),), dtype=torch.int8, device=device), n, channels, ld)
+
+    @classmethod
+    def _in(cls, memory, n, channels, ld):
+        """In one piece of memory, rows first (the tensors of it are made when they are asked for)."""
+        self = cls.__new__(cls)
+        self.n, self.C, self.device, self.given, self._memory, self._codes, self._scale = n, channels, memory.get_device(), None, memory, None, None
+        at = memory.data_ptr()
+        self.struct = Rows8S(at, ld, at + n * ld)
+        self.ref = C.byref(self.struct)
+        return self
 
     @classmethod
     def _like(cls, stream, device, like, n, channels):
-        ld = (channels + 15) // 16 * 16
-        codes = _new(stream, device, like, (n, ld), torch.int8)
-        return cls(codes if ld == channels else codes[:, :channels], _new(stream, device, like, (n,), torch.float32))
+        ld = (channels + 15) & ~15
+        return cls._in(like.new_empty(n * (ld + 4), dtype=torch.int8) if stream is None else _new_on(stream, device, like, (n * (ld + 4),), torch.int8),
+                       n, channels, ld)
+
+    @property
+    def codes(self):
+        if self._codes is None:
+            self._codes = self._memory[:self.n * self.struct.ld].view(self.n, self.struct.ld)[:, :self.C]
+        return self._codes
+
+    @property
+    def scale(self):
+        if self._scale is None:
+            self._scale = self._memory[self.n * self.struct.ld:].view(torch.float32)
+        return self._scale
 
 
 def _rows8(rows, n, channels, device, what):
@@ -776,12 +801,12 @@ def dsvt_keep_rows8(x, out=None, stream=None):
 def dsvt_read_rows8(rows, dtype, x=None, stream=None):
     """What Rows8 stand for, as rows [N, C] of "bf16" or "f32"."""
     if _recording():
-        _no_graph("dsvt_read_rows8", rows.scale, x)
+        _no_graph("dsvt_read_rows8", rows.given, x)
     code, dtype = _DT[dtype]
     n, c, dev = rows.n, rows.C, _current_device()
     ref = _rows8(rows, None, None, dev, "rows")
     if x is None:
-        x, ld = _new(stream, dev, rows.codes, (n, c), dtype), c
+        x, ld = _new_of(stream, dev, rows, (n, c), dtype), c
     else:
         ld = _rows(x, (n, c), dtype, dev, "x")
     rc = lib().dsvt_read_rows8(c, code, ref, n, x.data_ptr(), ld, _current_stream(dev) if stream is None else stream)
@@ -808,7 +833,7 @@ def _rms_norm(call, rms, x, res, z, y, rows, want_sum, stream, dev):
     ld_res, p_res = (0, None) if res is None else (_rows(res, (n, c), dtype, dev, "res"), res.data_ptr())
     ld_y, p_y = (0, None) if y is None else (_rows(y, (n, c), dtype, dev, "y"), y.data_ptr())
     if z is None and want_sum:
-        z = _new(stream, dev, x, (n, c), dtype)
+        z = torch.empty_like(x) if stream is None else _new_on(stream, dev, x, (n, c), dtype)
     ld_z, p_z = (0, None) if z is None else (_rows(z, (n, c), dtype, dev, "z"), z.data_ptr())
     rc = lib().dsvt_rms_norm(rms.ref, x.data_ptr(), ld_x, p_res, ld_res, n, p_z, ld_z, p_y, ld_y, None if rows is None else rows.ref,
                              _current_stream(dev) if stream is None else stream)
@@ -825,7 +850,7 @@ def dsvt_rms_norm(rms, x, res=None, y=None, z=None, want_sum=False, stream=None)
     if rms.device != dev:
         _elsewhere(dev, rms)
     if y is None:
-        y = _new(stream, dev, x, (x.shape[0], rms.C), rms.dtype)
+        y = torch.empty_like(x) if stream is None else _new_on(stream, dev, x, x.shape, x.dtype)
     z = _rms_norm("dsvt_rms_norm", rms, x, res, z, y, None, want_sum, stream, dev)
     return y if z is None else (y, z)
 
@@ -912,7 +937,7 @@ def dsvt_gelu_rows8(h, out=None, kept=None, want_kept=True, stream=None):
 def dsvt_gelu_rows8_backward(kept, dy, dh=None, stream=None):
     """Gradient of GELU's input from that of its output, dy [N, C], at the kept rows."""
     if _recording():
-        _no_graph("dsvt_gelu_rows8_backward", kept.scale, dy, dh)
+        _no_graph("dsvt_gelu_rows8_backward", kept.given, dy, dh)
     dtype, dev = _type_of(dy, "dy"), _current_device()
     n, c = dy.shape
     ref, ld = _rows8(kept, n, c, dev, "kept"), _rows(dy, (n, c), dtype, dev, "dy")
@@ -944,13 +969,13 @@ class Linear8:
 def dsvt_linear_rows8(linear, rows, y=None, stream=None):
     """The layer on Rows8 [N, C]; returns y [N, out]."""
     if _recording():
-        _no_graph("dsvt_linear_rows8", rows.scale, linear.weight.scale, linear.bias, y)
+        _no_graph("dsvt_linear_rows8", rows.given, linear.weight.given, linear.bias, y)
     n, dev = rows.n, _current_device()
     if linear.device != dev:
         _elsewhere(dev, linear)
     ref = _rows8(rows, None, linear.C, dev, "rows")
     if y is None:
-        y, ld = _new(stream, dev, rows.codes, (n, linear.out), linear.dtype), linear.out
+        y, ld = _new_of(stream, dev, rows, (n, linear.out), linear.dtype), linear.out
     else:
         ld = _rows(y, (n, linear.out), linear.dtype, dev, "y")
     rc = lib().dsvt_linear_rows8(linear.ref, ref, n, y.data_ptr(), ld, _current_stream(dev) if stream is None else stream)
@@ -970,7 +995,7 @@ def dsvt_linear_rows8_weight_grad(rows, dy, d_w=None, d_b=None, want_bias=True, 
     """Gradients of a linear layer's weight and bias, from that of its output, dy [N, out], and its input as Rows8 [N, C]: returns (d_w [out, C] of
     dy's type, d_b float32 [out], or None if it is not wanted)."""
     if _recording():
-        _no_graph("dsvt_linear_rows8_weight_grad", rows.scale, dy, d_w, d_b)
+        _no_graph("dsvt_linear_rows8_weight_grad", rows.given, dy, d_w, d_b)
     dtype, dev = _type_of(dy, "dy"), _current_device()
     n, c, o = rows.n, rows.C, dy.shape[1]
     ref, ld = _rows8(rows, None, None, dev, "rows"), _rows(dy, (n, o), dtype, dev, "dy")

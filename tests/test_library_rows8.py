@@ -122,9 +122,9 @@ def test_tensors_that_require_gradients_are_refused():
         return torch.zeros((4, 16), requires_grad=name == k)
 
     def calls(k):
-        rows = SimpleNamespace(scale=needing("scale", k), n=4, C=16, device=-1)
+        rows = SimpleNamespace(given=needing("scale", k), n=4, C=16, device=-1)
         rms = SimpleNamespace(gamma=needing("gamma", k))
-        lin = SimpleNamespace(weight=SimpleNamespace(scale=needing("w_scale", k)), bias=needing("bias", k), device=-1)
+        lin = SimpleNamespace(weight=SimpleNamespace(given=needing("w_scale", k)), bias=needing("bias", k), device=-1)
         t = lambda name: needing(name, k)  # noqa: E731
         return {"x": lambda: b.dsvt_keep_rows8(t("x")), "h": lambda: b.dsvt_gelu_rows8(t("h")),
                 "scale xx": lambda: b.dsvt_read_rows8(rows, "f32", x=t("xx")),
