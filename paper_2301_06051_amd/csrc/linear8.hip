@@ -104,76 +104,107 @@ template <typename T, int kTiles, int kAtOnce> __global__ __launch_bounds__(64 *
 __device__ __forceinline__ void load_to_lds(const void* base, uint32_t off, uint32_t to) {
   asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2" ::"s"(to), "v"(off), "s"(base) : "m0");
 }
+// 4 bytes a lane likewise.
+__device__ __forceinline__ void float_to_lds(const float* base, uint32_t off, uint32_t to) {
+  asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dword %1, %2" ::"s"(to), "v"(off), "s"(base) : "m0");
+}
 // Until at most kLater loads of this wavefront are on their way and its LDS reads are done; then until all wavefronts are there.
 template <int kLater> __device__ __forceinline__ void wait_for_stage() {
   asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)\n\ts_barrier" ::"n"(kLater) : "memory");
 }
 
-// Tiles of kRowsT rows and kOutsT outputs, shared by kM x kN wavefronts.  kColumns columns at a time go from memory into one of kBuffers buffers in
-// LDS, kBuffers - 1 steps ahead.
+// Tiles of kRowsT rows and kOutsT outputs, shared by kM x kN wavefronts.  Their columns, kColumns at a time, go from memory into one of kBuffers
+// buffers in LDS, kBuffers - 1 steps ahead.  kStay: a workgroup stays and takes tiles in turn, and the steps ahead go over the tiles' borders: while
+// one tile's results are written, the next one's rows and weights are on their way.
 //
 // The matrix instruction takes 32 outputs, 32 rows and 32 columns: lane 32 h + m holds 16 codes of row m, from column 16 h on.  In LDS a row's
 // 16-byte pieces are permuted, piece j of row r being at j ^ turn_of(r): the 16 lanes whose reads are served together (0-3, 12-15 and 20-27, or 4-11,
 // 16-19 and 28-31 of a half) then hit all banks once.  Weights are read in another order of their rows, so that a lane's 16 sums of a tile are 16
 // neighbouring outputs of one row.
-template <int kRowsT, int kOutsT, int kColumns, int kBuffers> constexpr size_t tiles_lds() {
-  return (size_t)kBuffers * (kRowsT + kOutsT) * kColumns + (2 * kOutsT + kRowsT) * sizeof(float);
-}
-
-template <typename T, int kRowsT, int kOutsT, int kM, int kN, int kColumns, int kBuffers>
-__global__ __launch_bounds__(64 * kM * kN) void k_linear8_tiles(Linear8Args a) {
-  constexpr int kWaves = kM * kN, TM = kRowsT / kM / 32, TN = kOutsT / kN / 32, kPieces = kColumns / 16, kSteps = kColumns / 32;
-  constexpr int kAtOnceRows = 64 / kPieces;       // rows of one load of a wavefront
-  constexpr int kLoads = (kRowsT + kOutsT) / (kWaves * kAtOnceRows), kLoadsX = kRowsT / (kWaves * kAtOnceRows);
+template <typename T, int kRowsT, int kOutsT, int kM, int kN, int kColumns, int kBuffers> struct Tiles {
+  static constexpr int kWaves = kM * kN, TM = kRowsT / kM / 32, TN = kOutsT / kN / 32, kPieces = kColumns / 16, kSteps = kColumns / 32;
+  static constexpr int kAtOnceRows = 64 / kPieces;            // rows of one load of a wavefront
+  static constexpr int kLoads = (kRowsT + kOutsT) / (kWaves * kAtOnceRows), kLoadsX = kRowsT / (kWaves * kAtOnceRows);
   static_assert(kRowsT % (kWaves * kAtOnceRows) == 0 && kOutsT % (kWaves * kAtOnceRows) == 0, "rows are fetched by all wavefronts together");
-  constexpr int kBuffer = (kRowsT + kOutsT) * kPieces;        // pieces of a buffer
+  static_assert(kWaves * kAtOnceRows % 16 == 0, "rows of one lane have one permutation");
+  static constexpr int kBuffer = (kRowsT + kOutsT) * kPieces;              // pieces of a buffer
+  // results of a wavefront on their way out: kRowsOut rows of kWide values, V to a piece
+  static constexpr int kRowsOut = sizeof(T) == 2 ? 32 : 16, kWide = TN * 32, V = 16 / (int)sizeof(T), PR = kWide / V, kOut = kRowsOut * PR;
+  static_assert(PR == 4 || PR == 8 || PR == 16, "pieces of a row are permuted within 4 or 8");
+  static constexpr int kEnds = 2 * kOutsT + kRowsT;           // scales of outputs, their biases, scales of rows
+  static constexpr int kEndLoads = (kEnds + 64 * kWaves - 1) / (64 * kWaves);
+  static constexpr int kEndPlaces = kEndLoads * 64 * kWaves;
+  static_assert(kWaves * kOut <= kBuffer, "the results of all wavefronts fit a buffer");
+  static constexpr int kStores = TM * 32 / (64 / PR);         // of a wavefront, of whole rows
+  static constexpr size_t lds() { return (size_t)kBuffers * (16 * kBuffer + 4 * kEndPlaces); }
+};
+
+template <typename T, int kRowsT, int kOutsT, int kM, int kN, int kColumns, int kBuffers, bool kStay>
+__global__ __launch_bounds__(64 * kM * kN) void k_linear8_tiles(Linear8Args a) {
+  typedef Tiles<T, kRowsT, kOutsT, kM, kN, kColumns, kBuffers> S;
+  constexpr int kWaves = S::kWaves, TM = S::TM, TN = S::TN, kPieces = S::kPieces, kSteps = S::kSteps, kLoads = S::kLoads, kLoadsX = S::kLoadsX;
+  constexpr int kBuffer = S::kBuffer, V = S::V, PR = S::PR, kWide = S::kWide, kRowsOut = S::kRowsOut;
   const auto turn_of = [](int r) { return kPieces == 4 ? r >> 2 & 3 : r >> 1 & 7; };
   extern __shared__ i32x4 lds[];
+  float* const all_ends = reinterpret_cast<float*>(lds + kBuffers * kBuffer);
+  typedef typename Piece<T, V>::type P;
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), wm = wave % kM, wn = wave / kM, m = lane & 31, h = lane >> 5;
-  // workgroups of one XCD (every eighth) take neighbouring tiles: eight along the rows, then the next outputs
-  const int tiles_m = (a.n + kRowsT - 1) / kRowsT, tiles_n = (a.O + kOutsT - 1) / kOutsT, all = tiles_m * tiles_n;
-  const int per = (all + 7) >> 3;
-  int id = (blockIdx.x & 7) * per + (blockIdx.x >> 3);
-  if ((blockIdx.x >> 3) >= per || id >= all) return;
-  const int band = id / (8 * tiles_n), bm = tiles_m - 8 * band < 8 ? tiles_m - 8 * band : 8;
-  id -= band * 8 * tiles_n;
-  const int64_t row0 = (int64_t)(8 * band + id % bm) * kRowsT;
-  const int out0 = id / bm * kOutsT;
 
-  // What this lane fetches: rows (i kWaves + wave) kAtOnceRows + lane / kPieces, past the last row the last one again, and of them the piece whose
-  // place in LDS is the lane's.  Pieces past a row's end are its last one.
-  const int8_t *x = a.x + row0 * a.ld_x, *w = a.w + (int64_t)out0 * a.ld_w;
-  uint32_t off[kLoads];
-  const int last_x = (int)(a.n - row0 < kRowsT ? a.n - row0 : kRowsT) - 1, last_w = (a.O - out0 < kOutsT ? a.O - out0 : kOutsT) - 1;
-  const int piece = (lane % kPieces) ^ turn_of(wave * kAtOnceRows + lane / kPieces);
-  static_assert(kWaves * kAtOnceRows % 16 == 0, "rows of one lane have one permutation");
-#pragma unroll
-  for (int i = 0; i < kLoads; ++i) {
-    const int r = ((i < kLoadsX ? i : i - kLoadsX) * kWaves + wave) * kAtOnceRows + lane / kPieces, last = i < kLoadsX ? last_x : last_w;
-    off[i] = (uint32_t)(r < last ? r : last) * (uint32_t)(i < kLoadsX ? a.ld_x : a.ld_w) + 16u * piece;
-  }
-  const int last_piece = (a.C - 1) >> 4 << 4, last_step = (a.C - 1) / kColumns * kColumns;
-  const uint32_t lds0 = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) const void*)lds + 1024u * wave;
-  const auto fetch = [&](int k0, int buffer) {
-    k0 = k0 < last_step ? k0 : last_step;
-    const uint32_t back = k0 + 16 * piece > last_piece ? k0 + 16 * piece - last_piece : 0;
-#pragma unroll
-    for (int i = 0; i < kLoads; ++i) load_to_lds((i < kLoadsX ? x : w) + k0, off[i] - back, lds0 + 16u * kBuffer * buffer + 1024u * kWaves * i);
+  // Workgroups of one XCD (every eighth) take neighbouring tiles side by side: eight along the rows, then the next outputs.
+  const int tiles_m = (a.n + kRowsT - 1) / kRowsT, tiles_n = (a.O + kOutsT - 1) / kOutsT, all = tiles_m * tiles_n;
+  const int share = (all + 7) >> 3, first = (blockIdx.x & 7) * share, end = first + share < all ? first + share : all, step = gridDim.x >> 3;
+  int id = first + (blockIdx.x >> 3);
+  if (id >= end) return;
+  struct Place { int64_t row0; int out0; };
+  const auto place_of = [&](int i) {
+    const int band = i / (8 * tiles_n), rest = tiles_m - 8 * band, bm = rest < 8 ? rest : 8;
+    i -= band * 8 * tiles_n;
+    return Place{(int64_t)(8 * band + i % bm) * kRowsT, i / bm * kOutsT};
   };
 
+  // The fetching side, ahead of the other: its tile and column.  A lane fetches rows (i kWaves + wave) kAtOnceRows + lane / kPieces, past the last row
+  // the last one again, and of them the piece whose place in LDS is the lane's; pieces past a row's end are its last one.  Behind the last
+  // tile it goes on with that one.
+  const int last_piece = (a.C - 1) >> 4 << 4, last_step = (a.C - 1) / kColumns * kColumns;
+  const int piece = (lane % kPieces) ^ turn_of(wave * S::kAtOnceRows + lane / kPieces);
+  const uint32_t lds0 = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) const void*)lds;
+  int next_id = id, next_k = 0, next_buffer = 0, next_ends = 0;
+  const int8_t *x, *w;
+  uint32_t off[kLoads];
+  const auto fetch = [&](bool begin) {
+    if (kStay ? next_k == 0 : begin) {
+      const Place at = place_of(next_id);
+      x = a.x + at.row0 * a.ld_x;
+      w = a.w + (int64_t)at.out0 * a.ld_w;
+      const int last_x = (int)(a.n - at.row0 < kRowsT ? a.n - at.row0 : kRowsT) - 1, last_w = (a.O - at.out0 < kOutsT ? a.O - at.out0 : kOutsT) - 1;
 #pragma unroll
-  for (int k = 0; k < kBuffers - 1; ++k) fetch(k * kColumns, k);
+      for (int i = 0; i < kLoads; ++i) {
+        const int r = ((i < kLoadsX ? i : i - kLoadsX) * kWaves + wave) * S::kAtOnceRows + lane / kPieces, last = i < kLoadsX ? last_x : last_w;
+        off[i] = (uint32_t)(r < last ? r : last) * (uint32_t)(i < kLoadsX ? a.ld_x : a.ld_w) + 16u * piece;
+      }
+      // scales and biases: 64 values a wavefront and load (without biases some that are not used)
+#pragma unroll
+      for (int i = 0; i < S::kEndLoads; ++i) {
+        const int from = (i * kWaves + wave) * 64;            // (kOutsT and kRowsT are multiples of 64)
+        const float* base = from < kOutsT ? a.t + at.out0 : from < 2 * kOutsT && a.bias ? a.bias + at.out0 : from < 2 * kOutsT ? a.t + at.out0 : a.s + at.row0;
+        const int at_end = from < kOutsT ? from : from < 2 * kOutsT ? from - kOutsT : from < S::kEnds ? from - 2 * kOutsT : 0, most = from < 2 * kOutsT ? last_w : last_x;
+        const int k = at_end + lane;
+        float_to_lds(base, 4u * (uint32_t)(k < most ? k : most), lds0 + 16u * kBuffers * kBuffer + 4u * (next_ends * S::kEndPlaces + from));
+      }
+      next_ends = next_ends + 1 < kBuffers ? next_ends + 1 : 0;
+    }
+    const uint32_t back = next_k + 16 * piece > last_piece ? next_k + 16 * piece - last_piece : 0;
+#pragma unroll
+    for (int i = 0; i < kLoads; ++i)
+      load_to_lds((i < kLoadsX ? x : w) + next_k, off[i] - back, lds0 + 16u * kBuffer * next_buffer + 1024u * (kWaves * i + wave));
+    next_buffer = next_buffer + 1 < kBuffers ? next_buffer + 1 : 0;
+    next_k += kColumns;
+    if (next_k > last_step) {
+      next_k = kStay ? 0 : last_step;
+      next_id = next_id + step < end ? next_id + step : next_id;
+    }
+  };
 
-  // the scales and biases of the tile, for its end
-  float* const ends = reinterpret_cast<float*>(lds + kBuffers * kBuffer);
-  for (int k = tid; k < kOutsT; k += 64 * kWaves) {
-    const int at = out0 + (k < last_w ? k : last_w);
-    ends[k] = a.t[at];
-    ends[kOutsT + k] = a.bias ? a.bias[at] : 0.f;
-  }
-  for (int k = tid; k < kRowsT; k += 64 * kWaves) ends[2 * kOutsT + k] = a.s[row0 + (k < last_x ? k : last_x)];
-
-  i32x16 acc[TM][TN] = {};
   const int out_m = (m >> 2 & 1) * 16 + (m >> 3) * 4 + (m & 3);
   const i32x4* const xs = lds + (wm * TM * 32 + m) * kPieces;
   const i32x4* const ws = lds + (kRowsT + wn * TN * 32 + out_m) * kPieces;
@@ -184,117 +215,144 @@ __global__ __launch_bounds__(64 * kM * kN) void k_linear8_tiles(Linear8Args a) {
 #pragma unroll
     for (int t = 0; t < TM; ++t) f.q[t] = xs[buffer * kBuffer + t * 32 * kPieces + ((2 * k + h) ^ turn_of(m))];
   };
+  i32x16 acc[TM][TN];
   const auto multiply = [&](const Frags& f) {
 #pragma unroll
     for (int i = 0; i < TM; ++i)
 #pragma unroll
       for (int j = 0; j < TN; ++j) acc[i][j] = __builtin_amdgcn_mfma_i32_32x32x32_i8(f.p[j], f.q[i], acc[i][j], 0, 0, 0);
   };
+  static_assert(kSteps % 2 == 0, "fragments change places");
+  const auto spot = [](int row, int p) { return row * PR + (p ^ (PR == 4 ? row >> 1 & 3 : row & 7)); };
 
   // The fragments of a product are read while the one before is under way, the first ones of a buffer behind the barrier at which it is waited for.
-  wait_for_stage<(kBuffers - 2) * kLoads>();
-  fetch((kBuffers - 1) * kColumns, kBuffers - 1);
-  read(frags[0], 0, 0);
-  int buffer = 0, k0 = 0;
-  for (; k0 < last_step; k0 += kColumns) {
+  // At that barrier all wavefronts are done with the buffer before, which is then fetched into.
 #pragma unroll
-    for (int k = 0; k < kSteps - 1; ++k) {
-      read(frags[(k + 1) & 1], buffer, k + 1);
-      multiply(frags[k & 1]);
-    }
-    const int free = buffer;
-    buffer = buffer + 1 < kBuffers ? buffer + 1 : 0;
-    wait_for_stage<(kBuffers - 2) * kLoads>();
-    fetch(k0 + kBuffers * kColumns, free);
+  for (int k = 0; k < kBuffers - 1; ++k) fetch(k == 0);
+  // Stores are counted with the loads.  Behind a whole tile's, which are as many for every such tile, the next kBuffers - 1 steps were fetched before
+  // them: waiting for those is not waiting for the stores.
+  int buffer = 0, ends_at = 0, stored = 0;
+  const auto wait = [&]() {
+    constexpr int kLater = (kBuffers - 2) * kLoads;
+    if (kStay && stored > 0 && kLater + S::kStores < 63) wait_for_stage<(kLater + S::kStores < 63 ? kLater + S::kStores : 0)>();
+    else wait_for_stage<kLater>();
+    --stored;
+  };
+  for (; id < end; id += step) {
+#pragma unroll
+    for (int i = 0; i < TM; ++i)
+#pragma unroll
+      for (int j = 0; j < TN; ++j) acc[i][j] = i32x16{};
+    wait();
+    fetch(false);
     read(frags[0], buffer, 0);
-    multiply(frags[1]);
-  }
-  // what lies past a row's end may be anything; zeros in one operand do
+    int k0 = 0;
+    for (; k0 < last_step; k0 += kColumns) {
 #pragma unroll
-  for (int k = 0; k < kSteps; ++k) {
-    if (k0 + 32 * k >= a.C) break;
-    if (k) read(frags[0], buffer, k);
+      for (int k = 0; k < kSteps - 1; ++k) {
+        read(frags[(k + 1) & 1], buffer, k + 1);
+        multiply(frags[k & 1]);
+      }
+      buffer = buffer + 1 < kBuffers ? buffer + 1 : 0;
+      wait();
+      fetch(false);
+      read(frags[0], buffer, 0);
+      multiply(frags[1]);
+    }
+    // what lies past a row's end may be anything; zeros in one operand do
 #pragma unroll
-    for (int t = 0; t < TN; ++t) frags[0].p[t] = first_bytes(frags[0].p[t], a.C - k0 - 32 * k - 16 * h);
-    multiply(frags[0]);
-  }
-  static_assert(kSteps % 2 == 0, "fragments change places");
+    for (int k = 0; k < kSteps; ++k) {
+      if (k0 + 32 * k >= a.C) break;
+      if (k) read(frags[0], buffer, k);
+#pragma unroll
+      for (int t = 0; t < TN; ++t) frags[0].p[t] = first_bytes(frags[0].p[t], a.C - k0 - 32 * k - 16 * h);
+      multiply(frags[0]);
+    }
 
-  // Results go through LDS, 32 rows of a wavefront at a time, so that a row's are written side by side: as they come out of the product, a store would
-  // write 32 pieces of 64 bytes.
-  constexpr int kWide = TN * 32, V = 16 / (int)sizeof(T), PR = kWide / V;
-  static_assert(PR == 4 || PR == 8 || PR == 16, "pieces of a row are permuted within 4 or 8");
-  const auto spot = [](int row, int p) { return row * PR + (p ^ (PR == 4 ? row >> 1 & 3 : row & 7)); };
-  typedef typename Piece<T, V>::type P;
-  static_assert(kWaves * 32 * PR <= kBuffers * kBuffer, "the results of all wavefronts fit the buffers");
-  P* const out = reinterpret_cast<P*>(lds) + wave * 32 * PR;
-  const int first_out = out0 + wn * kWide, outs = a.O - first_out < kWide ? a.O - first_out : kWide;
-  const bool wide = outs % V == 0 && ((uintptr_t)a.y & 15u) == 0 && a.ld_y * (int64_t)sizeof(T) % 16 == 0;
-  wait_for_stage<0>();                            // nothing is on its way to the buffers, and all wavefronts are done with them
-  if (outs <= 0) return;
-  float t[TN][16], bias[TN][16];
+    // Results go through LDS, kRowsOut rows of a wavefront at a time, so that a row's are written side by side: as they come out of the product, a store
+    // would write 32 pieces of 64 bytes.  There the buffer is free that was multiplied last, once all wavefronts are done with it.
+    lds_barrier();
+    P* const out = reinterpret_cast<P*>(lds + buffer * kBuffer) + wave * S::kOut;
+    buffer = buffer + 1 < kBuffers ? buffer + 1 : 0;
+    const Place at = place_of(id);
+    const float* const ends = all_ends + ends_at * S::kEndPlaces;
+    ends_at = ends_at + 1 < kBuffers ? ends_at + 1 : 0;
+    const int first_out = at.out0 + wn * kWide, outs = a.O - first_out < kWide ? a.O - first_out : kWide;
+    const bool whole_rows = a.n - at.row0 >= kRowsT && outs == kWide;
+    const bool wide = outs % V == 0 && ((uintptr_t)a.y & 15u) == 0 && a.ld_y * (int64_t)sizeof(T) % 16 == 0, whole = whole_rows && wide;
+    stored = whole ? kBuffers - 1 : 0;
 #pragma unroll
-  for (int j = 0; j < TN; ++j)
+    for (int i = 0; i < TM; ++i) {
+      const int64_t from = at.row0 + (wm * TM + i) * 32;
+      const float s = ends[2 * kOutsT + (wm * TM + i) * 32 + m];
 #pragma unroll
-    for (int e = 0; e < 16; e += 4) {
-      const int at = wn * kWide + j * 32 + 16 * h + e;
-      const f32x4 t4 = *reinterpret_cast<const f32x4*>(ends + at), b4 = *reinterpret_cast<const f32x4*>(ends + kOutsT + at);
+      for (int part = 0; part < 32 / kRowsOut; ++part) {
+        const int rows = (int)(a.n - from - kRowsOut * part < kRowsOut ? a.n - from - kRowsOut * part : kRowsOut);
+        if (rows <= 0 || outs <= 0) break;
+        if (m / kRowsOut == part) {
+          const auto results = [&](auto act) {
 #pragma unroll
-      for (int k = 0; k < 4; ++k) {
-        t[j][e + k] = t4[k];
-        bias[j][e + k] = b4[k];
-      }
-    }
+            for (int j = 0; j < TN; ++j)
 #pragma unroll
-  for (int i = 0; i < TM; ++i) {
-    const int64_t from = row0 + (wm * TM + i) * 32;
-    const int rows = (int)(a.n - from < 32 ? a.n - from : 32);
-    if (rows <= 0) break;
-    const float s = ends[2 * kOutsT + (wm * TM + i) * 32 + m];
-    const auto results = [&](auto act) {
+              for (int e = 0; e < 16; e += V) {
+                float f[V];
 #pragma unroll
-      for (int j = 0; j < TN; ++j)
+                for (int k = 0; k < V; k += 4) {
+                  const int o = wn * kWide + j * 32 + 16 * h + e + k;
+                  const f32x4 t = *reinterpret_cast<const f32x4*>(ends + o);
+                  f32x4 bias = {0.f, 0.f, 0.f, 0.f};
+                  if (a.bias) bias = *reinterpret_cast<const f32x4*>(ends + kOutsT + o);
 #pragma unroll
-        for (int e = 0; e < 16; e += V) {
-          float f[V];
-#pragma unroll
-          for (int k = 0; k < V; ++k) f[k] = act(fmaf((float)acc[i][j][e + k] * s, t[j][e + k], bias[j][e + k]));
-          out[spot(m, (32 * j + 16 * h + e) / V)] = narrow<T, V>(f);
+                  for (int u = 0; u < 4; ++u) f[k + u] = act(fmaf((float)acc[i][j][e + k + u] * s, t[u], bias[u]));
+                }
+                out[spot(m % kRowsOut, (32 * j + 16 * h + e) / V)] = narrow<T, V>(f);
+              }
+          };
+          if (a.act) results([](float v) { return gelu(v); });
+          else results([](float v) { return v; });
         }
-    };
-    if (a.act) results([](float v) { return gelu(v); });
-    else results([](float v) { return v; });
-    __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
-    __builtin_amdgcn_wave_barrier();
-    __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
-    T* y = static_cast<T*>(a.y) + from * a.ld_y + first_out;
-    if (wide) {
-      constexpr int kAtOnce = 64 / PR;            // rows of a store
+        __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
+        __builtin_amdgcn_wave_barrier();
+        __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
+        T* y = static_cast<T*>(a.y) + (from + kRowsOut * part) * a.ld_y + first_out;
+        constexpr int kAtOnce = 64 / PR;          // rows of a store
+        if (whole) {
 #pragma unroll
-      for (int r = 0; r < 32; r += kAtOnce) {
-        const int row = r + lane / PR, p = lane % PR;
-        if (row < rows && p * V < outs) *reinterpret_cast<P*>(y + row * a.ld_y + p * V) = out[spot(row, p)];
-      }
-    } else {
-      constexpr int kAtOnce = 64 / kWide;
-      for (int r = 0; r < 32; r += kAtOnce) {
-        const int row = r + lane / kWide, c = lane % kWide;
-        if (row < rows && c < outs) y[row * a.ld_y + c] = reinterpret_cast<const T*>(out + spot(row, c / V))[c % V];
+          for (int r = 0; r < kRowsOut; r += kAtOnce) {
+            const int row = r + lane / PR, p = lane % PR;
+            *reinterpret_cast<P*>(y + row * a.ld_y + p * V) = out[spot(row, p)];
+          }
+        } else if (wide) {
+#pragma unroll
+          for (int r = 0; r < kRowsOut; r += kAtOnce) {
+            const int row = r + lane / PR, p = lane % PR;
+            if (row < rows && p * V < outs) *reinterpret_cast<P*>(y + row * a.ld_y + p * V) = out[spot(row, p)];
+          }
+        } else {
+          constexpr int kAtOnce = 64 / kWide;
+          for (int r = 0; r < kRowsOut; r += kAtOnce) {
+            const int row = r + lane / kWide, c = lane % kWide;
+            if (row < rows && c < outs) y[row * a.ld_y + c] = reinterpret_cast<const T*>(out + spot(row, c / V))[c % V];
+          }
+        }
+        __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
+        __builtin_amdgcn_wave_barrier();
+        __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
       }
     }
-    __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
-    __builtin_amdgcn_wave_barrier();
-    __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
+    if (!kStay) break;
   }
+  wait_for_stage<0>();                            // nothing is on its way to LDS any more that will be another workgroup's
 }
 
-template <typename T, int kRowsT, int kOutsT, int kM, int kN, int kColumns, int kBuffers> int launch_tiles(const Linear8Args& a, hipStream_t st) {
+// stay: as many workgroups a compute unit; 0: one a tile
+template <typename T, int kRowsT, int kOutsT, int kM, int kN, int kColumns, int kBuffers, int kStay> int launch_tiles(const Linear8Args& a, hipStream_t st) {
+  typedef Tiles<T, kRowsT, kOutsT, kM, kN, kColumns, kBuffers> S;
   static std::atomic<uint64_t> allowed;
-  const auto kernel = k_linear8_tiles<T, kRowsT, kOutsT, kM, kN, kColumns, kBuffers>;
-  constexpr size_t lds = tiles_lds<kRowsT, kOutsT, kColumns, kBuffers>();
-  if (const int rc = dsvt_allow_lds(reinterpret_cast<const void*>(kernel), lds, allowed)) return rc;
-  const int64_t all = dsvt_ceil_div(a.n, kRowsT) * dsvt_ceil_div(a.O, kOutsT);
-  kernel<<<(unsigned)(dsvt_ceil_div(all, 8) * 8), 64 * kM * kN, lds, st>>>(a);
+  const auto kernel = k_linear8_tiles<T, kRowsT, kOutsT, kM, kN, kColumns, kBuffers, kStay != 0>;
+  if (const int rc = dsvt_allow_lds(reinterpret_cast<const void*>(kernel), S::lds(), allowed)) return rc;
+  const int64_t all = dsvt_ceil_div(dsvt_ceil_div(a.n, kRowsT) * dsvt_ceil_div(a.O, kOutsT), 8) * 8, at_once = (int64_t)kComputeUnits * kStay;
+  kernel<<<(unsigned)(kStay == 0 || all < at_once ? all : at_once), 64 * kM * kN, S::lds(), st>>>(a);
   return DSVT_OK;
 }
 template <typename T> int launch(const Linear8Args& a, hipStream_t st) {
@@ -312,13 +370,15 @@ template <typename T> int launch(const Linear8Args& a, hipStream_t st) {
     else few(std::integral_constant<int, 4>(), std::integral_constant<int, 2>());
     return DSVT_OK;
   }
-  // The largest tiles that leave little of a last round over the 256 compute units empty: they read least from LDS and memory for a product.  (8,192 x
-  // 4,096 -> 4,096: 149 us, 157 in tiles of 128, 301 of 64; 30,000 x 192 -> 576, 354 of the largest tiles: 20.1, 18.7 of 128, 19.0 of 64; 1,024 x 2,048 ->
-  // 2,048, 128 tiles of 128: 14.3, 11.2 of 64.)
+  // The largest tiles that leave little of a last round over the 256 compute units empty: they read least from LDS and memory for a product.  us a
+  // call with tiles of 256 x 256, 128 x 128, 128 x 64, 64 x 64 (the first two stay): 8,192 x 4,096 -> 4,096 (512 of the largest tiles) 132, 160, 198, 304;
+  // 800,000 x 192 -> 576 293, 333, 368, 423; 30,000 x 192 -> 576 (354) 18.3, 15.0, 15.5, 15.5; 10,000 x 512 -> 2,048 25.7, 22.6, 25.5, 31.3; 30,000 x 384 -> 192
+  // 12.9, 10.8, 9.4, 10.9; 1,024 x 2,048 -> 2,048 27.7, 15.4, 12.6, 11.2.
   const int64_t large = tiles(256, 256), rounds = dsvt_ceil_div(large, kComputeUnits);
-  if (10 * large >= 8 * rounds * kComputeUnits) return launch_tiles<T, 256, 256, 2, 4, 128, 2>(a, st);
-  if (tiles(128, 128) >= 2 * kComputeUnits) return launch_tiles<T, 128, 128, 2, 2, 128, 2>(a, st);
-  return launch_tiles<T, 64, 64, 2, 2, 64, 3>(a, st);
+  if (10 * large >= 8 * rounds * kComputeUnits) return launch_tiles<T, 256, 256, 2, 4, 128, 2, 1>(a, st);
+  if (tiles(128, 128) >= 4 * kComputeUnits) return launch_tiles<T, 128, 128, 4, 2, 128, 2, 2>(a, st);
+  if (tiles(128, 64) >= 2 * kComputeUnits) return launch_tiles<T, 128, 64, 4, 1, 128, 2, 0>(a, st);
+  return launch_tiles<T, 64, 64, 2, 2, 64, 3, 0>(a, st);
 }
 
 }  // namespace

@@ -423,3 +423,18 @@ def test_no_rows():
     assert dsvt.dsvt_linear_rows8(layer, kept).shape == (0, o)
     dw, db = dsvt.dsvt_linear_rows8_weight_grad(kept, torch.empty((0, o), dtype=torch.bfloat16, device="cuda"))
     assert dw.shape == (o, c) and not dw.any() and not db.any()
+
+
+@pytest.mark.parametrize("n,c,o,dtype,act", [(70001, 64, 130, "bf16", False), (66000, 192, 576, "f32", False), (40000, 99, 520, "bf16", True), (30000, 192, 576, "bf16", False),
+                                             (33001, 300, 641, "f32", True), (33000, 520, 1040, "bf16", False), (140000, 16, 136, "bf16", False)])
+def test_linear_in_parts(n, c, o, dtype, act):
+    """Many rows, where workgroups go from tile to tile: every row is that of a call on 1,000 rows, where each has one."""
+    g = _gen(n + c)
+    x, w = _random_codes(g, n, c), _random_codes(g, o, c)
+    layer = dsvt.Linear8(w, dtype, torch.randn((o,), generator=g).cuda(), act)
+    print("[case] linear in parts", n, c, o, dtype, flush=True)
+    y = dsvt.dsvt_linear_rows8(layer, x)
+    for at in range(0, n, 1000):
+        part = dsvt.Rows8.of(x.codes[at:at + 1000], x.scale[at:at + 1000])
+        assert torch.equal(y[at:at + 1000], dsvt.dsvt_linear_rows8(layer, part)), at
+    assert torch.equal(dsvt.dsvt_linear_rows8(layer, x), y)
