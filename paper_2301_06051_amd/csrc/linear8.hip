@@ -99,6 +99,8 @@ template <typename T, int kTiles, int kAtOnce> __global__ __launch_bounds__(64 *
   }
 }
 
+#pragma clang diagnostic push
+#pragma clang diagnostic ignored "-Winline-asm"    // m0 is the compiler's to reserve; it keeps nothing in it from one instruction to another
 // 16 bytes a lane from memory, at base + off, straight into LDS, where the wavefront's 64 pieces lie one behind the other from `to` on.  Counted by
 // vmcnt like other loads; the compiler does not know of it, so that only wait_for_stage() says when the data is there.
 __device__ __forceinline__ void load_to_lds(const void* base, uint32_t off, uint32_t to) {
@@ -108,6 +110,7 @@ __device__ __forceinline__ void load_to_lds(const void* base, uint32_t off, uint
 __device__ __forceinline__ void float_to_lds(const float* base, uint32_t off, uint32_t to) {
   asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dword %1, %2" ::"s"(to), "v"(off), "s"(base) : "m0");
 }
+#pragma clang diagnostic pop
 // Until at most kLater loads of this wavefront are on their way and its LDS reads are done; then until all wavefronts are there.
 template <int kLater> __device__ __forceinline__ void wait_for_stage() {
   asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)\n\ts_barrier" ::"n"(kLater) : "memory");

@@ -193,7 +193,7 @@ __global__ __launch_bounds__(kThreads) void k_rms_long(RmsArgs a, int32_t rows) 
         const float z = sum_at<T>(a, row, c), y = z * (rs * a.gamma[c]);
         if (a.z) static_cast<T*>(a.z)[row * a.ld_z + c] = (T)z;
         if (a.y) static_cast<T*>(a.y)[row * a.ld_y + c] = (T)y;
-        if (a.codes) a.codes[row * a.ld_codes + c] = (int8_t)by.code(y);
+        if (a.codes) a.codes[row * a.ld_codes + c] = by.code(y);
       }
     }
   }

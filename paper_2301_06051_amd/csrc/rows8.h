@@ -16,18 +16,6 @@ template <> struct Codes<4> { typedef uint32_t type; };
 template <> struct Codes<2> { typedef uint16_t type; };
 template <> struct Codes<1> { typedef uint8_t type; };
 
-template <int V> __device__ __forceinline__ typename Codes<V>::type pack_codes(const int (&q)[V]) {
-  const auto word = [&](int at) { return (uint32_t)(q[at] & 255) | (uint32_t)(q[at + 1] & 255) << 8 | (uint32_t)(q[at + 2] & 255) << 16 | (uint32_t)q[at + 3] << 24; };
-  typename Codes<V>::type p;
-  if constexpr (V == 1) p = (uint8_t)q[0];
-  else if constexpr (V == 2) p = (uint16_t)((q[0] & 255) | (q[1] & 255) << 8);
-  else if constexpr (V == 4) p = word(0);
-  else {
-#pragma unroll
-    for (int k = 0; k < V / 4; ++k) p[k] = word(4 * k);
-  }
-  return p;
-}
 // One code of four as a float, in one instruction (the compiler takes two: it cuts the byte out first).
 template <int kByte> __device__ __forceinline__ float code_of(uint32_t four) {
   float f;
@@ -59,6 +47,12 @@ template <int V> __device__ __forceinline__ void values_of(typename Codes<V>::ty
 
 // Sizes as whole numbers: of infinities above those of numbers, of NaN above all.
 __device__ __forceinline__ uint32_t size_bits(float v) { return __float_as_uint(v) & 0x7fffffffu; }
+// The largest size of three, NaN if one is.
+__device__ __forceinline__ float largest_size(float a, float b, float c) {
+  float r;
+  asm("v_maximum3_f32 %0, |%1|, |%2|, |%3|" : "=v"(r) : "v"(a), "v"(b), "v"(c));
+  return r;
+}
 
 struct RowScale {
   float scale, to_codes;                          // codes are v * to_codes, rounded; of a row without a scale 0
@@ -70,38 +64,59 @@ struct RowScale {
     scale = plain ? fminf(top / 127.f, kLargestScale) : numbers ? 0.f : __uint_as_float(0x7fc00000u);
     to_codes = plain ? 127.f / top : 0.f;
   }
-  // (the product is rounded, then the whole number is taken: not one fma, which could decide a tie otherwise)
-  __device__ __forceinline__ int code(float v) const { return plain ? (int)rintf(v * to_codes) : 0; }
+  // The code is the low byte.  With 1.5 * 2^23 added, a number's low bits are those of the nearest whole one, ties to the even one; the product is
+  // rounded first (the compiler would make one fma of the two, which could decide a tie otherwise).
+  __device__ __forceinline__ uint32_t code_bits(float v) const {
+    float r;
+    asm("v_add_f32 %0, %1, %2" : "=v"(r) : "s"(12582912.f), "v"(v * to_codes));
+    return __float_as_uint(r);
+  }
+  __device__ __forceinline__ int8_t code(float v) const { return plain ? (int8_t)code_bits(v) : (int8_t)0; }
+  // (what is not plain may be no number: its bits are cleared)
+  template <int V> __device__ __forceinline__ typename Codes<V>::type codes(const float (&v)[V]) const {
+    typename Codes<V>::type p;
+    if constexpr (V == 1) p = (uint8_t)code(v[0]);
+    else if constexpr (V == 2) p = plain ? (uint16_t)__builtin_amdgcn_perm(code_bits(v[1]), code_bits(v[0]), 0x0c0c0400u) : 0;
+    else if constexpr (V == 4) {
+      const uint32_t low = __builtin_amdgcn_perm(code_bits(v[1]), code_bits(v[0]), 0x0c0c0400u);
+      const uint32_t high = __builtin_amdgcn_perm(code_bits(v[3]), code_bits(v[2]), 0x0c0c0400u);
+      p = plain ? __builtin_amdgcn_perm(high, low, 0x05040100u) : 0u;
+    } else {
+#pragma unroll
+      for (int k = 0; k < V; k += 4) {
+        const float four[4] = {v[k], v[k + 1], v[k + 2], v[k + 3]};
+        p[k / 4] = codes<4>(four);
+      }
+    }
+    return p;
+  }
 };
 
 // The row's pieces v in 8 bits: what its kLanes lanes hold of it goes to `codes`, its scale to *scale.
 template <int V, int kLanes, int R>
 __device__ __forceinline__ void store_codes(const float (&v)[R][V], int part, int pieces, int8_t* codes, float* scale, uint32_t* s) {
-  uint32_t top = 0;
+  float top = 0.f;
 #pragma unroll
-  for (int r = 0; r < R; ++r)
+  for (int r = 0; r < R; ++r) {
+    if constexpr (V == 1) top = largest_size(top, v[r][0], v[r][0]);
+    else {
 #pragma unroll
-    for (int i = 0; i < V; ++i) {
-      const uint32_t b = size_bits(v[r][i]);
-      top = b > top ? b : top;
+      for (int i = 0; i < V; i += 2) top = largest_size(top, v[r][i], v[r][i + 1]);
     }
-  const RowScale by(lane_join<kLanes>(top, s, [](uint32_t a, uint32_t b) { return a > b ? a : b; }));
+  }
+  const RowScale by(lane_join<kLanes>(size_bits(top), s, [](uint32_t a, uint32_t b) { return a > b ? a : b; }));
   if (part == 0) *scale = by.scale;
   typedef typename Codes<V>::type P;
   P* row = reinterpret_cast<P*>(codes);
 #pragma unroll
-  for (int r = 0; r < R; ++r) {
-    int q[V];
-#pragma unroll
-    for (int i = 0; i < V; ++i) q[i] = by.code(v[r][i]);
-    if (r * kLanes + part < pieces) row[r * kLanes + part] = pack_codes<V>(q);
-  }
+  for (int r = 0; r < R; ++r)
+    if (r * kLanes + part < pieces) row[r * kLanes + part] = by.codes(v[r]);
 }
 
 // GELU, x Phi(x), and its slope Phi(x) + x phi(x).  Phi(-|x|) = phi-like exponential times a polynomial of 1 / (1 + p z), z = |x| / sqrt 2
 // (Abramowitz & Stegun 7.1.26, off by at most 1.5e-7 in erf and so 7.5e-8 in Phi); the slope needs the same exponential.
 struct Normal {
-  float cdf, density;
+  float below, density;                           // Phi(-|x|), phi(x)
   __device__ __forceinline__ explicit Normal(float x) {
     const float e = __builtin_amdgcn_exp2f(x * x * -0.72134752044448170368f);             // exp(-x^2 / 2)
     const float t = __builtin_amdgcn_rcpf(fmaf(fabsf(x), 0.3275911f * 0.70710678118654752440f, 1.f));
@@ -109,15 +124,17 @@ struct Normal {
     p = fmaf(t, p, 0.5f * 1.421413741f);
     p = fmaf(t, p, 0.5f * -0.284496736f);
     p = fmaf(t, p, 0.5f * 0.254829592f);
-    const float below = t * p * e;                // Phi(-|x|)
-    cdf = x < 0.f ? below : 1.f - below;
+    below = t * p * e;
     density = e * 0.39894228040143267794f;
   }
 };
-__device__ __forceinline__ float gelu(float x) { return x * Normal(x).cdf; }
+__device__ __forceinline__ float gelu(float x) {
+  const float positive = x < 0.f ? 0.f : x;       // (a NaN stays one)
+  return fmaf(-fabsf(x), Normal(x).below, positive);
+}
 __device__ __forceinline__ float gelu_slope(float x) {
   const Normal n(x);
-  return fmaf(x, n.density, n.cdf);
+  return fmaf(x, n.density, x < 0.f ? n.below : 1.f - n.below);
 }
 
 // n rows of C codes and their scales.  Rows of `ld` bytes, begin on 16.

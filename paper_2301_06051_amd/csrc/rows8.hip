@@ -60,8 +60,8 @@ template <bool kGelu, typename T> __global__ __launch_bounds__(kThreads) void k_
     }
     for (int c = threadIdx.x; c < a.C; c += kThreads) {
       const float v = (float)x[c];
-      if (a.kept) a.kept[row * a.ld_kept + c] = (int8_t)by.code(v);
-      if (kGelu && a.out) a.out[row * a.ld_out + c] = (int8_t)by_out.code(gelu(v));
+      if (a.kept) a.kept[row * a.ld_kept + c] = by.code(v);
+      if (kGelu && a.out) a.out[row * a.ld_out + c] = by_out.code(gelu(v));
     }
   }
 }
