@@ -434,7 +434,8 @@ typedef struct {
 } dsvt_rms_cfg;
 
 /* x, res, z, y [device] [n_rows, C]; res may be NULL (z = x), z and one of y and rows8 too: NULL is not wanted.  y and rows8 are of the sum in
- * 32 bits, not of the z that is rounded to the type.  z and y may each be x or res themselves (same stride). */
+ * 32 bits, not of the z that is rounded to the type.  z and y may each be x or res themselves (same stride), and
+ * not the same array. */
 int dsvt_rms_norm(const dsvt_rms_cfg* cfg, const void* x, int64_t ld_x, const void* res, int64_t ld_res, int32_t n_rows, void* z, int64_t ld_z,
                   void* y, int64_t ld_y, const dsvt_rows8* rows8, void* stream);
 
@@ -447,8 +448,9 @@ int dsvt_rms_norm_backward(const dsvt_rms_cfg* cfg, const void* dy, int64_t ld_d
                            const void* d_sum, int64_t ld_dsum, int32_t n_rows, void* dx, int64_t ld_dx, float* d_gamma, void* ws, size_t ws_bytes,
                            void* stream);
 
-/* The MLP's activation, GELU(h) = h Phi(h), of h [device] [n_rows, C], in 8 bits, and h itself in 8 bits (either may be NULL); and its gradient, dh =
- * dy (Phi(k) + k phi(k)) with k = code * scale of the kept rows (dh may be dy itself, same stride).  Phi is off by at most 2e-7. */
+/* The MLP's activation, GELU(h) = h Phi(h), of h [device] [n_rows, C], in 8 bits, and h itself in 8 bits (either may be NULL, and
+ * both not the same arrays); and its gradient, dh =
+ * dy (Phi(k) + k phi(k)) with k = code * scale of the kept rows (dh may be dy itself, same stride).  Phi is off by at most 3e-7. */
 int dsvt_gelu_rows8(int32_t C, int32_t dtype, const void* h, int64_t ld_h, int32_t n_rows, const dsvt_rows8* out, const dsvt_rows8* kept, void* stream);
 int dsvt_gelu_rows8_backward(int32_t C, int32_t dtype, const dsvt_rows8* kept, const void* dy, int64_t ld_dy, int32_t n_rows, void* dh,
                              int64_t ld_dh, void* stream);
@@ -465,8 +467,9 @@ int dsvt_linear_rows8(const dsvt_linear8_cfg* cfg, const dsvt_rows8* x, int32_t 
 
 /* The gradients of a linear layer's weights and bias, from dy [device] [n_rows, out] and the layer's input as it was kept: d_w [device] [out, C] of
  * dtype (dy's) = sum over n of dy[n][o] s_n x[n][c], d_b [device] [out] float = sum of dy (NULL: not wanted); both written, not added to.
- * All sums are of 32 bits or more and do not depend on the order in which the kernels run.
- * ws [device] as for dsvt_rms_norm_backward. */
+ * BF16: s_n x[n][c] is rounded to bf16 as an operand of the product (relative to their norm d_w is off by 2.3e-3 in all where the rounding of the
+ * result alone is 1.7e-3); all sums are of 32 bits or more, and do not depend on the order in which the kernels run.  Rows less than 16 MiB
+ * apart (dy: 2^24 elements; DSVT_EUNSUPPORTED otherwise).  ws [device] as for dsvt_rms_norm_backward. */
 int dsvt_linear_rows8_weight_grad_workspace_size(int32_t C, int32_t out, int32_t dtype, int32_t n_rows, size_t* bytes);
 int dsvt_linear_rows8_weight_grad(int32_t C, int32_t out, int32_t dtype, const dsvt_rows8* x, const void* dy, int64_t ld_dy, int32_t n_rows,
                                   void* d_w, int64_t ld_dw, float* d_b, void* ws, size_t ws_bytes, void* stream);

@@ -1013,9 +1013,10 @@ def dsvt_linear_rows8_weight_grad(rows, dy, d_w=None, d_b=None, want_bias=True, 
         rc = lib().dsvt_linear_rows8_weight_grad_workspace_size(c, o, code, n, C.byref(b))
         if rc:
             _check("dsvt_linear_rows8_weight_grad", rc)
-        ws_bytes = b.value
-        ws = _new(stream, dev, dy, ws_bytes, torch.uint8)
-        p_ws = ws.data_ptr()
+        ws_bytes, p_ws = b.value, None
+        if ws_bytes:
+            ws = _new(stream, dev, dy, ws_bytes, torch.uint8)
+            p_ws = ws.data_ptr()
     else:
         p_ws, ws_bytes = _scratch(ws, dev)
     rc = lib().dsvt_linear_rows8_weight_grad(c, o, code, ref, dy.data_ptr(), ld, n, d_w.data_ptr(), ld_w, None if d_b is None else d_b.data_ptr(),

@@ -39,8 +39,8 @@ constexpr int kFewWaves = 8;
 
 template <typename T, int kTiles, int kAtOnce> __global__ __launch_bounds__(64 * kFewWaves) void k_linear8_few(Linear8Args a) {
   __shared__ i32x4 sums[kFewWaves - 1][kTiles][64];
-  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), m = lane & 15, g = lane >> 4, out0 = blockIdx.x * 16;
-  const int64_t row0 = (int64_t)blockIdx.y * 16 * kTiles;
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), m = lane & 15, g = lane >> 4, out0 = blockIdx.y * 16;
+  const int64_t row0 = (int64_t)blockIdx.x * 16 * kTiles;
   const int8_t* const w = a.w + (int64_t)(out0 + m < a.O ? out0 + m : a.O - 1) * a.ld_w;
   const int8_t* x[kTiles];
 #pragma unroll
@@ -364,7 +364,7 @@ template <typename T> int launch(const Linear8Args& a, hipStream_t st) {
   if (a.n <= 64 || a.ld_x >= (1 << 23) || a.ld_w >= (1 << 23)) {
     const auto few = [&](auto rows, auto at_once) {
       constexpr int kTiles = decltype(rows)::value;
-      const dim3 grid((unsigned)dsvt_ceil_div(a.O, 16), (unsigned)dsvt_ceil_div(a.n, 16 * kTiles));
+      const dim3 grid((unsigned)dsvt_ceil_div(a.n, 16 * kTiles), (unsigned)dsvt_ceil_div(a.O, 16));
       k_linear8_few<T, kTiles, decltype(at_once)::value><<<grid, 64 * kFewWaves, 0, st>>>(a);
     };
     const bool long_rows = a.C > 64 * kFewWaves * 2;

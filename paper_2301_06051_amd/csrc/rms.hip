@@ -199,6 +199,9 @@ __global__ __launch_bounds__(kThreads) void k_rms_long(RmsArgs a, int32_t rows) 
   }
 }
 
+// Rows that one workgroup sums up by itself: a second launch takes longer than the three more turns of rows.
+constexpr int kTurnsAlone = 4;
+
 uintptr_t starts(const RmsArgs& a, int e) {
   return (uintptr_t)a.x | (uintptr_t)a.res | (uintptr_t)a.dy | (uintptr_t)a.d_sum | (uintptr_t)a.z | (uintptr_t)a.y |
          (uintptr_t)((a.ld_x | a.ld_res | a.ld_dy | a.ld_dsum | a.ld_z | a.ld_y) * e);
@@ -237,7 +240,7 @@ extern "C" int dsvt_rms_norm(const dsvt_rms_cfg* cfg, const void* x, int64_t ld_
   if (const int rc = check(cfg, n_rows)) return rc;
   if (n_rows == 0) return DSVT_OK;
   const int e = cfg->dtype == DSVT_BF16 ? 2 : 4;
-  if (!y && !rows8) return DSVT_EINVAL;
+  if ((!y && !rows8) || (z && z == y)) return DSVT_EINVAL;
   if (bad_rows(x, ld_x, cfg->C, e) || (res && bad_rows(res, ld_res, cfg->C, e)) || (z && bad_rows(z, ld_z, cfg->C, e)) ||
       (y && bad_rows(y, ld_y, cfg->C, e)) || (rows8 && bad_rows8(rows8, cfg->C))) return DSVT_EINVAL;
   RmsArgs a = {};
@@ -286,7 +289,7 @@ extern "C" int dsvt_rms_norm_backward(const dsvt_rms_cfg* cfg, const void* dy, i
     a.partial = static_cast<float*>(ws);
     const int v = piece_elems(starts(a, e), a.C, e), lanes = row_lanes(cfg->C / v, v * e);
     const int64_t per = lanes ? kThreads / lanes : 1, all = dsvt_ceil_div(n_rows, per);
-    groups = (int32_t)(all < kBackwardGroups ? all : kBackwardGroups);
+    groups = (int32_t)(all <= kTurnsAlone ? 1 : all < kBackwardGroups ? all : kBackwardGroups);
     const int32_t rows = (int32_t)dsvt_ceil_div(n_rows, groups);
     if (lanes == 0) groups = (int32_t)dsvt_ceil_div(n_rows, rows);       // every workgroup has a row
     if (groups == 1) a.d_gamma = d_gamma;

@@ -128,6 +128,7 @@ int write(bool with_gelu, int32_t C, int32_t dtype, const void* x, int64_t ld_x,
   if (n_rows == 0) return DSVT_OK;
   const int e = dtype == DSVT_BF16 ? 2 : 4;
   if (bad_rows(x, ld_x, C, e) || (!out && !kept) || (out && bad_rows8(out, C)) || (kept && bad_rows8(kept, C))) return DSVT_EINVAL;
+  if (out && kept && (out->codes == kept->codes || out->scale == kept->scale)) return DSVT_EINVAL;
   Rows8Args a = {};
   a.x = x; a.ld_x = ld_x; a.n = n_rows; a.C = C;
   if (out) { a.out = out->codes; a.out_scale = out->scale; a.ld_out = out->ld; }

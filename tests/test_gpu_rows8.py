@@ -138,6 +138,27 @@ def test_rms_norm(n, c, dtype, form, res):
         assert torch.equal(dsvt.dsvt_rms_norm_backward(norm, dyd, xd, rd, dsd, dx=dsd)[0], dx)
 
 
+@pytest.mark.parametrize("c", [5, 192, 700, 9000])
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_rms_norm_of_special_values(c, dtype):
+    """Rows of zeros, with an infinity, a NaN, and of numbers whose squares are not: each by itself, in rows and in 8 bits."""
+    x = torch.randn((6, c), generator=_gen(c)).to(DT[dtype])
+    x[0] = 0
+    x[1, c // 2] = math.inf
+    x[2, 0] = math.nan
+    x[3] = 1e30
+    x[4, c - 1] = -math.inf
+    print("[case] special norms", c, dtype, flush=True)
+    norm = dsvt.RmsNorm(torch.ones(c, device="cuda"), dtype, EPS)
+    y, z = dsvt.dsvt_rms_norm(norm, x.cuda(), want_sum=True)
+    rows = dsvt.dsvt_rms_norm_rows8(norm, x.cuda())
+    assert torch.equal(z.cpu().nan_to_num(7), x.nan_to_num(7)) and not y[[0, 3]].any() and y[5].isfinite().all()
+    assert y[2].isnan().all() and y[1, c // 2].isnan() and y[4, c - 1].isnan()               # (infinity by infinity)
+    assert rows.scale[[1, 2, 4]].isnan().all() and not rows.codes[:5].any() and not rows.scale[[0, 3]].any() and bool(rows.scale[5] > 0)
+    dx, dg = dsvt.dsvt_rms_norm_backward(norm, torch.ones_like(x).cuda(), x.cuda())
+    assert dx[2].isnan().all() and dx[5].isfinite().all() and dg.isnan().any()
+
+
 def test_rms_norm_by_differences():
     """The gradient against quotients of differences of the forward call, in fp32."""
     g, n, c = _gen(5), 6, 48

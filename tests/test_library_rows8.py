@@ -46,6 +46,12 @@ def test_rows_are_refused():
             assert L.dsvt_gelu_rows8(W, BF, P, W, N, bad, None, None) == E and L.dsvt_gelu_rows8(W, BF, P, W, N, None, bad, None) == E
             assert L.dsvt_rms_norm(_rms(), P, W, None, 0, N, None, 0, P, W, bad, None) == E
     assert L.dsvt_gelu_rows8(W, BF, P, W, N, None, None, None) == E
+    far = P + (1 << 24)                            # two results in one place
+    assert L.dsvt_gelu_rows8(W, BF, far, W, N, _r8(scale=far), _r8(), None) == E and L.dsvt_gelu_rows8(W, BF, far, W, N, _r8(codes=far), _r8(), None) == E
+    assert L.dsvt_rms_norm(_rms(), far, W, None, 0, N, P, W, P, W, None, None) == E
+    # rows too far apart for a step of the weight gradient
+    assert L.dsvt_linear_rows8_weight_grad(W, O, BF, _r8(ld=1 << 24), P, O, N, P, W, None, P, 1 << 40, None) == U
+    assert L.dsvt_linear_rows8_weight_grad(W, O, BF, _r8(), P, 1 << 24, N, P, W, None, P, 1 << 40, None) == U
     # addresses that are no multiple of an element, strides below a row, no address
     for at, ld in ((P + 1, W), (P, W - 1), (None, W)):
         assert L.dsvt_keep_rows8(W, BF, at, ld, N, _r8(), None) == E
