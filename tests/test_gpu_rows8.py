@@ -203,7 +203,7 @@ def test_gelu(n, c, dtype, form):
 
 
 LINEAR = [(1, 1, 1), (1, 192, 576), (1, 4096, 300), (2, 15, 3), (5, 16, 17), (15, 17, 16), (16, 63, 64), (17, 64, 130), (33, 65, 192), (64, 99, 130), (100, 192, 384),
-          (128, 128, 128), (129, 200, 129), (257, 384, 192), (300, 1000, 257), (1000, 99, 130), (513, 64, 1000), (2000, 192, 576), (700, 576, 520), (260, 1040, 516)]
+          (128, 128, 128), (129, 200, 129), (257, 384, 192), (300, 1000, 257), (1000, 99, 130), (513, 64, 1000), (2000, 192, 576), (700, 576, 520), (260, 1040, 516), (70, 1100, 130), (500, 2064, 100), (64, 300, 200)]
 
 
 @pytest.mark.parametrize("n,c,o", LINEAR)
