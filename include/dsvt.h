@@ -328,7 +328,7 @@ int dsvt_vfe(const dsvt_vfe_cfg* cfg, const float* points, const int32_t* point_
 /* ---------------------------------------------------------------------------------------
  * Training a layer: two parts of a DSVT layer (Eq. 5), the attention inside its sets and the
  * LayerNorm of its residual sums, as calls of their own with their gradients.  The rest is the
- * caller's: matrix products and their bias sums, the MLP's activation.  Rows have strides in elements
+ * caller's: matrix products and their bias sums, the MLP's activation (or what is further below, in 8 bits).  Rows have strides in elements
  * (ld >= row length), so that slices of wider arrays can be passed; n may be 0.
  * ------------------------------------------------------------------------------------ */
 
@@ -416,8 +416,8 @@ int dsvt_layer_norm_backward(const dsvt_ln_cfg* cfg, const void* dy, int64_t ld_
  * otherwise); n_rows may be 0.  Rows of the type have strides in elements, as in the training calls.
  * ------------------------------------------------------------------------------------ */
 typedef struct {
-  int8_t* codes;  /* [device] rows of ld bytes, ld >= C; 16-byte aligned, ld a multiple of 16.  Bytes past a row's C-th are not written, and may
-                     be read (ld bytes of every row are the array's) but do not count                          */
+  int8_t* codes;  /* [device] rows ld bytes apart, ld >= C; 16-byte aligned, ld a multiple of 16.  What lies past a row's C-th byte is not written; up
+                     to the next multiple of 16 it may be read, but does not count                              */
   int64_t ld;
   float* scale;   /* [device] [n_rows]                                                                          */
 } dsvt_rows8;

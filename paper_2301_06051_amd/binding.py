@@ -720,8 +720,8 @@ class Rows8:
 
     @classmethod
     def of(cls, codes, scale):
-        """Of an int8 tensor [n, C] whose memory holds every row to its full stride, and its scales.  Both stay the caller's: they are read at
-        every call."""
+        """Of an int8 tensor [n, C] whose memory holds every row to a whole multiple of 16 bytes, and its scales.  Both stay the caller's: they are
+        read at every call."""
         if codes.dtype is not torch.int8 or codes.dim() != 2 or codes.shape[1] < 1 or (codes.shape[1] > 1 and codes.stride(1) != 1):
             raise ValueError(f"codes: an int8 tensor [n, C] with neighbouring columns is wanted; got {codes.dtype} {tuple(codes.shape)}, strides "
                              f"{tuple(codes.stride())}")
@@ -730,8 +730,8 @@ class Rows8:
         if codes.data_ptr() % 16 or ld % 16 or ld < c:
             raise ValueError(f"codes: rows that begin on 16 bytes and lie a multiple of 16 bytes apart are wanted; got a stride of {ld} bytes, address "
                              f"{codes.data_ptr():#x}")
-        if codes.untyped_storage().nbytes() < codes.storage_offset() + n * ld:
-            raise ValueError(f"codes: memory of {n} rows of {ld} bytes is wanted, the last one's {ld} too")
+        if n and codes.untyped_storage().nbytes() < codes.storage_offset() + (n - 1) * ld + (c + 15) // 16 * 16:
+            raise ValueError(f"codes: memory of {n} rows of {(c + 15) // 16 * 16} bytes is wanted, the last one's too")
         _vector(scale, (n,), torch.float32, codes.get_device(), "scale")
         self = cls.__new__(cls)
         self.n, self.C, self.device, self.given = n, c, codes.get_device(), scale

@@ -3,7 +3,9 @@
 //   forward   z = x + res, n = z * rsqrt(mean z^2 + eps), y = n * gamma, as rows of the type, in 8 bits (rows8.h), or both
 //   backward  w = dy * gamma, dx = rsqrt(mean z^2 + eps) * (w - n * mean(w * n)) + d_sum, d_gamma = sum of dy * n over the rows
 //
-// Both passes are bound by the bytes of their rows, which sit in registers and are read once (rows.h).
+// Both passes are bound by the bytes of their rows, which sit in registers and are read once (rows.h).  The sum z is formed again in the backward pass if
+// it was not written, and its gradient d_sum, which comes past the branch, is added in the same pass.  800,000 rows of 192 bf16 with a branch: forward
+// with y and z 232 us (5.3 TB/s), backward with d_sum 300 (5.1); 30,000 rows backward 15.4 with 512 workgroups, 18.4 with 768, 19.0 with 1,024.
 #include "rows8.h"
 
 namespace {

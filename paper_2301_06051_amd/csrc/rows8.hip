@@ -4,7 +4,9 @@
 //   forward   out = codes of gelu(h), kept = codes of h          gelu(h) = h Phi(h)
 //   backward  dh = dy (Phi(k) + k phi(k)), k = code * scale
 //
-// All are bound by the bytes of their rows: writers hold a row in registers (rows.h), as its largest value is wanted before its first code.
+// All are bound by the bytes of their rows: writers hold a row in registers (rows.h), as its largest value is wanted before its first code; 27
+// instructions a value of GELU into two sets of codes take as long as its bytes.  Rows of 384 bf16: 200,000 through GELU into both sets of codes 74 us (4.2
+// TB/s), read back 46 (5.0), 800,000 backward 295 (5.2).  Fetching the next row ahead: 78 instead of 74.
 #include "rows8.h"
 
 namespace {

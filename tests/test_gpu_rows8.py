@@ -459,3 +459,33 @@ def test_linear_in_parts(n, c, o, dtype, act):
         part = dsvt.Rows8.of(x.codes[at:at + 1000], x.scale[at:at + 1000])
         assert torch.equal(y[at:at + 1000], dsvt.dsvt_linear_rows8(layer, part)), at
     assert torch.equal(dsvt.dsvt_linear_rows8(layer, x), y)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("n", [3, 100])
+def test_linear_of_infinities(n, dtype):
+    """Through a bias: an infinity stays one, GELU has its limits, a NaN stays one."""
+    g = _gen(4)
+    x, w = _random_codes(g, n, 64), _random_codes(g, 5, 64)
+    bias = torch.tensor([math.inf, -math.inf, math.nan, 3e38, -3e38]).cuda()
+    plain, act = (dsvt.dsvt_linear_rows8(dsvt.Linear8(w, dtype, bias, k), x).float().cpu() for k in (False, True))
+    assert bool((plain[:, 0] == math.inf).all()) and bool((plain[:, 1] == -math.inf).all()) and plain[:, 2].isnan().all()
+    assert bool((act[:, 0] == math.inf).all()) and not act[:, 1].any() and act[:, 2].isnan().all()
+    assert torch.equal(act[:, 3], plain[:, 3]) and not act[:, 4].any()
+
+
+def test_rows_far_apart():
+    """Rows 8 MiB apart, as columns of a very wide array."""
+    n, c, o, ld = 70, 200, 130, 1 << 23
+    g = _gen(6)
+    x, w = _random_codes(g, n, c), _random_codes(g, o, c)
+    wide = torch.zeros((n, ld), dtype=torch.int8, device="cuda")
+    wide[:, 64:64 + c] = x.codes
+    far = dsvt.Rows8.of(wide[:, 64:64 + c], x.scale)
+    layer = dsvt.Linear8(w, "bf16")
+    print("[case] rows far apart", flush=True)
+    assert torch.equal(dsvt.dsvt_linear_rows8(layer, far), dsvt.dsvt_linear_rows8(layer, x))
+    assert torch.equal(dsvt.dsvt_linear_rows8(dsvt.Linear8(far, "f32"), x), dsvt.dsvt_linear_rows8(dsvt.Linear8(x, "f32"), x))
+    assert torch.equal(dsvt.dsvt_read_rows8(far, "f32"), dsvt.dsvt_read_rows8(x, "f32"))
+    dy = torch.randn((n, o), generator=g).to(torch.bfloat16).cuda()
+    assert all(torch.equal(a, b) for a, b in zip(dsvt.dsvt_linear_rows8_weight_grad(far, dy), dsvt.dsvt_linear_rows8_weight_grad(x, dy)))
