@@ -708,6 +708,11 @@ def _new(stream, device, like, shape, dtype):
     return like.new_empty(shape, dtype=dtype) if stream is None else _new_on(stream, device, like, shape, dtype)
 
 
+def _new_like(stream, device, like):
+    """Uninitialised rows of the type and shape of rows `like`, with nothing between them."""
+    return torch.empty_like(like, memory_format=torch.contiguous_format) if stream is None else _new_on(stream, device, like, like.shape, like.dtype)
+
+
 def _new_of(stream, device, rows, shape, dtype):
     return _new(stream, device, rows._codes if rows._memory is None else rows._memory, shape, dtype)
 
@@ -827,19 +832,28 @@ class RmsNorm:
 
 
 def _rms_norm(call, rms, x, res, z, y, rows, want_sum, stream, dev):
-    """What dsvt_rms_norm and dsvt_rms_norm_rows8 share; returns z."""
+    """What dsvt_rms_norm (rows is None) and dsvt_rms_norm_rows8 share; returns (y, z).  New tensors have x's type and shape, which are looked at."""
     n, c, dtype = x.shape[0], rms.C, rms.dtype
     ld_x = _rows(x, (n, c), dtype, dev, "x")
     ld_res, p_res = (0, None) if res is None else (_rows(res, (n, c), dtype, dev, "res"), res.data_ptr())
-    ld_y, p_y = (0, None) if y is None else (_rows(y, (n, c), dtype, dev, "y"), y.data_ptr())
-    if z is None and want_sum:
-        z = torch.empty_like(x) if stream is None else _new_on(stream, dev, x, (n, c), dtype)
-    ld_z, p_z = (0, None) if z is None else (_rows(z, (n, c), dtype, dev, "z"), z.data_ptr())
-    rc = lib().dsvt_rms_norm(rms.ref, x.data_ptr(), ld_x, p_res, ld_res, n, p_z, ld_z, p_y, ld_y, None if rows is None else rows.ref,
+    ld_y, p_y, ld_z, p_z, ref = c, None, c, None, None
+    if rows is not None:
+        ref = rows.ref
+    elif y is None:
+        y = _new_like(stream, dev, x)
+        p_y = y.data_ptr()
+    else:
+        ld_y, p_y = _rows(y, (n, c), dtype, dev, "y"), y.data_ptr()
+    if z is not None:
+        ld_z, p_z = _rows(z, (n, c), dtype, dev, "z"), z.data_ptr()
+    elif want_sum:
+        z = _new_like(stream, dev, x)
+        p_z = z.data_ptr()
+    rc = lib().dsvt_rms_norm(rms.ref, x.data_ptr(), ld_x, p_res, ld_res, n, p_z, ld_z, p_y, ld_y, ref,
                              _current_stream(dev) if stream is None else stream)
     if rc:
         _check(call, rc)
-    return z
+    return y, z
 
 
 def dsvt_rms_norm(rms, x, res=None, y=None, z=None, want_sum=False, stream=None):
@@ -849,9 +863,7 @@ def dsvt_rms_norm(rms, x, res=None, y=None, z=None, want_sum=False, stream=None)
     dev = _current_device()
     if rms.device != dev:
         _elsewhere(dev, rms)
-    if y is None:
-        y = torch.empty_like(x) if stream is None else _new_on(stream, dev, x, x.shape, x.dtype)
-    z = _rms_norm("dsvt_rms_norm", rms, x, res, z, y, None, want_sum, stream, dev)
+    y, z = _rms_norm("dsvt_rms_norm", rms, x, res, z, y, None, want_sum, stream, dev)
     return y if z is None else (y, z)
 
 
@@ -866,7 +878,7 @@ def dsvt_rms_norm_rows8(rms, x, res=None, out=None, z=None, want_sum=False, stre
         out = Rows8._like(stream, dev, x, x.shape[0], rms.C)
     else:
         _rows8(out, x.shape[0], rms.C, dev, "out")
-    z = _rms_norm("dsvt_rms_norm_rows8", rms, x, res, z, None, out, want_sum, stream, dev)
+    z = _rms_norm("dsvt_rms_norm_rows8", rms, x, res, z, None, out, want_sum, stream, dev)[1]
     return out if z is None else (out, z)
 
 
@@ -892,7 +904,7 @@ def dsvt_rms_norm_backward(rms, dy, x, res=None, d_sum=None, dx=None, d_gamma=No
     ld_res, p_res = (0, None) if res is None else (_rows(res, (n, c), dtype, dev, "res"), res.data_ptr())
     ld_sum, p_sum = (0, None) if d_sum is None else (_rows(d_sum, (n, c), dtype, dev, "d_sum"), d_sum.data_ptr())
     if dx is None:
-        dx, ld_dx = _new(stream, dev, x, (n, c), dtype), c
+        dx, ld_dx = _new_like(stream, dev, x), c
     else:
         ld_dx = _rows(dx, (n, c), dtype, dev, "dx")
     if d_gamma is None:
