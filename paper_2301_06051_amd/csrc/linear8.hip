@@ -6,8 +6,9 @@
 //
 // Long rows are bound by the matrix cores, which three things feed at about the same rate: LDS (a wavefront of 128 x 64 reads 6 KB for eight
 // products of 32 clocks), the loads of the next step, and the barrier of a step.  4,096 x 16,384 -> 4,096: 230 us, 2,390 TOP/s (the library's product
-// of 8,192^3 in 8 bits 2,284 on the same card), 8,192 x 4,096 -> 4,096 with its 67 MB of results 122 to 132.  Short rows are bound by their results: 800,000 x 192 -> 576
-// 293 us, 3.7 TB/s, of which rows fetched and multiplied without being written take 217, written without being fetched 255.
+// of 8,192^3 in 8 bits 2,284 on the same card), 8,192 x 4,096 -> 4,096 with its 67 MB of results 120 to 130.  Short rows are bound by their results, whose
+// instructions (a conversion, a product and an fma each) and stores have to run beside the products: 800,000 x 192 -> 576 183 us, 5.9 TB/s, by wavefronts
+// on their own; 280 in tiles, whose workgroups do one after the other (220 without the results' instructions, 250 without their stores).
 #include "rows8.h"
 #include <cmath>
 #include <type_traits>
@@ -26,6 +27,7 @@ struct Linear8Args {
   int64_t ld_x, ld_w, ld_y;
   int32_t n, C, O;
   int32_t act;
+  bool leaves;                                    // rows_out
 };
 
 // The first `left` bytes of p, zeros behind them.
@@ -123,6 +125,148 @@ __device__ __forceinline__ void float_to_lds(const float* base, uint32_t off, ui
 // Until at most kLater loads of this wavefront are on their way and its LDS reads are done; then until all wavefronts are there.
 template <int kLater> __device__ __forceinline__ void wait_for_stage() {
   asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)\n\ts_barrier" ::"n"(kLater) : "memory");
+}
+
+// Results on their way out: kRowsOut rows of kWide values lie in a wavefront's LDS in pieces of 16 bytes, those of a row permuted, and are written row by
+// row, in pieces that begin on any value.  Where rows are whole cache lines, stores are marked to leave the caches first (`leaves`), as rows and weights
+// are to stay: 200,000 x 256 -> 1,024 132 -> 114 us, 100,000 x 384 -> 192 27 -> 24, and with a call that reads the results behind it 100,000 x 192 -> 576
+// 84 -> 79 (30,000 the same).  Where they are not, lines would leave in parts: 400,000 x 200 -> 131 107 us marked, 72 not, 84 a value at a time.
+template <int PR> __device__ __forceinline__ int spot(int row, int p) { return row * PR + (p ^ (PR == 4 ? row >> 1 & 3 : row & 7)); }
+template <typename T, int kWide, int kRowsOut>
+__device__ __forceinline__ void rows_out(const typename Piece<T, 16 / sizeof(T)>::type* out, T* y, int64_t ld_y, int rows, int outs, bool leaves, int lane) {
+  constexpr int V = 16 / (int)sizeof(T), PR = kWide / V, kAtOnce = 64 / PR;     // rows of a store
+  typedef typename Piece<T, V>::type P;
+  typedef T Anywhere __attribute__((ext_vector_type(V), aligned(sizeof(T))));   // (rows begin on their type's alignment)
+  const int row = lane / PR, c = lane % PR * V;
+  T* const to = y + row * ld_y + c;
+  const auto store = [&](int r, P p) {
+    Anywhere* const at = reinterpret_cast<Anywhere*>(to + r * ld_y);
+    if (leaves) {
+      asm volatile("");                           // (as in write_out)
+      __builtin_nontemporal_store((Anywhere)p, at);
+      asm volatile("");
+    } else *at = p;
+  };
+  if (rows == kRowsOut && outs == kWide) {
+#pragma unroll
+    for (int r = 0; r < kRowsOut; r += kAtOnce) store(r, out[spot<PR>(r + row, lane % PR)]);
+  } else {
+#pragma unroll
+    for (int r = 0; r < kRowsOut; r += kAtOnce) {
+      if (r + row >= rows || c >= outs) continue;
+      const P p = out[spot<PR>(r + row, lane % PR)];
+      if (c + V <= outs) store(r, p);
+      else {
+#pragma unroll
+        for (int i = 0; i < V - 1; ++i)
+          if (c + i < outs) to[r * ld_y + i] = p[i];
+      }
+    }
+  }
+}
+
+// Short rows: the weights of 64 outputs stay in a wavefront's registers, and it goes through blocks of 32 rows, which it reads straight into
+// fragments, one block ahead.  Nothing is waited for together, so that one wavefront's products, results and stores run beside those of others.
+// Wavefronts of the same rows are neighbours.  kSteps: of 32 columns, of which kWhole lie in the row for certain.
+constexpr int kShortWaves = 4;
+// Wavefronts a SIMD: two, a third one where registers allow it and it measured better (800,000 x 192 -> 576 198 -> 186 us; 100,000 x 64 -> 128 6.9 -> 8.7).
+constexpr int short_simd(int steps, int elem) { return steps == 6 && elem == 2 ? 3 : 2; }
+
+template <typename T, int kSteps, int kWhole> __global__ __launch_bounds__(64 * kShortWaves, short_simd(kSteps, sizeof(T))) void k_linear8_short(Linear8Args a, int shares) {
+  constexpr int V = 16 / (int)sizeof(T), PR = 64 / V, kRowsOut = sizeof(T) == 2 ? 32 : 16;
+  typedef typename Piece<T, V>::type P;
+  __shared__ P all_out[kShortWaves][kRowsOut * PR];
+  __shared__ float all_ends[kShortWaves][2][64];
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), m = lane & 31, h = lane >> 5;
+  const int blocks_n = (a.O + 63) / 64, blocks_m = (a.n + 31) / 32;
+  const int groups = gridDim.x >> 3, at = ((blockIdx.x & 7) * groups + (blockIdx.x >> 3)) * kShortWaves + wave, share = at / blocks_n;
+  if (share >= shares) return;
+  const int out0 = at % blocks_n * 64, outs = a.O - out0 < 64 ? a.O - out0 : 64;
+  const int last_piece = (a.C - 1) >> 4 << 4;
+
+  i32x4 w[2][kSteps];
+  const int out_m = (m >> 2 & 1) * 16 + (m >> 3) * 4 + (m & 3);
+#pragma unroll
+  for (int j = 0; j < 2; ++j) {
+    const int o = 32 * j + out_m;
+    const int8_t* row = a.w + (int64_t)(out0 + (o < outs ? o : outs - 1)) * a.ld_w;
+#pragma unroll
+    for (int k = 0; k < kSteps; ++k) {
+      const int c = 32 * k + 16 * h;
+      w[j][k] = first_bytes(*reinterpret_cast<const i32x4*>(row + (c < last_piece ? c : last_piece)), a.C - c);
+    }
+  }
+  float* const ends = all_ends[wave][0];
+  {
+    const int o = out0 + (lane < outs ? lane : outs - 1);
+    ends[lane] = a.t[o];
+    ends[64 + lane] = a.bias ? a.bias[o] : 0.f;
+  }
+  P* const out = all_out[wave];
+  const auto in_order = []() {
+    __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
+    __builtin_amdgcn_wave_barrier();
+    __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
+  };
+  in_order();
+
+  i32x4 x[kSteps];
+  float s;
+  const auto fetch = [&](int block) {
+    const int64_t row0 = (int64_t)block * 32;
+    const int8_t* const base = a.x + row0 * a.ld_x;
+    const uint32_t row = a.n - row0 > m ? m : (uint32_t)(a.n - row0) - 1u, off = row * (uint32_t)a.ld_x;
+#pragma unroll
+    for (int k = 0; k < kSteps; ++k) {
+      const int c = 32 * k + 16 * h;
+      x[k] = *reinterpret_cast<const i32x4*>(base + (off + (k < kWhole || c < last_piece ? c : last_piece)));
+    }
+    s = a.s[row0 + row];
+  };
+  int block = share;
+  if (block < blocks_m) fetch(block);
+  for (; block < blocks_m; block += shares) {
+    i32x16 acc[2];
+#pragma unroll
+    for (int j = 0; j < 2; ++j) {
+      acc[j] = i32x16{};
+#pragma unroll
+      for (int k = 0; k < kSteps; ++k) acc[j] = __builtin_amdgcn_mfma_i32_32x32x32_i8(w[j][k], x[k], acc[j], 0, 0, 0);
+    }
+    const float scale = s;
+    fetch(block + shares < blocks_m ? block + shares : block);
+    const int64_t row0 = (int64_t)block * 32;
+#pragma unroll
+    for (int part = 0; part < 32 / kRowsOut; ++part) {
+      const int left = (int)(a.n - row0 - kRowsOut * part < kRowsOut ? a.n - row0 - kRowsOut * part : kRowsOut);
+      if (left <= 0) break;
+      if (m / kRowsOut == part) {
+        const auto results = [&](auto act) {
+#pragma unroll
+          for (int j = 0; j < 2; ++j) {
+            int from = 32 * j + 16 * h;
+            asm volatile("" : "+v"(from));        // (read again for every block: registers hold the weights)
+#pragma unroll
+            for (int e = 0; e < 16; e += V) {
+              float f[V];
+#pragma unroll
+              for (int k = 0; k < V; k += 4) {
+                const f32x4 t = *reinterpret_cast<const f32x4*>(ends + from + e + k), bias = *reinterpret_cast<const f32x4*>(ends + 64 + from + e + k);
+#pragma unroll
+                for (int u = 0; u < 4; ++u) f[k + u] = act(fmaf((float)acc[j][e + k + u] * scale, t[u], bias[u]));
+              }
+              out[spot<PR>(m % kRowsOut, (32 * j + 16 * h + e) / V)] = narrow<T, V>(f);
+            }
+          }
+        };
+        if (a.act) results([](float v) { return activation(v); });
+        else results([](float v) { return v; });
+      }
+      in_order();
+      rows_out<T, 64, kRowsOut>(out, static_cast<T*>(a.y) + (row0 + kRowsOut * part) * a.ld_y + out0, a.ld_y, left, outs, a.leaves, lane);
+      in_order();
+    }
+  }
 }
 
 // Tiles of kRowsT rows and kOutsT outputs, shared by kM x kN wavefronts.  Their columns, kColumns at a time, go from memory into one of kBuffers
@@ -235,7 +379,6 @@ __global__ __launch_bounds__(64 * kM * kN) void k_linear8_tiles(Linear8Args a) {
       for (int j = 0; j < TN; ++j) acc[i][j] = __builtin_amdgcn_mfma_i32_32x32x32_i8(f.p[j], f.q[i], acc[i][j], 0, 0, 0);
   };
   static_assert(kSteps % 2 == 0, "fragments change places");
-  const auto spot = [](int row, int p) { return row * PR + (p ^ (PR == 4 ? row >> 1 & 3 : row & 7)); };
 
   // The fragments of a product are read while the one before is under way, the first ones of a buffer behind the barrier at which it is waited for.
   // At that barrier all wavefronts are done with the buffer before, which is then fetched into.
@@ -290,8 +433,7 @@ __global__ __launch_bounds__(64 * kM * kN) void k_linear8_tiles(Linear8Args a) {
     const float* const ends = all_ends + ends_at * S::kEndPlaces;
     ends_at = ends_at + 1 < kBuffers ? ends_at + 1 : 0;
     const int first_out = at.out0 + wn * kWide, outs = a.O - first_out < kWide ? a.O - first_out : kWide;
-    const bool whole_rows = a.n - at.row0 >= kRowsT && outs == kWide;
-    const bool wide = outs % V == 0 && ((uintptr_t)a.y & 15u) == 0 && a.ld_y * (int64_t)sizeof(T) % 16 == 0, whole = whole_rows && wide;
+    const bool whole = a.n - at.row0 >= kRowsT && outs == kWide;
     stored = whole ? kBuffers - 1 : 0;
 #pragma unroll
     for (int i = 0; i < TM; ++i) {
@@ -317,7 +459,7 @@ __global__ __launch_bounds__(64 * kM * kN) void k_linear8_tiles(Linear8Args a) {
 #pragma unroll
                   for (int u = 0; u < 4; ++u) f[k + u] = act(fmaf((float)acc[i][j][e + k + u] * s, t[u], bias[u]));
                 }
-                out[spot(m % kRowsOut, (32 * j + 16 * h + e) / V)] = narrow<T, V>(f);
+                out[spot<PR>(m % kRowsOut, (32 * j + 16 * h + e) / V)] = narrow<T, V>(f);
               }
           };
           if (a.act) results([](float v) { return activation(v); });
@@ -327,26 +469,7 @@ __global__ __launch_bounds__(64 * kM * kN) void k_linear8_tiles(Linear8Args a) {
         __builtin_amdgcn_wave_barrier();
         __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
         T* y = static_cast<T*>(a.y) + (from + kRowsOut * part) * a.ld_y + first_out;
-        constexpr int kAtOnce = 64 / PR;          // rows of a store
-        if (whole) {
-#pragma unroll
-          for (int r = 0; r < kRowsOut; r += kAtOnce) {
-            const int row = r + lane / PR, p = lane % PR;
-            *reinterpret_cast<P*>(y + row * a.ld_y + p * V) = out[spot(row, p)];
-          }
-        } else if (wide) {
-#pragma unroll
-          for (int r = 0; r < kRowsOut; r += kAtOnce) {
-            const int row = r + lane / PR, p = lane % PR;
-            if (row < rows && p * V < outs) *reinterpret_cast<P*>(y + row * a.ld_y + p * V) = out[spot(row, p)];
-          }
-        } else {
-          constexpr int kAtOnce = 64 / kWide;
-          for (int r = 0; r < kRowsOut; r += kAtOnce) {
-            const int row = r + lane / kWide, c = lane % kWide;
-            if (row < rows && c < outs) y[row * a.ld_y + c] = reinterpret_cast<const T*>(out + spot(row, c / V))[c % V];
-          }
-        }
+        rows_out<T, kWide, kRowsOut>(out, y, a.ld_y, rows, outs, a.leaves, lane);
         __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
         __builtin_amdgcn_wave_barrier();
         __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
@@ -382,13 +505,35 @@ template <typename T> int launch(const Linear8Args& a, hipStream_t st) {
     else long_rows ? few(std::integral_constant<int, 2>(), std::integral_constant<int, 4>()) : few(std::integral_constant<int, 2>(), std::integral_constant<int, 2>());
     return DSVT_OK;
   }
+  // Short rows of which every wavefront has two blocks at least; with results of 32 bits or GELU, which cost more, rows up to 256.  us by wavefronts on their
+  // own and in the best tiles: 800,000 x 192 -> 576 183 and 279, 30,000 11.7 and 13.0, 100,000 x 64 -> 128 6.9 and 10.2, 200,000 x 256 -> 1,024 122 and 112, of 32
+  // bits 155 and 177, with GELU 182 and 195, 100,000 x 384 -> 192 27 and 22; with one block 9,973 x 99 -> 130 5.9 and 5.0.
+  const bool costly = a.act || sizeof(T) == 4;       // results
+  if (a.C <= (costly ? 256 : 192)) {
+    const int64_t blocks_n = dsvt_ceil_div(a.O, 64), blocks_m = dsvt_ceil_div(a.n, 32);
+    const auto go = [&](auto steps, auto whole) {
+      constexpr int kSteps = decltype(steps)::value;
+      const int64_t at_once = (int64_t)kComputeUnits * 4 * short_simd(kSteps, sizeof(T)) / blocks_n, rounds = dsvt_ceil_div(blocks_m, at_once);
+      if (rounds < 2) return false;
+      const int64_t shares = rounds <= 3 ? dsvt_ceil_div(blocks_m, rounds) : at_once;
+      const unsigned grid = (unsigned)dsvt_ceil_div(dsvt_ceil_div(shares * blocks_n, kShortWaves), 8) * 8;
+      k_linear8_short<T, kSteps, decltype(whole)::value><<<grid, 64 * kShortWaves, 0, st>>>(a, (int)shares);
+      return true;
+    };
+    if (a.C <= 64 ? go(std::integral_constant<int, 2>(), std::integral_constant<int, 0>())
+        : a.C <= 128 ? go(std::integral_constant<int, 4>(), std::integral_constant<int, 2>())
+        : a.C <= 192 ? go(std::integral_constant<int, 6>(), std::integral_constant<int, 4>())
+                     : go(std::integral_constant<int, 8>(), std::integral_constant<int, 6>()))
+      return DSVT_OK;
+  }
   // The largest tiles that leave little of a last round over the 256 compute units empty: they read least from LDS and memory for a product.  us a
-  // call with tiles of 256 x 256, 128 x 128, 128 x 64, 64 x 64 (the first two stay): 8,192 x 4,096 -> 4,096 (512 of the largest tiles) 132, 160, 198, 304;
-  // 800,000 x 192 -> 576 293, 333, 368, 423; 30,000 x 192 -> 576 (354) 18.3, 15.0, 15.5, 15.5; 10,000 x 512 -> 2,048 25.7, 22.6, 25.5, 31.3; 30,000 x 384 -> 192
-  // 12.9, 10.8, 9.4, 10.9; 1,024 x 2,048 -> 2,048 27.7, 15.4, 12.6, 11.2.
-  const int64_t large = tiles(256, 256), rounds = dsvt_ceil_div(large, kComputeUnits);
-  if (10 * large >= 8 * rounds * kComputeUnits) return launch_tiles<T, 256, 256, 2, 4, 128, 2, 1>(a, st);
-  if (tiles(128, 128) >= 4 * kComputeUnits) return launch_tiles<T, 128, 128, 4, 2, 128, 2, 2>(a, st);
+  // call with tiles of 256 x 256, 128 x 128, 128 x 64, 64 x 64 (the first two stay): 8,192 x 4,096 -> 4,096 125, 150, 172, 300; 10,000 x 512 -> 2,048 26.6, 20.2,
+  // 24.4, 30.2; 30,000 x 384 -> 192 12.0, 9.0, 8.1, 9.9; 1,024 x 2,048 -> 2,048 27.2, 14.8, 12.3, 10.6; 200,000 x 512 -> 64 49, 32, 30.5; 100,000 x 1,024 -> 320 72, 58, 60.
+  // A workgroup alone on its compute unit does nothing beside results that cost more: 200,000 x 256 -> 1,024 112, 126, 156, but of 32 bits 191, 177, 209, with
+  // GELU 209, 195, 211; 16,384 x 512 -> 4,096 of 32 bits 75, 82, with GELU 86, 86.
+  const int64_t rounds = dsvt_ceil_div(tiles(256, 256), kComputeUnits);
+  if ((int64_t)a.n * a.O >= rounds * (kComputeUnits * 256 * 256 / 5 * 4) && !(costly && a.C < 512)) return launch_tiles<T, 256, 256, 2, 4, 128, 2, 1>(a, st);
+  if (tiles(128, 128) >= 4 * kComputeUnits && a.O > 64) return launch_tiles<T, 128, 128, 4, 2, 128, 2, 2>(a, st);
   if (tiles(128, 64) >= 2 * kComputeUnits) return launch_tiles<T, 128, 64, 4, 1, 128, 2, 0>(a, st);
   return launch_tiles<T, 64, 64, 2, 2, 64, 3, 0>(a, st);
 }
@@ -405,6 +550,7 @@ extern "C" int dsvt_linear_rows8(const dsvt_linear8_cfg* cfg, const dsvt_rows8* 
   if (bad_rows8(x, cfg->C) || bad_rows(y, ld_y, cfg->out, cfg->dtype == DSVT_BF16 ? 2 : 4)) return DSVT_EINVAL;
   Linear8Args a = {};
   a.x = x->codes; a.s = x->scale; a.ld_x = x->ld; a.w = cfg->w.codes; a.t = cfg->w.scale; a.ld_w = cfg->w.ld; a.bias = cfg->bias;
+  a.leaves = (((uintptr_t)y | (uintptr_t)(ld_y * (cfg->dtype == DSVT_BF16 ? 2 : 4))) & 127u) == 0;
   a.y = y; a.ld_y = ld_y; a.n = n_rows; a.C = cfg->C; a.O = cfg->out; a.act = cfg->act;
   hipStream_t st = (hipStream_t)stream;
   {

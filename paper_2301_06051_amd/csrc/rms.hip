@@ -5,7 +5,7 @@
 //
 // Both passes are bound by the bytes of their rows, which sit in registers and are read once (rows.h).  The sum z is formed again in the backward pass if
 // it was not written, and its gradient d_sum, which comes past the branch, is added in the same pass.  800,000 rows of 192 bf16 with a branch: forward
-// with y and z 232 us (5.3 TB/s), backward with d_sum 300 (5.1); 30,000 rows backward 15.4 with 512 workgroups, 18.4 with 768, 19.0 with 1,024.
+// with y and z 228 us (5.4 TB/s), backward with d_sum 287 (5.3); 30,000 rows backward 15.4 with 512 workgroups, 18.4 with 768, 19.0 with 1,024.
 #include "rows8.h"
 
 namespace {
@@ -20,6 +20,7 @@ struct RmsArgs {
   int64_t ld_x, ld_res, ld_dy, ld_dsum, ld_z, ld_y, ld_codes;
   int32_t n, C;
   float eps;
+  bool leaves;                                    // write_out
 };
 
 // z = x + res in 32 bits; returns rsqrt(mean z^2 + eps)
@@ -62,7 +63,7 @@ __global__ __launch_bounds__(kThreads) void k_rms_forward(RmsArgs a) {
       P* out = reinterpret_cast<P*>(static_cast<T*>(a.z) + row * a.ld_z);
 #pragma unroll
       for (int r = 0; r < R; ++r)
-        if (r * kLanes + part < pieces) out[r * kLanes + part] = narrow<T, V>(z[r]);
+        if (r * kLanes + part < pieces) write_out(out + r * kLanes + part, narrow<T, V>(z[r]), a.leaves);
     }
 #pragma unroll
     for (int r = 0; r < R; ++r)
@@ -72,7 +73,7 @@ __global__ __launch_bounds__(kThreads) void k_rms_forward(RmsArgs a) {
       P* out = reinterpret_cast<P*>(static_cast<T*>(a.y) + row * a.ld_y);
 #pragma unroll
       for (int r = 0; r < R; ++r)
-        if (r * kLanes + part < pieces) out[r * kLanes + part] = narrow<T, V>(z[r]);
+        if (r * kLanes + part < pieces) write_out(out + r * kLanes + part, narrow<T, V>(z[r]), a.leaves);
     }
     if (a.codes) store_codes<V, kLanes, R>(z, part, pieces, a.codes + row * a.ld_codes, a.scale + row, st);
   }
@@ -119,7 +120,7 @@ __global__ __launch_bounds__(kThreads) void k_rms_backward(RmsArgs a) {
 #pragma unroll
         for (int i = 0; i < V; ++i) n[r][i] += f[i];
       }
-      if (r * kLanes + part < pieces) out[r * kLanes + part] = narrow<T, V>(n[r]);
+      if (r * kLanes + part < pieces) write_out(out + r * kLanes + part, narrow<T, V>(n[r]), a.leaves);
     }
   }
   // the workgroup's sums: over the rows of a wavefront across lanes, over its wavefronts in LDS
@@ -250,6 +251,7 @@ extern "C" int dsvt_rms_norm(const dsvt_rms_cfg* cfg, const void* x, int64_t ld_
   a.ld_x = ld_x; a.ld_res = res ? ld_res : 0; a.ld_z = z ? ld_z : 0; a.ld_y = y ? ld_y : 0; a.n = n_rows; a.C = cfg->C; a.eps = cfg->eps;
   if (rows8) { a.codes = rows8->codes; a.scale = rows8->scale; a.ld_codes = rows8->ld; }
   const int v = piece_elems(starts(a, e), a.C, e), lanes = row_lanes(cfg->C / v, v * e);
+  a.leaves = v * e == 16 && leaves_caches(n_rows, cfg->C, (z != nullptr) + (y != nullptr), e);
   const int64_t per = lanes ? kThreads / lanes : 1, all = dsvt_ceil_div(n_rows, per);
   const unsigned groups = (unsigned)(all < kForwardGroups ? all : kForwardGroups);
   const int32_t rows = (int32_t)dsvt_ceil_div(n_rows, groups);
@@ -290,6 +292,7 @@ extern "C" int dsvt_rms_norm_backward(const dsvt_rms_cfg* cfg, const void* dy, i
     a.n = n_rows; a.C = cfg->C; a.eps = cfg->eps;
     a.partial = static_cast<float*>(ws);
     const int v = piece_elems(starts(a, e), a.C, e), lanes = row_lanes(cfg->C / v, v * e);
+    a.leaves = v * e == 16 && leaves_caches(n_rows, cfg->C, 1, e);
     const int64_t per = lanes ? kThreads / lanes : 1, all = dsvt_ceil_div(n_rows, per);
     groups = (int32_t)(all <= kTurnsAlone ? 1 : all < kBackwardGroups ? all : kBackwardGroups);
     const int32_t rows = (int32_t)dsvt_ceil_div(n_rows, groups);

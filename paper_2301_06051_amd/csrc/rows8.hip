@@ -5,8 +5,8 @@
 //   backward  dh = dy (Phi(k) + k phi(k)), k = code * scale
 //
 // All are bound by the bytes of their rows: writers hold a row in registers (rows.h), as its largest value is wanted before its first code; 27
-// instructions a value of GELU into two sets of codes take as long as its bytes.  Rows of 384 bf16: 200,000 through GELU into both sets of codes 74 us (4.2
-// TB/s), read back 46 (5.0), 800,000 backward 295 (5.2).  Fetching the next row ahead: 78 instead of 74.
+// instructions a value of GELU into two sets of codes take as long as its bytes.  Rows of 384 bf16: 200,000 through GELU into both sets of codes 72 us (4.3
+// TB/s), read back 37.5 (6.1, the codes from the caches), 800,000 backward 284 (5.4).  Fetching the next row ahead: 78 instead of 74.
 #include "rows8.h"
 
 namespace {
@@ -18,6 +18,7 @@ struct Rows8Args {
   float *out_scale, *kept_scale;
   int64_t ld_x, ld_dy, ld_y, ld_out, ld_kept;
   int32_t n, C;
+  bool leaves;                                    // readers: write_out
 };
 
 template <bool kGelu, typename T, int V, int kLanes, int R>
@@ -70,6 +71,7 @@ template <bool kGelu, typename T> __global__ __launch_bounds__(kThreads) void k_
 
 // kLanes lanes go along a row of any length.
 template <bool kGelu, typename T, int V, int kLanes> __global__ __launch_bounds__(kThreads) void k_read_rows8(Rows8Args a) {
+  constexpr int kAtOnce = kGelu ? 2 : 1;          // pieces asked for before one is used: 800,000 rows of 384 backward 289 us with one, 284 with two
   constexpr int kRows = kThreads / kLanes;
   const int part = threadIdx.x % kLanes, pieces = a.C / V;
   typedef typename Piece<T, V>::type P;
@@ -79,16 +81,28 @@ template <bool kGelu, typename T, int V, int kLanes> __global__ __launch_bounds_
     const float scale = a.kept_scale[row];
     P* out = reinterpret_cast<P*>(static_cast<T*>(a.y) + row * a.ld_y);
     const P* dy = kGelu ? reinterpret_cast<const P*>(static_cast<const T*>(a.dy) + row * a.ld_dy) : nullptr;
-    for (int p = part; p < pieces; p += kLanes) {
-      float f[V];
-      values_of<V>(codes[p], scale, f);
-      if constexpr (kGelu) {
-        float d[V];
-        widen<T, V>(dy[p], d);
+    for (int p0 = part; p0 < pieces; p0 += kAtOnce * kLanes) {
+      Q q[kAtOnce];
+      P d[kGelu ? kAtOnce : 1];
 #pragma unroll
-        for (int i = 0; i < V; ++i) f[i] = d[i] * gelu_slope(f[i]);
+      for (int u = 0; u < kAtOnce; ++u) {
+        const int p = p0 + u * kLanes < pieces ? p0 + u * kLanes : p0;
+        q[u] = codes[p];
+        if constexpr (kGelu) d[u] = dy[p];
       }
-      out[p] = narrow<T, V>(f);
+#pragma unroll
+      for (int u = 0; u < kAtOnce; ++u) {
+        if (p0 + u * kLanes >= pieces) break;
+        float f[V];
+        values_of<V>(q[u], scale, f);
+        if constexpr (kGelu) {
+          float g[V];
+          widen<T, V>(d[u], g);
+#pragma unroll
+          for (int i = 0; i < V; ++i) f[i] = g[i] * gelu_slope(f[i]);
+        }
+        write_out(out + p0 + u * kLanes, narrow<T, V>(f), a.leaves);
+      }
     }
   }
 }
@@ -157,6 +171,7 @@ int read(bool with_gelu, int32_t C, int32_t dtype, const dsvt_rows8* kept, const
   Rows8Args a = {};
   a.dy = dy; a.ld_dy = ld_dy; a.y = y; a.ld_y = ld_y; a.kept = kept->codes; a.kept_scale = kept->scale; a.ld_kept = kept->ld; a.n = n_rows; a.C = C;
   const int v = piece_elems((uintptr_t)dy | (uintptr_t)y | (uintptr_t)((ld_dy | ld_y) * e), C, e);
+  a.leaves = v * e == 16 && leaves_caches(n_rows, C, 1, e);
   hipStream_t st = (hipStream_t)stream;
   {
     dsvt_prof_scope ps(DSVT_K_ROWS8_READ, st);

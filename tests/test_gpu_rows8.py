@@ -461,6 +461,45 @@ def test_linear_in_parts(n, c, o, dtype, act):
     assert torch.equal(dsvt.dsvt_linear_rows8(layer, x), y)
 
 
+@pytest.mark.parametrize("n,c,o", [(70001, 64, 64), (33000, 16, 130), (25000, 33, 170), (40000, 192, 300), (33010, 1, 200), (30001, 250, 257), (9000, 100, 1000),
+                                   (140000, 99, 7), (300000, 65, 5), (70016, 129, 96)])
+@pytest.mark.parametrize("dtype,form,bias,act", [("bf16", "tight", True, False), ("bf16", "odd", False, True), ("bf16", "wide", True, True),
+                                                 ("f32", "tight", True, True), ("f32", "odd", True, False)])
+def test_linear_of_short_rows(n, c, o, dtype, form, bias, act):
+    """Many short rows, which wavefronts go through on their own."""
+    g = _gen(n + 7 * c + o)
+    x, w = _random_codes(g, n, c), _random_codes(g, o, c, fill=-127)
+    b = torch.randn((o,), generator=g) if bias else None
+    case = f"short rows {n} {c} {o} {dtype} {form} {bias} {act}"
+    print("[case]", case, flush=True)
+    layer = dsvt.Linear8(w, dtype, None if b is None else b.cuda(), act)
+    want = ref.linear(x.codes, x.scale, w.codes, w.scale, b, DT[dtype], act)
+    y = _placed(torch.zeros((n + 2, o), dtype=DT[dtype]), form)
+    y[n:] = 3
+    dsvt.dsvt_linear_rows8(layer, x, y=y[:n])
+    ref.check("y", y[:n], *want, case)
+    assert bool((y[n:] == 3).all()) and (form == "tight" or bool((y._base[:, -1] == 7).all()))
+
+
+@pytest.mark.parametrize("n,c,dtype", [(360000, 192, "bf16"), (90000, 385, "f32"), (90000, 384, "f32")])
+def test_large_results(n, c, dtype):
+    """Results of more than 128 MB, whose stores are marked: as in parts of 1 / 9."""
+    g = torch.Generator(device="cuda").manual_seed(9)
+    x, r, dy = (torch.randn((n, c), device="cuda", generator=g).to(DT[dtype]) for _ in range(3))
+    norm, part = dsvt.RmsNorm(1 + 0.1 * torch.randn(c, device="cuda", generator=g), dtype), n // 9
+    print("[case] large results", n, c, dtype, flush=True)
+    kept = dsvt.dsvt_keep_rows8(x)
+    (y, z), dx = dsvt.dsvt_rms_norm(norm, x, r, want_sum=True), dsvt.dsvt_rms_norm_backward(norm, dy, x, r)[0]
+    back, dh = dsvt.dsvt_read_rows8(kept, dtype), dsvt.dsvt_gelu_rows8_backward(kept, dy)
+    for at in range(0, n, part):
+        rows = slice(at, at + part)
+        some = dsvt.Rows8.of(kept.codes[rows], kept.scale[rows])
+        y1, z1 = dsvt.dsvt_rms_norm(norm, x[rows], r[rows], want_sum=True)
+        assert torch.equal(y[rows], y1) and torch.equal(z[rows], z1), at
+        assert torch.equal(dx[rows], dsvt.dsvt_rms_norm_backward(norm, dy[rows], x[rows], r[rows])[0]), at
+        assert torch.equal(back[rows], dsvt.dsvt_read_rows8(some, dtype)) and torch.equal(dh[rows], dsvt.dsvt_gelu_rows8_backward(some, dy[rows])), at
+
+
 @pytest.mark.parametrize("dtype", ["bf16", "f32"])
 @pytest.mark.parametrize("n", [3, 100])
 def test_linear_of_infinities(n, dtype):
