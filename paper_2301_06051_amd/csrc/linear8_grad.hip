@@ -24,7 +24,7 @@ struct Grad8Args {
   const float* s;
   const void* dy;
   void* d_w;                                      // written if there is one slice
-  float *d_b, *partial, *bias_partial;            // d_b: null if not wanted; [slices][O][C], [slices][O]
+  float *d_b, *partial, *bias_partial;            // d_b: null if not wanted; [slices] tiles, squares of 32 as lanes hold them; [slices][O]
   int64_t ld_x, ld_dy, ld_dw;
   int32_t n, C, O;
   int32_t slices, slice;                          // slices, rows of one (a multiple of a step's)
@@ -63,7 +63,10 @@ template <> struct Columns<float> {
 // does, in which case values are fetched one by one.
 enum Ends { kWhole, kShifted, kSingly };
 
-// kO outputs and kC columns, shared by kWO x kWC wavefronts; kN rows at a time.
+// A tile of kO outputs and kC columns, shared by kWO x kWC wavefronts, each of which has TO x TC squares of 32.
+struct Shape { int kO, kC, kWO, TO, TC; };
+
+// kN rows at a time; those of kAhead steps are on their way.
 template <typename T, int kO, int kC, int kWO, int kWC, int kN, int kAhead> struct Tile {
   static constexpr int kAll = 64 * kWO * kWC, TO = kO / kWO / 32, TC = kC / kWC / 32, V = 16 / (int)sizeof(T);
   static constexpr int kPitchO = kO * (int)sizeof(T) + Columns<T>::kPad, kPitchC = kC * (int)sizeof(T) + Columns<T>::kPad;
@@ -81,6 +84,18 @@ template <typename P> __device__ __forceinline__ P shifted(P p, int bits) {
   if (bits >= 64) v = Two{v.y >> (bits - 64), 0};
   else if (bits > 0) v = Two{v.x >> bits | v.y << (64 - bits), v.y >> bits};
   return __builtin_bit_cast(P, v);
+}
+
+// The first `left` of V values (all if there are more) to neighbouring places that begin on any value.
+template <typename T, int V> __device__ __forceinline__ void write_some(T* to, const float (&f)[V], int left) {
+  typedef T Anywhere __attribute__((ext_vector_type(V), aligned(sizeof(T))));
+  const typename Piece<T, V>::type p = narrow<T, V>(f);
+  if (left >= V) *reinterpret_cast<Anywhere*>(to) = p;
+  else {
+#pragma unroll
+    for (int k = 0; k < V - 1; ++k)
+      if (k < left) to[k] = p[k];
+  }
 }
 
 extern __shared__ __attribute__((aligned(16))) char grad_lds[];
@@ -227,30 +242,25 @@ template <typename T, int kO, int kC, int kWO, int kWC, int kN, int kAhead, Ends
   lds_barrier();
 
 #pragma unroll
-  for (int i = 0; i < TO; ++i) {
-    const int out = o0 + (wo * TO + i) * 32 + m;
-    if (out >= a.O) continue;
+  for (int i = 0; i < TO; ++i)
 #pragma unroll
     for (int j = 0; j < TC; ++j) {
-      const int col = c0 + (wc * TC + j) * 32 + 16 * h;
-      if (col >= a.C) continue;
-      if (a.slices > 1) {
-        float* to = a.partial + ((int64_t)slice * a.O + out) * a.C + col;
-        if (a.C % 4 == 0 && col + 16 <= a.C) {
+      const int out = o0 + (wo * TO + i) * 32 + m, col = c0 + (wc * TC + j) * 32 + 16 * h;
+      if (a.slices > 1) {                         // partial sums as the lanes hold them: whole lines, which the second kernel finds its way in
+        f32x4* to = reinterpret_cast<f32x4*>(a.partial) + (((int64_t)(slice * tiles + tile) * (kWO * kWC) + wave) * (TO * TC) + i * TC + j) * 256 + lane;
 #pragma unroll
-          for (int e = 0; e < 16; e += 4)
-            reinterpret_cast<f32x4*>(to)[e / 4] = f32x4{acc[i][j][e], acc[i][j][e + 1], acc[i][j][e + 2], acc[i][j][e + 3]};
-        } else {
-#pragma unroll
-          for (int e = 0; e < 16; ++e) if (col + e < a.C) to[e] = acc[i][j][e];
-        }
-      } else {
+        for (int e = 0; e < 16; e += 4) to[16 * e] = f32x4{acc[i][j][e], acc[i][j][e + 1], acc[i][j][e + 2], acc[i][j][e + 3]};
+      } else if (out < a.O) {
         T* to = static_cast<T*>(a.d_w) + out * a.ld_dw + col;
 #pragma unroll
-        for (int e = 0; e < 16; ++e) if (col + e < a.C) to[e] = (T)acc[i][j][e];
+        for (int e = 0; e < 16; e += V) {
+          float f[V];
+#pragma unroll
+          for (int k = 0; k < V; ++k) f[k] = acc[i][j][e + k];
+          write_some<T, V>(to + e, f, a.C - col - e);
+        }
       }
     }
-  }
   if (!sums) return;
   float* red = reinterpret_cast<float*>(grad_lds);
 #pragma unroll
@@ -263,25 +273,45 @@ template <typename T, int kO, int kC, int kWO, int kWC, int kN, int kAhead, Ends
   }
 }
 
-// The slices' sums added in their order, in 32 bits (there are few of them), those of the bias behind those of the weights.  No slices: zeros.
-template <typename T> __global__ __launch_bounds__(256) void k_linear8_grad_join(Grad8Args a) {
-  const int64_t all = (int64_t)a.O * a.C, end = all + (a.d_b ? a.O : 0);
-  for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < end; i += (int64_t)gridDim.x * 256) {
-    const float* from = i < all ? a.partial + i : a.bias_partial + (i - all);
-    const int64_t step = i < all ? all : a.O;
-    float v = 0.f;
-    int k = 0;
-    for (; k + 8 <= a.slices; k += 8) {           // eight loads on their way at a time
-      float f[8];
+// The slices' partial sums, added in an order of their numbers: a workgroup takes 32 outputs and columns, or 256 outputs of the bias, and its four
+// quarters take every fourth slice.  No slices: zeros.
+constexpr int kJoiners = 4;
+
+template <typename T> __global__ __launch_bounds__(256 * kJoiners) void k_linear8_grad_join(Grad8Args a, Shape t) {
+  __shared__ f32x4 parts[kJoiners - 1][256];
+  const int tid = threadIdx.x & 255, part = threadIdx.x >> 8, tiles_c = (a.C + t.kC - 1) / t.kC, tiles = tiles_c * ((a.O + t.kO - 1) / t.kO);
+  const int inner = t.kO * t.kC / 1024;           // squares of 32 of a tile
+  f32x4 v = {};
+  if ((int)blockIdx.x < tiles * inner) {
+    const f32x4* from = reinterpret_cast<const f32x4*>(a.partial) + (int64_t)blockIdx.x * 256 + tid;
+    const int64_t step = (int64_t)tiles * inner * 256;
+    int k = part;
+    for (; k + 7 * kJoiners < a.slices; k += 8 * kJoiners) {       // eight loads on their way at a time
+      f32x4 f[8];
 #pragma unroll
-      for (int j = 0; j < 8; ++j) f[j] = from[(k + j) * step];
+      for (int j = 0; j < 8; ++j) f[j] = from[(k + j * kJoiners) * step];
 #pragma unroll
       for (int j = 0; j < 8; ++j) v += f[j];
     }
-    for (; k < a.slices; ++k) v += from[k * step];
-    if (i < all) static_cast<T*>(a.d_w)[i / a.C * a.ld_dw + i % a.C] = (T)v;
-    else a.d_b[i - all] = v;
+#pragma unroll 4
+    for (; k < a.slices; k += kJoiners) v += from[k * step];
+  } else if (const int o = ((int)blockIdx.x - tiles * inner) * 256 + tid; o < a.O) {
+#pragma unroll 4
+    for (int k = part; k < a.slices; k += kJoiners) v[0] += a.bias_partial[(int64_t)k * a.O + o];
   }
+  if (part) parts[part - 1][tid] = v;
+  __syncthreads();
+  if (part) return;
+#pragma unroll
+  for (int k = 0; k < kJoiners - 1; ++k) v += parts[k][tid];
+  if ((int)blockIdx.x < tiles * inner) {
+    const int tile = blockIdx.x / inner, square = blockIdx.x - tile * inner, wave = square / (t.TO * t.TC), of_wave = square - wave * (t.TO * t.TC);
+    const int i = of_wave / t.TC, j = of_wave - i * t.TC, wo = wave % t.kWO, wc = wave / t.kWO, lane = tid & 63;
+    const int out = tile / tiles_c * t.kO + (wo * t.TO + i) * 32 + (lane & 31);
+    const int col = (tile - tile / tiles_c * tiles_c) * t.kC + (wc * t.TC + j) * 32 + 16 * (lane >> 5) + 4 * (tid >> 6);
+    const float f[4] = {v[0], v[1], v[2], v[3]};
+    if (out < a.O) write_some<T, 4>(static_cast<T*>(a.d_w) + out * a.ld_dw + col, f, a.C - col);
+  } else if (const int o = ((int)blockIdx.x - tiles * inner) * 256 + tid; o < a.O) a.d_b[o] = v[0];
 }
 
 // What tiles a call takes and how many slices.  A form's steps of 64 rows take `step` us with all its workgroups on the chip (`at_once`), and a slice
@@ -289,23 +319,29 @@ template <typename T> __global__ __launch_bounds__(256) void k_linear8_grad_join
 // form at its best, bf16, tiles of 64, 128, 192 and 256: 30,000 rows of 192 -> 576 26.5 us, 30, 34, 38; 800,000 512, 466, 335, 403; 16,384 of 1,024 -> 1,024 93,
 // 72, 84, 80; 65,536 of 1,024 -> 2,048 713, 433, 538, 340; fp32, tiles of 64 and 128: 30,000 of 192 -> 576 75, 106; 65,536 of 1,024 -> 2,048 2,831, 2,340.
 constexpr int kRowsStep = 64, kLongest = 16384;   // rows of fp32 that one slice adds up at most: each sum is a chain of additions
-struct Form { int tile, at_once; float step; };
-constexpr Form kForms[2][4] = {{{64, 768, 1.13f}, {128, 512, 1.75f}, {192, 256, 2.2f}, {256, 256, 2.55f}}, {{64, 768, 3.8f}, {128, 512, 9.1f}, {}, {}}};
+struct Form {
+  Shape tile;
+  int at_once;
+  float step;
+};
+constexpr Form kForms[2][4] = {{{{64, 64, 2, 1, 1}, 768, 1.13f}, {{128, 128, 2, 2, 2}, 512, 1.75f}, {{192, 192, 3, 2, 3}, 256, 2.2f}, {{256, 256, 2, 4, 2}, 256, 2.55f}},
+                               {{{64, 64, 2, 1, 1}, 768, 3.8f}, {{128, 128, 2, 2, 2}, 512, 9.1f}, {}, {}}};
 
 struct Plan {
   int form;                                       // of kForms
   int32_t slices, slice;
 };
+int64_t tile_values(const Shape& t, int32_t O, int32_t C) { return dsvt_ceil_div(O, t.kO) * dsvt_ceil_div(C, t.kC) * t.kO * t.kC; }
 Plan make_plan(int32_t C, int32_t O, int32_t dtype, int32_t n) {
   Plan p = {0, 0, kRowsStep};
   if (n <= 0) return p;
   const bool narrow = dtype == DSVT_BF16;
   const int64_t steps = dsvt_ceil_div(n, kRowsStep), least = narrow ? 1 : dsvt_ceil_div(n, kLongest);
-  const double slice_us = (double)O * C * 8. / 3e6;
   double best = 0.;
   for (int f = 0; f < (narrow ? 4 : 2); ++f) {
     const Form& form = kForms[!narrow][f];
-    const int64_t tiles = dsvt_ceil_div(O, form.tile) * dsvt_ceil_div(C, form.tile);
+    const int64_t tiles = dsvt_ceil_div(O, form.tile.kO) * dsvt_ceil_div(C, form.tile.kC);
+    const double slice_us = (double)tile_values(form.tile, O, C) * 8. / 3e6;
     int64_t most = form.at_once / tiles, slices = (int64_t)sqrt((double)steps * form.step / slice_us);
     most = most < steps / 4 ? most : steps / 4;    // (a slice of fewer steps is mostly its beginning and end)
     slices = slices < most ? slices : most;
@@ -320,8 +356,11 @@ Plan make_plan(int32_t C, int32_t O, int32_t dtype, int32_t n) {
   return p;
 }
 
-template <typename T, int kO, int kC, int kWO, int kWC, int kN, int kAhead> int launch_tile(const Grad8Args& a, hipStream_t st) {
+template <typename T, int kForm, int kN, int kAhead> int launch_tile(const Grad8Args& a, hipStream_t st) {
+  constexpr Shape t = kForms[sizeof(T) == 4][kForm].tile;
+  constexpr int kO = t.kO, kC = t.kC, kWO = t.kWO, kWC = t.kC / 32 / t.TC;
   typedef Tile<T, kO, kC, kWO, kWC, kN, kAhead> S;
+  static_assert(S::TO == t.TO && S::TC == t.TC, "the second kernel goes by the form's tile");
   static std::atomic<uint64_t> allowed[3];
   const Ends ends = a.O % S::V == 0 ? kWhole : a.O > S::V ? kShifted : kSingly;
   const auto kernel = ends == kWhole     ? k_linear8_grad<T, kO, kC, kWO, kWC, kN, kAhead, kWhole>
@@ -337,19 +376,20 @@ template <typename T> int launch(const Grad8Args& a, int form, hipStream_t st) {
   if (a.slices > 0) {
     int rc = DSVT_OK;
     if constexpr (sizeof(T) == 2) {
-      rc = form == 3   ? launch_tile<T, 256, 256, 2, 4, 32, 2>(a, st)
-           : form == 2 ? launch_tile<T, 192, 192, 3, 2, 32, 2>(a, st)
-           : form == 1 ? launch_tile<T, 128, 128, 2, 2, 64, 1>(a, st)
-                       : launch_tile<T, 64, 64, 2, 2, 64, 1>(a, st);
+      rc = form == 3   ? launch_tile<T, 3, 32, 2>(a, st)
+           : form == 2 ? launch_tile<T, 2, 32, 2>(a, st)
+           : form == 1 ? launch_tile<T, 1, 64, 1>(a, st)
+                       : launch_tile<T, 0, 64, 1>(a, st);
     } else {
-      rc = form == 1 ? launch_tile<T, 128, 128, 2, 2, 32, 1>(a, st) : launch_tile<T, 64, 64, 2, 2, 32, 1>(a, st);
+      rc = form == 1 ? launch_tile<T, 1, 32, 1>(a, st) : launch_tile<T, 0, 32, 1>(a, st);
     }
     if (rc) return rc;
   }
   if (a.slices == 1) return DSVT_OK;
-  const int64_t blocks = dsvt_ceil_div((int64_t)a.O * a.C + a.O, 256);
+  const Shape& t = kForms[sizeof(T) == 4][form].tile;
+  const int64_t blocks = tile_values(t, a.O, a.C) / 1024 + (a.d_b ? dsvt_ceil_div(a.O, 256) : 0);
   dsvt_prof_scope ps(DSVT_K_LINEAR8_JOIN, st);
-  k_linear8_grad_join<T><<<(unsigned)(blocks < 8192 ? blocks : 8192), 256, 0, st>>>(a);
+  k_linear8_grad_join<T><<<(unsigned)blocks, 256 * kJoiners, 0, st>>>(a, t);
   return DSVT_OK;
 }
 
@@ -364,7 +404,7 @@ extern "C" int dsvt_linear_rows8_weight_grad_workspace_size(int32_t C, int32_t o
   if (!bytes) return DSVT_EINVAL;
   if (const int rc = check(C, out, dtype, n_rows)) return rc;
   const Plan p = make_plan(C, out, dtype, n_rows);
-  *bytes = p.slices > 1 ? (size_t)p.slices * (size_t)out * ((size_t)C + 1) * sizeof(float) : 0;
+  *bytes = p.slices > 1 ? (size_t)p.slices * ((size_t)tile_values(kForms[dtype == DSVT_F32][p.form].tile, out, C) + (size_t)out) * sizeof(float) : 0;
   return DSVT_OK;
 }
 
@@ -383,7 +423,7 @@ extern "C" int dsvt_linear_rows8_weight_grad(int32_t C, int32_t out, int32_t dty
   a.dy = dy; a.ld_dy = ld_dy; a.n = n_rows; a.C = C; a.O = out; a.slices = p.slices; a.slice = p.slice;
   a.d_w = d_w; a.ld_dw = ld_dw; a.d_b = d_b;
   a.partial = static_cast<float*>(ws);
-  a.bias_partial = a.partial + (int64_t)p.slices * out * C;
+  a.bias_partial = a.partial + p.slices * tile_values(kForms[e == 4][p.form].tile, out, C);
   if (n_rows > 0) { a.x = x->codes; a.s = x->scale; a.ld_x = x->ld; }
   hipStream_t st = (hipStream_t)stream;
   if (const int rc = dtype == DSVT_BF16 ? launch<bf16_t>(a, p.form, st) : launch<float>(a, p.form, st)) return rc;
