@@ -9,8 +9,8 @@
 //
 // Both operands run along the rows, so both have to be turned round, which the LDS loads do (bf16).  With tiles of 256 the matrix cores, LDS and the
 // instructions that make values of codes are each busy for 1,024 clocks of a step of 32 rows, which takes 2,500: 65,536 rows of 1,024 -> 2,048 300 to 340
-// us (917 TFLOP/s; codes used as they are 45 us less, every step's rows the first ones 25), 2,048 -> 4,096 1,106 (994; the library's product of 8,192^3 in bf16
-// 1,362).  Few columns leave the partial sums and a step's latency: 30,000 rows of 192 -> 576 26 us, four of them the second kernel.
+// us (920 TFLOP/s; codes used as they are 45 us less, every step's rows the first ones 25), 2,048 -> 4,096 1,106 (994; the library's product of 8,192^3 in bf16
+// 1,362).  Few columns leave the partial sums and a step's latency: 30,000 rows of 192 -> 576 23 us, four of them the second kernel.
 #include "rows8.h"
 #include <cmath>
 
@@ -314,18 +314,23 @@ template <typename T> __global__ __launch_bounds__(256 * kJoiners) void k_linear
   } else if (const int o = ((int)blockIdx.x - tiles * inner) * 256 + tid; o < a.O) a.d_b[o] = v[0];
 }
 
-// What tiles a call takes and how many slices.  A form's steps of 64 rows take `step` us with all its workgroups on the chip (`at_once`), and a slice
-// costs the writing and reading of its partial sums, at 3 TB/s; the form and number of slices of the smallest sum are taken.  Measured, each
-// form at its best, bf16, tiles of 64, 128, 192 and 256: 30,000 rows of 192 -> 576 26.5 us, 30, 34, 38; 800,000 512, 466, 335, 403; 16,384 of 1,024 -> 1,024 93,
-// 72, 84, 80; 65,536 of 1,024 -> 2,048 713, 433, 538, 340; fp32, tiles of 64 and 128: 30,000 of 192 -> 576 75, 106; 65,536 of 1,024 -> 2,048 2,831, 2,340.
+// What tiles a call takes and how many slices.  A form's steps of 64 rows take `step` us with all its workgroups on the chip (`at_once`), its beginning
+// `begin` more than that of the smallest tiles, and a slice costs the writing and reading of its partial sums, at 3 TB/s; the form and number of slices
+// of the smallest sum are taken.  Measured, each form at its best, bf16, tiles of 64, 128, 192, 256 and 192 x 64, whose many rows at a time share a
+// column's values among more outputs: 30,000 rows of 192 -> 576 25.1 us, 28.8, 26.3, 35.6, 23.1; 8,000 of 192 -> 192 12.8, 15.5, 17.4, -, 13.5; 800,000 of 192 ->
+// 576 480, 415, 290, 368, 366; 16,384 of 1,024 -> 1,024 92, 61, 72, 60, 95; 65,536 of 1,024 -> 2,048 777, 392, 522, 298, 669; fp32, tiles of 64 and 128: 30,000 of
+// 192 -> 576 74, 105; 65,536 of 1,024 -> 2,048 2,551, 2,304.
 constexpr int kRowsStep = 64, kLongest = 16384;   // rows of fp32 that one slice adds up at most: each sum is a chain of additions
 struct Form {
   Shape tile;
   int at_once;
-  float step;
+  float step, begin;
 };
-constexpr Form kForms[2][4] = {{{{64, 64, 2, 1, 1}, 768, 1.13f}, {{128, 128, 2, 2, 2}, 512, 1.75f}, {{192, 192, 3, 2, 3}, 256, 2.2f}, {{256, 256, 2, 4, 2}, 256, 2.55f}},
-                               {{{64, 64, 2, 1, 1}, 768, 3.8f}, {{128, 128, 2, 2, 2}, 512, 9.1f}, {}, {}}};
+constexpr int kWideForms = 5;                     // of bf16
+constexpr Form kForms[2][kWideForms] = {
+    {{{64, 64, 2, 1, 1}, 768, 1.13f, 0.f}, {{128, 128, 2, 2, 2}, 512, 1.75f, 0.f}, {{192, 192, 3, 2, 3}, 256, 2.2f, 0.f}, {{256, 256, 2, 4, 2}, 256, 2.55f, 0.f},
+     {{192, 64, 6, 1, 1}, 256, 0.9f, 2.f}},
+    {{{64, 64, 2, 1, 1}, 768, 3.8f, 0.f}, {{128, 128, 2, 2, 2}, 512, 9.1f, 0.f}, {}, {}, {}}};
 
 struct Plan {
   int form;                                       // of kForms
@@ -338,7 +343,7 @@ Plan make_plan(int32_t C, int32_t O, int32_t dtype, int32_t n) {
   const bool narrow = dtype == DSVT_BF16;
   const int64_t steps = dsvt_ceil_div(n, kRowsStep), least = narrow ? 1 : dsvt_ceil_div(n, kLongest);
   double best = 0.;
-  for (int f = 0; f < (narrow ? 4 : 2); ++f) {
+  for (int f = 0; f < (O < (narrow ? 8 : 4) ? 1 : narrow ? kWideForms : 2); ++f) {       // (fewer outputs than a piece: the first form)
     const Form& form = kForms[!narrow][f];
     const int64_t tiles = dsvt_ceil_div(O, form.tile.kO) * dsvt_ceil_div(C, form.tile.kC);
     const double slice_us = (double)tile_values(form.tile, O, C) * 8. / 3e6;
@@ -348,7 +353,7 @@ Plan make_plan(int32_t C, int32_t O, int32_t dtype, int32_t n) {
     slices = slices > least ? slices : least;      // (one at least)
     const int64_t per = dsvt_ceil_div(steps, slices);
     slices = dsvt_ceil_div(steps, per);
-    const double us = (double)per * form.step * (tiles * slices > form.at_once ? (double)(tiles * slices) / form.at_once : 1.) + (slices > 1 ? slices * slice_us + 4. : 0.);
+    const double us = (double)per * form.step * (tiles * slices > form.at_once ? (double)(tiles * slices) / form.at_once : 1.) + (slices > 1 ? slices * slice_us + 4. : 0.) + form.begin;
     if (f > 0 && us >= best) continue;
     best = us;
     p = {f, (int32_t)slices, (int32_t)(per * kRowsStep)};
@@ -363,9 +368,10 @@ template <typename T, int kForm, int kN, int kAhead> int launch_tile(const Grad8
   static_assert(S::TO == t.TO && S::TC == t.TC, "the second kernel goes by the form's tile");
   static std::atomic<uint64_t> allowed[3];
   const Ends ends = a.O % S::V == 0 ? kWhole : a.O > S::V ? kShifted : kSingly;
-  const auto kernel = ends == kWhole     ? k_linear8_grad<T, kO, kC, kWO, kWC, kN, kAhead, kWhole>
-                      : ends == kShifted ? k_linear8_grad<T, kO, kC, kWO, kWC, kN, kAhead, kShifted>
-                                         : k_linear8_grad<T, kO, kC, kWO, kWC, kN, kAhead, kSingly>;
+  auto kernel = ends == kWhole ? k_linear8_grad<T, kO, kC, kWO, kWC, kN, kAhead, kWhole> : k_linear8_grad<T, kO, kC, kWO, kWC, kN, kAhead, kShifted>;
+  if constexpr (kForm == 0) {
+    if (ends == kSingly) kernel = k_linear8_grad<T, kO, kC, kWO, kWC, kN, kAhead, kSingly>;
+  }
   if (const int rc = dsvt_allow_lds(reinterpret_cast<const void*>(kernel), S::lds(), allowed[ends])) return rc;
   const int64_t all = dsvt_ceil_div(a.O, kO) * dsvt_ceil_div(a.C, kC) * a.slices;
   dsvt_prof_scope ps(DSVT_K_LINEAR8_GRAD, st);
@@ -376,7 +382,8 @@ template <typename T> int launch(const Grad8Args& a, int form, hipStream_t st) {
   if (a.slices > 0) {
     int rc = DSVT_OK;
     if constexpr (sizeof(T) == 2) {
-      rc = form == 3   ? launch_tile<T, 3, 32, 2>(a, st)
+      rc = form == 4   ? launch_tile<T, 4, 96, 2>(a, st)
+           : form == 3 ? launch_tile<T, 3, 32, 2>(a, st)
            : form == 2 ? launch_tile<T, 2, 32, 2>(a, st)
            : form == 1 ? launch_tile<T, 1, 64, 1>(a, st)
                        : launch_tile<T, 0, 64, 1>(a, st);

@@ -259,6 +259,24 @@ def test_weight_grad(n, c, o, dtype, form):
     assert none is None and torch.equal(plain, d_w)
 
 
+@pytest.mark.parametrize("n,c,o", [(30001, 190, 575), (30000, 192, 576), (40000, 130, 570), (100003, 127, 191)])
+@pytest.mark.parametrize("form", ["tight", "odd"])
+def test_weight_grad_of_many_rows(n, c, o, form):
+    """Many slices of few columns, whose partial sums are joined."""
+    g = _gen(n + 3 * c + o)
+    x, dy = _random_codes(g, n, c), torch.randn((n, o), generator=g).to(torch.bfloat16)
+    case = f"wgrad of many rows {n} {c} {o} {form}"
+    print("[case]", case, flush=True)
+    want = ref.weight_grad(x.codes, x.scale, dy)
+    dyd, d_w = _placed(dy, form), _placed(torch.zeros((o, c), dtype=torch.bfloat16), form)
+    _, d_b = dsvt.dsvt_linear_rows8_weight_grad(x, dyd, d_w=d_w)
+    ref.check("d_w", d_w, *want["d_w"], case)
+    ref.check("d_b", d_b, *want["d_b"], case)
+    assert form == "tight" or bool((d_w._base[:, -1] == 7).all())
+    plain, _ = dsvt.dsvt_linear_rows8_weight_grad(x, dyd, want_bias=False)
+    assert torch.equal(plain, d_w)
+
+
 def test_rows_past_31_bits():
     """Arrays of more than 2^31 bytes and values: the last rows are those of a call on them alone."""
     n, c = 12_000_000, 192
