@@ -273,12 +273,10 @@ template <typename T, int kO, int kC, int kWO, int kWC, int kN, int kAhead, Ends
   }
 }
 
-// The slices' partial sums, added in an order of their numbers: a workgroup takes 32 outputs and columns, or 256 outputs of the bias, and its four
-// quarters take every fourth slice.  No slices: zeros.
-constexpr int kJoiners = 4;
-
-template <typename T> __global__ __launch_bounds__(256 * kJoiners) void k_linear8_grad_join(Grad8Args a, Shape t) {
-  __shared__ f32x4 parts[kJoiners - 1][256];
+// The slices' partial sums, added in an order of their numbers: a workgroup takes 32 outputs and columns, or 256 outputs of the bias; where there are
+// few such workgroups, four quarters of it take every fourth slice each (kJoiners).  No slices: zeros.
+template <typename T, int kJoiners> __global__ __launch_bounds__(256 * kJoiners) void k_linear8_grad_join(Grad8Args a, Shape t) {
+  __shared__ f32x4 parts[kJoiners][256];
   const int tid = threadIdx.x & 255, part = threadIdx.x >> 8, tiles_c = (a.C + t.kC - 1) / t.kC, tiles = tiles_c * ((a.O + t.kO - 1) / t.kO);
   const int inner = t.kO * t.kC / 1024;           // squares of 32 of a tile
   f32x4 v = {};
@@ -299,11 +297,13 @@ template <typename T> __global__ __launch_bounds__(256 * kJoiners) void k_linear
 #pragma unroll 4
     for (int k = part; k < a.slices; k += kJoiners) v[0] += a.bias_partial[(int64_t)k * a.O + o];
   }
-  if (part) parts[part - 1][tid] = v;
-  __syncthreads();
-  if (part) return;
+  if constexpr (kJoiners > 1) {
+    parts[part][tid] = v;
+    __syncthreads();
+    if (part) return;
 #pragma unroll
-  for (int k = 0; k < kJoiners - 1; ++k) v += parts[k][tid];
+    for (int k = 1; k < kJoiners; ++k) v += parts[k][tid];
+  }
   if ((int)blockIdx.x < tiles * inner) {
     const int tile = blockIdx.x / inner, square = blockIdx.x - tile * inner, wave = square / (t.TO * t.TC), of_wave = square - wave * (t.TO * t.TC);
     const int i = of_wave / t.TC, j = of_wave - i * t.TC, wo = wave % t.kWO, wc = wave / t.kWO, lane = tid & 63;
@@ -396,7 +396,8 @@ template <typename T> int launch(const Grad8Args& a, int form, hipStream_t st) {
   const Shape& t = kForms[sizeof(T) == 4][form].tile;
   const int64_t blocks = tile_values(t, a.O, a.C) / 1024 + (a.d_b ? dsvt_ceil_div(a.O, 256) : 0);
   dsvt_prof_scope ps(DSVT_K_LINEAR8_JOIN, st);
-  k_linear8_grad_join<T><<<(unsigned)blocks, 256 * kJoiners, 0, st>>>(a, t);
+  if (blocks < 4 * 256) k_linear8_grad_join<T, 4><<<(unsigned)blocks, 1024, 0, st>>>(a, t);
+  else k_linear8_grad_join<T, 1><<<(unsigned)blocks, 256, 0, st>>>(a, t);
   return DSVT_OK;
 }
 
