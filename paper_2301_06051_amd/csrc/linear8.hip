@@ -172,7 +172,8 @@ constexpr int kShortWaves = 4;
 // Wavefronts a SIMD: two, a third one where registers allow it and it measured better (800,000 x 192 -> 576 198 -> 186 us; 100,000 x 64 -> 128 6.9 -> 8.7).
 constexpr int short_simd(int steps, int elem) { return steps == 6 && elem == 2 ? 3 : 2; }
 
-template <typename T, int kSteps, int kWhole> __global__ __launch_bounds__(64 * kShortWaves, short_simd(kSteps, sizeof(T))) void k_linear8_short(Linear8Args a, int shares) {
+template <typename T, int kSteps, int kWhole>
+__global__ __launch_bounds__(64 * kShortWaves, short_simd(kSteps, sizeof(T))) void k_linear8_short(Linear8Args a, int shares) {
   constexpr int V = 16 / (int)sizeof(T), PR = 64 / V, kRowsOut = sizeof(T) == 2 ? 32 : 16;
   typedef typename Piece<T, V>::type P;
   __shared__ P all_out[kShortWaves][kRowsOut * PR];
@@ -183,32 +184,6 @@ template <typename T, int kSteps, int kWhole> __global__ __launch_bounds__(64 * 
   if (share >= shares) return;
   const int out0 = at % blocks_n * 64, outs = a.O - out0 < 64 ? a.O - out0 : 64;
   const int last_piece = (a.C - 1) >> 4 << 4;
-
-  i32x4 w[2][kSteps];
-  const int out_m = (m >> 2 & 1) * 16 + (m >> 3) * 4 + (m & 3);
-#pragma unroll
-  for (int j = 0; j < 2; ++j) {
-    const int o = 32 * j + out_m;
-    const int8_t* row = a.w + (int64_t)(out0 + (o < outs ? o : outs - 1)) * a.ld_w;
-#pragma unroll
-    for (int k = 0; k < kSteps; ++k) {
-      const int c = 32 * k + 16 * h;
-      w[j][k] = first_bytes(*reinterpret_cast<const i32x4*>(row + (c < last_piece ? c : last_piece)), a.C - c);
-    }
-  }
-  float* const ends = all_ends[wave][0];
-  {
-    const int o = out0 + (lane < outs ? lane : outs - 1);
-    ends[lane] = a.t[o];
-    ends[64 + lane] = a.bias ? a.bias[o] : 0.f;
-  }
-  P* const out = all_out[wave];
-  const auto in_order = []() {
-    __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
-    __builtin_amdgcn_wave_barrier();
-    __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
-  };
-  in_order();
 
   i32x4 x[kSteps];
   float s;
@@ -223,8 +198,37 @@ template <typename T, int kSteps, int kWhole> __global__ __launch_bounds__(64 * 
     }
     s = a.s[row0 + row];
   };
+  // The first rows, scales, biases and weights are on their way together.  (There are no more shares than blocks.)
   int block = share;
-  if (block < blocks_m) fetch(block);
+  fetch(block);
+  const int end = out0 + (lane < outs ? lane : outs - 1);
+  const float scale_out = a.t[end], bias_out = a.bias ? a.bias[end] : 0.f;
+  i32x4 w[2][kSteps];
+  const int out_m = (m >> 2 & 1) * 16 + (m >> 3) * 4 + (m & 3);
+#pragma unroll
+  for (int j = 0; j < 2; ++j) {
+    const int o = 32 * j + out_m;
+    const int8_t* row = a.w + (int64_t)(out0 + (o < outs ? o : outs - 1)) * a.ld_w;
+#pragma unroll
+    for (int k = 0; k < kSteps; ++k) {
+      const int c = 32 * k + 16 * h;
+      w[j][k] = *reinterpret_cast<const i32x4*>(row + (k < kWhole || c < last_piece ? c : last_piece));
+    }
+  }
+  float* const ends = all_ends[wave][0];
+  ends[lane] = scale_out;
+  ends[64 + lane] = bias_out;
+#pragma unroll
+  for (int j = 0; j < 2; ++j)
+#pragma unroll
+    for (int k = kWhole; k < kSteps; ++k) w[j][k] = first_bytes(w[j][k], a.C - 32 * k - 16 * h);
+  P* const out = all_out[wave];
+  const auto in_order = []() {
+    __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
+    __builtin_amdgcn_wave_barrier();
+    __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
+  };
+  in_order();
   for (; block < blocks_m; block += shares) {
     i32x16 acc[2];
 #pragma unroll
