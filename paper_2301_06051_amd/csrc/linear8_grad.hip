@@ -77,15 +77,6 @@ template <typename T, int kO, int kC, int kWO, int kWC, int kN, int kAhead> stru
   static constexpr size_t lds() { return 2 * (size_t)kBuffer > (size_t)kRowsO * kO * 4 ? 2 * (size_t)kBuffer : (size_t)kRowsO * kO * 4; }
 };
 
-// 16 bytes less their first `bits` bits, zeros behind them.
-template <typename P> __device__ __forceinline__ P shifted(P p, int bits) {
-  typedef uint64_t Two __attribute__((ext_vector_type(2)));
-  Two v = __builtin_bit_cast(Two, p);
-  if (bits >= 64) v = Two{v.y >> (bits - 64), 0};
-  else if (bits > 0) v = Two{v.x >> bits | v.y << (64 - bits), v.y >> bits};
-  return __builtin_bit_cast(P, v);
-}
-
 // The first `left` of V values (all if there are more) to neighbouring places that begin on any value.
 template <typename T, int V> __device__ __forceinline__ void write_some(T* to, const float (&f)[V], int left) {
   typedef T Anywhere __attribute__((ext_vector_type(V), aligned(sizeof(T))));

@@ -24,8 +24,8 @@ struct RmsArgs {
 };
 
 // z = x + res in 32 bits; returns rsqrt(mean z^2 + eps)
-template <typename T, int V, int kLanes, int R>
-__device__ __forceinline__ float sum_row(const RowPieces<T, V, kLanes, R>& x, const RowPieces<T, V, kLanes, R>& res, bool with_res, float inv_c,
+template <typename T, int V, int kLanes, int R, bool kLoose>
+__device__ __forceinline__ float sum_row(const RowOf<T, V, kLanes, R, kLoose>& x, const RowOf<T, V, kLanes, R, kLoose>& res, bool with_res, float inv_c,
                                          float eps, float (&z)[R][V], float* s) {
   float sq = 0.f;
 #pragma unroll
@@ -43,59 +43,49 @@ __device__ __forceinline__ float sum_row(const RowPieces<T, V, kLanes, R>& x, co
   return 1.f / sqrtf(lane_sum<kLanes>(sq, s) * inv_c + eps);
 }
 
-template <typename T, int V, int kLanes, int R>
+template <typename T, int V, int kLanes, int R, bool kLoose>
 __global__ __launch_bounds__(kThreads) void k_rms_forward(RmsArgs a) {
+  typedef RowOf<T, V, kLanes, R, kLoose> Row;
   constexpr int kRows = kThreads / kLanes;
   __shared__ float s[kThreads / 64];
   __shared__ uint32_t st[kThreads / 64];
-  const int part = threadIdx.x % kLanes, pieces = a.C / V;
+  const int part = threadIdx.x % kLanes;
   const float inv_c = 1.f / (float)a.C;
   float gamma[R][V];
-  load_vector<V, kLanes, R>(a.gamma, part, pieces, gamma);
-  typedef typename Piece<T, V>::type P;
+  load_values<V, kLanes, R, kLoose>(a.gamma, part, a.C, gamma);
   for (int64_t row = (int64_t)blockIdx.x * kRows + threadIdx.x / kLanes; row < a.n; row += (int64_t)gridDim.x * kRows) {
-    RowPieces<T, V, kLanes, R> x, res;
-    x.load(a.x, row * a.ld_x, part, pieces, true);
-    if (a.res) res.load(a.res, row * a.ld_res, part, pieces, true);
+    Row x, res;
+    x.load(a.x, row * a.ld_x, part, a.C);
+    if (a.res) res.load(a.res, row * a.ld_res, part, a.C);
     float z[R][V];
-    const float rs = sum_row<T, V, kLanes, R>(x, res, a.res != nullptr, inv_c, a.eps, z, s);
-    if (a.z) {
-      P* out = reinterpret_cast<P*>(static_cast<T*>(a.z) + row * a.ld_z);
-#pragma unroll
-      for (int r = 0; r < R; ++r)
-        if (r * kLanes + part < pieces) write_out(out + r * kLanes + part, narrow<T, V>(z[r]), a.leaves);
-    }
+    const float rs = sum_row<T, V, kLanes, R, kLoose>(x, res, a.res != nullptr, inv_c, a.eps, z, s);
+    if (a.z) Row::store(a.z, row * a.ld_z, part, a.C, z, a.leaves);
 #pragma unroll
     for (int r = 0; r < R; ++r)
 #pragma unroll
       for (int i = 0; i < V; ++i) z[r][i] *= rs * gamma[r][i];
-    if (a.y) {
-      P* out = reinterpret_cast<P*>(static_cast<T*>(a.y) + row * a.ld_y);
-#pragma unroll
-      for (int r = 0; r < R; ++r)
-        if (r * kLanes + part < pieces) write_out(out + r * kLanes + part, narrow<T, V>(z[r]), a.leaves);
-    }
-    if (a.codes) store_codes<V, kLanes, R>(z, part, pieces, a.codes + row * a.ld_codes, a.scale + row, st);
+    if (a.y) Row::store(a.y, row * a.ld_y, part, a.C, z, a.leaves);
+    if (a.codes) store_codes<V, kLanes, R, kLoose>(z, part, a.C, a.codes + row * a.ld_codes, a.scale + row, st);
   }
 }
 
-template <typename T, int V, int kLanes, int R>
+template <typename T, int V, int kLanes, int R, bool kLoose>
 __global__ __launch_bounds__(kThreads) void k_rms_backward(RmsArgs a) {
+  typedef RowOf<T, V, kLanes, R, kLoose> Row;
   constexpr int kRows = kThreads / kLanes;
   __shared__ float s[kThreads / 64];
-  const int part = threadIdx.x % kLanes, pieces = a.C / V;
+  const int part = threadIdx.x % kLanes;
   const float inv_c = 1.f / (float)a.C;
   float gamma[R][V], dg[R][V] = {};
-  load_vector<V, kLanes, R>(a.gamma, part, pieces, gamma);
-  typedef typename Piece<T, V>::type P;
+  load_values<V, kLanes, R, kLoose>(a.gamma, part, a.C, gamma);
   for (int64_t row = (int64_t)blockIdx.x * kRows + threadIdx.x / kLanes; row < a.n; row += (int64_t)gridDim.x * kRows) {
-    RowPieces<T, V, kLanes, R> x, res, dy, more;
-    x.load(a.x, row * a.ld_x, part, pieces, true);
-    if (a.res) res.load(a.res, row * a.ld_res, part, pieces, true);
-    dy.load(a.dy, row * a.ld_dy, part, pieces, true);
-    if (a.d_sum) more.load(a.d_sum, row * a.ld_dsum, part, pieces, true);
+    Row x, res, dy, more;
+    x.load(a.x, row * a.ld_x, part, a.C);
+    if (a.res) res.load(a.res, row * a.ld_res, part, a.C);
+    dy.load(a.dy, row * a.ld_dy, part, a.C);
+    if (a.d_sum) more.load(a.d_sum, row * a.ld_dsum, part, a.C);
     float n[R][V], w[R][V];
-    const float rs = sum_row<T, V, kLanes, R>(x, res, a.res != nullptr, inv_c, a.eps, n, s);
+    const float rs = sum_row<T, V, kLanes, R, kLoose>(x, res, a.res != nullptr, inv_c, a.eps, n, s);
     float sum_wn = 0.f;
 #pragma unroll
     for (int r = 0; r < R; ++r) {
@@ -109,7 +99,6 @@ __global__ __launch_bounds__(kThreads) void k_rms_backward(RmsArgs a) {
       }
     }
     const float mean_wn = lane_sum<kLanes>(sum_wn, s) * inv_c;
-    P* out = reinterpret_cast<P*>(static_cast<T*>(a.y) + row * a.ld_y);
 #pragma unroll
     for (int r = 0; r < R; ++r) {
 #pragma unroll
@@ -120,8 +109,8 @@ __global__ __launch_bounds__(kThreads) void k_rms_backward(RmsArgs a) {
 #pragma unroll
         for (int i = 0; i < V; ++i) n[r][i] += f[i];
       }
-      if (r * kLanes + part < pieces) write_out(out + r * kLanes + part, narrow<T, V>(n[r]), a.leaves);
     }
+    Row::store(a.y, row * a.ld_y, part, a.C, n, a.leaves);
   }
   // the workgroup's sums: over the rows of a wavefront across lanes, over its wavefronts in LDS
   constexpr int kCopies = kLanes > 64 ? 1 : kThreads / 64;
@@ -210,22 +199,22 @@ uintptr_t starts(const RmsArgs& a, int e) {
          (uintptr_t)((a.ld_x | a.ld_res | a.ld_dy | a.ld_dsum | a.ld_z | a.ld_y) * e);
 }
 
-struct Forward {
+template <bool kLoose> struct Forward {
   template <typename T, int V, int kLanes, int R> static void rows(const RmsArgs& a, unsigned groups, hipStream_t st) {
-    k_rms_forward<T, V, kLanes, R><<<groups, kThreads, 0, st>>>(a);
+    k_rms_forward<T, V, kLanes, R, kLoose><<<groups, kThreads, 0, st>>>(a);
   }
 };
-struct Backward {
+template <bool kLoose> struct Backward {
   template <typename T, int V, int kLanes, int R> static void rows(const RmsArgs& a, unsigned groups, hipStream_t st) {
-    k_rms_backward<T, V, kLanes, R><<<groups, kThreads, 0, st>>>(a);
+    k_rms_backward<T, V, kLanes, R, kLoose><<<groups, kThreads, 0, st>>>(a);
   }
 };
-template <typename T> void launch(const RmsArgs& a, bool back, int v, int lanes, unsigned groups, int32_t rows, hipStream_t st) {
+template <typename T> void launch(const RmsArgs& a, bool back, RowForm form, int lanes, unsigned groups, int32_t rows, hipStream_t st) {
   if (lanes == 0) {
     if (back) k_rms_long<T, true><<<groups, kThreads, 0, st>>>(a, rows);
     else k_rms_long<T, false><<<groups, kThreads, 0, st>>>(a, rows);
-  } else if (back) launch_rows<Backward, T>(a, v, lanes, groups, st);
-  else launch_rows<Forward, T>(a, v, lanes, groups, st);
+  } else if (back) launch_form<Backward, T>(a, form, lanes, groups, st);
+  else launch_form<Forward, T>(a, form, lanes, groups, st);
 }
 
 int check(const dsvt_rms_cfg* cfg, int32_t n_rows) {
@@ -250,16 +239,17 @@ extern "C" int dsvt_rms_norm(const dsvt_rms_cfg* cfg, const void* x, int64_t ld_
   a.x = x; a.res = res; a.z = z; a.y = y; a.gamma = cfg->gamma;
   a.ld_x = ld_x; a.ld_res = res ? ld_res : 0; a.ld_z = z ? ld_z : 0; a.ld_y = y ? ld_y : 0; a.n = n_rows; a.C = cfg->C; a.eps = cfg->eps;
   if (rows8) { a.codes = rows8->codes; a.scale = rows8->scale; a.ld_codes = rows8->ld; }
-  const int v = piece_elems(starts(a, e), a.C, e), lanes = row_lanes(cfg->C / v, v * e);
-  a.leaves = v * e == 16 && leaves_caches(n_rows, cfg->C, (z != nullptr) + (y != nullptr), e);
+  const RowForm form = row_form(starts(a, e), a.C, e);
+  const int lanes = form_lanes(form, a.C, e);
+  a.leaves = leaves_caches((uintptr_t)z | (uintptr_t)y | (uintptr_t)((a.ld_z | a.ld_y) * e), n_rows, cfg->C, (z != nullptr) + (y != nullptr), e);
   const int64_t per = lanes ? kThreads / lanes : 1, all = dsvt_ceil_div(n_rows, per);
   const unsigned groups = (unsigned)(all < kForwardGroups ? all : kForwardGroups);
   const int32_t rows = (int32_t)dsvt_ceil_div(n_rows, groups);
   hipStream_t st = (hipStream_t)stream;
   {
     dsvt_prof_scope ps(DSVT_K_RMS_FORWARD, st);
-    if (cfg->dtype == DSVT_BF16) launch<bf16_t>(a, false, v, lanes, groups, rows, st);
-    else launch<float>(a, false, v, lanes, groups, rows, st);
+    if (cfg->dtype == DSVT_BF16) launch<bf16_t>(a, false, form, lanes, groups, rows, st);
+    else launch<float>(a, false, form, lanes, groups, rows, st);
   }
   DSVT_HIP_TRY(hipGetLastError());
   return DSVT_OK;
@@ -291,16 +281,17 @@ extern "C" int dsvt_rms_norm_backward(const dsvt_rms_cfg* cfg, const void* dy, i
     a.ld_x = ld_x; a.ld_res = res ? ld_res : 0; a.ld_dy = ld_dy; a.ld_dsum = d_sum ? ld_dsum : 0; a.ld_y = ld_dx;
     a.n = n_rows; a.C = cfg->C; a.eps = cfg->eps;
     a.partial = static_cast<float*>(ws);
-    const int v = piece_elems(starts(a, e), a.C, e), lanes = row_lanes(cfg->C / v, v * e);
-    a.leaves = v * e == 16 && leaves_caches(n_rows, cfg->C, 1, e);
+    const RowForm form = row_form(starts(a, e), a.C, e);
+    const int lanes = form_lanes(form, a.C, e);
+    a.leaves = leaves_caches((uintptr_t)dx | (uintptr_t)(ld_dx * e), n_rows, cfg->C, 1, e);
     const int64_t per = lanes ? kThreads / lanes : 1, all = dsvt_ceil_div(n_rows, per);
     groups = (int32_t)(all <= kTurnsAlone ? 1 : all < kBackwardGroups ? all : kBackwardGroups);
     const int32_t rows = (int32_t)dsvt_ceil_div(n_rows, groups);
     if (lanes == 0) groups = (int32_t)dsvt_ceil_div(n_rows, rows);       // every workgroup has a row
     if (groups == 1) a.d_gamma = d_gamma;
     dsvt_prof_scope ps(DSVT_K_RMS_BACKWARD, st);
-    if (cfg->dtype == DSVT_BF16) launch<bf16_t>(a, true, v, lanes, (unsigned)groups, rows, st);
-    else launch<float>(a, true, v, lanes, (unsigned)groups, rows, st);
+    if (cfg->dtype == DSVT_BF16) launch<bf16_t>(a, true, form, lanes, (unsigned)groups, rows, st);
+    else launch<float>(a, true, form, lanes, (unsigned)groups, rows, st);
   }
   if (groups != 1) {
     dsvt_prof_scope ps(DSVT_K_RMS_SUM, st);

@@ -115,7 +115,7 @@ inline int row_lanes(int32_t pieces, int bytes) {
 
 // Launches Kernel::rows<T, V, kLanes, R>(a, groups, st) for rows of a.C values in pieces of V on `lanes` lanes, as piece_elems and row_lanes say.
 template <typename Kernel, typename T, int V, typename Args> void launch_pieces(const Args& a, int lanes, unsigned groups, hipStream_t st) {
-  const int r = (int)dsvt_ceil_div(a.C / V, lanes);
+  const int r = (int)dsvt_ceil_div(dsvt_ceil_div(a.C, V), lanes);
   if (lanes == 8) {
     if (r == 1) Kernel::template rows<T, V, 8, 1>(a, groups, st);
     else if (r == 2) Kernel::template rows<T, V, 8, 2>(a, groups, st);

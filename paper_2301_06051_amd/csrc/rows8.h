@@ -17,6 +17,9 @@ template <> struct Codes<4> { typedef uint32_t type; };
 template <> struct Codes<2> { typedef uint16_t type; };
 template <> struct Codes<1> { typedef uint8_t type; };
 
+__device__ __forceinline__ int8_t byte_of(uint32_t p, int i) { return (int8_t)(p >> 8 * i); }
+__device__ __forceinline__ int8_t byte_of(Codes<8>::type p, int i) { return byte_of(i < 4 ? p.x : p.y, i & 3); }
+
 // One code of four as a float, in one instruction (the compiler takes two: it cuts the byte out first).
 template <int kByte> __device__ __forceinline__ float code_of(uint32_t four) {
   float f;
@@ -93,9 +96,18 @@ struct RowScale {
   }
 };
 
-// Rows of the type on their way out, in pieces of 16 bytes.  Where a call writes more of them than half of the 256 MB of the memory-side cache, they are
-// marked to leave the caches first, so that its other rows stay: a norm of 800,000 rows of 192 bf16 that also writes its sum 235 -> 229 us, with the call
-// that reads the results 362 -> 346; 200,000 rows of 384 read back from 8 bits 46 -> 37.5.  Of fewer, the next call finds them there: two norms of
+// 16 bytes less their first `bits` bits, zeros behind them.
+template <typename P> __device__ __forceinline__ P shifted(P p, int bits) {
+  typedef uint64_t Two __attribute__((ext_vector_type(2)));
+  Two v = __builtin_bit_cast(Two, p);
+  if (bits >= 64) v = Two{v.y >> (bits - 64), 0};
+  else if (bits > 0) v = Two{v.x >> bits | v.y << (64 - bits), v.y >> bits};
+  return __builtin_bit_cast(P, v);
+}
+
+// Results on their way out.  Where a call writes more rows of whole cache lines than half of the 256 MB of the memory-side cache, they are marked to
+// leave the caches first, so that its other rows stay: a norm of 800,000 rows of 192 bf16 that also writes its sum 235 -> 229 us, with the call that
+// reads the results 362 -> 346; 200,000 rows of 384 read back from 8 bits 46 -> 37.5.  Of fewer, the next call finds them there: two norms of
 // 100,000 rows one after the other 48.7 us, marked 51.3.
 template <typename P> __device__ __forceinline__ void write_out(P* to, P p, bool leaves) {
   if (leaves) {
@@ -104,11 +116,77 @@ template <typename P> __device__ __forceinline__ void write_out(P* to, P p, bool
     asm volatile("");
   } else *to = p;
 }
-inline bool leaves_caches(int64_t n, int32_t C, int arrays, int elem) { return n * C * arrays * elem > (128 << 20); }
+// all: addresses and strides in bytes of the results, joined
+inline bool leaves_caches(uintptr_t all, int64_t n, int32_t C, int arrays, int elem) {
+  return (all & 127u) == 0 && n * C * arrays * elem > (128 << 20);
+}
+
+// The pieces of one row that a lane holds: piece r is number r * kLanes + part, past the row's end zero.  kLoose: rows begin on any value, and the last
+// piece may hold fewer than V of them (a row holds V at least); it is read so that it ends with the row, shifted, and written value by value.  Of
+// the first whole_pieces() every lane has a whole one, as launch_pieces takes no more pieces a lane than it has to, but for four where three would do.
+template <int kLanes, int R> constexpr int whole_pieces() { return kLanes == kThreads && R == kVectors ? R - 2 : R - 1; }
+template <typename T, int V, int kLanes, int R, bool kLoose> struct RowOf {
+  typedef typename Piece<T, V>::type P;
+  typedef T Anywhere __attribute__((ext_vector_type(V), aligned(sizeof(T))));
+  P p[R];
+  __device__ __forceinline__ void load(const void* base, int64_t at, int part, int C) {
+    const T* row = static_cast<const T*>(base) + at;
+#pragma unroll
+    for (int r = 0; r < R; ++r) {
+      const int first = (r * kLanes + part) * V;
+      P zero = {};
+      if constexpr (!kLoose) p[r] = first < C ? *reinterpret_cast<const P*>(row + first) : zero;
+      else if (r < whole_pieces<kLanes, R>()) p[r] = *reinterpret_cast<const Anywhere*>(row + first);
+      else {
+        const int past = first < C && first + V > C ? first + V - C : 0;
+        p[r] = first < C ? (P)*reinterpret_cast<const Anywhere*>(row + (first - past)) : zero;
+        if (past) p[r] = shifted<P>(p[r], 8 * (int)sizeof(T) * past);
+      }
+    }
+  }
+  __device__ __forceinline__ static void store(void* base, int64_t at, int part, int C, const float (&f)[R][V], bool leaves) {
+    T* row = static_cast<T*>(base) + at;
+#pragma unroll
+    for (int r = 0; r < R; ++r) {
+      const int first = (r * kLanes + part) * V;
+      const P q = narrow<T, V>(f[r]);
+      if constexpr (!kLoose) {
+        if (first < C) write_out(reinterpret_cast<P*>(row + first), q, leaves);
+      } else if (r < whole_pieces<kLanes, R>() || first + V <= C) *reinterpret_cast<Anywhere*>(row + first) = q;
+      else {
+#pragma unroll
+        for (int i = 0; i < V - 1; ++i)
+          if (first + i < C) row[first + i] = q[i];
+      }
+    }
+  }
+};
+template <int V, int kLanes, int R, bool kLoose> __device__ __forceinline__ void load_values(const float* v, int part, int C, float (&f)[R][V]) {
+#pragma unroll
+  for (int r = 0; r < R; ++r)
+#pragma unroll
+    for (int i = 0; i < V; ++i) {
+      const int first = (r * kLanes + part) * V, at = kLoose ? first + i : first;
+      f[r][i] = at < C ? v[first + i] : 0.f;
+    }
+}
+
+// What pieces a call's rows go in: of 16 bytes, if all rows begin on 16 and are whole pieces (kPieces) or begin and end on any value (kLooseEnds: 300,000
+// rows of 191 bf16, norm backward 464 us in values, LOOSE in pieces); rows of fewer values than a piece value by value.
+enum RowForm { kPieces, kLooseEnds, kValues };
+inline RowForm row_form(uintptr_t all, int32_t C, int e) { return C * e < 16 ? kValues : (all & 15u) == 0 && C * e % 16 == 0 ? kPieces : kLooseEnds; }
+inline int form_lanes(RowForm form, int32_t C, int e) { return form == kValues ? 8 : row_lanes((int32_t)dsvt_ceil_div(C, 16 / e), 16); }
+// Launches Kernel<kLoose>::rows<T, V, kLanes, R>(a, groups, st).
+template <template <bool> class Kernel, typename T, typename Args> void launch_form(const Args& a, RowForm form, int lanes, unsigned groups, hipStream_t st) {
+  constexpr int V = 16 / (int)sizeof(T);
+  if (form == kPieces) launch_pieces<Kernel<false>, T, V>(a, lanes, groups, st);
+  else if (form == kLooseEnds) launch_pieces<Kernel<true>, T, V>(a, lanes, groups, st);
+  else Kernel<false>::template rows<T, 1, 8, 1>(a, groups, st);
+}
 
 // The row's pieces v in 8 bits: what its kLanes lanes hold of it goes to `codes`, its scale to *scale.
-template <int V, int kLanes, int R>
-__device__ __forceinline__ void store_codes(const float (&v)[R][V], int part, int pieces, int8_t* codes, float* scale, uint32_t* s) {
+template <int V, int kLanes, int R, bool kLoose>
+__device__ __forceinline__ void store_codes(const float (&v)[R][V], int part, int C, int8_t* codes, float* scale, uint32_t* s) {
   float top = 0.f;
 #pragma unroll
   for (int r = 0; r < R; ++r) {
@@ -121,10 +199,17 @@ __device__ __forceinline__ void store_codes(const float (&v)[R][V], int part, in
   const RowScale by(lane_join<kLanes>(size_bits(top), s, [](uint32_t a, uint32_t b) { return a > b ? a : b; }));
   if (part == 0) *scale = by.scale;
   typedef typename Codes<V>::type P;
-  P* row = reinterpret_cast<P*>(codes);
 #pragma unroll
-  for (int r = 0; r < R; ++r)
-    if (r * kLanes + part < pieces) row[r * kLanes + part] = by.codes(v[r]);
+  for (int r = 0; r < R; ++r) {
+    const int first = (r * kLanes + part) * V;
+    const P q = by.template codes<V>(v[r]);
+    if (!kLoose ? first < C : r < whole_pieces<kLanes, R>() || first + V <= C) *reinterpret_cast<P*>(codes + first) = q;
+    else if constexpr (kLoose) {
+#pragma unroll
+      for (int i = 0; i < V - 1; ++i)
+        if (first + i < C) codes[first + i] = byte_of(q, i);
+    }
+  }
 }
 
 // GELU, x Phi(x), and its slope Phi(x) + x phi(x).  Phi(-|x|) = phi-like exponential times a polynomial of 1 / (1 + p z), z = |x| / sqrt 2

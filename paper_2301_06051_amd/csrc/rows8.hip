@@ -21,25 +21,25 @@ struct Rows8Args {
   bool leaves;                                    // readers: write_out
 };
 
-template <bool kGelu, typename T, int V, int kLanes, int R>
+template <bool kGelu, typename T, int V, int kLanes, int R, bool kLoose>
 __global__ __launch_bounds__(kThreads) void k_write_rows8(Rows8Args a) {
   constexpr int kRows = kThreads / kLanes;
   __shared__ uint32_t s[kThreads / 64];
-  const int part = threadIdx.x % kLanes, pieces = a.C / V;
+  const int part = threadIdx.x % kLanes;
   for (int64_t row = (int64_t)blockIdx.x * kRows + threadIdx.x / kLanes; row < a.n; row += (int64_t)gridDim.x * kRows) {
-    RowPieces<T, V, kLanes, R> x;
-    x.load(a.x, row * a.ld_x, part, pieces, true);
+    RowOf<T, V, kLanes, R, kLoose> x;
+    x.load(a.x, row * a.ld_x, part, a.C);
     float v[R][V];
 #pragma unroll
     for (int r = 0; r < R; ++r) widen<T, V>(x.p[r], v[r]);
-    if (a.kept) store_codes<V, kLanes, R>(v, part, pieces, a.kept + row * a.ld_kept, a.kept_scale + row, s);
+    if (a.kept) store_codes<V, kLanes, R, kLoose>(v, part, a.C, a.kept + row * a.ld_kept, a.kept_scale + row, s);
     if constexpr (kGelu) {
       if (!a.out) continue;
 #pragma unroll
       for (int r = 0; r < R; ++r)
 #pragma unroll
         for (int i = 0; i < V; ++i) v[r][i] = gelu(v[r][i]);
-      store_codes<V, kLanes, R>(v, part, pieces, a.out + row * a.ld_out, a.out_scale + row, s);
+      store_codes<V, kLanes, R, kLoose>(v, part, a.C, a.out + row * a.ld_out, a.out_scale + row, s);
     }
   }
 }
@@ -70,67 +70,69 @@ template <bool kGelu, typename T> __global__ __launch_bounds__(kThreads) void k_
 }
 
 // kLanes lanes go along a row of any length.
-template <bool kGelu, typename T, int V, int kLanes> __global__ __launch_bounds__(kThreads) void k_read_rows8(Rows8Args a) {
+template <bool kGelu, typename T, int V, int kLanes, bool kLoose> __global__ __launch_bounds__(kThreads) void k_read_rows8(Rows8Args a) {
   constexpr int kAtOnce = kGelu ? 2 : 1;          // pieces asked for before one is used: 800,000 rows of 384 backward 289 us with one, 284 with two
   constexpr int kRows = kThreads / kLanes;
-  const int part = threadIdx.x % kLanes, pieces = a.C / V;
-  typedef typename Piece<T, V>::type P;
+  typedef RowOf<T, V, 1, 1, kLoose> Row;          // (a piece by itself)
   typedef typename Codes<V>::type Q;
+  const int part = threadIdx.x % kLanes;
   for (int64_t row = (int64_t)blockIdx.x * kRows + threadIdx.x / kLanes; row < a.n; row += (int64_t)gridDim.x * kRows) {
-    const Q* codes = reinterpret_cast<const Q*>(a.kept + row * a.ld_kept);
+    const int8_t* codes = a.kept + row * a.ld_kept;
     const float scale = a.kept_scale[row];
-    P* out = reinterpret_cast<P*>(static_cast<T*>(a.y) + row * a.ld_y);
-    const P* dy = kGelu ? reinterpret_cast<const P*>(static_cast<const T*>(a.dy) + row * a.ld_dy) : nullptr;
-    for (int p0 = part; p0 < pieces; p0 += kAtOnce * kLanes) {
+    for (int p0 = part * V; p0 < a.C; p0 += kAtOnce * kLanes * V) {
       Q q[kAtOnce];
-      P d[kGelu ? kAtOnce : 1];
+      Row d[kGelu ? kAtOnce : 1];
 #pragma unroll
       for (int u = 0; u < kAtOnce; ++u) {
-        const int p = p0 + u * kLanes < pieces ? p0 + u * kLanes : p0;
-        q[u] = codes[p];
-        if constexpr (kGelu) d[u] = dy[p];
+        const int p = p0 + u * kLanes * V < a.C ? p0 + u * kLanes * V : p0;
+        q[u] = *reinterpret_cast<const Q*>(codes + p);
+        if constexpr (kGelu) d[u].load(a.dy, row * a.ld_dy, p / V, a.C);
       }
 #pragma unroll
       for (int u = 0; u < kAtOnce; ++u) {
-        if (p0 + u * kLanes >= pieces) break;
-        float f[V];
-        values_of<V>(q[u], scale, f);
+        const int p = p0 + u * kLanes * V;
+        if (p >= a.C) break;
+        float f[1][V];
+        values_of<V>(q[u], scale, f[0]);
         if constexpr (kGelu) {
           float g[V];
-          widen<T, V>(d[u], g);
+          widen<T, V>(d[u].p[0], g);
 #pragma unroll
-          for (int i = 0; i < V; ++i) f[i] = g[i] * gelu_slope(f[i]);
+          for (int i = 0; i < V; ++i) f[0][i] = g[i] * gelu_slope(f[0][i]);
         }
-        write_out(out + p0 + u * kLanes, narrow<T, V>(f), a.leaves);
+        Row::store(a.y, row * a.ld_y, p / V, a.C, f, a.leaves);
       }
     }
   }
 }
 
 template <bool kGelu> struct Write {
-  template <typename T, int V, int kLanes, int R> static void rows(const Rows8Args& a, unsigned groups, hipStream_t st) {
-    k_write_rows8<kGelu, T, V, kLanes, R><<<groups, kThreads, 0, st>>>(a);
-  }
+  template <bool kLoose> struct Kernel {
+    template <typename T, int V, int kLanes, int R> static void rows(const Rows8Args& a, unsigned groups, hipStream_t st) {
+      k_write_rows8<kGelu, T, V, kLanes, R, kLoose><<<groups, kThreads, 0, st>>>(a);
+    }
+  };
 };
-template <bool kGelu, typename T> void launch_write(const Rows8Args& a, int v, int lanes, unsigned groups, hipStream_t st) {
+template <bool kGelu, typename T> void launch_write(const Rows8Args& a, RowForm form, int lanes, unsigned groups, hipStream_t st) {
   if (lanes == 0) k_write_rows8_long<kGelu, T><<<groups, kThreads, 0, st>>>(a);
-  else launch_rows<Write<kGelu>, T>(a, v, lanes, groups, st);
+  else launch_form<Write<kGelu>::template Kernel, T>(a, form, lanes, groups, st);
 }
-template <bool kGelu, typename T, int V> void launch_read(const Rows8Args& a, hipStream_t st) {
+template <bool kGelu, typename T, int V, bool kLoose> void launch_read(const Rows8Args& a, hipStream_t st) {
   int lanes = 8;
   while (lanes < 64 && lanes * 4 < a.C / V) lanes *= 2;
   const int64_t all = dsvt_ceil_div(a.n, kThreads / lanes);
   const unsigned groups = (unsigned)(all < 2 * kForwardGroups ? all : 2 * kForwardGroups);
-  if (lanes == 8) k_read_rows8<kGelu, T, V, 8><<<groups, kThreads, 0, st>>>(a);
-  else if (lanes == 16) k_read_rows8<kGelu, T, V, 16><<<groups, kThreads, 0, st>>>(a);
-  else if (lanes == 32) k_read_rows8<kGelu, T, V, 32><<<groups, kThreads, 0, st>>>(a);
-  else k_read_rows8<kGelu, T, V, 64><<<groups, kThreads, 0, st>>>(a);
+  if (V == 1 || lanes == 8) k_read_rows8<kGelu, T, V, 8, kLoose><<<groups, kThreads, 0, st>>>(a);
+  else if constexpr (V == 1) return;
+  else if (lanes == 16) k_read_rows8<kGelu, T, V, 16, kLoose><<<groups, kThreads, 0, st>>>(a);
+  else if (lanes == 32) k_read_rows8<kGelu, T, V, 32, kLoose><<<groups, kThreads, 0, st>>>(a);
+  else k_read_rows8<kGelu, T, V, 64, kLoose><<<groups, kThreads, 0, st>>>(a);
 }
-template <bool kGelu, typename T> void launch_read(const Rows8Args& a, int v, hipStream_t st) {
-  if (v == 1) launch_read<kGelu, T, 1>(a, st);
-  else if (v == 2) launch_read<kGelu, T, 2>(a, st);
-  else if (v * sizeof(T) == 8) launch_read<kGelu, T, 8 / (int)sizeof(T)>(a, st);
-  else launch_read<kGelu, T, 16 / (int)sizeof(T)>(a, st);
+template <bool kGelu, typename T> void launch_read(const Rows8Args& a, RowForm form, hipStream_t st) {
+  constexpr int V = 16 / (int)sizeof(T);
+  if (form == kPieces) launch_read<kGelu, T, V, false>(a, st);
+  else if (form == kLooseEnds) launch_read<kGelu, T, V, true>(a, st);
+  else launch_read<kGelu, T, 1, false>(a, st);
 }
 
 int check(int32_t C, int32_t dtype, int32_t n_rows) {
@@ -149,14 +151,15 @@ int write(bool with_gelu, int32_t C, int32_t dtype, const void* x, int64_t ld_x,
   a.x = x; a.ld_x = ld_x; a.n = n_rows; a.C = C;
   if (out) { a.out = out->codes; a.out_scale = out->scale; a.ld_out = out->ld; }
   if (kept) { a.kept = kept->codes; a.kept_scale = kept->scale; a.ld_kept = kept->ld; }
-  const int v = piece_elems((uintptr_t)x | (uintptr_t)(ld_x * e), C, e), lanes = row_lanes(C / v, v * e);
+  const RowForm form = row_form((uintptr_t)x | (uintptr_t)(ld_x * e), C, e);
+  const int lanes = form_lanes(form, C, e);
   const int64_t all = dsvt_ceil_div(n_rows, lanes ? kThreads / lanes : 1);
   const unsigned groups = (unsigned)(all < kForwardGroups ? all : kForwardGroups);
   hipStream_t st = (hipStream_t)stream;
   {
     dsvt_prof_scope ps(DSVT_K_ROWS8_WRITE, st);
-    if (dtype == DSVT_BF16) with_gelu ? launch_write<true, bf16_t>(a, v, lanes, groups, st) : launch_write<false, bf16_t>(a, v, lanes, groups, st);
-    else with_gelu ? launch_write<true, float>(a, v, lanes, groups, st) : launch_write<false, float>(a, v, lanes, groups, st);
+    if (dtype == DSVT_BF16) with_gelu ? launch_write<true, bf16_t>(a, form, lanes, groups, st) : launch_write<false, bf16_t>(a, form, lanes, groups, st);
+    else with_gelu ? launch_write<true, float>(a, form, lanes, groups, st) : launch_write<false, float>(a, form, lanes, groups, st);
   }
   DSVT_HIP_TRY(hipGetLastError());
   return DSVT_OK;
@@ -170,13 +173,13 @@ int read(bool with_gelu, int32_t C, int32_t dtype, const dsvt_rows8* kept, const
   if (bad_rows8(kept, C) || bad_rows(y, ld_y, C, e) || (with_gelu && bad_rows(dy, ld_dy, C, e))) return DSVT_EINVAL;
   Rows8Args a = {};
   a.dy = dy; a.ld_dy = ld_dy; a.y = y; a.ld_y = ld_y; a.kept = kept->codes; a.kept_scale = kept->scale; a.ld_kept = kept->ld; a.n = n_rows; a.C = C;
-  const int v = piece_elems((uintptr_t)dy | (uintptr_t)y | (uintptr_t)((ld_dy | ld_y) * e), C, e);
-  a.leaves = v * e == 16 && leaves_caches(n_rows, C, 1, e);
+  const RowForm form = row_form((uintptr_t)dy | (uintptr_t)y | (uintptr_t)((ld_dy | ld_y) * e), C, e);
+  a.leaves = leaves_caches((uintptr_t)y | (uintptr_t)(ld_y * e), n_rows, C, 1, e);
   hipStream_t st = (hipStream_t)stream;
   {
     dsvt_prof_scope ps(DSVT_K_ROWS8_READ, st);
-    if (dtype == DSVT_BF16) with_gelu ? launch_read<true, bf16_t>(a, v, st) : launch_read<false, bf16_t>(a, v, st);
-    else with_gelu ? launch_read<true, float>(a, v, st) : launch_read<false, float>(a, v, st);
+    if (dtype == DSVT_BF16) with_gelu ? launch_read<true, bf16_t>(a, form, st) : launch_read<false, bf16_t>(a, form, st);
+    else with_gelu ? launch_read<true, float>(a, form, st) : launch_read<false, float>(a, form, st);
   }
   DSVT_HIP_TRY(hipGetLastError());
   return DSVT_OK;
