@@ -106,6 +106,43 @@ template <bool kGelu, typename T, int V, int kLanes, bool kLoose> __global__ __l
   }
 }
 
+// The same for rows that begin and end on any value: a lane asks for all its pieces before it uses one.
+template <bool kGelu, typename T, int V, int kLanes, int R> __global__ __launch_bounds__(kThreads) void k_read_rows8_loose(Rows8Args a) {
+  constexpr int kRows = kThreads / kLanes;
+  typedef RowOf<T, V, kLanes, R, true> Row;
+  typedef typename Codes<V>::type Q;
+  const int part = threadIdx.x % kLanes, last = (a.C - 1) / V * V;
+  for (int64_t row = (int64_t)blockIdx.x * kRows + threadIdx.x / kLanes; row < a.n; row += (int64_t)gridDim.x * kRows) {
+    const int8_t* codes = a.kept + row * a.ld_kept;
+    const float scale = a.kept_scale[row];
+    Q q[R];
+#pragma unroll
+    for (int r = 0; r < R; ++r) {
+      const int first = (r * kLanes + part) * V;
+      q[r] = *reinterpret_cast<const Q*>(codes + (first < last ? first : last));
+    }
+    Row d;
+    if constexpr (kGelu) d.load(a.dy, row * a.ld_dy, part, a.C);
+    float f[R][V];
+#pragma unroll
+    for (int r = 0; r < R; ++r) {
+      values_of<V>(q[r], scale, f[r]);
+      if constexpr (kGelu) {
+        float g[V];
+        widen<T, V>(d.p[r], g);
+#pragma unroll
+        for (int i = 0; i < V; ++i) f[r][i] = g[i] * gelu_slope(f[r][i]);
+      }
+    }
+    Row::store(a.y, row * a.ld_y, part, a.C, f, false);
+  }
+}
+
+template <bool kGelu> struct Read {
+  template <typename T, int V, int kLanes, int R> static void rows(const Rows8Args& a, unsigned groups, hipStream_t st) {
+    k_read_rows8_loose<kGelu, T, V, kLanes, R><<<groups, kThreads, 0, st>>>(a);
+  }
+};
 template <bool kGelu> struct Write {
   template <bool kLoose> struct Kernel {
     template <typename T, int V, int kLanes, int R> static void rows(const Rows8Args& a, unsigned groups, hipStream_t st) {
@@ -131,7 +168,12 @@ template <bool kGelu, typename T, int V, bool kLoose> void launch_read(const Row
 template <bool kGelu, typename T> void launch_read(const Rows8Args& a, RowForm form, hipStream_t st) {
   constexpr int V = 16 / (int)sizeof(T);
   if (form == kPieces) launch_read<kGelu, T, V, false>(a, st);
-  else if (form == kLooseEnds) launch_read<kGelu, T, V, true>(a, st);
+  else if (form == kLooseEnds) {
+    const int lanes = form_lanes(form, a.C, sizeof(T));
+    const int64_t all = dsvt_ceil_div(a.n, lanes ? kThreads / lanes : 1);
+    if (lanes == 0) launch_read<kGelu, T, V, true>(a, st);       // (longer ones)
+    else launch_pieces<Read<kGelu>, T, V>(a, lanes, (unsigned)(all < kForwardGroups ? all : kForwardGroups), st);
+  }
   else launch_read<kGelu, T, 1, false>(a, st);
 }
 

@@ -499,6 +499,39 @@ def test_linear_of_short_rows(n, c, o, dtype, form, bias, act):
     assert bool((y[n:] == 3).all()) and (form == "tight" or bool((y._base[:, -1] == 7).all()))
 
 
+@pytest.mark.parametrize("c", [3, 7, 9, 99, 191, 300, 1025, 2057, 4100, 8189, 9001])
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_what_lies_beside_rows(c, dtype):
+    """Rows that begin and end on any value: what lies before and behind them stays as it is, in rows and in codes."""
+    n, g, ld = 13, _gen(c), (c + 15) // 16 * 16 + 16
+    print("[case] beside rows", c, dtype, flush=True)
+    x, r, dy = (_placed(torch.randn((n, c), generator=g).to(DT[dtype]), "odd") for _ in range(3))
+    norm = dsvt.RmsNorm((1 + 0.1 * torch.randn((c,), generator=g)).cuda(), dtype)
+
+    def rows():
+        return torch.full((n, c + 3), 5.0, dtype=DT[dtype], device="cuda")
+
+    def codes():
+        wide = torch.full((n, ld), 77, dtype=torch.int8, device="cuda")
+        return wide, dsvt.Rows8.of(wide[:, :c], torch.zeros((n,), device="cuda"))
+
+    (a, b, d, e, f), (p, k8), (q, o8), (w, r8) = (rows() for _ in range(5)), codes(), codes(), codes()
+    inner = slice(1, 1 + c)
+    dsvt.dsvt_rms_norm(norm, x, r, y=a[:, inner], z=b[:, inner])
+    dsvt.dsvt_rms_norm_rows8(norm, x, r, out=r8)
+    dsvt.dsvt_rms_norm_backward(norm, dy, x, r, dx=d[:, inner])
+    dsvt.dsvt_gelu_rows8(x, out=o8, kept=k8)
+    dsvt.dsvt_read_rows8(k8, dtype, x=e[:, inner])
+    dsvt.dsvt_gelu_rows8_backward(k8, dy, dh=f[:, inner])
+    y, z = dsvt.dsvt_rms_norm(norm, x.contiguous(), r.contiguous(), want_sum=True)
+    kept = dsvt.dsvt_keep_rows8(x.contiguous())
+    assert torch.equal(k8.codes, kept.codes) and torch.equal(k8.scale, kept.scale)
+    assert torch.equal(a[:, inner], y) and torch.equal(b[:, inner], z) and torch.equal(e[:, inner], dsvt.dsvt_read_rows8(kept, dtype))
+    assert torch.equal(f[:, inner], dsvt.dsvt_gelu_rows8_backward(kept, dy.contiguous()))
+    assert all(bool((t[:, 0] == 5).all()) and bool((t[:, 1 + c:] == 5).all()) for t in (a, b, d, e, f))
+    assert all(bool((t[:, c:] == 77).all()) for t in (p, q, w))
+
+
 @pytest.mark.parametrize("n,c,dtype", [(360000, 192, "bf16"), (90000, 385, "f32"), (90000, 384, "f32")])
 def test_large_results(n, c, dtype):
     """Results of more than 128 MB, whose stores are marked: as in parts of 1 / 9."""
