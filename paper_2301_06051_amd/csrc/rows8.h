@@ -123,8 +123,8 @@ inline bool leaves_caches(uintptr_t all, int64_t n, int32_t C, int arrays, int e
 
 // The pieces of one row that a lane holds: piece r is number r * kLanes + part, past the row's end zero.  kLoose: rows begin on any value, and the last
 // piece may hold fewer than V of them (a row holds V at least); it is read so that it ends with the row, shifted, and written value by value.  Of
-// the first whole_pieces() every lane has a whole one, as launch_pieces takes no more pieces a lane than it has to, but for four where three would do.
-template <int kLanes, int R> constexpr int whole_pieces() { return kLanes == kThreads && R == kVectors ? R - 2 : R - 1; }
+// the first whole_pieces() every lane has a whole one, as launch_form takes no more pieces a lane than it has to, but for four where three would do and so on.
+template <int kLanes, int R> constexpr int whole_pieces() { return kLanes == kThreads && R >= kVectors ? R - 2 : R - 1; }
 template <typename T, int V, int kLanes, int R, bool kLoose> struct RowOf {
   typedef typename Piece<T, V>::type P;
   typedef T Anywhere __attribute__((ext_vector_type(V), aligned(sizeof(T))));
@@ -171,16 +171,29 @@ template <int V, int kLanes, int R, bool kLoose> __device__ __forceinline__ void
     }
 }
 
-// What pieces a call's rows go in: of 16 bytes, if all rows begin on 16 and are whole pieces (kPieces) or begin and end on any value (kLooseEnds: 300,000
-// rows of 191 bf16, norm backward 464 us in values, LOOSE in pieces); rows of fewer values than a piece value by value.
+// What pieces a call's rows go in: of 16 bytes, if all rows begin on 16 and are whole pieces (kPieces) or begin and end on any value (kLooseEnds: norm
+// backward of 300,000 rows of 191 bf16 464 us in values, 104 in pieces, of 192 91); rows of fewer values than a piece value by value.
 enum RowForm { kPieces, kLooseEnds, kValues };
 inline RowForm row_form(uintptr_t all, int32_t C, int e) { return C * e < 16 ? kValues : (all & 15u) == 0 && C * e % 16 == 0 ? kPieces : kLooseEnds; }
-inline int form_lanes(RowForm form, int32_t C, int e) { return form == kValues ? 8 : row_lanes((int32_t)dsvt_ceil_div(C, 16 / e), 16); }
+// Lanes of a row, none if registers do not hold it: a lane takes 32 values at most, which are eight pieces in 32 bits (8,000 rows of 8,192, norm backward:
+// 1,007 us read again, 204 held).
+inline int form_lanes(RowForm form, int32_t C, int e) {
+  const int32_t pieces = (int32_t)dsvt_ceil_div(C, 16 / e);
+  return form == kValues ? 8 : e == 4 && pieces > kThreads * kVectors && pieces <= 2 * kThreads * kVectors ? kThreads : row_lanes(pieces, 16);
+}
+template <typename Kernel, typename T, typename Args> void launch_form(const Args& a, int lanes, unsigned groups, hipStream_t st) {
+  constexpr int V = 16 / (int)sizeof(T);
+  if constexpr (sizeof(T) == 4) {
+    const int64_t r = dsvt_ceil_div(dsvt_ceil_div(a.C, V), lanes);
+    if (r > kVectors && r <= 6) return Kernel::template rows<T, V, kThreads, 6>(a, groups, st);
+    if (r > 6) return Kernel::template rows<T, V, kThreads, 2 * kVectors>(a, groups, st);
+  }
+  launch_pieces<Kernel, T, V>(a, lanes, groups, st);
+}
 // Launches Kernel<kLoose>::rows<T, V, kLanes, R>(a, groups, st).
 template <template <bool> class Kernel, typename T, typename Args> void launch_form(const Args& a, RowForm form, int lanes, unsigned groups, hipStream_t st) {
-  constexpr int V = 16 / (int)sizeof(T);
-  if (form == kPieces) launch_pieces<Kernel<false>, T, V>(a, lanes, groups, st);
-  else if (form == kLooseEnds) launch_pieces<Kernel<true>, T, V>(a, lanes, groups, st);
+  if (form == kPieces) launch_form<Kernel<false>, T>(a, lanes, groups, st);
+  else if (form == kLooseEnds) launch_form<Kernel<true>, T>(a, lanes, groups, st);
   else Kernel<false>::template rows<T, 1, 8, 1>(a, groups, st);
 }
 

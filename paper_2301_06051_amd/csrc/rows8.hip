@@ -172,7 +172,7 @@ template <bool kGelu, typename T> void launch_read(const Rows8Args& a, RowForm f
     const int lanes = form_lanes(form, a.C, sizeof(T));
     const int64_t all = dsvt_ceil_div(a.n, lanes ? kThreads / lanes : 1);
     if (lanes == 0) launch_read<kGelu, T, V, true>(a, st);       // (longer ones)
-    else launch_pieces<Read<kGelu>, T, V>(a, lanes, (unsigned)(all < kForwardGroups ? all : kForwardGroups), st);
+    else launch_form<Read<kGelu>, T>(a, lanes, (unsigned)(all < kForwardGroups ? all : kForwardGroups), st);
   }
   else launch_read<kGelu, T, 1, false>(a, st);
 }

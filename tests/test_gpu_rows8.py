@@ -499,7 +499,7 @@ def test_linear_of_short_rows(n, c, o, dtype, form, bias, act):
     assert bool((y[n:] == 3).all()) and (form == "tight" or bool((y._base[:, -1] == 7).all()))
 
 
-@pytest.mark.parametrize("c", [3, 7, 9, 99, 191, 300, 1025, 2057, 4100, 8189, 9001])
+@pytest.mark.parametrize("c", [3, 7, 9, 99, 191, 300, 1025, 2057, 4100, 6001, 8189, 9001])
 @pytest.mark.parametrize("dtype", ["bf16", "f32"])
 def test_what_lies_beside_rows(c, dtype):
     """Rows that begin and end on any value: what lies before and behind them stays as it is, in rows and in codes."""
