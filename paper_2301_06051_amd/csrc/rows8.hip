@@ -75,23 +75,23 @@ template <bool kGelu, typename T, int V, int kLanes, bool kLoose> __global__ __l
   constexpr int kRows = kThreads / kLanes;
   typedef RowOf<T, V, 1, 1, kLoose> Row;          // (a piece by itself)
   typedef typename Codes<V>::type Q;
-  const int part = threadIdx.x % kLanes;
+  const int part = threadIdx.x % kLanes, pieces = (a.C + V - 1) / V;
   for (int64_t row = (int64_t)blockIdx.x * kRows + threadIdx.x / kLanes; row < a.n; row += (int64_t)gridDim.x * kRows) {
-    const int8_t* codes = a.kept + row * a.ld_kept;
+    const Q* codes = reinterpret_cast<const Q*>(a.kept + row * a.ld_kept);
     const float scale = a.kept_scale[row];
-    for (int p0 = part * V; p0 < a.C; p0 += kAtOnce * kLanes * V) {
+    for (int p0 = part; p0 < pieces; p0 += kAtOnce * kLanes) {
       Q q[kAtOnce];
       Row d[kGelu ? kAtOnce : 1];
 #pragma unroll
       for (int u = 0; u < kAtOnce; ++u) {
-        const int p = p0 + u * kLanes * V < a.C ? p0 + u * kLanes * V : p0;
-        q[u] = *reinterpret_cast<const Q*>(codes + p);
-        if constexpr (kGelu) d[u].load(a.dy, row * a.ld_dy, p / V, a.C);
+        const int p = p0 + u * kLanes < pieces ? p0 + u * kLanes : p0;
+        q[u] = codes[p];
+        if constexpr (kGelu) d[u].load(a.dy, row * a.ld_dy, p, a.C);
       }
 #pragma unroll
       for (int u = 0; u < kAtOnce; ++u) {
-        const int p = p0 + u * kLanes * V;
-        if (p >= a.C) break;
+        const int p = p0 + u * kLanes;
+        if (p >= pieces) break;
         float f[1][V];
         values_of<V>(q[u], scale, f[0]);
         if constexpr (kGelu) {
@@ -100,7 +100,7 @@ template <bool kGelu, typename T, int V, int kLanes, bool kLoose> __global__ __l
 #pragma unroll
           for (int i = 0; i < V; ++i) f[0][i] = g[i] * gelu_slope(f[0][i]);
         }
-        Row::store(a.y, row * a.ld_y, p / V, a.C, f, a.leaves);
+        Row::store(a.y, row * a.ld_y, p, a.C, f, a.leaves);
       }
     }
   }
