@@ -238,6 +238,7 @@ template <typename T, int kO, int kC, int kWO, int kWC, int kN, int kAhead, Ends
     for (int j = 0; j < TC; ++j) {
       const int out = o0 + (wo * TO + i) * 32 + m, col = c0 + (wc * TC + j) * 32 + 16 * h;
       if (a.slices > 1) {                         // partial sums as the lanes hold them: whole lines, which the second kernel finds its way in
+        if (out - m >= a.O || col - 16 * h >= a.C) continue;
         f32x4* to = reinterpret_cast<f32x4*>(a.partial) + (((int64_t)(slice * tiles + tile) * (kWO * kWC) + wave) * (TO * TC) + i * TC + j) * 256 + lane;
 #pragma unroll
         for (int e = 0; e < 16; e += 4) to[16 * e] = f32x4{acc[i][j][e], acc[i][j][e + 1], acc[i][j][e + 2], acc[i][j][e + 3]};
@@ -270,8 +271,13 @@ template <typename T, int kJoiners> __global__ __launch_bounds__(256 * kJoiners)
   __shared__ f32x4 parts[kJoiners][256];
   const int tid = threadIdx.x & 255, part = threadIdx.x >> 8, tiles_c = (a.C + t.kC - 1) / t.kC, tiles = tiles_c * ((a.O + t.kO - 1) / t.kO);
   const int inner = t.kO * t.kC / 1024;           // squares of 32 of a tile
+  const int tile = blockIdx.x / inner, square = blockIdx.x - tile * inner, wave = square / (t.TO * t.TC), of_wave = square - wave * (t.TO * t.TC);
+  const int i = of_wave / t.TC, j = of_wave - i * t.TC, wo = wave % t.kWO, wc = wave / t.kWO;
+  const int out0 = tile / tiles_c * t.kO + (wo * t.TO + i) * 32, col0 = (tile - tile / tiles_c * tiles_c) * t.kC + (wc * t.TC + j) * 32;
+  const bool weights = tile < tiles;
+  if (weights && (out0 >= a.O || col0 >= a.C)) return;             // (no workgroup wrote it)
   f32x4 v = {};
-  if ((int)blockIdx.x < tiles * inner) {
+  if (weights) {
     const f32x4* from = reinterpret_cast<const f32x4*>(a.partial) + (int64_t)blockIdx.x * 256 + tid;
     const int64_t step = (int64_t)tiles * inner * 256;
     int k = part;
@@ -295,11 +301,8 @@ template <typename T, int kJoiners> __global__ __launch_bounds__(256 * kJoiners)
 #pragma unroll
     for (int k = 1; k < kJoiners; ++k) v += parts[k][tid];
   }
-  if ((int)blockIdx.x < tiles * inner) {
-    const int tile = blockIdx.x / inner, square = blockIdx.x - tile * inner, wave = square / (t.TO * t.TC), of_wave = square - wave * (t.TO * t.TC);
-    const int i = of_wave / t.TC, j = of_wave - i * t.TC, wo = wave % t.kWO, wc = wave / t.kWO, lane = tid & 63;
-    const int out = tile / tiles_c * t.kO + (wo * t.TO + i) * 32 + (lane & 31);
-    const int col = (tile - tile / tiles_c * tiles_c) * t.kC + (wc * t.TC + j) * 32 + 16 * (lane >> 5) + 4 * (tid >> 6);
+  if (weights) {
+    const int lane = tid & 63, out = out0 + (lane & 31), col = col0 + 16 * (lane >> 5) + 4 * (tid >> 6);
     const float f[4] = {v[0], v[1], v[2], v[3]};
     if (out < a.O) write_some<T, 4>(static_cast<T*>(a.d_w) + out * a.ld_dw + col, f, a.C - col);
   } else if (const int o = ((int)blockIdx.x - tiles * inner) * 256 + tid; o < a.O) a.d_b[o] = v[0];
