@@ -535,9 +535,13 @@ template <typename T> int launch(const Linear8Args& a, hipStream_t st) {
   // 24.4, 30.2; 30,000 x 384 -> 192 12.0, 9.0, 8.1, 9.9; 1,024 x 2,048 -> 2,048 27.2, 14.8, 12.3, 10.6; 200,000 x 512 -> 64 49, 32, 30.5; 100,000 x 1,024 -> 320 72, 58, 60.
   // A workgroup alone on its compute unit does nothing beside results that cost more: 200,000 x 256 -> 1,024 112, 126, 156, but of 32 bits 191, 177, 209, with
   // GELU 209, 195, 211; 16,384 x 512 -> 4,096 of 32 bits 75, 82, with GELU 86, 86.
+  // Of long rows a round of the largest tiles may leave more of the chip empty: 28,652 x 4,153 -> 384 70, 84, 90, 136; 20,000 x 4,096 -> 512 57, 62, 66, 105;
+  // 6,000 x 4,096 -> 2,048 58, 60, 67, 121; 2,000 x 4,096 -> 4,096 52, 40, 50, 82; 30,000 x 1,024 -> 1,152 59, 52, 59, 88.
+  const bool more = a.C >= 2048;
   const int64_t rounds = dsvt_ceil_div(tiles(256, 256), kComputeUnits);
-  if ((int64_t)a.n * a.O >= rounds * (kComputeUnits * 256 * 256 / 5 * 4) && !(costly && a.C < 512)) return launch_tiles<T, 256, 256, 2, 4, 128, 2, 1>(a, st);
-  if (tiles(128, 128) >= 4 * kComputeUnits && a.O > 64) return launch_tiles<T, 128, 128, 4, 2, 128, 2, 2>(a, st);
+  if ((int64_t)a.n * a.O >= rounds * (kComputeUnits * 256 * 256 / 10 * (more ? 6 : 8)) && !(costly && a.C < 512))
+    return launch_tiles<T, 256, 256, 2, 4, 128, 2, 1>(a, st);
+  if (tiles(128, 128) >= kComputeUnits * (more ? 3 : 8) / 2 && a.O > 64) return launch_tiles<T, 128, 128, 4, 2, 128, 2, 2>(a, st);
   if (tiles(128, 64) >= 2 * kComputeUnits) return launch_tiles<T, 128, 64, 4, 1, 128, 2, 0>(a, st);
   return launch_tiles<T, 64, 64, 2, 2, 64, 3, 0>(a, st);
 }
