@@ -499,6 +499,22 @@ def test_linear_of_short_rows(n, c, o, dtype, form, bias, act):
     assert bool((y[n:] == 3).all()) and (form == "tight" or bool((y._base[:, -1] == 7).all()))
 
 
+@pytest.mark.parametrize("n,c,o,dtype,act", [(60000, 260, 250, "bf16", False), (120000, 272, 251, "bf16", False), (60001, 520, 253, "f32", True), (66001, 300, 200, "bf16", True),
+                                             (66000, 257, 130, "f32", False), (26000, 2100, 401, "bf16", False), (7000, 2053, 1000, "bf16", True), (7001, 2048, 999, "f32", False)])
+@pytest.mark.parametrize("form", ["tight", "odd"])
+def test_linear_of_large_tiles(n, c, o, dtype, act, form):
+    """Many rows, of which workgroups take large tiles, several of them each or as many as the chip has room for."""
+    g = _gen(n + 7 * c + o)
+    x, w, b = _random_codes(g, n, c), _random_codes(g, o, c, fill=-127), torch.randn((o,), generator=g)
+    case = f"large tiles {n} {c} {o} {dtype} {act} {form}"
+    print("[case]", case, flush=True)
+    y = _placed(torch.zeros((n + 2, o), dtype=DT[dtype]), form)
+    y[n:] = 3
+    dsvt.dsvt_linear_rows8(dsvt.Linear8(w, dtype, b.cuda(), act), x, y=y[:n])
+    ref.check("y", y[:n], *ref.linear(x.codes, x.scale, w.codes, w.scale, b, DT[dtype], act), case)
+    assert bool((y[n:] == 3).all()) and (form == "tight" or bool((y._base[:, -1] == 7).all()))
+
+
 @pytest.mark.parametrize("c", [3, 7, 9, 99, 191, 300, 1025, 2057, 4100, 6001, 8189, 9001])
 @pytest.mark.parametrize("dtype", ["bf16", "f32"])
 def test_what_lies_beside_rows(c, dtype):
