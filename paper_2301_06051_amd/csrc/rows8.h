@@ -176,10 +176,10 @@ template <int V, int kLanes, int R, bool kLoose> __device__ __forceinline__ void
 enum RowForm { kPieces, kLooseEnds, kValues };
 inline RowForm row_form(uintptr_t all, int32_t C, int e) { return C * e < 16 ? kValues : (all & 15u) == 0 && C * e % 16 == 0 ? kPieces : kLooseEnds; }
 // Lanes of a row, none if registers do not hold it: a lane takes 32 values at most, which are eight pieces in 32 bits (8,000 rows of 8,192, norm backward:
-// 1,007 us read again, 204 held).
+// 1,007 us read again, 204 held).  Rows of four pieces at most take four lanes (2,000,000 of 32 bf16, GELU 122 -> 64 us).
 inline int form_lanes(RowForm form, int32_t C, int e) {
   const int32_t pieces = (int32_t)dsvt_ceil_div(C, 16 / e);
-  return form == kValues ? 8 : e == 4 && pieces > kThreads * kVectors && pieces <= 2 * kThreads * kVectors ? kThreads : row_lanes(pieces, 16);
+  return form == kValues ? 8 : pieces <= 4 ? 4 : e == 4 && pieces > kThreads * kVectors && pieces <= 2 * kThreads * kVectors ? kThreads : row_lanes(pieces, 16);
 }
 template <typename Kernel, typename T, typename Args> void launch_form(const Args& a, int lanes, unsigned groups, hipStream_t st) {
   constexpr int V = 16 / (int)sizeof(T);
@@ -188,7 +188,8 @@ template <typename Kernel, typename T, typename Args> void launch_form(const Arg
     if (r > kVectors && r <= 6) return Kernel::template rows<T, V, kThreads, 6>(a, groups, st);
     if (r > 6) return Kernel::template rows<T, V, kThreads, 2 * kVectors>(a, groups, st);
   }
-  launch_pieces<Kernel, T, V>(a, lanes, groups, st);
+  if (lanes == 4) Kernel::template rows<T, V, 4, 1>(a, groups, st);
+  else launch_pieces<Kernel, T, V>(a, lanes, groups, st);
 }
 // Launches Kernel<kLoose>::rows<T, V, kLanes, R>(a, groups, st).
 template <template <bool> class Kernel, typename T, typename Args> void launch_form(const Args& a, RowForm form, int lanes, unsigned groups, hipStream_t st) {

@@ -155,12 +155,13 @@ template <bool kGelu, typename T> void launch_write(const Rows8Args& a, RowForm 
   else launch_form<Write<kGelu>::template Kernel, T>(a, form, lanes, groups, st);
 }
 template <bool kGelu, typename T, int V, bool kLoose> void launch_read(const Rows8Args& a, hipStream_t st) {
-  int lanes = 8;
-  while (lanes < 64 && lanes * 4 < a.C / V) lanes *= 2;
+  int lanes = V > 1 && a.C <= 4 * V ? 4 : 8;
+  while (lanes > 4 && lanes < 64 && lanes * 4 < a.C / V) lanes *= 2;
   const int64_t all = dsvt_ceil_div(a.n, kThreads / lanes);
   const unsigned groups = (unsigned)(all < 2 * kForwardGroups ? all : 2 * kForwardGroups);
   if (V == 1 || lanes == 8) k_read_rows8<kGelu, T, V, 8, kLoose><<<groups, kThreads, 0, st>>>(a);
   else if constexpr (V == 1) return;
+  else if (lanes == 4) k_read_rows8<kGelu, T, V, 4, kLoose><<<groups, kThreads, 0, st>>>(a);
   else if (lanes == 16) k_read_rows8<kGelu, T, V, 16, kLoose><<<groups, kThreads, 0, st>>>(a);
   else if (lanes == 32) k_read_rows8<kGelu, T, V, 32, kLoose><<<groups, kThreads, 0, st>>>(a);
   else k_read_rows8<kGelu, T, V, 64, kLoose><<<groups, kThreads, 0, st>>>(a);
