@@ -337,7 +337,8 @@ Plan make_plan(int32_t C, int32_t O, int32_t dtype, int32_t n) {
   const bool narrow = dtype == DSVT_BF16;
   const int64_t steps = dsvt_ceil_div(n, kRowsStep), least = narrow ? 1 : dsvt_ceil_div(n, kLongest);
   double best = 0.;
-  for (int f = 0; f < (O < (narrow ? 8 : 4) ? 1 : narrow ? kWideForms : 2); ++f) {       // (fewer outputs than a piece: the first form)
+  const int forms = O < (narrow ? 8 : 4) ? 1 : narrow ? kWideForms : 2;           // (fewer outputs than a piece: the first form)
+  for (int f = 0; f < forms; ++f) {
     const Form& form = kForms[!narrow][f];
     const int64_t tiles = dsvt_ceil_div(O, form.tile.kO) * dsvt_ceil_div(C, form.tile.kC);
     const double slice_us = (double)tile_values(form.tile, O, C) * 8. / 3e6;
@@ -347,7 +348,8 @@ Plan make_plan(int32_t C, int32_t O, int32_t dtype, int32_t n) {
     slices = slices > least ? slices : least;      // (one at least)
     const int64_t per = dsvt_ceil_div(steps, slices);
     slices = dsvt_ceil_div(steps, per);
-    const double us = (double)per * form.step * (tiles * slices > form.at_once ? (double)(tiles * slices) / form.at_once : 1.) + (slices > 1 ? slices * slice_us + 4. : 0.) + form.begin;
+    const double turns = tiles * slices > form.at_once ? (double)(tiles * slices) / form.at_once : 1.;
+    const double us = (double)per * form.step * turns + (slices > 1 ? slices * slice_us + 4. : 0.) + form.begin;
     if (f > 0 && us >= best) continue;
     best = us;
     p = {f, (int32_t)slices, (int32_t)(per * kRowsStep)};
