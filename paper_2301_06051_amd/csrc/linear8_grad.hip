@@ -4,13 +4,14 @@
 //
 // The sums run over the rows: workgroups take a tile of outputs and columns and a slice of the rows each, and leave partial sums in 32 bits, which
 // a second kernel adds up in the slices' order; one slice writes the results itself.  Rows go from memory through registers into one of two buffers in
-// LDS, the kept ones as s_n x[n][c]; in bf16 that is rounded to bf16, as an operand of the product (products of 32-bit operands run at a sixteenth of
-// the rate; the result, itself rounded, is off by 2.3e-3 of its norm instead of 1.7e-3).
+// LDS, the kept ones as s_n x[n][c].  Products of 32-bit operands run at a sixteenth of the rate of bf16, of which one would round s_n x[n][c] to 8 bits; it is
+// taken as two, its first bits and the rest, at twice the products: the result is off by its own rounding, 1.7e-3 of its norm (2.3e-3 with one
+// operand, and no number where that passes bf16), for 1.1 to 1.6 times the time.
 //
-// Both operands run along the rows, so both have to be turned round, which the LDS loads do (bf16).  With tiles of 256 the matrix cores, LDS and the
-// instructions that make values of codes are each busy for 1,024 clocks of a step of 32 rows, which takes 2,500: 65,536 rows of 1,024 -> 2,048 300 to 340
-// us (920 TFLOP/s; codes used as they are 45 us less, every step's rows the first ones 25), 2,048 -> 4,096 1,106 (994; the library's product of 8,192^3 in bf16
-// 1,362).  Few columns leave the partial sums and a step's latency: 30,000 rows of 192 -> 576 23 us, four of them the second kernel.
+// Both operands run along the rows, so both have to be turned round, which the LDS loads do (bf16).  With tiles of 256 the matrix cores are busy for 2,048
+// clocks of a step of 32 rows, LDS for 1,400, the instructions that make values of codes for 800: 65,536 rows of 1,024 -> 2,048 455 to 480 us (1,200 TFLOP/s of
+// products; the library's of 8,192^3 in bf16 1,362).  Few columns leave the partial sums and a step's latency: 30,000 rows of 192 -> 576 28 us, four of them the
+// second kernel.
 #include "rows8.h"
 #include <cmath>
 
@@ -33,7 +34,8 @@ struct Grad8Args {
 // Operand fragments out of LDS, where rows lie one after the other: 32 neighbouring columns, and the rows of one matrix instruction.
 template <typename T> struct Columns;
 template <> struct Columns<bf16_t> {
-  static constexpr int kStep = 16, kPad = 64;     // rows of an instruction; bytes that pad a row in LDS: a fragment's four rows then lie in all banks
+  static constexpr int kStep = 16, kTerms = 2;    // rows of an instruction; operands that a kept value is taken as
+  static constexpr int kPad = 64;                 // bytes that pad a row in LDS: a fragment's four rows then lie in all banks
   typedef bf16x8 Frag;
   static __device__ __forceinline__ f32x16 mma(Frag a, Frag b, f32x16 c) { return __builtin_amdgcn_mfma_f32_32x32x16_bf16(a, b, c, 0, 0, 0); }
   // Lane 32 h + m gets rows 8 h .. 8 h + 7 of column m.  Of 16 lanes, the load takes four rows of four pieces of four columns, and hands lane i the
@@ -49,7 +51,7 @@ template <> struct Columns<bf16_t> {
   }
 };
 template <> struct Columns<float> {
-  static constexpr int kStep = 2, kPad = 128;
+  static constexpr int kStep = 2, kTerms = 1, kPad = 128;
   typedef float Frag;
   static __device__ __forceinline__ f32x16 mma(Frag a, Frag b, f32x16 c) { return __builtin_amdgcn_mfma_f32_32x32x2f32(a, b, c, 0, 0, 0); }
   template <bool kTurn> static __device__ __forceinline__ Frag load(const char* p, int pitch) {
@@ -69,7 +71,7 @@ struct Shape { int kO, kC, kWO, TO, TC; };
 // kN rows at a time; those of kAhead steps are on their way.
 template <typename T, int kO, int kC, int kWO, int kWC, int kN, int kAhead> struct Tile {
   static constexpr int kAll = 64 * kWO * kWC, TO = kO / kWO / 32, TC = kC / kWC / 32, V = 16 / (int)sizeof(T);
-  static constexpr int kPitchO = kO * (int)sizeof(T) + Columns<T>::kPad, kPitchC = kC * (int)sizeof(T) + Columns<T>::kPad;
+  static constexpr int kPitchO = kO * (int)sizeof(T) + Columns<T>::kPad, kPlaneC = kC * (int)sizeof(T), kPitchC = Columns<T>::kTerms * kPlaneC + Columns<T>::kPad;
   static constexpr int kBuffer = kN * (kPitchO + kPitchC);
   static constexpr int kRowsO = kAll / (kO / V), kRowsC = kAll / (kC / 8);      // rows that all threads fetch at once, in pieces of 16 bytes of dy and 8 codes
   static constexpr int PO = kN / kRowsO, PC = kN / kRowsC;
@@ -161,10 +163,29 @@ template <typename T, int kO, int kC, int kWO, int kWC, int kN, int kAhead, Ends
       asm volatile("" : "+v"(g.x[i].x), "+v"(g.x[i].y), "+v"(g.s[i]));
       const int r = row_c + i * S::kRowsC;
       const typename Codes<8>::type codes = {g.x[i].x, g.x[i].y};
-      float f[8];
-      values_of<8>(codes, r >= before && r < rows ? g.s[i] : 0.f, f);
+      const float scale = r >= before && r < rows ? g.s[i] : 0.f;
       typedef typename Piece<T, 8>::type P8;
-      *reinterpret_cast<P8*>(to + kN * S::kPitchO + r * S::kPitchC + 8 * (int)sizeof(T) * piece_c) = narrow<T, 8>(f);
+      P8* const at = reinterpret_cast<P8*>(to + kN * S::kPitchO + r * S::kPitchC + 8 * (int)sizeof(T) * piece_c);
+      float f[8];
+      if constexpr (F::kTerms == 1) {
+        values_of<8>(codes, scale, f);
+        *at = narrow<T, 8>(f);
+      } else {
+        // The value is taken as the first 8 bits of one a little smaller, and the rest, at most 2^-7 of it, rounded to bf16: off by 2^-15 of it.  The first
+        // term then is never past bf16's numbers, and the second is zero only if the value is, and of its sign: the products with an infinity are one.
+        const float below = scale * (1.f - 0x1p-21f);
+        values_of<8>(codes, 1.f, f);
+        uint32_t firsts[4];
+#pragma unroll
+        for (int e = 0; e < 8; e += 2) {
+          const uint32_t p = __float_as_uint(f[e] * below), q = __float_as_uint(f[e + 1] * below);
+          firsts[e / 2] = __builtin_amdgcn_perm(q, p, 0x07060302u);
+          f[e] = fmaf(f[e], scale, -__uint_as_float(p & 0xffff0000u));
+          f[e + 1] = fmaf(f[e + 1], scale, -__uint_as_float(q & 0xffff0000u));
+        }
+        *at = __builtin_bit_cast(P8, firsts);
+        at[S::kPlaneC / 16] = narrow<T, 8>(f);
+      }
     }
 #pragma unroll
     for (int i = k; i < PO; i += kSteps) {
@@ -186,20 +207,24 @@ template <typename T, int kO, int kC, int kWO, int kWC, int kN, int kAhead, Ends
   };
 
   f32x16 acc[TO][TC] = {};
-  struct Frags { typename F::Frag p[TC], q[TO]; } frags[2];
+  struct Frags { typename F::Frag p[F::kTerms][TC], q[TO]; } frags[2];
   const auto read = [&](Frags& f, int buffer, int step) {
     const char* dys = grad_lds + buffer * S::kBuffer + wo * TO * 32 * (int)sizeof(T) + step * F::kStep * S::kPitchO;
     const char* xs = grad_lds + buffer * S::kBuffer + kN * S::kPitchO + wc * TC * 32 * (int)sizeof(T) + step * F::kStep * S::kPitchC;
 #pragma unroll
-    for (int t = 0; t < TC; ++t) f.p[t] = F::template load<true>(xs + t * 32 * (int)sizeof(T), S::kPitchC);
+    for (int u = 0; u < F::kTerms; ++u)
+#pragma unroll
+      for (int t = 0; t < TC; ++t) f.p[u][t] = F::template load<true>(xs + u * S::kPlaneC + t * 32 * (int)sizeof(T), S::kPitchC);
 #pragma unroll
     for (int t = 0; t < TO; ++t) f.q[t] = F::template load<false>(dys + t * 32 * (int)sizeof(T), S::kPitchO);
   };
   const auto multiply = [&](const Frags& f) {
 #pragma unroll
-    for (int i = 0; i < TO; ++i)
+    for (int u = F::kTerms - 1; u >= 0; --u)
 #pragma unroll
-      for (int j = 0; j < TC; ++j) acc[i][j] = F::mma(f.p[j], f.q[i], acc[i][j]);
+      for (int i = 0; i < TO; ++i)
+#pragma unroll
+        for (int j = 0; j < TC; ++j) acc[i][j] = F::mma(f.p[u][j], f.q[i], acc[i][j]);
   };
 
   // The fragments of a product are read while the one before is under way, and so goes what was fetched to LDS; the first fragments of a
@@ -309,11 +334,11 @@ template <typename T, int kJoiners> __global__ __launch_bounds__(256 * kJoiners)
 }
 
 // What tiles a call takes and how many slices.  A form's steps of 64 rows take `step` us with all its workgroups on the chip (`at_once`), its beginning
-// `begin` more than that of the smallest tiles, and a slice costs the writing and reading of its partial sums, at 3 TB/s; the form and number of slices
+// `begin` more than that of the smallest tiles, and a slice costs the writing and reading of its partial sums, at 4.5 TB/s; the form and number of slices
 // of the smallest sum are taken.  Measured, each form at its best, bf16, tiles of 64, 128, 192, 256 and 192 x 64, whose many rows at a time share a
-// column's values among more outputs: 30,000 rows of 192 -> 576 25.1 us, 28.8, 26.3, 35.6, 23.1; 8,000 of 192 -> 192 12.8, 15.5, 17.4, -, 13.5; 800,000 of 192 ->
-// 576 480, 415, 290, 368, 366; 16,384 of 1,024 -> 1,024 92, 61, 72, 60, 95; 65,536 of 1,024 -> 2,048 777, 392, 522, 298, 669; fp32, tiles of 64 and 128: 30,000 of
-// 192 -> 576 74, 105; 65,536 of 1,024 -> 2,048 2,551, 2,304.
+// column's values among more outputs: 30,000 rows of 192 -> 576 33.2 us, 35.7, 32.1, 36.6, 28.0; 8,000 of 192 -> 192 12.9, 16.8, 20.0, 21.6, 14.5; 800,000 of
+// 192 -> 576 604, 622, 431, 561, 497; 16,384 of 1,024 -> 1,024 116, 87, 103, 78, 121; 65,536 of 1,024 -> 2,048 872, 612, 771, 475, 845; fp32, tiles of 64 and 128:
+// 30,000 of 192 -> 576 74, 105; 65,536 of 1,024 -> 2,048 2,551, 2,304.
 constexpr int kRowsStep = 64, kLongest = 16384;   // rows of fp32 that one slice adds up at most: each sum is a chain of additions
 struct Form {
   Shape tile;
@@ -322,8 +347,8 @@ struct Form {
 };
 constexpr int kWideForms = 5;                     // of bf16
 constexpr Form kForms[2][kWideForms] = {
-    {{{64, 64, 2, 1, 1}, 768, 1.13f, 0.f}, {{128, 128, 2, 2, 2}, 512, 1.75f, 0.f}, {{192, 192, 3, 2, 3}, 256, 2.2f, 0.f}, {{256, 256, 2, 4, 2}, 256, 2.55f, 0.f},
-     {{192, 64, 6, 1, 1}, 256, 0.9f, 2.f}},
+    {{{64, 64, 2, 1, 1}, 1024, 1.72f, 0.f}, {{128, 128, 2, 2, 2}, 512, 2.35f, 0.f}, {{192, 192, 3, 2, 3}, 256, 2.8f, 0.f}, {{256, 256, 2, 4, 2}, 256, 3.5f, 0.f},
+     {{192, 64, 6, 1, 1}, 256, 1.06f, 4.f}},
     {{{64, 64, 2, 1, 1}, 768, 3.8f, 0.f}, {{128, 128, 2, 2, 2}, 512, 9.1f, 0.f}, {}, {}, {}}};
 
 struct Plan {
@@ -341,7 +366,7 @@ Plan make_plan(int32_t C, int32_t O, int32_t dtype, int32_t n) {
   for (int f = 0; f < forms; ++f) {
     const Form& form = kForms[!narrow][f];
     const int64_t tiles = dsvt_ceil_div(O, form.tile.kO) * dsvt_ceil_div(C, form.tile.kC);
-    const double slice_us = (double)tile_values(form.tile, O, C) * 8. / 3e6;
+    const double slice_us = (double)tile_values(form.tile, O, C) * 8. / 4.5e6;
     int64_t most = form.at_once / tiles, slices = (int64_t)sqrt((double)steps * form.step / slice_us);
     most = most < steps / 4 ? most : steps / 4;    // (a slice of fewer steps is mostly its beginning and end)
     slices = slices < most ? slices : most;
@@ -379,10 +404,10 @@ template <typename T> int launch(const Grad8Args& a, int form, hipStream_t st) {
     int rc = DSVT_OK;
     if constexpr (sizeof(T) == 2) {
       rc = form == 4   ? launch_tile<T, 4, 96, 2>(a, st)
-           : form == 3 ? launch_tile<T, 3, 32, 2>(a, st)
+           : form == 3 ? launch_tile<T, 3, 32, 1>(a, st)
            : form == 2 ? launch_tile<T, 2, 32, 2>(a, st)
-           : form == 1 ? launch_tile<T, 1, 64, 1>(a, st)
-                       : launch_tile<T, 0, 64, 1>(a, st);
+           : form == 1 ? launch_tile<T, 1, 32, 2>(a, st)
+                       : launch_tile<T, 0, 32, 2>(a, st);
     } else {
       rc = form == 1 ? launch_tile<T, 1, 32, 1>(a, st) : launch_tile<T, 0, 32, 1>(a, st);
     }
