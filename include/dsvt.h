@@ -468,7 +468,8 @@ int dsvt_linear_rows8(const dsvt_linear8_cfg* cfg, const dsvt_rows8* x, int32_t 
 /* The gradients of a linear layer's weights and bias, from dy [device] [n_rows, out] and the layer's input as it was kept: d_w [device] [out, C] of
  * dtype (dy's) = sum over n of dy[n][o] s_n x[n][c], d_b [device] [out] float = sum of dy (NULL: not wanted); both written, not added to.
  * BF16: s_n x[n][c] is taken as the sum of two bf16 operands of the product, off by at most 2^-15 of it, so d_w is off by the rounding of the
- * result (1.7e-3 of its norm); all sums are of 32 bits or more, and do not depend on the order in which the kernels run.  Rows less than 16 MiB
+ * result (1.7e-3 of its norm).  Sums over a slice of the rows (at most 16,384 of F32, 65,536 of BF16) are of 32 bits, sums over the slices of 64; they do
+ * not depend on the order in which the kernels run.  Rows less than 16 MiB
  * apart (dy: 2^24 elements; DSVT_EUNSUPPORTED otherwise).  ws [device] as for dsvt_rms_norm_backward. */
 int dsvt_linear_rows8_weight_grad_workspace_size(int32_t C, int32_t out, int32_t dtype, int32_t n_rows, size_t* bytes);
 int dsvt_linear_rows8_weight_grad(int32_t C, int32_t out, int32_t dtype, const dsvt_rows8* x, const void* dy, int64_t ld_dy, int32_t n_rows,

@@ -18,6 +18,7 @@
 namespace {
 
 typedef float f32x16 __attribute__((ext_vector_type(16)));
+typedef double f64x4 __attribute__((ext_vector_type(4)));
 typedef short short4_t __attribute__((ext_vector_type(4)));
 
 struct Grad8Args {
@@ -284,16 +285,16 @@ template <typename T, int kO, int kC, int kWO, int kWC, int kN, int kAhead, Ends
   for (int e = 0; e < V; ++e) red[row_o * kO + V * piece_o + e] = db[e];
   __syncthreads();
   for (int k = tid; k < kO; k += S::kAll) {
-    float v = 0.f;
-    for (int r = 0; r < S::kRowsO; ++r) v += red[r * kO + k];
-    if (o0 + k < a.O) (a.slices > 1 ? a.bias_partial + (int64_t)slice * a.O : a.d_b)[o0 + k] = v;
+    double v = 0.;
+    for (int r = 0; r < S::kRowsO; ++r) v += (double)red[r * kO + k];
+    if (o0 + k < a.O) (a.slices > 1 ? a.bias_partial + (int64_t)slice * a.O : a.d_b)[o0 + k] = (float)v;
   }
 }
 
-// The slices' partial sums, added in an order of their numbers: a workgroup takes 32 outputs and columns, or 256 outputs of the bias; where there are
-// few such workgroups, four quarters of it take every fourth slice each (kJoiners).  No slices: zeros.
+// The slices' partial sums, added in 64 bits in an order of their numbers: a workgroup takes 32 outputs and columns, or 256 outputs of the bias; where there
+// are few such workgroups, four quarters of it take every fourth slice each (kJoiners).  No slices: zeros.
 template <typename T, int kJoiners> __global__ __launch_bounds__(256 * kJoiners) void k_linear8_grad_join(Grad8Args a, Shape t) {
-  __shared__ f32x4 parts[kJoiners][256];
+  __shared__ f64x4 parts[kJoiners][256];
   const int tid = threadIdx.x & 255, part = threadIdx.x >> 8, tiles_c = (a.C + t.kC - 1) / t.kC, tiles = tiles_c * ((a.O + t.kO - 1) / t.kO);
   const int inner = t.kO * t.kC / 1024;           // squares of 32 of a tile
   const int tile = blockIdx.x / inner, square = blockIdx.x - tile * inner, wave = square / (t.TO * t.TC), of_wave = square - wave * (t.TO * t.TC);
@@ -301,7 +302,7 @@ template <typename T, int kJoiners> __global__ __launch_bounds__(256 * kJoiners)
   const int out0 = tile / tiles_c * t.kO + (wo * t.TO + i) * 32, col0 = (tile - tile / tiles_c * tiles_c) * t.kC + (wc * t.TC + j) * 32;
   const bool weights = tile < tiles;
   if (weights && (out0 >= a.O || col0 >= a.C)) return;             // (no workgroup wrote it)
-  f32x4 v = {};
+  f64x4 v = {};
   if (weights) {
     const f32x4* from = reinterpret_cast<const f32x4*>(a.partial) + (int64_t)blockIdx.x * 256 + tid;
     const int64_t step = (int64_t)tiles * inner * 256;
@@ -311,13 +312,13 @@ template <typename T, int kJoiners> __global__ __launch_bounds__(256 * kJoiners)
 #pragma unroll
       for (int j = 0; j < 8; ++j) f[j] = from[(k + j * kJoiners) * step];
 #pragma unroll
-      for (int j = 0; j < 8; ++j) v += f[j];
+      for (int j = 0; j < 8; ++j) v += __builtin_convertvector(f[j], f64x4);
     }
 #pragma unroll 4
-    for (; k < a.slices; k += kJoiners) v += from[k * step];
+    for (; k < a.slices; k += kJoiners) v += __builtin_convertvector(from[k * step], f64x4);
   } else if (const int o = ((int)blockIdx.x - tiles * inner) * 256 + tid; o < a.O) {
 #pragma unroll 4
-    for (int k = part; k < a.slices; k += kJoiners) v[0] += a.bias_partial[(int64_t)k * a.O + o];
+    for (int k = part; k < a.slices; k += kJoiners) v[0] += (double)a.bias_partial[(int64_t)k * a.O + o];
   }
   if constexpr (kJoiners > 1) {
     parts[part][tid] = v;
@@ -328,9 +329,9 @@ template <typename T, int kJoiners> __global__ __launch_bounds__(256 * kJoiners)
   }
   if (weights) {
     const int lane = tid & 63, out = out0 + (lane & 31), col = col0 + 16 * (lane >> 5) + 4 * (tid >> 6);
-    const float f[4] = {v[0], v[1], v[2], v[3]};
+    const float f[4] = {(float)v[0], (float)v[1], (float)v[2], (float)v[3]};
     if (out < a.O) write_some<T, 4>(static_cast<T*>(a.d_w) + out * a.ld_dw + col, f, a.C - col);
-  } else if (const int o = ((int)blockIdx.x - tiles * inner) * 256 + tid; o < a.O) a.d_b[o] = v[0];
+  } else if (const int o = ((int)blockIdx.x - tiles * inner) * 256 + tid; o < a.O) a.d_b[o] = (float)v[0];
 }
 
 // What tiles a call takes and how many slices.  A form's steps of 64 rows take `step` us with all its workgroups on the chip (`at_once`), its beginning
@@ -339,7 +340,9 @@ template <typename T, int kJoiners> __global__ __launch_bounds__(256 * kJoiners)
 // column's values among more outputs: 30,000 rows of 192 -> 576 33.2 us, 35.7, 32.1, 36.6, 28.0; 8,000 of 192 -> 192 12.9, 16.8, 20.0, 21.6, 14.5; 800,000 of
 // 192 -> 576 604, 622, 431, 561, 497; 16,384 of 1,024 -> 1,024 116, 87, 103, 78, 121; 65,536 of 1,024 -> 2,048 872, 612, 771, 475, 845; fp32, tiles of 64 and 128:
 // 30,000 of 192 -> 576 74, 105; 65,536 of 1,024 -> 2,048 2,551, 2,304.
-constexpr int kRowsStep = 64, kLongest = 16384;   // rows of fp32 that one slice adds up at most: each sum is a chain of additions
+constexpr int kRowsStep = 64;
+// Rows that one slice adds up at most, of fp32 and bf16: each of its sums is a chain of additions in 32 bits, of which d_b has one for every 16 rows or more.
+constexpr int kLongest[2] = {16384, 65536};
 struct Form {
   Shape tile;
   int at_once;
@@ -360,7 +363,7 @@ Plan make_plan(int32_t C, int32_t O, int32_t dtype, int32_t n) {
   Plan p = {0, 0, kRowsStep};
   if (n <= 0) return p;
   const bool narrow = dtype == DSVT_BF16;
-  const int64_t steps = dsvt_ceil_div(n, kRowsStep), least = narrow ? 1 : dsvt_ceil_div(n, kLongest);
+  const int64_t steps = dsvt_ceil_div(n, kRowsStep), least = dsvt_ceil_div(n, kLongest[narrow]);
   double best = 0.;
   const int forms = O < (narrow ? 8 : 4) ? 1 : narrow ? kWideForms : 2;           // (fewer outputs than a piece: the first form)
   for (int f = 0; f < forms; ++f) {

@@ -134,3 +134,22 @@ def test_weight_grad_of_infinities(dtype, n, c, o):
     same = lambda a, b: torch.equal(a.isnan(), b.isnan()) and torch.equal(a.nan_to_num(7, 1e30, -1e30), b.nan_to_num(7, 1e30, -1e30))  # noqa: E731
     bias[1], bias[3] = float("-inf"), float("nan")
     assert bool(got[1, 0].isnan()) and same(got, want) and same(got_bias, bias)
+
+
+@pytest.mark.parametrize("dtype,n,c,o", [("f32", 300007, 63, 130), ("f32", 200001, 1001, 900), ("bf16", 400007, 63, 130), ("bf16", 150001, 2049, 4097)])
+def test_weight_grad_joins_slices_in_64_bits(dtype, n, c, o):
+    """Positive whole numbers: a slice's sums (of at most 16,384 rows of fp32, 65,536 of bf16) are below 2^24, those over all rows above; they are added as
+    64 bits hold them and rounded once.  bf16: the bias, and of the weights, whose slices' sums pass 2^24, the first bits."""
+    print("[case] weight grad of long sums", dtype, n, c, o, flush=True)
+    g = torch.Generator(device="cuda").manual_seed(n)
+    wide = torch.randint(50, 128, (n, (c + 15) // 16 * 16), device="cuda", dtype=torch.int8, generator=g)
+    rows = dsvt.Rows8.of(wide[:, :c], torch.ones(n, device="cuda"))
+    dy = torch.randint(*((1, 5) if dtype == "f32" else (100, 128)), (n, o), device="cuda", generator=g, dtype=torch.int32).to(DT[dtype])
+    d_w, d_b = _sums(rows, dy)
+    assert float((d_w if dtype == "f32" else d_b).min()) > 2 ** 24
+    got, bias = dsvt.dsvt_linear_rows8_weight_grad(rows, dy)
+    assert torch.equal(bias, d_b.float())
+    if dtype == "f32":
+        assert torch.equal(got, d_w.float())
+    else:
+        assert bool(((got.double() - d_w).abs() <= d_w * (2.0 ** -8 + 2.0 ** -14)).all())
