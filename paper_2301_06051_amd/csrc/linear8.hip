@@ -179,7 +179,7 @@ __global__ __launch_bounds__(64 * kShortWaves, short_simd(kSteps, sizeof(T))) vo
   __shared__ P all_out[kShortWaves][kRowsOut * PR];
   __shared__ float all_ends[kShortWaves][2][64];
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), m = lane & 31, h = lane >> 5;
-  const int blocks_n = (a.O + 63) / 64, blocks_m = (a.n + 31) / 32;
+  const int blocks_n = (a.O + 63) / 64, blocks_m = (a.n - 1) / 32 + 1;         // (n + 31 may pass 32 bits)
   const int groups = gridDim.x >> 3, at = ((blockIdx.x & 7) * groups + (blockIdx.x >> 3)) * kShortWaves + wave, share = at / blocks_n;
   if (share >= shares) return;
   const int out0 = at % blocks_n * 64, outs = a.O - out0 < 64 ? a.O - out0 : 64;
@@ -311,7 +311,7 @@ __global__ __launch_bounds__(64 * kM * kN) void k_linear8_tiles(Linear8Args a) {
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), wm = wave % kM, wn = wave / kM, m = lane & 31, h = lane >> 5;
 
   // Workgroups of one XCD (every eighth) take neighbouring tiles side by side: eight along the rows, then the next outputs.
-  const int tiles_m = (a.n + kRowsT - 1) / kRowsT, tiles_n = (a.O + kOutsT - 1) / kOutsT, all = tiles_m * tiles_n;
+  const int tiles_m = (a.n - 1) / kRowsT + 1, tiles_n = (a.O + kOutsT - 1) / kOutsT, all = tiles_m * tiles_n;
   const int share = (all + 7) >> 3, first = (blockIdx.x & 7) * share, end = first + share < all ? first + share : all, step = gridDim.x >> 3;
   int id = first + (blockIdx.x >> 3);
   if (id >= end) return;
