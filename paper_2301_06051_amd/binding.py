@@ -475,13 +475,25 @@ _current_device = getattr(torch._C, "_cuda_getDevice", torch.cuda.current_device
 _current_stream = getattr(torch._C, "_cuda_getCurrentRawStream", lambda device: torch.cuda.current_stream(device).cuda_stream)
 
 
+_MOST = (1 << 31) - 1                               # rows and columns of a call; ctypes would hand on the low 32 bits of more without a word
+
+
+def _too_many(what, *shape):
+    raise ValueError(f"{what}: a call takes at most {_MOST} rows and columns; got {shape}")
+
+
 def _rows(t, shape, dtype, device, what):
     """The row stride of a [rows, columns] tensor of the current device (`device`) whose columns are neighbours; of one row, whatever its tensor
     says, the row's length."""
     if t.shape != shape or t.dtype is not dtype or t.get_device() != device or (shape[1] > 1 and t.stride(1) != 1):
         raise ValueError(f"{what}: a {dtype} tensor of shape {tuple(shape)} with neighbouring columns on the current device, cuda:{device}, is wanted; "
                          f"got {t.dtype} {tuple(t.shape)}, strides {tuple(t.stride())}, on {t.device}")
-    return t.stride(0) if shape[0] > 1 else shape[1]
+    n = shape[0]
+    if 1 < n <= _MOST:
+        return t.stride(0)
+    if n > 1:
+        _too_many(what, *shape)
+    return shape[1]
 
 
 def _elsewhere(device, *owners):
@@ -626,6 +638,8 @@ class LayerNorm:
     def __init__(self, gamma, beta, dtype, eps=1e-5):
         code, self.dtype = _DT[dtype]
         self.C, self.gamma, self.beta = gamma.shape[0], gamma, beta
+        if self.C > _MOST:
+            _too_many("gamma", self.C)
         _vector(gamma, (self.C,), torch.float32, _current_device(), "gamma")
         _vector(beta, (self.C,), torch.float32, _current_device(), "beta")
         self.struct = LnCfg(self.C, code, gamma.data_ptr(), beta.data_ptr(), eps)
@@ -654,6 +668,8 @@ def dsvt_layer_norm(ln, x, res=None, y=None, stream=None):
 def dsvt_layer_norm_backward_workspace_size(ln, n_rows):
     last, size = ln.size
     if n_rows != last:
+        if n_rows > _MOST:
+            _too_many("n_rows", n_rows)
         b = C.c_size_t(0)
         _check("dsvt_layer_norm_backward_workspace_size", lib().dsvt_layer_norm_backward_workspace_size(ln.ref, n_rows, C.byref(b)))
         size = b.value
@@ -731,6 +747,8 @@ class Rows8:
             raise ValueError(f"codes: an int8 tensor [n, C] with neighbouring columns is wanted; got {codes.dtype} {tuple(codes.shape)}, strides "
                              f"{tuple(codes.stride())}")
         n, c = codes.shape
+        if n > _MOST or c > _MOST:
+            _too_many("codes", n, c)
         ld = codes.stride(0) if n > 1 else (c + 15) // 16 * 16
         if codes.data_ptr() % 16 or ld % 16 or ld < c:
             raise ValueError(f"codes: rows that begin on 16 bytes and lie a multiple of 16 bytes apart are wanted; got a stride of {ld} bytes, address "
@@ -747,6 +765,8 @@ class Rows8:
 
     @classmethod
     def empty(cls, n, channels, device="cuda"):
+        if n > _MOST or channels > _MOST:
+            _too_many("rows in 8 bits", n, channels)
         ld = (channels + 15) & ~15
         return cls._in(torch.empty((n * (ld + 4),), dtype=torch.int8, device=device), n, channels, ld)
 
@@ -792,6 +812,8 @@ def dsvt_keep_rows8(x, out=None, stream=None):
         _no_graph("dsvt_keep_rows8", x)
     dtype, dev = _type_of(x, "x"), _current_device()
     n, c = x.shape
+    if c > _MOST:
+        _too_many("x", n, c)
     ld = _rows(x, (n, c), dtype, dev, "x")
     if out is None:
         out = Rows8._like(stream, dev, x, n, c)
@@ -826,6 +848,8 @@ class RmsNorm:
     def __init__(self, gamma, dtype, eps=1e-5):
         code, self.dtype = _DT[dtype]
         self.C, self.gamma = gamma.shape[0], gamma
+        if self.C > _MOST:
+            _too_many("gamma", self.C)
         _vector(gamma, (self.C,), torch.float32, _current_device(), "gamma")
         self.struct = RmsCfg(self.C, code, gamma.data_ptr(), eps)
         self.ref, self.size, self.device = C.byref(self.struct), (None, 0), _current_device()     # size: the last shape and its workspace bytes
@@ -885,6 +909,8 @@ def dsvt_rms_norm_rows8(rms, x, res=None, out=None, z=None, want_sum=False, stre
 def dsvt_rms_norm_backward_workspace_size(rms, n_rows):
     last, size = rms.size
     if n_rows != last:
+        if n_rows > _MOST:
+            _too_many("n_rows", n_rows)
         b = C.c_size_t(0)
         _check("dsvt_rms_norm_backward_workspace_size", lib().dsvt_rms_norm_backward_workspace_size(rms.ref, n_rows, C.byref(b)))
         size = b.value
@@ -930,6 +956,8 @@ def dsvt_gelu_rows8(h, out=None, kept=None, want_kept=True, stream=None):
         _no_graph("dsvt_gelu_rows8", h)
     dtype, dev = _type_of(h, "h"), _current_device()
     n, c = h.shape
+    if c > _MOST:
+        _too_many("h", n, c)
     ld = _rows(h, (n, c), dtype, dev, "h")
     if out is None:
         out = Rows8._like(stream, dev, h, n, c)
@@ -997,6 +1025,8 @@ def dsvt_linear_rows8(linear, rows, y=None, stream=None):
 
 
 def dsvt_linear_rows8_weight_grad_workspace_size(channels, out, dtype, n_rows):
+    if max(channels, out, n_rows) > _MOST:
+        _too_many("channels, out, n_rows", channels, out, n_rows)
     b = C.c_size_t(0)
     _check("dsvt_linear_rows8_weight_grad_workspace_size",
            lib().dsvt_linear_rows8_weight_grad_workspace_size(channels, out, _DT[dtype][0], n_rows, C.byref(b)))
@@ -1010,6 +1040,8 @@ def dsvt_linear_rows8_weight_grad(rows, dy, d_w=None, d_b=None, want_bias=True, 
         _no_graph("dsvt_linear_rows8_weight_grad", rows.given, dy, d_w, d_b)
     dtype, dev = _type_of(dy, "dy"), _current_device()
     n, c, o = rows.n, rows.C, dy.shape[1]
+    if o > _MOST:
+        _too_many("dy", n, o)
     ref, ld = _rows8(rows, None, None, dev, "rows"), _rows(dy, (n, o), dtype, dev, "dy")
     if d_w is None:
         d_w, ld_w = _new(stream, dev, dy, (o, c), dtype), c
