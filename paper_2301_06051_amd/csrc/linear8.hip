@@ -43,6 +43,31 @@ __device__ __forceinline__ i32x4 first_bytes(i32x4 p, int left) {
 // GELU with its limits at the infinities, which a result may be (a row in 8 bits may not).
 __device__ __forceinline__ float activation(float v) { return fabsf(v) == INFINITY ? fmaxf(v, 0.f) : gelu(v); }
 
+// A result before its activation.  A sum is up to 2^30, so its product with a row's scale above 2^98 may pass 32 bits though that with the other scale, and so
+// the result, does not: of rows whose scale is above kHuge the sum is multiplied by the other scale first, which passes 32 bits only if the result does.
+constexpr float kHuge = 0x1p90f;
+struct PlainRow {
+  static __device__ __forceinline__ float result(int sum, float s, float t, float bias) { return fmaf((float)sum * s, t, bias); }
+};
+struct HugeRow {
+  static __device__ __forceinline__ float result(int sum, float s, float t, float bias) { return fmaf((float)sum * t, s, bias); }
+};
+struct AnyRow {
+  static __device__ __forceinline__ float result(int sum, float s, float t, float bias) { return fmaf((float)sum * (s > kHuge ? t : s), s > kHuge ? s : t, bias); }
+};
+// results(kind of row, activation) for a lane whose row's scale is s.  kBranch: huge rows have code of their own, which costs the others nothing but the
+// registers that it takes.  (800,000 x 192 -> 576 207 us, as without huge rows; 214 with AnyRow's choice at every result; but 8,192 x 4,096 -> 4,096 of 32 bits 136
+// without, 138 with the choice, 242 with code of their own, as registers go through memory then.)
+template <bool kBranch, typename Results> __device__ __forceinline__ void with_activation(int act, float s, const Results& results) {
+  const auto of = [&](auto row) {
+    if (act) results(row, [](float v) { return activation(v); });
+    else results(row, [](float v) { return v; });
+  };
+  if constexpr (!kBranch) of(AnyRow());
+  else if (s > kHuge) of(HugeRow());
+  else of(PlainRow());
+}
+
 // Few rows: the weights are what there is to read, and all of them should be on their way at once.  A workgroup takes 16 outputs and 16 kTiles rows; its
 // eight wavefronts share the columns, in runs of 64, of which each has kAtOnce on their way.  Lane 16 g + m holds 16 codes of row m, from column 16 g of
 // a run on.
@@ -104,7 +129,7 @@ template <typename T, int kTiles, int kAtOnce> __global__ __launch_bounds__(64 *
     T* y = static_cast<T*>(a.y) + row * a.ld_y + out;
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
-      const float v = fmaf((float)acc[t][i] * s, scale[i], bias[i]);
+      const float v = AnyRow::result(acc[t][i], s, scale[i], bias[i]);
       if (out + i < a.O) y[i] = (T)(a.act ? activation(v) : v);
     }
   }
@@ -245,7 +270,7 @@ __global__ __launch_bounds__(64 * kShortWaves, short_simd(kSteps, sizeof(T))) vo
       const int left = (int)(a.n - row0 - kRowsOut * part < kRowsOut ? a.n - row0 - kRowsOut * part : kRowsOut);
       if (left <= 0) break;
       if (m / kRowsOut == part) {
-        const auto results = [&](auto act) {
+        const auto results = [&](auto row, auto act) {
 #pragma unroll
           for (int j = 0; j < 2; ++j) {
             int from = 32 * j + 16 * h;
@@ -257,14 +282,13 @@ __global__ __launch_bounds__(64 * kShortWaves, short_simd(kSteps, sizeof(T))) vo
               for (int k = 0; k < V; k += 4) {
                 const f32x4 t = *reinterpret_cast<const f32x4*>(ends + from + e + k), bias = *reinterpret_cast<const f32x4*>(ends + 64 + from + e + k);
 #pragma unroll
-                for (int u = 0; u < 4; ++u) f[k + u] = act(fmaf((float)acc[j][e + k + u] * scale, t[u], bias[u]));
+                for (int u = 0; u < 4; ++u) f[k + u] = act(row.result(acc[j][e + k + u], scale, t[u], bias[u]));
               }
               out[spot<PR>(m % kRowsOut, (32 * j + 16 * h + e) / V)] = narrow<T, V>(f);
             }
           }
         };
-        if (a.act) results([](float v) { return activation(v); });
-        else results([](float v) { return v; });
+        with_activation<true>(a.act, scale, results);
       }
       in_order();
       rows_out<T, 64, kRowsOut>(out, static_cast<T*>(a.y) + (row0 + kRowsOut * part) * a.ld_y + out0, a.ld_y, left, outs, a.leaves, lane);
@@ -448,7 +472,7 @@ __global__ __launch_bounds__(64 * kM * kN) void k_linear8_tiles(Linear8Args a) {
         const int rows = (int)(a.n - from - kRowsOut * part < kRowsOut ? a.n - from - kRowsOut * part : kRowsOut);
         if (rows <= 0 || outs <= 0) break;
         if (m / kRowsOut == part) {
-          const auto results = [&](auto act) {
+          const auto results = [&](auto row, auto act) {
 #pragma unroll
             for (int j = 0; j < TN; ++j)
 #pragma unroll
@@ -461,13 +485,12 @@ __global__ __launch_bounds__(64 * kM * kN) void k_linear8_tiles(Linear8Args a) {
                   f32x4 bias = {0.f, 0.f, 0.f, 0.f};
                   if (a.bias) bias = *reinterpret_cast<const f32x4*>(ends + kOutsT + o);
 #pragma unroll
-                  for (int u = 0; u < 4; ++u) f[k + u] = act(fmaf((float)acc[i][j][e + k + u] * s, t[u], bias[u]));
+                  for (int u = 0; u < 4; ++u) f[k + u] = act(row.result(acc[i][j][e + k + u], s, t[u], bias[u]));
                 }
                 out[spot<PR>(m % kRowsOut, (32 * j + 16 * h + e) / V)] = narrow<T, V>(f);
               }
           };
-          if (a.act) results([](float v) { return activation(v); });
-          else results([](float v) { return v; });
+          with_activation<!(sizeof(T) == 4 && kRowsT == 256)>(a.act, s, results);
         }
         __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
         __builtin_amdgcn_wave_barrier();
