@@ -23,8 +23,54 @@ def test_as_many_rows_as_a_call_can_have():
     one = dsvt.dsvt_keep_rows8(torch.ones((1, 1), device="cuda"))
     y = back.fill_(7)
     assert torch.equal(dsvt.dsvt_linear_rows8(dsvt.Linear8(one, "bf16"), kept, y=y), x)
+    # their weight gradient with a dy of ones: the sum of all rows, whose terms are off by 2^-15 of at most 6, of no order, and the number of rows
+    d_w, d_b = dsvt.dsvt_linear_rows8_weight_grad(kept, torch.ones_like(x))
+    total = float(x.sum(dtype=torch.float64))
+    assert float(d_b) == 2.0 ** 31 and abs(float(d_w) - total) <= 8 * n ** 0.5 * 6 * 2.0 ** -15 + 2.0 ** -8 * abs(total)
     del x, kept, back, y
     torch.cuda.empty_cache()
+
+
+@pytest.mark.parametrize("n,c", [(300, 192), (257, 99), (33, 700), (700, 24), (9, 3), (5, 4100), (3, 8200), (2, 9001), (60, 1025)])
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("odd", [False, True])
+def test_norm_in_rows_and_in_8_bits_at_once(n, c, dtype, odd):
+    """The library's call with y, z and rows8 together: each as the calls for one of them write it, and nothing beside them."""
+    print("[case] rows and 8 bits", n, c, dtype, odd, flush=True)
+    from paper_2301_06051_amd import binding as b
+    g = torch.Generator(device="cuda").manual_seed(n + c)
+    at, behind = (3, 2) if odd else (0, 0)
+    wide = lambda: torch.full((n, at + c + behind), 7.0, dtype=DT[dtype], device="cuda")  # noqa: E731
+    y, z = wide(), wide()
+    x, r = (torch.randn((n, c), device="cuda", generator=g).to(DT[dtype]) for _ in range(2))
+    norm = dsvt.RmsNorm(1 + 0.1 * torch.randn(c, device="cuda", generator=g), dtype)
+    codes = torch.full((n, (c + 15) // 16 * 16 + 16), 77, dtype=torch.int8, device="cuda")
+    rows = dsvt.Rows8.of(codes[:, :c], torch.zeros(n, device="cuda"))
+    inner = slice(at, at + c)
+    ld, e = at + c + behind, x.element_size()
+    rc = b.lib().dsvt_rms_norm(norm.ref, x.data_ptr(), c, r.data_ptr(), c, n, z.data_ptr() + at * e, ld, y.data_ptr() + at * e, ld, rows.ref,
+                               torch.cuda.current_stream().cuda_stream)
+    assert rc == 0
+    y1, z1 = dsvt.dsvt_rms_norm(norm, x, r, want_sum=True)
+    rows1 = dsvt.dsvt_rms_norm_rows8(norm, x, r)
+    assert torch.equal(y[:, inner], y1) and torch.equal(z[:, inner], z1) and torch.equal(rows.codes, rows1.codes) and torch.equal(rows.scale, rows1.scale)
+    assert all(bool((t[:, :at] == 7).all()) and bool((t[:, at + c:] == 7).all()) for t in (y, z)) and bool((codes[:, c:] == 77).all())
+
+
+@pytest.mark.parametrize("n,c,o", [(1, 4096, 300), (5, 16, 17), (17, 64, 131), (33, 65, 3), (64, 4096, 191), (64, 99, 130), (300, 1000, 257), (70001, 64, 67), (40000, 192, 301), (30001, 250, 257),
+                                   (300000, 65, 5), (60000, 260, 250), (120000, 272, 251), (66000, 257, 130), (7001, 2048, 999), (26000, 2100, 401)])
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("at,behind", [(1, 1), (5, 2), (8, 8), (64, 63)])
+def test_what_lies_around_results_of_the_linear_layer(n, c, o, dtype, at, behind):
+    """Results as columns of a wider array, and rows behind the last: all around them stays as it is; they are those of a call that makes its own."""
+    print("[case] around a linear layer", n, c, o, dtype, at, behind, flush=True)
+    g = torch.Generator(device="cuda").manual_seed(n + c + o)
+    rows = lambda k: dsvt.dsvt_keep_rows8(torch.randn((k, c), device="cuda", generator=g))  # noqa: E731
+    x, layer = rows(n), dsvt.Linear8(rows(o), dtype, torch.randn(o, device="cuda", generator=g))
+    wide = torch.full((n + 3, at + o + behind), 7.0, dtype=DT[dtype], device="cuda")
+    dsvt.dsvt_linear_rows8(layer, x, y=wide[:n, at:at + o])
+    assert torch.equal(wide[:n, at:at + o], dsvt.dsvt_linear_rows8(layer, x))
+    assert bool((wide[:, :at] == 7).all()) and bool((wide[:, at + o:] == 7).all()) and bool((wide[n:] == 7).all())
 
 
 @pytest.mark.parametrize("n,c,o", [(3, 64, 20), (100, 64, 70), (100, 4096, 20), (70000, 64, 64), (40000, 192, 200), (60000, 260, 250), (120000, 272, 251), (26000, 2100, 401), (200, 300, 130)])
