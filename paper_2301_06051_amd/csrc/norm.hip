@@ -14,6 +14,7 @@
 // held in 32 bits, that over the workgroups in 64, and none depends on the order in which workgroups run.  800,000 rows of 192 bf16 with a
 // branch: forward 175 us, backward 233 (5.3 TB/s each; a copy of 2 GiB reaches 4.8 on the same card).
 #include "rows.h"
+#include "sum_parts.h"
 
 namespace {
 

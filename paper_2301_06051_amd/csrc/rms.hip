@@ -7,6 +7,7 @@
 // it was not written, and its gradient d_sum, which comes past the branch, is added in the same pass.  800,000 rows of 192 bf16 with a branch: forward
 // with y and z 228 us (5.4 TB/s), backward with d_sum 287 (5.3); 30,000 rows backward 15.4 with 512 workgroups, 18.4 with 768, 19.0 with 1,024.
 #include "rows8.h"
+#include "sum_parts.h"
 
 namespace {
 

@@ -1,5 +1,5 @@
-// What kernels that go over rows share (norm.hip, rms.hip, rows8.hip): a row sits in the registers of kLanes neighbouring lanes (8 to 64, or a
-// workgroup's 256), in pieces of up to 16 bytes; sums over a row across lanes; which pieces and lanes a call's rows take; sums over rows.
+// What kernels that go over rows share (norm.hip, rms.hip, rows8.hip): a row sits in the registers of kLanes neighbouring lanes (4 to 64, or a
+// workgroup's 256), in pieces of up to 16 bytes; sums over a row across lanes; which pieces and lanes a call's rows take.
 #pragma once
 #include "common.h"
 #include "mma.h"
@@ -7,7 +7,7 @@
 namespace {
 
 constexpr int kThreads = 256;
-constexpr int kVectors = 4;                       // 16-byte pieces of a row in one lane, at most
+constexpr int kVectors = 4;                       // 16-byte pieces of a row in one lane, at most (of the longest rows of 32 bits twice as many: rows8.h)
 constexpr int narrow_max(int bytes) { return bytes == 8 ? 8 : 16; }      // and smaller ones
 constexpr int kBackwardGroups = 512;              // workgroups of a pass that sums over rows, at most: two a compute unit
 constexpr int kForwardGroups = 2048;
@@ -70,34 +70,6 @@ __device__ __forceinline__ void load_vector(const float* v, int part, int pieces
   for (int r = 0; r < R; ++r)
 #pragma unroll
     for (int i = 0; i < V; ++i) f[r][i] = r * kLanes + part < pieces ? v[(r * kLanes + part) * V + i] : 0.f;
-}
-
-// Sums over rows from the workgroups' partial sums [groups][cols], of which the first `split` columns go to `first` and the others to `second`: 32
-// columns a workgroup, 32 slices of the partial rows, added in a fixed order.  In 64 bits: 512 numbers added one after the other in 32
-// would be most of the error of these sums, and the adds are not what the kernel waits for.  No rows (groups == 0): zeros.
-__global__ __launch_bounds__(1024) void k_sum_parts(const float* __restrict__ partial, int32_t groups, int32_t cols, int32_t split,
-                                                    float* __restrict__ first, float* __restrict__ second) {
-  __shared__ double s[32][33];
-  const int col = threadIdx.x & 31, slice = threadIdx.x >> 5, c = blockIdx.x * 32 + col;
-  double v = 0.;
-  if (c < cols) {
-    int k = slice;
-    for (; k + 7 * 32 < groups; k += 8 * 32) {    // eight loads on their way at a time
-      float f[8];
-#pragma unroll
-      for (int j = 0; j < 8; ++j) f[j] = partial[(int64_t)(k + j * 32) * cols + c];
-#pragma unroll
-      for (int j = 0; j < 8; ++j) v += (double)f[j];
-    }
-    for (; k < groups; k += 32) v += (double)partial[(int64_t)k * cols + c];
-  }
-  s[slice][col] = v;
-  __syncthreads();
-  if (threadIdx.x >= 32 || c >= cols) return;
-  v = 0.;
-#pragma unroll
-  for (int k = 0; k < 32; ++k) v += s[k][col];
-  (c < split ? first : second)[c < split ? c : c - split] = (float)v;
 }
 
 // The widest pieces of 16, 8, 4 or 2 bytes on which every row of every array starts and of which C is a whole number (`all`: the addresses and the

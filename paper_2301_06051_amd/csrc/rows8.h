@@ -14,7 +14,6 @@ constexpr float kLargestScale = 0x1.020406p+121f; // the largest whose product w
 
 template <int V> struct Codes { typedef uint32_t type __attribute__((ext_vector_type(V / 4))); };
 template <> struct Codes<4> { typedef uint32_t type; };
-template <> struct Codes<2> { typedef uint16_t type; };
 template <> struct Codes<1> { typedef uint8_t type; };
 
 __device__ __forceinline__ int8_t byte_of(uint32_t p, int i) { return (int8_t)(p >> 8 * i); }
@@ -33,8 +32,8 @@ template <int kByte> __device__ __forceinline__ float code_of(uint32_t four) {
 template <int V> __device__ __forceinline__ void values_of(typename Codes<V>::type p, float scale, float (&f)[V]) {
   if constexpr (V <= 4) {
     f[0] = code_of<0>(p) * scale;
-    if constexpr (V > 1) f[1] = code_of<1>(p) * scale;
-    if constexpr (V > 2) {
+    if constexpr (V > 1) {
+      f[1] = code_of<1>(p) * scale;
       f[2] = code_of<2>(p) * scale;
       f[3] = code_of<3>(p) * scale;
     }
@@ -80,7 +79,6 @@ struct RowScale {
   template <int V> __device__ __forceinline__ typename Codes<V>::type codes(const float (&v)[V]) const {
     typename Codes<V>::type p;
     if constexpr (V == 1) p = (uint8_t)code(v[0]);
-    else if constexpr (V == 2) p = plain ? (uint16_t)__builtin_amdgcn_perm(code_bits(v[1]), code_bits(v[0]), 0x0c0c0400u) : 0;
     else if constexpr (V == 4) {
       const uint32_t low = __builtin_amdgcn_perm(code_bits(v[1]), code_bits(v[0]), 0x0c0c0400u);
       const uint32_t high = __builtin_amdgcn_perm(code_bits(v[3]), code_bits(v[2]), 0x0c0c0400u);
@@ -254,6 +252,4 @@ __device__ __forceinline__ float gelu_slope(float x) {
 inline bool bad_rows8(const dsvt_rows8* r, int32_t C) {
   return !r || !r->codes || !r->scale || ((uintptr_t)r->codes & 15u) != 0 || ((uintptr_t)r->scale & 3u) != 0 || r->ld < C || r->ld % 16 != 0;
 }
-// Pieces of 16 bf16 or fp32 values do not exist, so codes, whose rows begin on 16 bytes, never make pieces narrower.
-
 }  // namespace

@@ -154,28 +154,26 @@ template <bool kGelu, typename T> void launch_write(const Rows8Args& a, RowForm 
   if (lanes == 0) k_write_rows8_long<kGelu, T><<<groups, kThreads, 0, st>>>(a);
   else launch_form<Write<kGelu>::template Kernel, T>(a, form, lanes, groups, st);
 }
-template <bool kGelu, typename T, int V, bool kLoose> void launch_read(const Rows8Args& a, hipStream_t st) {
-  int lanes = V > 1 && a.C <= 4 * V ? 4 : 8;
-  while (lanes > 4 && lanes < 64 && lanes * 4 < a.C / V) lanes *= 2;
-  const int64_t all = dsvt_ceil_div(a.n, kThreads / lanes);
-  const unsigned groups = (unsigned)(all < 2 * kForwardGroups ? all : 2 * kForwardGroups);
-  if (V == 1 || lanes == 8) k_read_rows8<kGelu, T, V, 8, kLoose><<<groups, kThreads, 0, st>>>(a);
-  else if constexpr (V == 1) return;
-  else if (lanes == 4) k_read_rows8<kGelu, T, V, 4, kLoose><<<groups, kThreads, 0, st>>>(a);
-  else if (lanes == 16) k_read_rows8<kGelu, T, V, 16, kLoose><<<groups, kThreads, 0, st>>>(a);
-  else if (lanes == 32) k_read_rows8<kGelu, T, V, 32, kLoose><<<groups, kThreads, 0, st>>>(a);
-  else k_read_rows8<kGelu, T, V, 64, kLoose><<<groups, kThreads, 0, st>>>(a);
+template <bool kGelu, typename T, int V, int kLanes, bool kLoose> void launch_read(const Rows8Args& a, hipStream_t st) {
+  const int64_t all = dsvt_ceil_div(a.n, kThreads / kLanes);
+  k_read_rows8<kGelu, T, V, kLanes, kLoose><<<(unsigned)(all < 2 * kForwardGroups ? all : 2 * kForwardGroups), kThreads, 0, st>>>(a);
 }
 template <bool kGelu, typename T> void launch_read(const Rows8Args& a, RowForm form, hipStream_t st) {
   constexpr int V = 16 / (int)sizeof(T);
-  if (form == kPieces) launch_read<kGelu, T, V, false>(a, st);
-  else if (form == kLooseEnds) {
+  if (form == kPieces) {
+    int lanes = a.C <= 4 * V ? 4 : 8;
+    while (lanes > 4 && lanes < 64 && lanes * 4 < a.C / V) lanes *= 2;
+    if (lanes == 4) launch_read<kGelu, T, V, 4, false>(a, st);
+    else if (lanes == 8) launch_read<kGelu, T, V, 8, false>(a, st);
+    else if (lanes == 16) launch_read<kGelu, T, V, 16, false>(a, st);
+    else if (lanes == 32) launch_read<kGelu, T, V, 32, false>(a, st);
+    else launch_read<kGelu, T, V, 64, false>(a, st);
+  } else if (form == kLooseEnds) {
     const int lanes = form_lanes(form, a.C, sizeof(T));
     const int64_t all = dsvt_ceil_div(a.n, lanes ? kThreads / lanes : 1);
-    if (lanes == 0) launch_read<kGelu, T, V, true>(a, st);       // (longer ones)
+    if (lanes == 0) launch_read<kGelu, T, V, 64, true>(a, st);   // (longer ones)
     else launch_form<Read<kGelu>, T>(a, lanes, (unsigned)(all < kForwardGroups ? all : kForwardGroups), st);
-  }
-  else launch_read<kGelu, T, 1, false>(a, st);
+  } else launch_read<kGelu, T, 1, 8, false>(a, st);
 }
 
 int check(int32_t C, int32_t dtype, int32_t n_rows) {
