@@ -426,7 +426,8 @@ typedef struct {
 int dsvt_keep_rows8(int32_t C, int32_t dtype, const void* x, int64_t ld_x, int32_t n_rows, const dsvt_rows8* kept, void* stream);
 int dsvt_read_rows8(int32_t C, int32_t dtype, const dsvt_rows8* rows, int32_t n_rows, void* x, int64_t ld_x, void* stream);
 
-/* Root-mean-square norm of a residual sum: z = x + res, y = z / sqrt(mean z^2 + eps) * gamma, row by row. */
+/* Root-mean-square norm of a residual sum: z = x + res, y = z / sqrt(mean z^2 + eps) * gamma, row by row.  The sum of z^2 is one of 32 bits: where it
+ * passes them (never for values below 1.8e19 / sqrt(C)), y is zeros. */
 typedef struct {
   int32_t C, dtype;           /* dtype of x, res, z, y and their gradients                                  */
   const float* gamma;         /* [C] [device]                                                               */
@@ -469,8 +470,8 @@ int dsvt_linear_rows8(const dsvt_linear8_cfg* cfg, const dsvt_rows8* x, int32_t 
  * dtype (dy's) = sum over n of dy[n][o] s_n x[n][c], d_b [device] [out] float = sum of dy (NULL: not wanted); both written, not added to.
  * BF16: s_n x[n][c] is taken as the sum of two bf16 operands of the product, off by at most 2^-15 of it, so d_w is off by the rounding of the
  * result (1.7e-3 of its norm).  Sums over a slice of the rows (at most 16,384 of F32, 65,536 of BF16) are of 32 bits, sums over the slices of 64; they do
- * not depend on the order in which the kernels run.  Rows less than 16 MiB
- * apart (dy: 2^24 elements; DSVT_EUNSUPPORTED otherwise).  ws [device] as for dsvt_rms_norm_backward. */
+ * not depend on the order in which the kernels run.  Rows less than 16 MiB apart (dy: 2^24 elements; DSVT_EUNSUPPORTED otherwise).  ws [device] as for
+ * dsvt_rms_norm_backward. */
 int dsvt_linear_rows8_weight_grad_workspace_size(int32_t C, int32_t out, int32_t dtype, int32_t n_rows, size_t* bytes);
 int dsvt_linear_rows8_weight_grad(int32_t C, int32_t out, int32_t dtype, const dsvt_rows8* x, const void* dy, int64_t ld_dy, int32_t n_rows,
                                   void* d_w, int64_t ld_dw, float* d_b, void* ws, size_t ws_bytes, void* stream);

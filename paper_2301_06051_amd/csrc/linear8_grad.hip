@@ -8,9 +8,9 @@
 // taken as two, its first bits and the rest, at twice the products: the result is off by its own rounding, 1.7e-3 of its norm (2.3e-3 with one
 // operand, and no number where that passes bf16), for 1.1 to 1.6 times the time.
 //
-// Both operands run along the rows, so both have to be turned round, which the LDS loads do (bf16).  With tiles of 256 the matrix cores are busy for 2,048
-// clocks of a step of 32 rows, LDS for 1,400, the instructions that make values of codes for 800: 65,536 rows of 1,024 -> 2,048 455 to 480 us (1,200 TFLOP/s of
-// products; the library's of 8,192^3 in bf16 1,362).  Few columns leave the partial sums and a step's latency: 30,000 rows of 192 -> 576 28 us, four of them the
+// Both operands run along the rows, so both have to be turned round, which the LDS loads do (bf16).  With tiles of 256 a step of 32 rows is 2,048 clocks of
+// the matrix cores, 1,400 of LDS and some 900 of the making of values from codes, only partly at once: 65,536 rows of 1,024 -> 2,048 475 to 480 us (1,190 TFLOP/s
+// of products; the library's of 8,192^3 in bf16 1,362).  Few columns leave the partial sums and a step's latency: 30,000 rows of 192 -> 576 28 us, five of them the
 // second kernel.
 #include "rows8.h"
 #include <cmath>
